@@ -17,10 +17,16 @@ Parity status (each function's own docstring names its pins):
   float64 rms_norm, ties, closed forms, finite differences, float64 autograd).
 * ``ppo_loss``  pinned (float64 autograd through the textbook loss, closed
   forms, clip regions, response sums).
+* ``mxfp4_*``  pinned (the values by hand, brute force, ties, an element loop).
+* ``change_logits``, ``changed_logprobs``, ``changed_logprobs_grad``  pinned
+  (hand-made rows, float64 autograd, finite differences, ``logprobs``).
 """
 
 from .logprobs import bf16_to_f64, logits, logprobs  # noqa: F401
 from .grads import logit_grads, logprob_grads  # noqa: F401
 from .mismatch import mismatch, mismatch_seq  # noqa: F401
+from .mxfp4 import (mxfp4_code_values, mxfp4_logits, mxfp4_pack, mxfp4_quantize, mxfp4_unpack,  # noqa: F401
+                    mxfp4_values)
 from .ppo import ppo_loss  # noqa: F401
 from .rmsnorm import f64_to_bf16_bits, rmsnorm, rmsnorm_grads, round_bf16  # noqa: F401
+from .rules import change_logits, changed_logprobs, changed_logprobs_grad  # noqa: F401

@@ -10,8 +10,10 @@ library is missing or no GPU is present the calls raise.
 from __future__ import annotations
 
 import ctypes
+import dataclasses
 import enum
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -50,6 +52,16 @@ class TimError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{msg} (status {status})")
         self.status = Status(status)
+
+
+class _LogitRules(ctypes.Structure):
+    """tim_logit_rules"""
+    _fields_ = [("history", ctypes.c_void_p), ("history_len", ctypes.c_int64), ("hist_begin", ctypes.c_void_p),
+                ("hist_split", ctypes.c_void_p), ("hist_end", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
+                ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p), ("bias_ids", ctypes.c_void_p),
+                ("bias_values", ctypes.c_void_p), ("bias_len", ctypes.c_int64), ("bias_begin", ctypes.c_void_p),
+                ("bias_end", ctypes.c_void_p), ("mask", ctypes.c_void_p), ("n_masks", ctypes.c_int64),
+                ("mask_ld", ctypes.c_int64), ("mask_rows", ctypes.c_void_p)]
 
 
 _lib = None
@@ -114,6 +126,29 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.tim_logits.restype = c.c_int
     lib.tim_logits.argtypes = [c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int32, c.c_float,
                                c.c_int32, c.c_void_p, c.c_void_p]
+    lib.tim_mxfp4_quantize.restype = c.c_int
+    lib.tim_mxfp4_quantize.argtypes = [c.c_void_p, c.c_int32, c.c_int64, c.c_int32, c.c_int64, c.c_void_p, c.c_void_p,
+                                       c.c_void_p]
+    lib.tim_mxfp4_dequantize.restype = c.c_int
+    lib.tim_mxfp4_dequantize.argtypes = [c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_void_p, c.c_int32,
+                                         c.c_void_p]
+    lib.tim_mxfp4_logits.restype = c.c_int
+    lib.tim_mxfp4_logits.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int32,
+                                     c.c_float, c.c_void_p, c.c_int32, c.c_int64, c.c_void_p]
+    rules = c.POINTER(_LogitRules)
+    lib.tim_logits_adjust.restype = c.c_int
+    lib.tim_logits_adjust.argtypes = [c.c_void_p, c.c_int32, c.c_int64, c.c_int32, c.c_int64, rules, c.c_float,
+                                      c.c_void_p, c.c_int64, c.c_void_p]
+    lib.tim_logits_logprobs_workspace_size.restype = c.c_size_t
+    lib.tim_logits_logprobs_workspace_size.argtypes = [c.c_int64, c.c_int32]
+    lib.tim_logits_logprobs.restype = c.c_int
+    lib.tim_logits_logprobs.argtypes = [c.c_void_p, c.c_int32, c.c_int64, c.c_int32, c.c_int64, c.c_void_p, rules,
+                                        c.c_float, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t,
+                                        c.c_void_p]
+    lib.tim_logits_logprobs_backward.restype = c.c_int
+    lib.tim_logits_logprobs_backward.argtypes = [c.c_void_p, c.c_int32, c.c_int64, c.c_int32, c.c_int64, c.c_void_p,
+                                                 rules, c.c_float, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
+                                                 c.c_void_p, c.c_int32, c.c_int64, c.c_void_p]
     lib.tim_status_string.restype = c.c_char_p
     lib.tim_status_string.argtypes = [c.c_int]
     _lib = lib
@@ -470,4 +505,299 @@ def ppo_loss(logp: torch.Tensor, logp_old: torch.Tensor, advantages: torch.Tenso
                             float(eps_low), float(eps_high), _ptr(out["seq_loss"]), _ptr(out["batch_loss"]),
                             _ptr(out["token_loss"]), _ptr(out["grad"]), _ptr(out["contribution"]),
                             _ptr(out["clipped"]), _stream(dev)))
+    return out
+
+
+# ------------------------------------------------------------------ the distribution a rollout engine samples from
+# (include/tim_policy.h)
+
+MXFP4_BLOCK = 32  # TIM_MXFP4_BLOCK
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # TIM_F32, TIM_BF16, TIM_F16
+
+
+def _on_one_gpu(name, device, *tensors):
+    """The operators below take tensors of one GPU, whatever the current one is."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device != device):
+            raise ValueError(f"tim.{name}: tensors must be on one GPU")
+
+
+def _launch(device, call, *args):
+    """call(*args, stream) on the device's current stream, with the device current while it launches."""
+    if torch.cuda.current_device() == device.index:
+        _check(call(*args, _stream(device)))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, _stream(device)))
+
+
+def _row_stride(t) -> int:
+    """Elements from row to row of a [rows, n] tensor (a lone row's stride means nothing)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _dense_rows(name, what, t):
+    """Refuses all but a matrix of dense rows that do not share elements."""
+    if t.dim() != 2:
+        raise ValueError(f"tim.{name}: {what} must be a matrix")
+    if t.numel() and ((t.shape[1] > 1 and t.stride(1) != 1) or _row_stride(t) < t.shape[1]):
+        raise ValueError(f"tim.{name}: {what} must have dense rows that do not overlap")
+
+
+class Mxfp4(NamedTuple):
+    """Rows in 4-bit microscaled floating point: codes uint8 [rows, d / 2] (element 2j in the low half of byte j)
+    and scales uint8 [rows, d / 32]; element k stands for E2M1(code) * 2^(scale of block k // 32 - 127)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+def _mxfp4_shape(name, q) -> tuple[int, int]:
+    if q.codes.dtype != torch.uint8 or q.scales.dtype != torch.uint8:
+        raise TypeError(f"tim.{name}: codes and scales must be uint8")
+    if q.codes.dim() != 2 or q.scales.dim() != 2:
+        raise ValueError(f"tim.{name}: codes [rows, d / 2] and scales [rows, d / 32]")
+    rows, d = q.codes.shape[0], 2 * q.codes.shape[1]
+    if d % MXFP4_BLOCK or tuple(q.scales.shape) != (rows, d // MXFP4_BLOCK):
+        raise ValueError(f"tim.{name}: codes [rows, d / 2] and scales [rows, d / 32]")
+    _require_gpu(q.codes, q.scales)
+    return rows, d
+
+
+def mxfp4_quantize(x: torch.Tensor, out: Mxfp4 | None = None) -> Mxfp4:
+    """4-bit microscaled rows of x (fp32, bf16 or fp16 [rows, d], dense rows, d a multiple of 32): each block of 32
+    gets the scale 2^(floor(log2 max|x|) - 2) and its elements the nearest E2M1 values (see include/tim_policy.h)."""
+    lib = load_library()
+    if x.dtype not in _DTYPES:
+        raise TypeError("tim.mxfp4_quantize: x must be fp32, bf16 or fp16")
+    _dense_rows("mxfp4_quantize", "x", x)
+    rows, d = x.shape
+    if d < MXFP4_BLOCK or d % MXFP4_BLOCK:
+        raise ValueError("tim.mxfp4_quantize: d must be a multiple of 32")
+    if out is None:
+        out = Mxfp4(torch.empty((rows, d // 2), dtype=torch.uint8, device=x.device),
+                    torch.empty((rows, d // MXFP4_BLOCK), dtype=torch.uint8, device=x.device))
+    elif _mxfp4_shape("mxfp4_quantize", out) != (rows, d):
+        raise ValueError("tim.mxfp4_quantize: out must hold [rows, d]")
+    _on_one_gpu("mxfp4_quantize", x.device, x, *out)
+    _launch(x.device, lib.tim_mxfp4_quantize, _ptr(x), _DTYPES[x.dtype], rows, d, _row_stride(x), _ptr(out.codes),
+            _ptr(out.scales))
+    return out
+
+
+def mxfp4_dequantize(q: Mxfp4, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values the codes stand for, exactly, as bf16 or fp32 [rows, d]."""
+    lib = load_library()
+    rows, d = _mxfp4_shape("mxfp4_dequantize", q)
+    if out is not None:
+        dtype = out.dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("tim.mxfp4_dequantize: values are bf16 or fp32")
+    if d == 0:
+        raise ValueError("tim.mxfp4_dequantize: d must be a multiple of 32")
+    if out is None:
+        out = torch.empty((rows, d), dtype=dtype, device=q.codes.device)
+    elif out.shape != (rows, d):
+        raise ValueError("tim.mxfp4_dequantize: out must be [rows, d]")
+    _require_gpu(out)
+    _on_one_gpu("mxfp4_dequantize", q.codes.device, *q, out)
+    _launch(q.codes.device, lib.tim_mxfp4_dequantize, _ptr(q.codes), _ptr(q.scales), rows, d, _ptr(out),
+            _DTYPES[dtype])
+    return out
+
+
+def mxfp4_logits(hidden: Mxfp4, w_vocab: Mxfp4, temperature: float = 1.0, dtype: torch.dtype = torch.float32,
+                 out: torch.Tensor | None = None) -> torch.Tensor:
+    """[T, V] logits of 4-bit hidden rows [T, d] against a 4-bit head [V, d] (d a multiple of 128), accumulated in
+    fp32 and rounded once to dtype (fp32, bf16 or fp16). out, if given, may have padded rows."""
+    lib = load_library()
+    T, d = _mxfp4_shape("mxfp4_logits", hidden)
+    V, dw = _mxfp4_shape("mxfp4_logits", w_vocab)
+    if d != dw:
+        raise ValueError("tim.mxfp4_logits: hidden [T, d] and w_vocab [V, d] must share d")
+    dev = hidden.codes.device
+    if out is None:
+        out = torch.empty((T, V), dtype=dtype, device=dev)
+    elif out.shape != (T, V):
+        raise ValueError("tim.mxfp4_logits: out must be [T, V]")
+    if out.dtype not in _DTYPES:
+        raise TypeError("tim.mxfp4_logits: logits are fp32, bf16 or fp16")
+    _dense_rows("mxfp4_logits", "out", out)
+    _on_one_gpu("mxfp4_logits", dev, *hidden, *w_vocab, out)
+    _launch(dev, lib.tim_mxfp4_logits, _ptr(hidden.codes), _ptr(hidden.scales), _ptr(w_vocab.codes),
+            _ptr(w_vocab.scales), T, d, V, float(temperature), _ptr(out), _DTYPES[out.dtype], _row_stride(out))
+    return out
+
+
+@dataclasses.dataclass
+class LogitRules:
+    """What changes the logits of T rows before sampling (tim_logit_rules in include/tim_policy.h); leave out what
+    does not apply. All tensors on the logits' GPU.
+
+    history int32 [N] tokens; row i's are history[hist_begin[i]:hist_end[i]], generated from hist_split[i] on
+    (int64 [T] each; no hist_split: all generated). repetition divides positive and multiplies other logits of
+    tokens in the history, frequency is subtracted per occurrence in the generated part, presence once (fp32 [T]).
+    bias_ids int32 [M] and bias_values fp32 [M]; row i adds the entries bias_begin[i]:bias_end[i] (int64 [T]; of an
+    id listed twice the last). mask int32 [n, >= ceil(V / 32)], bit v % 32 of word v // 32 set where v is allowed;
+    row i takes mask mask_rows[i] (int32 [T], outside [0, n): none) or, without mask_rows, mask i."""
+    history: torch.Tensor | None = None
+    hist_begin: torch.Tensor | None = None
+    hist_split: torch.Tensor | None = None
+    hist_end: torch.Tensor | None = None
+    repetition: torch.Tensor | None = None
+    frequency: torch.Tensor | None = None
+    presence: torch.Tensor | None = None
+    bias_ids: torch.Tensor | None = None
+    bias_values: torch.Tensor | None = None
+    bias_begin: torch.Tensor | None = None
+    bias_end: torch.Tensor | None = None
+    mask: torch.Tensor | None = None
+    mask_rows: torch.Tensor | None = None
+
+    def _struct(self, name, T, V, device) -> _LogitRules:
+        s = _LogitRules()
+
+        def take(field, dtype, n=None):
+            t = getattr(self, field)
+            if t is None:
+                return
+            if t.dtype != dtype:
+                raise TypeError(f"tim.{name}: {field} must be {dtype}")
+            if t.dim() != 1 or (n is not None and t.shape[0] != n):
+                raise ValueError(f"tim.{name}: {field} must be a vector" + ("" if n is None else " of one value a row"))
+            if t.device != device:
+                raise ValueError(f"tim.{name}: tensors must be on one GPU")
+            if not t.is_contiguous():
+                raise ValueError(f"tim.{name}: {field} must be contiguous")
+            setattr(s, field, t.data_ptr())
+
+        if self.history is not None:
+            if self.hist_begin is None or self.hist_end is None:
+                raise ValueError(f"tim.{name}: history needs hist_begin and hist_end")
+            take("history", torch.int32)
+            s.history_len = self.history.shape[0]
+            for f in ("hist_begin", "hist_split", "hist_end"):
+                take(f, torch.int64, T)
+        for f in ("repetition", "frequency", "presence"):
+            take(f, torch.float32, T)
+        if self.bias_ids is not None:
+            if self.bias_values is None or self.bias_begin is None or self.bias_end is None:
+                raise ValueError(f"tim.{name}: bias_ids needs bias_values, bias_begin and bias_end")
+            take("bias_ids", torch.int32)
+            s.bias_len = self.bias_ids.shape[0]
+            take("bias_values", torch.float32, s.bias_len)
+            take("bias_begin", torch.int64, T)
+            take("bias_end", torch.int64, T)
+        if self.mask is not None:
+            if self.mask.dtype != torch.int32:
+                raise TypeError(f"tim.{name}: mask must be torch.int32")
+            _dense_rows(name, "mask", self.mask)
+            if self.mask.device != device:
+                raise ValueError(f"tim.{name}: tensors must be on one GPU")
+            if self.mask.shape[1] < (V + 31) // 32:
+                raise ValueError(f"tim.{name}: mask must have ceil(V / 32) words a row")
+            if self.mask_rows is None and self.mask.shape[0] != T:
+                raise ValueError(f"tim.{name}: without mask_rows there is one mask a row")
+            s.mask, s.n_masks, s.mask_ld = self.mask.data_ptr(), self.mask.shape[0], _row_stride(self.mask)
+            take("mask_rows", torch.int32, T)
+        return s
+
+
+def _changed(name, logits, rules):
+    """(T, V, C rules or None) of the operators on changed logits."""
+    if logits.dtype not in _DTYPES:
+        raise TypeError(f"tim.{name}: logits must be fp32, bf16 or fp16")
+    _dense_rows(name, "logits", logits)
+    if not logits.is_cuda:
+        raise ValueError("tim: tensors must be on the GPU")
+    T, V = logits.shape
+    return T, V, None if rules is None else ctypes.byref(rules._struct(name, T, V, logits.device))
+
+
+def _row_vector(name, what, t, T, dtype):
+    if t is None:
+        return
+    if t.dtype != dtype:
+        raise TypeError(f"tim.{name}: {what} must be {dtype}")
+    if t.shape != (T,):
+        raise ValueError(f"tim.{name}: {what} must be [T]")
+    _require_gpu(t)
+
+
+def logits_adjust(logits: torch.Tensor, rules: LogitRules | None = None, temperature: float = 1.0,
+                  out: torch.Tensor | None = None) -> torch.Tensor:
+    """The logits [T, V] (fp32, bf16 or fp16, dense rows) as a sampler reads them: penalties, bias, temperature and
+    mask applied, each entry rounded once to the logits' type. out may be logits itself (in place)."""
+    lib = load_library()
+    T, V, r = _changed("logits_adjust", logits, rules)
+    if out is None:
+        out = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+    if out.shape != (T, V) or out.dtype != logits.dtype:
+        raise ValueError("tim.logits_adjust: out must be like logits")
+    _dense_rows("logits_adjust", "out", out)
+    _on_one_gpu("logits_adjust", logits.device, logits, out)
+    _launch(logits.device, lib.tim_logits_adjust, _ptr(logits), _DTYPES[logits.dtype], T, V, _row_stride(logits), r,
+            float(temperature), _ptr(out), _row_stride(out))
+    return out
+
+
+def logits_logprobs_workspace_size(T: int, V: int) -> int:
+    """Bytes of workspace tim_logits_logprobs needs (0 for T == 0 or invalid shapes)."""
+    return int(load_library().tim_logits_logprobs_workspace_size(int(T), int(V)))
+
+
+def logits_logprobs(logits: torch.Tensor, tokens: torch.Tensor, rules: LogitRules | None = None,
+                    temperature: float = 1.0, entropy: bool = True, lse: bool = False,
+                    workspace: torch.Tensor | None = None, out: tuple | None = None):
+    """Log-probabilities (and entropies, log-normalisers) of tokens int32 [T] under the changed logits of
+    logits_adjust, from the logits themselves. Returns (logp, entropy or None, lse or None), fp32 [T] each."""
+    lib = load_library()
+    T, V, r = _changed("logits_logprobs", logits, rules)
+    dev = logits.device
+    _row_vector("logits_logprobs", "tokens", tokens, T, torch.int32)
+    if out is None:
+        lp = torch.empty(T, dtype=torch.float32, device=dev)
+        ent = torch.empty(T, dtype=torch.float32, device=dev) if entropy else None
+        ls = torch.empty(T, dtype=torch.float32, device=dev) if lse else None
+    else:
+        lp, ent, ls = out
+        for what, t in (("logp", lp), ("entropy", ent), ("lse", ls)):
+            _row_vector("logits_logprobs", what, t, T, torch.float32)
+    if T == 0:
+        return lp, ent, ls
+    if workspace is None:
+        workspace = torch.empty(logits_logprobs_workspace_size(T, V), dtype=torch.uint8, device=dev)
+    _require_gpu(workspace)
+    _on_one_gpu("logits_logprobs", dev, tokens, lp, ent, ls, workspace)
+    _launch(dev, lib.tim_logits_logprobs, _ptr(logits), _DTYPES[logits.dtype], T, V, _row_stride(logits), _ptr(tokens),
+            r, float(temperature), _ptr(lp), _ptr(ent), _ptr(ls), _ptr(workspace),
+            workspace.numel() * workspace.element_size())
+    return lp, ent, ls
+
+
+def logits_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: torch.Tensor, grad_logp: torch.Tensor,
+                             rules: LogitRules | None = None, temperature: float = 1.0,
+                             entropy: torch.Tensor | None = None, grad_entropy: torch.Tensor | None = None,
+                             dtype: torch.dtype | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient [T, V] of sum_t grad_logp[t] logp[t] + grad_entropy[t] entropy[t] with respect to the logits, through
+    the changes. lse (and entropy, when grad_entropy is given) are logits_logprobs' outputs for the same inputs.
+    dtype (the logits' by default) is the gradient's type; out may be logits itself where the types agree."""
+    lib = load_library()
+    T, V, r = _changed("logits_logprobs_backward", logits, rules)
+    dev = logits.device
+    _row_vector("logits_logprobs_backward", "tokens", tokens, T, torch.int32)
+    for what, t in (("lse", lse), ("grad_logp", grad_logp), ("entropy", entropy), ("grad_entropy", grad_entropy)):
+        _row_vector("logits_logprobs_backward", what, t, T, torch.float32)
+    if out is None:
+        out = torch.empty((T, V), dtype=logits.dtype if dtype is None else dtype, device=dev)
+    elif dtype is not None and out.dtype != dtype:
+        raise ValueError("tim.logits_logprobs_backward: out must have the dtype asked for")
+    if out.dtype not in _DTYPES:
+        raise TypeError("tim.logits_logprobs_backward: the gradient is fp32, bf16 or fp16")
+    if out.shape != (T, V):
+        raise ValueError("tim.logits_logprobs_backward: out must be [T, V]")
+    _dense_rows("logits_logprobs_backward", "out", out)
+    _on_one_gpu("logits_logprobs_backward", dev, tokens, lse, grad_logp, entropy, grad_entropy, out)
+    _launch(dev, lib.tim_logits_logprobs_backward, _ptr(logits), _DTYPES[logits.dtype], T, V, _row_stride(logits),
+            _ptr(tokens), r, float(temperature), _ptr(lse), _ptr(entropy), _ptr(grad_logp), _ptr(grad_entropy),
+            _ptr(out), _DTYPES[out.dtype], _row_stride(out))
     return out
