@@ -44,6 +44,8 @@ typedef enum {
  *   scales uint8 [rows, d / 32] row-major
  */
 #define TIM_MXFP4_BLOCK 32
+/* Largest d of tim_mxfp4_logits. */
+#define TIM_MXFP4_MAX_D (1 << 20)
 
 /* Quantises rows of d elements (d a positive multiple of 32). Per block, with
  * top = max |x|:
@@ -69,8 +71,8 @@ tim_status tim_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int
 
 /* Logits of a quantised head, as tim_logits forms them for a bf16 one:
  *   logits[t, v] = (sum_k h[t, k] w[v, k]) * (float)(1 / temperature)
- * for MXFP4 h [T, d] and w [V, d] (d a positive multiple of 128), written as
- * dtype [T, V], row t at logits + t * ld elements, ld >= V.
+ * for MXFP4 h [T, d] and w [V, d] (d a positive multiple of 128, at most
+ * TIM_MXFP4_MAX_D), written as dtype [T, V], row t at logits + t * ld elements, ld >= V.
  *
  * Arithmetic: the products of 4-bit codes with their scales on the matrix
  * cores, accumulated in fp32 with one chain per logit in an order that depends

@@ -1,15 +1,11 @@
-// 4-bit microscaled floating point on gfx950: quantisation, the values of the
-// codes, and the logits of a quantised head.
+// 4-bit microscaled floating point on gfx950: quantisation and the values of
+// the codes.
 //
 // Quantisation: 2^E = 2^(floor(log2 top) - 2) places a block's largest
 // magnitude in [4, 8), the upper binade of E2M1; x 2^-E is exact in fp32, and
 // the conversion to E2M1 is the hardware's (nearest even, saturating at 6).
 // HBM-bound: 2 bytes read and 17/32 written per bf16 element. Four lanes share
 // a block, so a wave reads and writes consecutive memory.
-//
-// Product: v_mfma_scale_f32_16x16x128_f8f6f4 on 4-bit operands, W as its first
-// operand: lane l holds 32 elements, one scale block, of row l % 16, and its
-// four results are consecutive vocabulary entries of one hidden row.
 
 #include <hip/hip_runtime.h>
 
@@ -18,10 +14,6 @@
 
 namespace tim {
 namespace {
-
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kGroup = 8;       // elements of one lane: a quarter of a block
@@ -114,43 +106,6 @@ __global__ __launch_bounds__(kThreads) void dequantise(const uint8_t* __restrict
   }
 }
 
-__device__ __forceinline__ f32x4 mfma_fp4(i32x4 a, int sa, i32x4 b, int sb, f32x4 c) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  const i32x8 a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
-  const i32x8 b8 = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, 0, sa, 0, sb);
-#else
-  return c;
-#endif
-}
-
-// One wave per 16 vocabulary entries and 16 hidden rows.
-template <class T>
-__global__ __launch_bounds__(256) void mxfp4_product(const Mxfp4LogitsArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int v0 = ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)) * 16;
-  const int64_t t0 = (int64_t)blockIdx.y * 16;
-  if (v0 >= a.V) return;
-  const int r = lane & 15, q = lane >> 4;
-  // rows past the end repeat the last one; their results are not written
-  const int64_t w = v0 + r < a.V ? v0 + r : a.V - 1;
-  const int64_t h = t0 + r < a.T ? t0 + r : a.T - 1;
-  const uint8_t* wc = a.w_codes + w * (a.d / 2) + q * 16;
-  const uint8_t* hc = a.h_codes + h * (a.d / 2) + q * 16;
-  const uint8_t* ws = a.w_scales + w * (a.d / 32) + q;
-  const uint8_t* hs = a.h_scales + h * (a.d / 32) + q;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < a.d / 128; ++k)
-    acc = mfma_fp4(*(const i32x4*)(wc + k * 64), ws[k * 4], *(const i32x4*)(hc + k * 64), hs[k * 4], acc);
-  if (t0 + r >= a.T) return;
-  T* out = (T*)a.logits + (t0 + r) * a.ld;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int v = v0 + 4 * q + i;
-    if (v < a.V) out[v] = narrow<T>(acc[i] * a.inv_tau);
-  }
-}
-
 template <class T>
 hipError_t quantise_as(const void* x, int64_t rows, int d, int64_t ld, uint8_t* codes, uint8_t* scales,
                        hipStream_t s) {
@@ -179,23 +134,6 @@ hipError_t dequantise_as(const uint8_t* codes, const uint8_t* scales, int64_t ro
   return hipSuccess;
 }
 
-template <class T>
-hipError_t product_as(const Mxfp4LogitsArgs& a, hipStream_t s) {
-  const int64_t across = (a.V + 63) / 64;  // at most 8192
-  const int64_t rows = kLaunchBlocks / across < 65535 ? kLaunchBlocks / across * 16 : 65535 * 16;
-  for (int64_t t0 = 0; t0 < a.T; t0 += rows) {
-    Mxfp4LogitsArgs b = a;
-    b.T = a.T - t0 < rows ? a.T - t0 : rows;
-    b.h_codes = a.h_codes + t0 * (a.d / 2);
-    b.h_scales = a.h_scales + t0 * (a.d / 32);
-    b.logits = (T*)a.logits + t0 * a.ld;
-    mxfp4_product<T><<<dim3((unsigned)across, (unsigned)((b.T + 15) / 16)), 256, 0, s>>>(b);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
-}
-
 }  // namespace
 
 hipError_t launch_mxfp4_quantize(const void* x, int dtype, int64_t rows, int d, int64_t ld, uint8_t* codes,
@@ -209,12 +147,6 @@ hipError_t launch_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, 
                                    int dtype, hipStream_t s) {
   if (dtype == TIM_F32) return dequantise_as<float>(codes, scales, rows, d, out, s);
   return dequantise_as<__bf16>(codes, scales, rows, d, out, s);
-}
-
-hipError_t launch_mxfp4_logits(const Mxfp4LogitsArgs& a, int dtype, hipStream_t s) {
-  if (dtype == TIM_F32) return product_as<float>(a, s);
-  if (dtype == TIM_BF16) return product_as<__bf16>(a, s);
-  return product_as<_Float16>(a, s);
 }
 
 }  // namespace tim

@@ -45,7 +45,7 @@ inline tim_status validate_mxfp4_logits(const uint8_t* h_codes, const uint8_t* h
   if (!h_codes || !h_scales || !w_codes || !w_scales || !logits) return TIM_ERR_NULL;
   const tim_status s = check_shape(T, d, V, TIM_ORDER_INVARIANT);
   if (s != TIM_OK) return s;
-  if (ld < V) return TIM_ERR_SHAPE;
+  if (d > TIM_MXFP4_MAX_D || ld < V) return TIM_ERR_SHAPE;
   if (!positive_finite(temperature) || !valid_dtype(dtype)) return TIM_ERR_VALUE;
   if (!aligned16(h_codes) || !aligned16(w_codes) || !aligned_to(h_scales, 4) || !aligned_to(w_scales, 4) ||
       !aligned_to(logits, dtype_bytes(dtype)))

@@ -96,7 +96,7 @@ def _product(lib, hc=FAKE, hs=FAKE, wc=FAKE, ws=FAKE, T=4, d=256, V=100, tau=1.0
 
 @pytest.mark.parametrize("kw,expect", [
     (dict(T=-1), Status.ERR_SHAPE), (dict(d=0), Status.ERR_SHAPE), (dict(d=64), Status.ERR_SHAPE),
-    (dict(d=192), Status.ERR_SHAPE), (dict(V=0), Status.ERR_SHAPE), (dict(V=2048 * 256 + 1, ld=1 << 20), Status.ERR_SHAPE),
+    (dict(d=192), Status.ERR_SHAPE), (dict(d=2 ** 20 + 128), Status.ERR_SHAPE), (dict(V=0), Status.ERR_SHAPE), (dict(V=2048 * 256 + 1, ld=1 << 20), Status.ERR_SHAPE),
     (dict(ld=99), Status.ERR_SHAPE), (dict(tau=0.0), Status.ERR_VALUE), (dict(tau=float("nan")), Status.ERR_VALUE),
     (dict(tau=float("inf")), Status.ERR_VALUE), (dict(tau=-1.0), Status.ERR_VALUE), (dict(dtype=3), Status.ERR_VALUE),
     (dict(hc=None), Status.ERR_NULL), (dict(hs=None), Status.ERR_NULL), (dict(wc=None), Status.ERR_NULL),
