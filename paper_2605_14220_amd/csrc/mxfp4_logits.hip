@@ -9,9 +9,16 @@
 // depend on the shape.
 //
 // A stage is 256 elements of the tile's rows: 128 bytes of codes per row, DMA
-// loaded into LDS and XOR-swizzled as in tilepass.h, and 8 scale bytes per
-// row beside them. Few rows are bound by the stream of W; many by the MFMAs
-// and, with them, by the fp32 logits going out.
+// loaded into LDS and XOR-swizzled as in tilepass.h. Scales are few bytes but
+// many requests: 8 bytes a row and stage in 4-byte loads cost 2000 rows at
+// d = 4096 a fifth of their time, and reading a row's four bytes to use one of
+// them a tenth. So they come in groups of 512 elements, 16 bytes a row, and
+// the wave that loaded a row's group turns it (a 4 x 4 transpose of bytes), so
+// that a lane reads the four bytes of its block column with one ds_read_b32
+// and the MFMA picks the k-step's by its byte select.
+//
+// Few rows are bound by the stream of W; many by the MFMAs, the LDS reads
+// that feed them, and the fp32 logits going out.
 
 #include <hip/hip_runtime.h>
 
@@ -22,12 +29,12 @@
 namespace tim {
 namespace {
 
-typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStageCodes = 128;  // bytes of a row's codes in a stage (two k-steps)
-constexpr int kStageScales = 8;   // and of its scales
+constexpr int kGroupScales = 16;  // bytes of a row's scales in a group (two stages)
+constexpr int kMinD = 512;        // a row holds a whole group
 
 // A workgroup of WV x WT waves, each NA x NB blocks of 16 x 16, and PER_CU
 // workgroups on a CU.
@@ -37,23 +44,31 @@ struct Fp4Tile {
   static constexpr int NW = WV * WT;
   static constexpr int TA = WV * NA * 16;  // vocabulary entries
   static constexpr int TB = WT * NB * 16;  // hidden rows
-  // DMA loads of a stage: 1 KB of codes (8 rows) or 256 bytes of scales (32 rows) each
-  static constexpr int CA = TA / 8, CB = TB / 8, SA = (TA + 31) / 32, SC = (TB + 31) / 32;
-  // Stage layout: W codes, hidden codes, W scales, hidden scales
-  static constexpr int kCodesB = CA * 1024, kScalesA = kCodesB + CB * 1024, kScalesB = kScalesA + SA * 256;
-  static constexpr int SB = kScalesB + SC * 256;
-  static constexpr int FIT = 160 * 1024 / PER_CU / SB;
-  static constexpr int NBUF = FIT < 8 ? FIT : 8;
-  // Loads per wave, each kind dealt round the waves; a kind that does not fill its last round has blocks loaded
-  // twice (with the same bytes)
-  static constexpr int LA = (CA + NW - 1) / NW, LB = (CB + NW - 1) / NW, XA = (SA + NW - 1) / NW,
-                       XB = (SC + NW - 1) / NW;
-  static constexpr int L = LA + LB + XA + XB;
+  // DMA loads of 1 KB: of a stage's codes (8 rows each), and of a group's scales (64 rows each)
+  static constexpr int CA = TA / 8, CB = TB / 8, SA = (TA + 63) / 64, SC = (TB + 63) / 64;
+  // per wave, each kind dealt round the waves; a kind of codes that does not fill its last round has blocks loaded
+  // twice (with the same bytes), scales that do not have loads into a spare KB
+  static constexpr int LA = (CA + NW - 1) / NW, LB = (CB + NW - 1) / NW, LX = (SA + SC + NW - 1) / NW;
+  static constexpr int L = LA + LB;
+  static constexpr int kCodesB = CA * 1024;
+  static constexpr int SB = kCodesB + CB * 1024;  // a stage buffer: W codes, hidden codes
+  static constexpr int XB = (SA + SC) * 1024;     // a group's scales: W, hidden
+  static constexpr int kSpare = (SA + SC) % NW ? 1024 : 0;
+  // NBUF stages and SBUF groups: group j + 1 is requested with stage 2 j + 1, NBUF stages ahead, into the buffer
+  // of group j + 1 - SBUF, whose last reads are in stage 2 (j + 1 - SBUF) - 1
+  static constexpr int lds_bytes(int n) { return n * SB + (n / 2 + 1) * XB + kSpare; }
+  static constexpr int kRoom = 160 * 1024 / PER_CU;
+  static constexpr int NBUF = lds_bytes(6) <= kRoom ? 6 : lds_bytes(5) <= kRoom ? 5 : lds_bytes(4) <= kRoom ? 4
+                              : lds_bytes(3) <= kRoom                                                       ? 3
+                                                                                                            : 2;
+  static constexpr int SBUF = NBUF / 2 + 1;
+  static constexpr int kScales = NBUF * SB, kSpareAt = kScales + SBUF * XB;
+  static constexpr int LDS = kSpareAt + kSpare;
   static_assert(NW % 2 == 0, "a wave's blocks of 8 rows are all even or all odd ones, so one swizzle serves them");
-  static_assert(NBUF >= 2, "double buffering at least");
+  static_assert(LDS <= kRoom, "double buffering at least");
 };
 
-// a += the product of one k-step, the scales in byte S of sa and sb.
+// c + the product of one k-step, the scales in byte S of sa and sb.
 template <int S>
 __device__ __forceinline__ f32x4 mfma_fp4(i32x4 a, int sa, i32x4 b, int sb, f32x4 c) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -65,15 +80,32 @@ __device__ __forceinline__ f32x4 mfma_fp4(i32x4 a, int sa, i32x4 b, int sb, f32x
 #endif
 }
 
+// Four consecutive logits from v on, as far as they lie in the vocabulary.
+template <class T>
+__device__ __forceinline__ void store_logits(T* row, int v, int V, const f32x4& acc, float inv_tau) {
+  T z[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) z[e] = narrow<T>(acc[e] * inv_tau);
+  if (v + 4 <= V) {
+    __builtin_memcpy(row + v, z, sizeof(z));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (v + e < V) row[v + e] = z[e];
+  }
+}
+
 // Where a tile's stages come from: the operands' resources, each over the
 // tile's own rows, so that loads of rows past its end return zeros (the range
-// is checked on the per-lane offsets; the stage is in the scalar offset), and
-// the lane's offsets within the first round of loads. The last stage of an odd
-// number of k-steps holds one: its second half would lie in the next row, or
-// past the last one, and repeats the first half instead.
+// is checked on the per-lane offsets; the place along the row is in the scalar
+// offset), and the lane's offsets within the first round of loads. The last
+// stage of an odd number of k-steps holds one: its second half would lie in the
+// next row, or past the last one, and repeats the first half instead; the last
+// group of a row that is no whole number of them starts where it ends with the
+// row, and is moved down as it is turned.
 struct Fp4Source {
   rsrc_t ac, bc, as, bs;  // codes and scales of W and of the hidden rows
-  int code, code_tail, scale, scale_tail;
+  int code, code_tail, scale;
   int rowc, rows;         // bytes of a row's codes and scales
 };
 
@@ -91,111 +123,150 @@ __device__ __forceinline__ Fp4Source fp4_source(const Mxfp4LogitsArgs& a, int v0
   const int r = wave * 8 + (lane >> 3), c = (lane & 7) ^ swz(r);
   o.code = (lane >> 3) * o.rowc + c * 16;
   o.code_tail = (lane >> 3) * o.rowc + (c & 3) * 16;
-  o.scale_tail = (lane >> 1) * o.rows;
-  o.scale = o.scale_tail + (lane & 1) * 4;
+  o.scale = lane * o.rows;
   return o;
 }
 
-// Load q of a wave's request of a stage into `buf`.
+// Load q of a wave's request of a stage's codes into `buf`.
 template <class TL>
 __device__ __forceinline__ void fp4_load(unsigned char* buf, const Fp4Source& o, int stage, bool tail, int wave, int q) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  // block b of kind of n: past the last one, a block of an earlier round (for NW even, of the same parity)
+  // block b of n of a kind: past the last one, a block of an earlier round (for NW even, of the same parity)
   auto block = [wave](int j, int n) {
     const int b = j * TL::NW + wave;
-    return n % TL::NW == 0 || b < n ? b : n >= TL::NW ? b - TL::NW : n >= 2 ? (wave & 1) : 0;
+    return n % TL::NW == 0 || b < n ? b : n >= TL::NW ? b - TL::NW : (wave & 1);
   };
-  const int code = tail ? o.code_tail : o.code, scale = tail ? o.scale_tail : o.scale;
-  if (q < TL::LA) {
-    const int b = block(q, TL::CA);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(o.ac, (lds_void*)(buf + b * 1024), 16, (uint32_t)(code + b * 8 * o.rowc),
-                                             stage * kStageCodes, 0, 0);
-  } else if (q < TL::LA + TL::LB) {
-    const int b = block(q - TL::LA, TL::CB);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(o.bc, (lds_void*)(buf + TL::kCodesB + b * 1024), 16,
-                                             (uint32_t)(code + b * 8 * o.rowc), stage * kStageCodes, 0, 0);
-  } else if (q < TL::LA + TL::LB + TL::XA) {
-    const int b = block(q - TL::LA - TL::LB, TL::SA);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(o.as, (lds_void*)(buf + TL::kScalesA + b * 256), 4,
-                                             (uint32_t)(scale + b * 32 * o.rows), stage * kStageScales, 0, 0);
-  } else {
-    const int b = block(q - TL::LA - TL::LB - TL::XA, TL::SC);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(o.bs, (lds_void*)(buf + TL::kScalesB + b * 256), 4,
-                                             (uint32_t)(scale + b * 32 * o.rows), stage * kStageScales, 0, 0);
-  }
+  const int code = tail ? o.code_tail : o.code;
+  const bool first = q < TL::LA;
+  const int b = first ? block(q, TL::CA) : block(q - TL::LA, TL::CB);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(first ? o.ac : o.bc, (lds_void*)(buf + (first ? 0 : TL::kCodesB) + b * 1024),
+                                           16, (uint32_t)(code + b * 8 * o.rowc), stage * kStageCodes, 0, 0);
 #endif
 }
 
-// A wave's operands of one k-step, and the scales of the stage's two: byte 0
-// for the first k-step, byte 1 for the second. The hidden rows' codes alternate
-// between two sets by k-step; W's are refilled in place.
+// The wave's request of a group's scales into the group's buffer, and, once it
+// has landed, the turning of those rows: dword s of a row holds the four bytes
+// of k-step s, and will hold those of block column s.
+template <class TL>
+__device__ __forceinline__ void fp4_load_scales(unsigned char* lds, int slot, const Fp4Source& o, int group, int wave) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int at = 16 * group < o.rows - 16 ? 16 * group : o.rows - 16;
+#pragma unroll
+  for (int q = 0; q < TL::LX; ++q) {
+    const int b = q * TL::NW + wave;
+    unsigned char* dst = lds + (b < TL::SA + TL::SC ? TL::kScales + slot * TL::XB + b * 1024 : TL::kSpareAt);
+    const bool first = b < TL::SA;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(first ? o.as : o.bs, (lds_void*)dst, 16,
+                                             (uint32_t)(o.scale + (first ? b : b - TL::SA) * 64 * o.rows), at, 0, 0);
+  }
+#endif
+}
+template <class TL>
+__device__ __forceinline__ i32x4* fp4_turned(unsigned char* lds, int slot, int q, int wave, int lane) {
+  const int b = q * TL::NW + wave;
+  return (i32x4*)(lds + (b < TL::SA + TL::SC ? TL::kScales + slot * TL::XB + b * 1024 : TL::kSpareAt) + lane * 16);
+}
+__device__ __forceinline__ i32x4 fp4_turn(i32x4 w, int down) {
+  if (down == 1) w = {w[1], w[2], w[3], w[3]};
+  if (down == 2) w = {w[2], w[3], w[3], w[3]};
+  if (down >= 3) w = {w[3], w[3], w[3], w[3]};
+  const uint32_t lo01 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), hi01 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+  const uint32_t lo23 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), hi23 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  return {(int)__builtin_amdgcn_perm(lo23, lo01, 0x05040100u), (int)__builtin_amdgcn_perm(lo23, lo01, 0x07060302u),
+          (int)__builtin_amdgcn_perm(hi23, hi01, 0x05040100u), (int)__builtin_amdgcn_perm(hi23, hi01, 0x07060302u)};
+}
+// Dwords by which a group starts before its place.
+__device__ __forceinline__ int fp4_down(const Fp4Source& o, int group) {
+  return 16 * group < o.rows - 16 ? 0 : (16 * group - (o.rows - 16)) / 4;
+}
+
+// A wave's operands: one k-step's codes, the hidden rows' alternating between
+// two sets by k-step and W's refilled in place, and a group's scales.
 template <class TL>
 struct Fp4Operands {
   i32x4 fa[TL::NA], fb[2][TL::NB];
   int sa[TL::NA], sb[TL::NB];
 };
 
-// Addresses of a lane's operands in a stage buffer.
+// Offsets of a lane's operands within a block of 16 rows.
 struct Fp4Lane {
-  int code[2];  // k-step 0 and 1, within a block of 16 rows
+  int code[2];  // of k-step 0 and 1 of a stage
   int scale;
-  uint32_t pick;  // bytes g of two dwords
 };
 __device__ __forceinline__ Fp4Lane fp4_lane(int lane) {
   const int r = lane & 15, g = lane >> 4;
-  return {{r * kStageCodes + (g ^ swz(r)) * 16, r * kStageCodes + ((4 + g) ^ swz(r)) * 16}, r * kStageScales,
-          0x0C0C0400u + 0x0101u * (uint32_t)g};
-}
-__device__ __forceinline__ int fp4_scales(i32x2 raw, uint32_t pick) {
-  return (int)__builtin_amdgcn_perm((uint32_t)raw[1], (uint32_t)raw[0], pick);
+  return {{r * kStageCodes + (g ^ swz(r)) * 16, r * kStageCodes + ((4 + g) ^ swz(r)) * 16}, r * kGroupScales + g * 4};
 }
 
-// One k-step (P: the stage's first or second), unit by unit; with LOAD the
-// wave's share of a stage request into lb, with READ the next step's operands
-// from rb (with P = 1 the next stage's, scales too).
-template <class TL, int P, bool LOAD, bool READ>
-__device__ __forceinline__ void fp4_step(Fp4Operands<TL>& f, f32x4 (&acc)[TL::NA][TL::NB], unsigned char* lb,
-                                         const Fp4Source& o, int stage, bool tail, const unsigned char* rb,
-                                         const Fp4Lane& at, int wave, int wv, int wt) {
-  constexpr int NA = TL::NA, NB = TL::NB, NM = NA * NB, L = TL::L;
+// K-step P of a group, unit by unit, and beside it the next k-step's operands:
+// from this stage's buffer rb, or (P odd) the next one's, and after the group's
+// last k-step the next group's scales from xb. P odd also issues the wave's
+// share of a stage request into lb; P = 2 turns the next group's scales in
+// slot `turn`.
+template <class TL, int P>
+__device__ __forceinline__ void fp4_step(Fp4Operands<TL>& f, f32x4 (&acc)[TL::NA][TL::NB], unsigned char* lds,
+                                         unsigned char* lb, const Fp4Source& o, int stage, bool tail,
+                                         const unsigned char* rb, const unsigned char* xb, int turn, int down,
+                                         const Fp4Lane& at, int wave, int wv, int wt, int lane) {
+  constexpr int NA = TL::NA, NB = TL::NB, NM = NA * NB, L = TL::L, Q = P & 1;
   static_assert(NA <= NM && NB <= NM, "a unit for every read");
-  const unsigned char* ca = rb + wv * NA * 2048 + at.code[P ^ 1];
-  const unsigned char* cb = rb + TL::kCodesB + wt * NB * 2048 + at.code[P ^ 1];
-  const unsigned char* xa = rb + TL::kScalesA + wv * NA * 128 + at.scale;
-  const unsigned char* xb = rb + TL::kScalesB + wt * NB * 128 + at.scale;
-  i32x2 ra[NA], rs[NB];
+  const unsigned char* ca = rb + wv * NA * 2048 + at.code[Q ^ 1];
+  const unsigned char* cb = rb + TL::kCodesB + wt * NB * 2048 + at.code[Q ^ 1];
+  const unsigned char* xa = xb + wv * NA * 256 + at.scale;
+  const unsigned char* xt = xb + TL::SA * 1024 + wt * NB * 256 + at.scale;
+  int na[NA], nb[NB];
+  i32x4 raw[TL::LX];
 #pragma unroll
   for (int i = 0; i < NM; ++i) {
     const int bi = i / NB, bq = i % NB, bj = (bi & 1) ? NB - 1 - bq : bq;
-    acc[bi][bj] = mfma_fp4<P>(f.fa[bi], f.sa[bi], f.fb[P][bj], f.sb[bj], acc[bi][bj]);
-    if (LOAD) {
+    acc[bi][bj] = mfma_fp4<P>(f.fa[bi], f.sa[bi], f.fb[Q][bj], f.sb[bj], acc[bi][bj]);
+    if (Q == 1) {
 #pragma unroll
       for (int q = 0; q < L; ++q)
         if (q * NM / L == i) fp4_load<TL>(lb, o, stage, tail, wave, q);
     }
-    if (READ) {
-      if (i < NB) f.fb[P ^ 1][i] = *(const i32x4*)(cb + i * 2048);
-      if (bq == NB - 1) f.fa[bi] = *(const i32x4*)(ca + bi * 2048);
-      if (P == 1) {
-        if (i >= NM - NB) rs[i - (NM - NB)] = *(const i32x2*)(xb + (i - (NM - NB)) * 128);
-        if (i >= NM - NA) ra[i - (NM - NA)] = *(const i32x2*)(xa + (i - (NM - NA)) * 128);
-      }
+    if (P == 2 && i == 0) {
+#pragma unroll
+      for (int q = 0; q < TL::LX; ++q) raw[q] = *fp4_turned<TL>(lds, turn, q, wave, lane);
+    }
+    if (P == 2 && i == NM - 1) {
+#pragma unroll
+      for (int q = 0; q < TL::LX; ++q) *fp4_turned<TL>(lds, turn, q, wave, lane) = fp4_turn(raw[q], down);
+    }
+    if (i < NB) f.fb[Q ^ 1][i] = *(const i32x4*)(cb + i * 2048);
+    if (bq == NB - 1) f.fa[bi] = *(const i32x4*)(ca + bi * 2048);
+    if (P == 3) {
+      if (i >= NM - NB) nb[i - (NM - NB)] = *(const int*)(xt + (i - (NM - NB)) * 256);
+      if (i >= NM - NA) na[i - (NM - NA)] = *(const int*)(xa + (i - (NM - NA)) * 256);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-  if (READ && P == 1) {
+  if (P == 3) {
 #pragma unroll
-    for (int j = 0; j < NB; ++j) f.sb[j] = fp4_scales(rs[j], at.pick);
+    for (int j = 0; j < NB; ++j) f.sb[j] = nb[j];
 #pragma unroll
-    for (int j = 0; j < NA; ++j) f.sa[j] = fp4_scales(ra[j], at.pick);
+    for (int j = 0; j < NA; ++j) f.sa[j] = na[j];
   }
+}
+
+// This wave's LDS accesses and its DMA up to the next stage's are done; the
+// barrier makes that stage (and turned scales) visible and frees this one's
+// buffer. The count ignores scale requests, which only makes the wait stricter.
+template <class TL>
+__device__ __forceinline__ void fp4_boundary() {
+  wait_lgkm0_vmem<(TL::NBUF - 2) * TL::L>();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 template <class TL, class T>
 __global__ __launch_bounds__(TL::NW * 64, TL::PER_CU * TL::NW / 4) void fp4_logits(const Mxfp4LogitsArgs a, int n_vt,
                                                                                     int n_tt) {
-  constexpr int NA = TL::NA, NB = TL::NB, NBUF = TL::NBUF, L = TL::L, SB = TL::SB;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[NBUF * SB];
+  constexpr int NA = TL::NA, NB = TL::NB, NBUF = TL::NBUF, SBUF = TL::SBUF, L = TL::L, SB = TL::SB;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[TL::LDS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wv = wave % TL::WV, wt = wave / TL::WV;
   const int lane = threadIdx.x & 63;
@@ -212,13 +283,21 @@ __global__ __launch_bounds__(TL::NW * 64, TL::PER_CU * TL::NW / 4) void fp4_logi
   const int whole = a.d / 256;
   const Fp4Source o = fp4_source<TL>(a, v0, t0, wave, lane);
 
+  // stage s is requested after group (s + 1) / 2 for s odd
+  fp4_load_scales<TL>(lds, 0, o, 0, wave);
 #pragma unroll
   for (int s = 0; s < NBUF; ++s) {
+    if (s & 1) fp4_load_scales<TL>(lds, (s + 1) / 2 % SBUF, o, (s + 1) / 2, wave);
     const int st = s < nk ? s : nk - 1;
 #pragma unroll
     for (int q = 0; q < L; ++q) fp4_load<TL>(lds + s * SB, o, st, st >= whole, wave, q);
   }
-  wait_vmem<(NBUF - 1) * L>();  // stage 0 landed
+  wait_vmem<(NBUF - 1) * L>();  // group 0 and stage 0 landed
+#pragma unroll
+  for (int q = 0; q < TL::LX; ++q) {
+    i32x4* p = fp4_turned<TL>(lds, 0, q, wave, lane);
+    *p = fp4_turn(*p, 0);
+  }
   __syncthreads();
 
   f32x4 acc[NA][NB];
@@ -231,30 +310,44 @@ __global__ __launch_bounds__(TL::NW * 64, TL::PER_CU * TL::NW / 4) void fp4_logi
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
     f.fb[0][j] = *(const i32x4*)(lds + TL::kCodesB + (wt * NB + j) * 2048 + at.code[0]);
-    f.sb[j] = fp4_scales(*(const i32x2*)(lds + TL::kScalesB + (wt * NB + j) * 128 + at.scale), at.pick);
+    f.sb[j] = *(const int*)(lds + TL::kScales + TL::SA * 1024 + (wt * NB + j) * 256 + at.scale);
   }
 #pragma unroll
   for (int j = 0; j < NA; ++j) {
     f.fa[j] = *(const i32x4*)(lds + (wv * NA + j) * 2048 + at.code[0]);
-    f.sa[j] = fp4_scales(*(const i32x2*)(lds + TL::kScalesA + (wv * NA + j) * 128 + at.scale), at.pick);
+    f.sa[j] = *(const int*)(lds + TL::kScales + (wv * NA + j) * 256 + at.scale);
   }
-  int bk = 0;  // buffer of the current stage
-  for (int k = 0; k < whole; ++k) {
-    unsigned char* cb = lds + bk * SB;
-    fp4_step<TL, 0, false, true>(f, acc, cb, o, 0, false, cb, at, wave, wv, wt);
-    // this wave's reads of stage k and its DMA of stage k + 1 are done; the barrier makes that stage visible and
-    // frees this one's buffer, which takes stage k + NBUF (past the end: the last stage again, never read)
-    wait_lgkm0_vmem<(NBUF - 2) * L>();
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    if (++bk == NBUF) bk = 0;
-    const int st = k + NBUF < nk ? k + NBUF : nk - 1;
-    fp4_step<TL, 1, true, true>(f, acc, cb, o, st, st >= whole, lds + bk * SB, at, wave, wv, wt);
+  // buffers of the current stage and of the current group; past the row's end, stage requests repeat the last stage
+  // and operand reads take what a buffer holds, none of it used
+  int bk = 0, sk = 0;
+  auto next = [](int i, int n) { return i + 1 == n ? 0 : i + 1; };
+  for (int k = 0;; k += 2) {
+    {
+      unsigned char* cb = lds + bk * SB;
+      fp4_step<TL, 0>(f, acc, lds, cb, o, 0, false, cb, lds, 0, 0, at, wave, wv, wt, lane);
+      if (k == whole) break;
+      fp4_boundary<TL>();
+      if constexpr (NBUF & 1) fp4_load_scales<TL>(lds, (sk + (NBUF + 1) / 2) % SBUF, o, (k + NBUF + 1) / 2, wave);
+      bk = next(bk, NBUF);
+      const int st = k + NBUF < nk ? k + NBUF : nk - 1;
+      fp4_step<TL, 1>(f, acc, lds, cb, o, st, st >= whole, lds + bk * SB, lds, 0, 0, at, wave, wv, wt, lane);
+      if (k + 1 == nk) break;
+    }
+    {
+      unsigned char* cb = lds + bk * SB;
+      sk = next(sk, SBUF);
+      // the next group's scales were requested before this stage
+      fp4_step<TL, 2>(f, acc, lds, cb, o, 0, false, cb, lds, sk, fp4_down(o, k / 2 + 1), at, wave, wv, wt, lane);
+      if (k + 1 == whole) break;
+      fp4_boundary<TL>();
+      if constexpr (!(NBUF & 1)) fp4_load_scales<TL>(lds, (sk + NBUF / 2) % SBUF, o, (k + NBUF + 2) / 2, wave);
+      bk = next(bk, NBUF);
+      const int st = k + 1 + NBUF < nk ? k + 1 + NBUF : nk - 1;
+      fp4_step<TL, 3>(f, acc, lds, cb, o, st, st >= whole, lds + bk * SB, lds + TL::kScales + sk * TL::XB, 0, 0, at,
+                      wave, wv, wt, lane);
+      if (k + 2 == nk) break;
+    }
   }
-  if (whole < nk) fp4_step<TL, 0, false, false>(f, acc, lds, o, 0, false, lds, at, wave, wv, wt);
   wait_vmem<0>();  // no global->LDS request may outlive the workgroup
 
   // lane l holds hidden row l % 16 of a block and its vocabulary entries 4 (l / 16) .. + 3
@@ -263,22 +356,31 @@ __global__ __launch_bounds__(TL::NW * 64, TL::PER_CU * TL::NW / 4) void fp4_logi
   for (int j = 0; j < NB; ++j) {
     const int64_t t = t0 + (wt * NB + j) * 16 + (lane & 15);
     if (t >= a.T) continue;
-    T* out = (T*)a.logits + t * a.ld;
 #pragma unroll
-    for (int i = 0; i < NA; ++i) {
-      const int v = vl + i * 16;
-      T z[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) z[e] = narrow<T>(acc[i][j][e] * a.inv_tau);
-      if (v + 4 <= a.V) {
-        __builtin_memcpy(out + v, z, sizeof(z));
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (v + e < a.V) out[v + e] = z[e];
-      }
-    }
+    for (int i = 0; i < NA; ++i) store_logits<T>((T*)a.logits + t * a.ld, vl + i * 16, a.V, acc[i][j], a.inv_tau);
   }
+}
+
+// Rows shorter than a group of scales: one wave per block of 16 x 16, operands
+// from memory.
+template <class T>
+__global__ __launch_bounds__(256) void fp4_logits_short(const Mxfp4LogitsArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int v0 = ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)) * 16;
+  const int64_t t0 = (int64_t)blockIdx.y * 16;
+  if (v0 >= a.V) return;
+  const int r = lane & 15, g = lane >> 4;
+  // rows past the end repeat the last one; their results are not written
+  const int64_t w = v0 + r < a.V ? v0 + r : a.V - 1;
+  const int64_t h = t0 + r < a.T ? t0 + r : a.T - 1;
+  const uint8_t* wc = a.w_codes + w * (a.d / 2) + g * 16;
+  const uint8_t* hc = a.h_codes + h * (a.d / 2) + g * 16;
+  const uint8_t* ws = a.w_scales + w * (a.d / 32) + g;
+  const uint8_t* hs = a.h_scales + h * (a.d / 32) + g;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < a.d / 128; ++k)
+    acc = mfma_fp4<0>(*(const i32x4*)(wc + k * 64), ws[k * 4], *(const i32x4*)(hc + k * 64), hs[k * 4], acc);
+  if (t0 + r < a.T) store_logits<T>((T*)a.logits + (t0 + r) * a.ld, v0 + 4 * g, a.V, acc, a.inv_tau);
 }
 
 template <class TL, class T>
@@ -300,16 +402,32 @@ hipError_t launch_tiles(const Mxfp4LogitsArgs& a, hipStream_t s) {
   return hipSuccess;
 }
 
-#ifndef FP4_SHAPE
-#define FP4_SHAPE 0
-#endif
+template <class T>
+hipError_t launch_short(const Mxfp4LogitsArgs& a, hipStream_t s) {
+  const int64_t across = (a.V + 63) / 64;  // at most 8192
+  const int64_t down = ((int64_t)1 << 23) / across;  // a grid holds fewer than 2^32 threads
+  const int64_t rows = (down < 65535 ? down : 65535) * 16;
+  for (int64_t t0 = 0; t0 < a.T; t0 += rows) {
+    Mxfp4LogitsArgs b = a;
+    b.T = a.T - t0 < rows ? a.T - t0 : rows;
+    b.h_codes = a.h_codes + t0 * (a.d / 2);
+    b.h_scales = a.h_scales + t0 * (a.d / 32);
+    b.logits = (T*)a.logits + t0 * a.ld;
+    fp4_logits_short<T><<<dim3((unsigned)across, (unsigned)((b.T + 15) / 16)), 256, 0, s>>>(b);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <class T>
 hipError_t product_as(const Mxfp4LogitsArgs& a, hipStream_t s) {
+  if (a.d < kMinD) return launch_short<T>(a, s);
   if (a.T <= 16) return launch_tiles<Fp4Tile<4, 1, 2, 1, 3>, T>(a, s);
   if (a.T <= 32) return launch_tiles<Fp4Tile<4, 1, 2, 2, 3>, T>(a, s);
   if (a.T <= 64) return launch_tiles<Fp4Tile<4, 1, 2, 4, 2>, T>(a, s);
-  if (a.T <= 128) return launch_tiles<Fp4Tile<4, 1, 4, 8, 1>, T>(a, s);
-  return launch_tiles<Fp4Tile<2, 2, 8, 8, 1>, T>(a, s);
+  if (a.T <= 128) return launch_tiles<Fp4Tile<2, 2, 8, 4, 1>, T>(a, s);
+  return launch_tiles<Fp4Tile<2, 4, 8, 4, 1>, T>(a, s);
 }
 
 }  // namespace
