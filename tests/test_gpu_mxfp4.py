@@ -218,3 +218,28 @@ def test_no_rows():
     h, _ = _random(1, 256, 1, 0)
     w, _ = _random(40, 256, 2, 0)
     assert tim.mxfp4_logits(tim.Mxfp4(h.codes[:0], h.scales[:0]), w).shape == (0, 40)
+
+
+@pytest.mark.parametrize("dtype,T,V", [(torch.float32, 600, 131071), (torch.bfloat16, 1100, 131073), (torch.float16, 1030, 140002)])
+def test_logits_larger_than_the_caches(dtype, T, V):
+    """More than 256 MB of logits in rows of odd lengths: the same bits as the rows a few at a time."""
+    h, _ = _random(T, 512, 11, 3)
+    w, _ = _random(V, 512, 12, 3)
+    z = tim.mxfp4_logits(h, w, 0.9, dtype=dtype)
+    for a, b in ((0, 64), (T - 40, T), (T // 2, T // 2 + 3)):
+        part = tim.mxfp4_logits(tim.Mxfp4(h.codes[a:b], h.scales[a:b]), w, 0.9, dtype=dtype)
+        assert torch.equal(z[a:b], part)
+
+
+@pytest.mark.parametrize("d", [512, 640, 768, 896, 1024, 1152, 1280, 1408, 1536, 1664, 2048 + 128])
+@pytest.mark.parametrize("T", [9, 30, 50, 100, 300])
+def test_every_end_of_a_row(T, d):
+    """Rows that end after each k-step of a scale group, in every tile shape: exact."""
+    print(f"case T={T} d={d}", flush=True)
+    h, hv = _random(T, d, T, 0)
+    w, wv = _random(331, d, d, 0)
+    hs = torch.randint(126, 129, h.scales.shape, generator=torch.Generator().manual_seed(1)).to(torch.uint8).cuda()
+    h = tim.Mxfp4(h.codes, hs)  # scales that differ from block to block show a misplaced one
+    hv = hv * torch.exp2(hs.double() - 127).repeat_interleave(32, 1)
+    # sums of multiples of 1/8 below 36 * 2 * d < 2^21 units: exact in fp32
+    assert torch.equal(tim.mxfp4_logits(h, w).double(), hv @ wv.T)
