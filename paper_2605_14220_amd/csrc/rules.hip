@@ -29,6 +29,7 @@ constexpr int kChunk = TIM_RULE_CHUNK;
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
 constexpr int kPer = kChunk / kThreads;  // entries per thread
+constexpr int kMaxGroup = 16;            // rows of one workgroup
 constexpr int kMaxChunks = (TIM_MAX_VOCAB + kChunk - 1) / kChunk;
 static_assert(kMaxChunks <= 64, "the merge holds a row's chunks in one wave");
 constexpr uint32_t kPromptBit = 0x80000000u;
@@ -101,71 +102,113 @@ __device__ __forceinline__ void count_tokens(uint32_t* cnt, const int32_t* __res
   }
 }
 
+// What a workgroup needs of one of its rows, read once for all of them.
+struct Row {
+  int64_t begin, split, end;  // of the history
+  int64_t bias0, bias1;
+  int64_t mask;               // row of the mask, -1: none
+  float rho, inv_rho, freq, pres;
+  int tok;                    // relative to the chunk; negative or past it: elsewhere
+  float lse, ent, g, e;
+  int zero;                   // the gradient is 0 everywhere
+};
+
+template <Op OP>
+__device__ __forceinline__ Row read_row(const RuleArgs& a, int64_t row, int v0, bool hist, bool bias) {
+  Row w = {};
+  w.mask = -1;
+  if (a.r.mask) {
+    const int64_t m = a.r.mask_rows ? (int64_t)a.r.mask_rows[row] : row;
+    if (m >= 0 && m < a.r.n_masks) w.mask = m;
+  }
+  // a penalty that is left out takes the value that changes nothing
+  w.rho = 1.f;
+  if (hist) {
+    const int64_t N = a.r.history_len;
+    w.begin = clamp64(a.r.hist_begin[row], 0, N);
+    w.split = a.r.hist_split ? clamp64(a.r.hist_split[row], w.begin, N) : w.begin;
+    w.end = clamp64(a.r.hist_end[row], w.split, N);
+    if (a.r.repetition) w.rho = a.r.repetition[row];
+    if (a.r.frequency) w.freq = a.r.frequency[row];
+    if (a.r.presence) w.pres = a.r.presence[row];
+  }
+  w.inv_rho = 1.f / w.rho;
+  if (bias) {
+    w.bias0 = clamp64(a.r.bias_begin[row], 0, a.r.bias_len);
+    w.bias1 = clamp64(a.r.bias_end[row], w.bias0, a.r.bias_len);
+  }
+  w.tok = -1;
+  if constexpr (OP != Op::kAdjust) {
+    const bool valid = (unsigned)a.tokens[row] < (unsigned)a.V;
+    if (valid) w.tok = a.tokens[row] - v0;
+    if constexpr (OP == Op::kGrad) {
+      w.lse = a.lse[row];
+      w.g = valid ? a.grad_logp[row] : 0.f;
+      if (a.grad_entropy) {
+        w.e = a.grad_entropy[row];
+        w.ent = a.entropy[row];
+      }
+      w.zero = (w.g == 0.f && w.e == 0.f) || w.lse == kNegInf;
+    }
+  }
+  return w;
+}
+
 template <Op OP, class TI, class TO, bool SPARSE>
 __global__ __launch_bounds__(kThreads) void rules_kernel(const RuleArgs a, int n_chunks, int rows_per_group) {
   constexpr int E = 16 / (int)sizeof(TI);  // entries per load
   constexpr int NV = kPer / E;             // loads per thread
-  extern __shared__ uint32_t lds[];
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  __shared__ Row rows[kMaxGroup];
   __shared__ Stat wstat[kWaves];
   __shared__ float tok_x;
 
   const int chunk = (int)(blockIdx.x % (unsigned)n_chunks);
   const int64_t r0 = (int64_t)(blockIdx.x / (unsigned)n_chunks) * rows_per_group;
-  const int64_t r1 = r0 + rows_per_group < a.T ? r0 + rows_per_group : a.T;
+  const int n_rows = (int)(a.T - r0 < rows_per_group ? a.T - r0 : rows_per_group);
   const int v0 = chunk * kChunk;
   const int n = a.V - v0 < kChunk ? a.V - v0 : kChunk;
   const bool hist = SPARSE && a.r.history != nullptr;
   const bool bias = SPARSE && a.r.bias_ids != nullptr;
   uint32_t* cnt = lds;
   uint32_t* last = lds + (hist ? kChunk : 0);
+  if ((int)threadIdx.x < n_rows) rows[threadIdx.x] = read_row<OP>(a, r0 + threadIdx.x, v0, hist, bias);
+  __syncthreads();
 
   int64_t pb = -1, ps = 0, pe = 0;  // the history counted in cnt; pb < 0: none, cnt not cleared
   int64_t qb = -1, qe = -1;         // the bias list in last
 
-  for (int64_t row = r0; row < r1; ++row) {
+  for (int i = 0; i < n_rows; ++i) {
+    const int64_t row = r0 + i;
+    const Row& w = rows[i];
     const TI* z = (const TI*)a.logits + row * a.ld + v0;
     TO* out = OP == Op::kStats ? nullptr : (TO*)a.out + row * a.out_ld + v0;
-    float lse = 0.f, ent = 0.f, g = 0.f, e = 0.f;
-    int tok = -1;  // of the row, relative to the chunk
-    if constexpr (OP != Op::kAdjust) tok = (unsigned)a.tokens[row] < (unsigned)a.V ? a.tokens[row] - v0 : -1;
-    if constexpr (OP == Op::kGrad) {
-      lse = a.lse[row];
-      g = (unsigned)a.tokens[row] < (unsigned)a.V ? a.grad_logp[row] : 0.f;
-      if (a.grad_entropy) {
-        e = a.grad_entropy[row];
-        ent = a.entropy[row];
-      }
-      if ((g == 0.f && e == 0.f) || lse == kNegInf) {
-        for (int i = threadIdx.x; i < n; i += kThreads) out[i] = (TO)0.f;
-        continue;
-      }
+    if (OP == Op::kGrad && w.zero) {
+      for (int c = threadIdx.x; c < n; c += kThreads) out[c] = (TO)0.f;
+      continue;
     }
-    const int64_t mrow = a.r.mask ? (a.r.mask_rows ? (int64_t)a.r.mask_rows[row] : row) : -1;
-    const bool masked = a.r.mask && mrow >= 0 && mrow < a.r.n_masks;
 
     Vec<TI, E> in[NV];
-    uint32_t word[NV];
+    uint32_t open[NV];  // bit k: entry k of the load is allowed and lies in the vocabulary
+    const bool some_off = w.mask >= 0 || n < kChunk;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int i = (j * kThreads + (int)threadIdx.x) * E;
-      word[j] = ~0u;
-      if (i + E <= n) {
-        in[j] = load_vec<TI, E>(z + i);
+      const int c = (j * kThreads + (int)threadIdx.x) * E;
+      if (c + E <= n) {
+        in[j] = load_vec<TI, E>(z + c);
       } else {
 #pragma unroll
-        for (int k = 0; k < E; ++k) in[j].v[k] = i + k < n ? z[i + k] : (TI)0.f;
+        for (int k = 0; k < E; ++k) in[j].v[k] = c + k < n ? z[c + k] : (TI)0.f;
       }
-      if (masked && i < n) word[j] = a.r.mask[mrow * a.r.mask_ld + ((v0 + i) >> 5)] >> ((v0 + i) & 31);
+      open[j] = c + E <= n ? ~0u : c < n ? (1u << (n - c)) - 1u : 0u;
+      if (w.mask >= 0 && c < n) open[j] &= a.r.mask[w.mask * a.r.mask_ld + ((v0 + c) >> 5)] >> ((v0 + c) & 31);
     }
 
     if (hist) {
-      const int64_t N = a.r.history_len;
-      const int64_t b = clamp64(a.r.hist_begin[row], 0, N);
-      const int64_t s = a.r.hist_split ? clamp64(a.r.hist_split[row], b, N) : b;
-      const int64_t t = clamp64(a.r.hist_end[row], s, N);
+      const int64_t b = w.begin, s = w.split, t = w.end;
       int64_t from = pe;
       if (b != pb || s != ps || t < pe) {
-        for (int i = threadIdx.x; i < kChunk; i += kThreads) cnt[i] = 0;
+        for (int c = threadIdx.x * 4; c < kChunk; c += kThreads * 4) *(uint4*)(cnt + c) = uint4{0, 0, 0, 0};
         from = b;
         __syncthreads();
       }
@@ -175,10 +218,9 @@ __global__ __launch_bounds__(kThreads) void rules_kernel(const RuleArgs a, int n
       pe = t;
     }
     if (bias) {
-      const int64_t b = clamp64(a.r.bias_begin[row], 0, a.r.bias_len);
-      const int64_t t = clamp64(a.r.bias_end[row], b, a.r.bias_len);
+      const int64_t b = w.bias0, t = w.bias1;
       if (b != qb || t != qe) {
-        for (int i = threadIdx.x; i < kChunk; i += kThreads) last[i] = 0;
+        for (int c = threadIdx.x * 4; c < kChunk; c += kThreads * 4) *(uint4*)(last + c) = uint4{0, 0, 0, 0};
         __syncthreads();
         for (int64_t k = b + threadIdx.x; k < t; k += kThreads) {
           const uint32_t id = (uint32_t)a.r.bias_ids[k] - (uint32_t)v0;
@@ -189,85 +231,89 @@ __global__ __launch_bounds__(kThreads) void rules_kernel(const RuleArgs a, int n
       }
     }
     if constexpr (SPARSE) __syncthreads();
-    const float rho = hist && a.r.repetition ? a.r.repetition[row] : 1.f;
-    const float inv_rho = 1.f / rho;
-    const float freq = hist && a.r.frequency ? a.r.frequency[row] : 0.f;
-    const float pres = hist && a.r.presence ? a.r.presence[row] : 0.f;
 
-    float x[kPer], slope[OP == Op::kGrad ? kPer : 1];
+    float x[kPer];
+    float m = kNegInf;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int i = (j * kThreads + (int)threadIdx.x) * E;
+      const int c = (j * kThreads + (int)threadIdx.x) * E;
+      float* y = x + j * E;
+      float slope[E];
 #pragma unroll
       for (int k = 0; k < E; ++k) {
-        float y = widen(in[j].v[k]);
-        float sl = 1.f;
-        if (hist) {
-          const uint32_t w = cnt[i + k];
-          if (w) {
-            if (a.r.repetition) {
-              sl = y > 0.f ? inv_rho : rho;
-              y = y > 0.f ? y / rho : y * rho;
-            }
-            const uint32_t c = w & ~kPromptBit;
-            if (c) {
-              if (a.r.frequency) y = y - freq * (float)c;
-              if (a.r.presence) y = y - pres;
-            }
+        y[k] = widen(in[j].v[k]);
+        slope[k] = a.inv_tau;
+      }
+      if (hist) {
+        uint32_t u[E], any = 0;
+#pragma unroll
+        for (int k = 0; k < E; k += 4) __builtin_memcpy(u + k, __builtin_assume_aligned(cnt + c + k, 16), 16);
+#pragma unroll
+        for (int k = 0; k < E; ++k) any |= u[k];
+        if (any) {
+#pragma unroll
+          for (int k = 0; k < E; ++k) {
+            const float up = y[k] / w.rho, down = y[k] * w.rho;
+            const bool pos = y[k] > 0.f;
+            float v = u[k] ? (pos ? up : down) : y[k];
+            if constexpr (OP == Op::kGrad) slope[k] = u[k] ? (pos ? w.inv_rho : w.rho) * a.inv_tau : a.inv_tau;
+            const uint32_t count = u[k] & ~kPromptBit;
+            const float less = v - w.freq * (float)count - w.pres;
+            y[k] = count ? less : v;
           }
         }
-        if (bias) {
-          const uint32_t w = last[i + k];
-          if (w) y = y + a.r.bias_values[w - 1];
+      }
+      if (bias) {
+        uint32_t u[E], any = 0;
+#pragma unroll
+        for (int k = 0; k < E; k += 4) __builtin_memcpy(u + k, __builtin_assume_aligned(last + c + k, 16), 16);
+#pragma unroll
+        for (int k = 0; k < E; ++k) any |= u[k];
+        if (any) {
+#pragma unroll
+          for (int k = 0; k < E; ++k)
+            if (u[k]) y[k] = y[k] + a.r.bias_values[u[k] - 1];
         }
-        y = y * a.inv_tau;
-        const bool off = !((word[j] >> k) & 1u) || i + k >= n;
-        x[j * E + k] = off ? kNegInf : y;
-        if constexpr (OP == Op::kGrad) slope[j * E + k] = off ? 0.f : sl * a.inv_tau;
+      }
+#pragma unroll
+      for (int k = 0; k < E; ++k) y[k] = y[k] * a.inv_tau;
+      if (some_off) {
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+          const bool off = !((open[j] >> k) & 1u);
+          y[k] = off ? kNegInf : y[k];
+          slope[k] = off ? 0.f : slope[k];
+        }
+      }
+      if constexpr (OP == Op::kStats) {
+#pragma unroll
+        for (int k = 0; k < E; ++k) m = fmaxf(m, y[k]);
+      } else {
+        Vec<TO, E> o;
+        if constexpr (OP == Op::kAdjust) {
+#pragma unroll
+          for (int k = 0; k < E; ++k) o.v[k] = narrow<TO>(y[k]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < E; ++k) {
+            const float q = y[k] - w.lse;
+            const float p = exp_hw(q);
+            float up = c + k == w.tok ? w.g : 0.f;
+            up = up - p * (w.g + w.e * (fmaxf(q, kFloor) + w.ent));
+            o.v[k] = narrow<TO>(slope[k] == 0.f ? 0.f : up * slope[k]);
+          }
+        }
+        if (c + E <= n) {
+          store_vec<TO, E>(out + c, o);
+        } else {
+#pragma unroll
+          for (int k = 0; k < E; ++k)
+            if (c + k < n) out[c + k] = o.v[k];
+        }
       }
     }
 
-    if constexpr (OP == Op::kAdjust) {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int i = (j * kThreads + (int)threadIdx.x) * E;
-        Vec<TO, E> o;
-#pragma unroll
-        for (int k = 0; k < E; ++k) o.v[k] = narrow<TO>(x[j * E + k]);
-        if (i + E <= n) {
-          store_vec<TO, E>(out + i, o);
-        } else {
-#pragma unroll
-          for (int k = 0; k < E; ++k)
-            if (i + k < n) out[i + k] = o.v[k];
-        }
-      }
-    } else if constexpr (OP == Op::kGrad) {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int i = (j * kThreads + (int)threadIdx.x) * E;
-        Vec<TO, E> o;
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-          const float q = x[j * E + k] - lse;
-          const float p = exp_hw(q);
-          float up = i + k == tok ? g : 0.f;
-          up = up - p * (g + e * (fmaxf(q, kFloor) + ent));
-          const float sl = slope[j * E + k];
-          o.v[k] = narrow<TO>(sl == 0.f ? 0.f : up * sl);
-        }
-        if (i + E <= n) {
-          store_vec<TO, E>(out + i, o);
-        } else {
-#pragma unroll
-          for (int k = 0; k < E; ++k)
-            if (i + k < n) out[i + k] = o.v[k];
-        }
-      }
-    } else {
-      float m = kNegInf;
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) m = fmaxf(m, x[k]);
+    if constexpr (OP == Op::kStats) {
       m = wave_max(m);
       const float at = m == kNegInf ? 0.f : m;
       float s = 0.f, u = 0.f;
@@ -281,22 +327,21 @@ __global__ __launch_bounds__(kThreads) void rules_kernel(const RuleArgs a, int n
       s = wave_sum(s);
       u = wave_sum(u);
       if ((threadIdx.x & 63) == 0) wstat[threadIdx.x >> 6] = {m, s, u};
+      const int tok = w.tok;
+      if (tok >= 0 && tok < n && tok / E % kThreads == (int)threadIdx.x) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int i = (j * kThreads + (int)threadIdx.x) * E;
-#pragma unroll
-        for (int k = 0; k < E; ++k)
-          if (i + k == tok) tok_x = x[j * E + k];
+        for (int k = 0; k < kPer; ++k)
+          if (tok / E / kThreads * E + tok % E == k) tok_x = x[k];
       }
       __syncthreads();
       if (threadIdx.x == 0) {
         float top = wstat[0].m;
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, wstat[w].m);
+        for (int v = 1; v < kWaves; ++v) top = fmaxf(top, wstat[v].m);
         Partial p = {top, 0.f, 0.f, tok >= 0 && tok < n ? tok_x : 0.f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          const Stat t = shift(wstat[w], top);
+        for (int v = 0; v < kWaves; ++v) {
+          const Stat t = shift(wstat[v], top);
           p.s += t.s;
           p.u += t.u;
         }
@@ -304,7 +349,7 @@ __global__ __launch_bounds__(kThreads) void rules_kernel(const RuleArgs a, int n
       }
     }
     // the next row changes what this one read from LDS
-    if (row + 1 < r1) __syncthreads();
+    if (SPARSE || OP == Op::kStats) __syncthreads();
   }
 }
 
@@ -381,7 +426,7 @@ hipError_t launch_rules(const RuleArgs& a, hipStream_t s) {
     int group = 1;
     if (b.r.history) {
       const int64_t fill = rows * n_chunks / 4096;
-      group = fill < 1 ? 1 : fill > 16 ? 16 : (int)fill;
+      group = fill < 1 ? 1 : fill > kMaxGroup ? kMaxGroup : (int)fill;
     }
     const unsigned grid = (unsigned)((rows + group - 1) / group * n_chunks);
     const int lds = rule_lds_bytes(b);
