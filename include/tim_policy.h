@@ -157,7 +157,8 @@ size_t tim_logits_logprobs_workspace_size(int64_t T, int32_t V);
  *
  * logits, dtype, ld, rules, temperature as tim_logits_adjust; tokens int32
  * [T]; logp fp32 [T] (required), entropy, lse fp32 [T] or NULL. x is not
- * rounded to dtype. Statistics are fp32 over chunks of TIM_RULE_CHUNK entries
+ * rounded to dtype, and the temperature is applied to differences from the
+ * row's maximum. Statistics are fp32 over chunks of TIM_RULE_CHUNK entries
  * merged in a fixed order. workspace 16-byte aligned; also TIM_ERR_WORKSPACE. */
 tim_status tim_logits_logprobs(const void* logits, int32_t dtype, int64_t T, int32_t V, int64_t ld,
                                const int32_t* tokens, const tim_logit_rules* rules, float temperature,

@@ -2,25 +2,36 @@
 // logits of T rows, the softmax statistics of the result and their gradient.
 //
 // Mathematics, per entry (include/tim_policy.h has the order and the roundings):
-//   x = rule(z): penalties of the tokens in the row's history, bias, 1/tau, mask
-//   logprobs: per chunk m = max x, s = sum e^(x-m), u = sum e^(x-m) (x-m); a
-//             merge over the chunks gives lse = M + log S, H = log S - U / S
+//   y = rule(z): penalties of the tokens in the row's history, bias, mask;
+//       x = y / tau
+//   logprobs: per chunk m = max y, and with t = (y - m) log2(e) / tau the sums
+//             s = sum 2^t, u = sum 2^t t; a merge over the chunks gives
+//             lse = M / tau + log S, H = log S - ln 2 U / S
 //   backward: dz = slope (g [v = tok] - p (g + e (log p + H))), p = e^(x-lse)
 //
 // All three are one pass over the logits (read once; adjust and backward write
 // as many) and bound by HBM. A workgroup takes one chunk of TIM_RULE_CHUNK
-// vocabulary entries of consecutive rows, its part of a row in registers. The
-// sparse changes live in LDS, one word per entry of the chunk: bit 31 = token
-// of the prompt, the rest = count in the output (integer atomics, so the order
-// of the tokens does not matter), and in a second word the last bias entry of
-// that id (an integer maximum). A chunk's workgroup reads the row's whole
-// history and keeps what falls into it; rows whose history extends the last
-// row's (the rows of one response in a packed stream) add only the new tokens.
+// vocabulary entries of consecutive rows. The sparse changes live in LDS, one
+// word per entry of the chunk: bit 31 = token of the prompt, the rest = count in
+// the output (integer atomics, so the order of the tokens does not matter), and
+// in a second word the last bias entry of that id (an integer maximum). A
+// chunk's workgroup reads the row's whole history and keeps what falls into it;
+// rows whose history extends the last row's (the rows of one response in a
+// packed stream) add only the new tokens.
+//
+// Few entries of a row are touched. A bitmap tells a thread which of its
+// entries are, and it walks those by themselves, picking each out of its
+// registers; with the penalties' code inside the pass over the row, once per
+// entry of a load, 4096 rows of 151936 logits with up to 1280 tokens of history
+// took 574 us against 533.
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kernels.h"
 #include "policy.h"
+#include "tilepass.h"
 
 namespace tim {
 namespace {
@@ -28,191 +39,309 @@ namespace {
 constexpr int kChunk = TIM_RULE_CHUNK;
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
+static_assert(kWaves == 8, "the workgroup's merge rotates over eight lanes");
 constexpr int kPer = kChunk / kThreads;  // entries per thread
 constexpr int kMaxGroup = 16;            // rows of one workgroup
 constexpr int kMaxChunks = (TIM_MAX_VOCAB + kChunk - 1) / kChunk;
 static_assert(kMaxChunks <= 64, "the merge holds a row's chunks in one wave");
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr uint32_t kPromptBit = 0x80000000u;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNegInf = -__builtin_inff();
-// Below this distance from the maximum e^x is 0 in fp32; it takes the place
-// of -inf in the products p * log p.
-constexpr float kFloor = -200.f;
+// 2^kFloor is 0 in fp32; it takes the place of -inf in the products p * log p.
+constexpr float kFloor = -300.f;
 
 enum class Op { kAdjust, kStats, kGrad };
-
-__device__ __forceinline__ float exp_hw(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 template <class T>
 __device__ __forceinline__ float widen(T x) { return (float)x; }
 
-// N consecutive elements at p, which is aligned to its element only.
+// N consecutive elements of a chunk at entry c of it: p the chunk's first, the
+// same in every lane (one 32-bit offset per lane then makes the address), and
+// aligned to its element only.
 template <class T, int N>
 struct Vec {
   T v[N];
 };
+template <class T>
+__device__ __forceinline__ T* entry(T* p, int c) {
+  return (T*)((std::conditional_t<std::is_const_v<T>, const char, char>*)p + (uint32_t)(c * (int)sizeof(T)));
+}
 template <class T, int N>
-__device__ __forceinline__ Vec<T, N> load_vec(const T* p) {
+__device__ __forceinline__ Vec<T, N> load_vec(const T* p, int c) {
   Vec<T, N> r;
-  __builtin_memcpy(&r, p, sizeof(r));
+  __builtin_memcpy(&r, entry(p, c), sizeof(r));
   return r;
 }
 template <class T, int N>
-__device__ __forceinline__ void store_vec(T* p, const Vec<T, N>& r) { __builtin_memcpy(p, &r, sizeof(r)); }
+__device__ __forceinline__ void store_vec(T* p, int c, const Vec<T, N>& r) {
+  __builtin_memcpy(entry(p, c), &r, sizeof(r));
+}
 
+// Softmax statistics of a set of entries, the logits short of the temperature:
+// m = max y, and with t = (y - m) log2(e) / tau: s = sum 2^t, u = sum 2^t t.
+// Differences first, then the factor, so that rows of the type's lowest value
+// do not overflow.
 struct Stat {
   float m, s, u;
 };
 
-// (m, s, u) of two disjoint sets of entries. A side with no finite maximum has
-// s = u = 0 (or NaN), so any finite shift keeps it.
-__device__ __forceinline__ Stat shift(const Stat& a, float m) {
-  const float dm = fmaxf(a.m - m, -1e30f);
-  const float k = exp_hw(dm);
-  return {m, a.s * k, k * (a.u + a.s * dm)};
+// The statistics over a higher maximum, c = log2(e) / tau. A set without a
+// finite maximum has s = u = 0 (or NaN), so any finite shift keeps it.
+__device__ __forceinline__ Stat shift(const Stat& a, float m, float c) {
+  const float t = fmaxf((a.m - m) * c, -1e30f);
+  const float k = exp2_hw(t);
+  return {m, a.s * k, k * (a.u + a.s * t)};
 }
 
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+// Over the wave, the same in every lane: rotations within 16 lanes, then the
+// four groups of them.
+template <int N>
+__device__ __forceinline__ float ror(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xF, 0xF, false));
+#else
   return x;
+#endif
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, ror<8>(x));
+  x = fmaxf(x, ror<4>(x));
+  x = fmaxf(x, ror<2>(x));
+  x = fmaxf(x, ror<1>(x));
+  return group_max(x);
 }
 __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
-  return x;
+  x += ror<8>(x);
+  x += ror<4>(x);
+  x += ror<2>(x);
+  x += ror<1>(x);
+  return group_sum(x);
 }
 
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
   return x < lo ? lo : x > hi ? hi : x;
 }
 
-// Tokens history[from .. to) that fall into the chunk [v0, v0 + n): before
-// split marked, from there on counted.
-__device__ __forceinline__ void count_tokens(uint32_t* cnt, const int32_t* __restrict__ history, int64_t from,
-                                             int64_t split, int64_t to, int v0, int n) {
-  for (int64_t i = from + threadIdx.x; i < to; i += kThreads) {
-    const uint32_t t = (uint32_t)history[i] - (uint32_t)v0;
-    if (t < (uint32_t)n) {
-      if (i < split)
-        atomicOr(&cnt[t], kPromptBit);
-      else
-        atomicAdd(&cnt[t], 1u);
-    }
+// A token less the chunk's first entry, if it falls into the chunk's n: marked
+// as the prompt's, or counted.
+__device__ __forceinline__ void count_token(uint32_t* cnt, uint32_t* touched, uint32_t t, bool given, int n) {
+  if (t < (uint32_t)n) {
+    atomicOr(&touched[t >> 5], 1u << (t & 31));
+    if (given)
+      atomicOr(&cnt[t], kPromptBit);
+    else
+      atomicAdd(&cnt[t], 1u);
   }
 }
 
-// What a workgroup needs of one of its rows, read once for all of them.
+// Tokens history[from .. to), the prompt's before split. Two loads a thread are
+// in flight at a time (more take registers from the rows': with eight 4096 rows
+// of 151936 logits took 602 us, with two 533).
+__device__ __forceinline__ void count_tokens(uint32_t* cnt, uint32_t* touched, const int32_t* __restrict__ history,
+                                             int64_t from, int64_t split, int64_t to, int v0, int n) {
+  constexpr int kStep = 2 * kThreads;
+  for (int64_t i = from; i < to; i += kStep) {
+    const int left = to - i < kStep ? (int)(to - i) : kStep;
+    const int given = split <= i ? 0 : split - i < kStep ? (int)(split - i) : kStep;  // of them, the prompt's
+    const int32_t* h = history + i;
+    uint32_t t[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int c = k * kThreads + (int)threadIdx.x;
+      t[k] = c < left ? (uint32_t)*entry(h, c) - (uint32_t)v0 : ~0u;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) count_token(cnt, touched, t[k], k * kThreads + (int)threadIdx.x < given, n);
+  }
+}
+
+// p[i] for an index that is the same in every lane, through the scalar cache:
+// no kernel here writes what these arrays hold.
+template <class T>
+__device__ __forceinline__ T scalar(const T* p, int64_t i) {
+  typedef const __attribute__((address_space(4))) T* constant;
+  return ((constant)(uint64_t)p)[i];
+}
+
+// The kernel's arguments where the launch left them, read again where they are
+// used (through the scalar cache): they are more than the scalar registers hold,
+// and a spilled one costs a vector instruction each way. Opaque, so that the
+// reads are not gathered in one place.
+typedef const __attribute__((address_space(4))) RuleArgs* ArgsPtr;
+__device__ __forceinline__ ArgsPtr kernel_args() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  ArgsPtr p = (ArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();
+#else
+  ArgsPtr p = nullptr;
+#endif
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
+// What a row's changes are.
 struct Row {
   int64_t begin, split, end;  // of the history
   int64_t bias0, bias1;
   int64_t mask;               // row of the mask, -1: none
-  float rho, inv_rho, freq, pres;
-  int tok;                    // relative to the chunk; negative or past it: elsewhere
-  float lse, ent, g, e;
-  int zero;                   // the gradient is 0 everywhere
+  float rho, freq, pres;
 };
 
-template <Op OP>
-__device__ __forceinline__ Row read_row(const RuleArgs& a, int64_t row, int v0, bool hist, bool bias) {
+__device__ __forceinline__ Row read_row(int64_t row, bool hist, bool bias) {
+  const ArgsPtr a = kernel_args();
   Row w = {};
   w.mask = -1;
-  if (a.r.mask) {
-    const int64_t m = a.r.mask_rows ? (int64_t)a.r.mask_rows[row] : row;
-    if (m >= 0 && m < a.r.n_masks) w.mask = m;
+  if (a->r.mask) {
+    const int64_t m = a->r.mask_rows ? (int64_t)scalar(a->r.mask_rows, row) : row;
+    if (m >= 0 && m < a->r.n_masks) w.mask = m;
   }
   // a penalty that is left out takes the value that changes nothing
   w.rho = 1.f;
   if (hist) {
-    const int64_t N = a.r.history_len;
-    w.begin = clamp64(a.r.hist_begin[row], 0, N);
-    w.split = a.r.hist_split ? clamp64(a.r.hist_split[row], w.begin, N) : w.begin;
-    w.end = clamp64(a.r.hist_end[row], w.split, N);
-    if (a.r.repetition) w.rho = a.r.repetition[row];
-    if (a.r.frequency) w.freq = a.r.frequency[row];
-    if (a.r.presence) w.pres = a.r.presence[row];
+    const int64_t N = a->r.history_len;
+    w.begin = clamp64(scalar(a->r.hist_begin, row), 0, N);
+    w.split = a->r.hist_split ? clamp64(scalar(a->r.hist_split, row), w.begin, N) : w.begin;
+    w.end = clamp64(scalar(a->r.hist_end, row), w.split, N);
+    if (a->r.repetition) w.rho = scalar(a->r.repetition, row);
+    if (a->r.frequency) w.freq = scalar(a->r.frequency, row);
+    if (a->r.presence) w.pres = scalar(a->r.presence, row);
   }
-  w.inv_rho = 1.f / w.rho;
   if (bias) {
-    w.bias0 = clamp64(a.r.bias_begin[row], 0, a.r.bias_len);
-    w.bias1 = clamp64(a.r.bias_end[row], w.bias0, a.r.bias_len);
-  }
-  w.tok = -1;
-  if constexpr (OP != Op::kAdjust) {
-    const bool valid = (unsigned)a.tokens[row] < (unsigned)a.V;
-    if (valid) w.tok = a.tokens[row] - v0;
-    if constexpr (OP == Op::kGrad) {
-      w.lse = a.lse[row];
-      w.g = valid ? a.grad_logp[row] : 0.f;
-      if (a.grad_entropy) {
-        w.e = a.grad_entropy[row];
-        w.ent = a.entropy[row];
-      }
-      w.zero = (w.g == 0.f && w.e == 0.f) || w.lse == kNegInf;
-    }
+    w.bias0 = clamp64(scalar(a->r.bias_begin, row), 0, a->r.bias_len);
+    w.bias1 = clamp64(scalar(a->r.bias_end, row), w.bias0, a->r.bias_len);
   }
   return w;
 }
 
+// y with the penalties of an entry whose word in the row's counts is u; the
+// factor the repetition penalty puts on the entry's slope in `factor`.
+__device__ __forceinline__ float penalise(float y, uint32_t u, const Row& w, float inv_rho, float& factor) {
+  const bool pos = y > 0.f;
+  factor = pos ? inv_rho : w.rho;
+  const float v = pos ? y / w.rho : y * w.rho;
+  const uint32_t count = u & ~kPromptBit;
+  return count ? v - w.freq * (float)count - w.pres : v;
+}
+
+// x where the bit is set, else z.
+__device__ __forceinline__ float choose(uint32_t bits, int k, float x, float z) {
+  const int m = __builtin_amdgcn_sbfe((int)bits, k, 1);
+  return __int_as_float((m & __float_as_int(x)) | (~m & __float_as_int(z)));
+}
+
+// LDS words of a history or a bias list: one per entry, and their bitmap.
+constexpr int kWords = kChunk + kChunk / 32;
+
+// Three workgroups a CU (80 registers): two (90 registers) took 8-20% longer, four spill.
 template <Op OP, class TI, class TO, bool SPARSE>
-__global__ __launch_bounds__(kThreads) void rules_kernel(const RuleArgs a, int n_chunks, int rows_per_group) {
+__global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args, int n_chunks, int rows_per_group) {
+  const ArgsPtr a = kernel_args();  // args
+  (void)args;
   constexpr int E = 16 / (int)sizeof(TI);  // entries per load
   constexpr int NV = kPer / E;             // loads per thread
   extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
-  __shared__ Row rows[kMaxGroup];
-  __shared__ Stat wstat[kWaves];
-  __shared__ float tok_x;
+  __shared__ Stat wstat[2][kWaves];  // by row in turn, so that a row need not wait for the last one's merge
+  __shared__ float tok_x[2];
 
   const int chunk = (int)(blockIdx.x % (unsigned)n_chunks);
   const int64_t r0 = (int64_t)(blockIdx.x / (unsigned)n_chunks) * rows_per_group;
-  const int n_rows = (int)(a.T - r0 < rows_per_group ? a.T - r0 : rows_per_group);
+  const int n_rows = (int)(a->T - r0 < rows_per_group ? a->T - r0 : rows_per_group);
   const int v0 = chunk * kChunk;
-  const int n = a.V - v0 < kChunk ? a.V - v0 : kChunk;
-  const bool hist = SPARSE && a.r.history != nullptr;
-  const bool bias = SPARSE && a.r.bias_ids != nullptr;
+  int n = a->V - v0 < kChunk ? a->V - v0 : kChunk;
+  int tid = threadIdx.x;
+  const bool hist = SPARSE && a->r.history != nullptr;
+  const bool bias = SPARSE && a->r.bias_ids != nullptr;
   uint32_t* cnt = lds;
-  uint32_t* last = lds + (hist ? kChunk : 0);
-  if ((int)threadIdx.x < n_rows) rows[threadIdx.x] = read_row<OP>(a, r0 + threadIdx.x, v0, hist, bias);
-  __syncthreads();
+  uint32_t* last = lds + (hist ? kWords : 0);
+  const float log2e_tau = kLog2e * a->inv_tau;
 
-  int64_t pb = -1, ps = 0, pe = 0;  // the history counted in cnt; pb < 0: none, cnt not cleared
-  int64_t qb = -1, qe = -1;         // the bias list in last
-
-  for (int i = 0; i < n_rows; ++i) {
-    const int64_t row = r0 + i;
-    const Row& w = rows[i];
-    const TI* z = (const TI*)a.logits + row * a.ld + v0;
-    TO* out = OP == Op::kStats ? nullptr : (TO*)a.out + row * a.out_ld + v0;
-    if (OP == Op::kGrad && w.zero) {
-      for (int c = threadIdx.x; c < n; c += kThreads) out[c] = (TO)0.f;
-      continue;
-    }
-
-    Vec<TI, E> in[NV];
-    uint32_t open[NV];  // bit k: entry k of the load is allowed and lies in the vocabulary
-    const bool some_off = w.mask >= 0 || n < kChunk;
+  Vec<TI, E> in[NV];  // the row's logits, requested ahead
+  auto request = [&](int64_t row) {
+    const ArgsPtr a = kernel_args();
+    const TI* z = (const TI*)a->logits + row * a->ld + v0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * kThreads + (int)threadIdx.x) * E;
+      const int c = (j * kThreads + tid) * E;
       if (c + E <= n) {
-        in[j] = load_vec<TI, E>(z + c);
+        in[j] = load_vec<TI, E>(z, c);
       } else {
 #pragma unroll
-        for (int k = 0; k < E; ++k) in[j].v[k] = c + k < n ? z[c + k] : (TI)0.f;
+        for (int k = 0; k < E; ++k) in[j].v[k] = c + k < n ? entry(z, c)[k] : (TI)0.f;
       }
-      open[j] = c + E <= n ? ~0u : c < n ? (1u << (n - c)) - 1u : 0u;
-      if (w.mask >= 0 && c < n) open[j] &= a.r.mask[w.mask * a.r.mask_ld + ((v0 + c) >> 5)] >> ((v0 + c) & 31);
+    }
+  };
+  request(r0);
+  auto clear = [&](uint32_t* words) {
+    for (int c = tid * 4; c < kWords; c += kThreads * 4) *(uint4*)(words + c) = uint4{0, 0, 0, 0};
+  };
+  if (hist) clear(cnt);
+  if (bias) clear(last);
+  if constexpr (SPARSE) __syncthreads();
+
+  int64_t pb = -1, ps = 0, pe = 0;  // the history counted in cnt; pb < 0: none yet
+  int64_t qb = -1, qe = -1;         // the bias list in last; qb < 0: none yet
+  Row w = read_row(r0, hist, bias);
+  // With `ahead`, the tokens by which this row's history extends the last one's, at most one per thread, were
+  // requested with the row.
+  bool ahead = false;
+  uint32_t token_ahead = ~0u;
+
+  for (int i = 0; i < n_rows; ++i) {
+    // Opaque copies: the entries' bounds and offsets are worked out where they are used, not once for all rows and
+    // kept in (spilled) registers.
+    asm volatile("" : "+s"(n), "+v"(tid));
+    const int64_t row = r0 + i;
+    const ArgsPtr a = kernel_args();
+    const float inv_tau = a->inv_tau;
+    TO* out = OP == Op::kStats ? nullptr : (TO*)a->out + row * a->out_ld + v0;
+    int tok = -1;  // relative to the chunk; negative or past it: elsewhere
+    float lse = 0.f, ent = 0.f, g = 0.f, e = 0.f;
+    if constexpr (OP != Op::kAdjust) {
+      const int token = scalar(a->tokens, row);
+      const bool valid = (unsigned)token < (unsigned)a->V;
+      if (valid) tok = token - v0;
+      if constexpr (OP == Op::kGrad) {
+        lse = scalar(a->lse, row);
+        g = valid ? scalar(a->grad_logp, row) : 0.f;
+        if (a->grad_entropy) {
+          e = scalar(a->grad_entropy, row);
+          ent = scalar(a->entropy, row);
+        }
+        if ((g == 0.f && e == 0.f) || lse == kNegInf) {
+          for (int c = tid; c < n; c += kThreads) *entry(out, c) = (TO)0.f;
+          if (i + 1 < n_rows) {
+            request(row + 1);
+            w = read_row(row + 1, hist, bias);
+            ahead = false;
+          }
+          continue;
+        }
+      }
+    }
+
+    // bit k: entry k of the load is allowed and lies in the vocabulary
+    uint32_t open[NV];
+    const uint32_t* mask = a->r.mask + w.mask * a->r.mask_ld + v0 / 32;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (j * kThreads + tid) * E;
+      open[j] = ~0u;
+      if (n < kChunk) open[j] = c + E <= n ? ~0u : c < n ? (1u << (n - c)) - 1u : 0u;
+      if (w.mask >= 0 && c < n) open[j] &= *entry(mask, c >> 5) >> (c & 31);
     }
 
     if (hist) {
       const int64_t b = w.begin, s = w.split, t = w.end;
       int64_t from = pe;
       if (b != pb || s != ps || t < pe) {
-        for (int c = threadIdx.x * 4; c < kChunk; c += kThreads * 4) *(uint4*)(cnt + c) = uint4{0, 0, 0, 0};
         from = b;
-        __syncthreads();
+        if (pb >= 0) {
+          clear(cnt);
+          __syncthreads();
+        }
       }
-      count_tokens(cnt, a.r.history, from, s, t, v0, n);
+      if (ahead)
+        count_token(cnt, cnt + kChunk, token_ahead, from + tid < s, n);
+      else
+        count_tokens(cnt, cnt + kChunk, a->r.history, from, s, t, v0, n);
       pb = b;
       ps = s;
       pe = t;
@@ -220,11 +349,16 @@ __global__ __launch_bounds__(kThreads) void rules_kernel(const RuleArgs a, int n
     if (bias) {
       const int64_t b = w.bias0, t = w.bias1;
       if (b != qb || t != qe) {
-        for (int c = threadIdx.x * 4; c < kChunk; c += kThreads * 4) *(uint4*)(last + c) = uint4{0, 0, 0, 0};
-        __syncthreads();
-        for (int64_t k = b + threadIdx.x; k < t; k += kThreads) {
-          const uint32_t id = (uint32_t)a.r.bias_ids[k] - (uint32_t)v0;
-          if (id < (uint32_t)n) atomicMax(&last[id], (uint32_t)k + 1u);
+        if (qb >= 0) {
+          clear(last);
+          __syncthreads();
+        }
+        for (int64_t k = b + tid; k < t; k += kThreads) {
+          const uint32_t id = (uint32_t)a->r.bias_ids[k] - (uint32_t)v0;
+          if (id < (uint32_t)n) {
+            atomicOr(&last[kChunk + (id >> 5)], 1u << (id & 31));
+            atomicMax(&last[id], (uint32_t)k + 1u);
+          }
         }
         qb = b;
         qe = t;
@@ -232,154 +366,193 @@ __global__ __launch_bounds__(kThreads) void rules_kernel(const RuleArgs a, int n
     }
     if constexpr (SPARSE) __syncthreads();
 
-    float x[kPer];
-    float m = kNegInf;
+    float x[kPer];  // entry k of the thread: number k % E of its load k / E
+    uint32_t opened = 0, touched = 0;
+    constexpr uint32_t kAll = (1u << E) - 1u, kAllOpen = (uint32_t)((1ull << kPer) - 1u);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * kThreads + (int)threadIdx.x) * E;
-      float* y = x + j * E;
-      float slope[E];
-#pragma unroll
-      for (int k = 0; k < E; ++k) {
-        y[k] = widen(in[j].v[k]);
-        slope[k] = a.inv_tau;
-      }
-      if (hist) {
-        uint32_t u[E], any = 0;
-#pragma unroll
-        for (int k = 0; k < E; k += 4) __builtin_memcpy(u + k, __builtin_assume_aligned(cnt + c + k, 16), 16);
-#pragma unroll
-        for (int k = 0; k < E; ++k) any |= u[k];
-        if (any) {
-#pragma unroll
-          for (int k = 0; k < E; ++k) {
-            const float up = y[k] / w.rho, down = y[k] * w.rho;
-            const bool pos = y[k] > 0.f;
-            float v = u[k] ? (pos ? up : down) : y[k];
-            if constexpr (OP == Op::kGrad) slope[k] = u[k] ? (pos ? w.inv_rho : w.rho) * a.inv_tau : a.inv_tau;
-            const uint32_t count = u[k] & ~kPromptBit;
-            const float less = v - w.freq * (float)count - w.pres;
-            y[k] = count ? less : v;
-          }
-        }
-      }
-      if (bias) {
-        uint32_t u[E], any = 0;
-#pragma unroll
-        for (int k = 0; k < E; k += 4) __builtin_memcpy(u + k, __builtin_assume_aligned(last + c + k, 16), 16);
-#pragma unroll
-        for (int k = 0; k < E; ++k) any |= u[k];
-        if (any) {
-#pragma unroll
-          for (int k = 0; k < E; ++k)
-            if (u[k]) y[k] = y[k] + a.r.bias_values[u[k] - 1];
-        }
+      opened |= (open[j] & kAll) << (j * E);
+      if constexpr (SPARSE) {
+        const int c = (j * kThreads + tid) * E;
+        const uint32_t t = (hist ? cnt[kChunk + (c >> 5)] : 0u) | (bias ? last[kChunk + (c >> 5)] : 0u);
+        touched |= (t >> (c & 31) & kAll) << (j * E);
       }
 #pragma unroll
-      for (int k = 0; k < E; ++k) y[k] = y[k] * a.inv_tau;
-      if (some_off) {
+      for (int k = 0; k < E; ++k) x[j * E + k] = widen(in[j].v[k]);
+    }
+    const bool some_off = __any(opened != kAllOpen);
+    const float inv_rho = SPARSE ? 1.f / w.rho : 1.f;
+
+    // The gradient of an entry: y short of the temperature.
+    auto grad = [&](float y) {
+      const float q = fmaf(y, inv_tau, -lse);
+      const float p = exp2_hw(q * kLog2e);
+      return e == 0.f ? -p * g : -p * (g + e * (fmaxf(q, kFloor) + ent));
+    };
+    float r[OP == Op::kGrad ? kPer : 1];
+    if constexpr (OP == Op::kGrad) {
+      if (e == 0.f) {
+        const float gs = -g * inv_tau;
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-          const bool off = !((open[j] >> k) & 1u);
-          y[k] = off ? kNegInf : y[k];
-          slope[k] = off ? 0.f : slope[k];
-        }
-      }
-      if constexpr (OP == Op::kStats) {
-#pragma unroll
-        for (int k = 0; k < E; ++k) m = fmaxf(m, y[k]);
+        for (int k = 0; k < kPer; ++k) r[k] = exp2_hw(fmaf(x[k], inv_tau, -lse) * kLog2e) * gs;
       } else {
-        Vec<TO, E> o;
-        if constexpr (OP == Op::kAdjust) {
 #pragma unroll
-          for (int k = 0; k < E; ++k) o.v[k] = narrow<TO>(y[k]);
-        } else {
+        for (int k = 0; k < kPer; ++k) r[k] = grad(x[k]) * inv_tau;
+      }
+      if (tok >= 0 && tok < n && tok / E % kThreads == tid) {
 #pragma unroll
-          for (int k = 0; k < E; ++k) {
-            const float q = y[k] - w.lse;
-            const float p = exp_hw(q);
-            float up = c + k == w.tok ? w.g : 0.f;
-            up = up - p * (w.g + w.e * (fmaxf(q, kFloor) + w.ent));
-            o.v[k] = narrow<TO>(slope[k] == 0.f ? 0.f : up * slope[k]);
+        for (int k = 0; k < kPer; ++k)
+          if ((k / E * kThreads + tid) * E + k % E == tok) r[k] = (g + grad(x[k])) * inv_tau;
+      }
+    }
+    if constexpr (SPARSE) {
+      // the touched ones by themselves, picked out of the registers and put back
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        for (uint32_t left = touched >> (j * E) & kAll; left; left &= left - 1) {
+          const int at = __builtin_ctz(left);
+          const int c = (j * kThreads + tid) * E + at;
+          float y = x[j * E];
+#pragma unroll
+          for (int k = 1; k < E; ++k) y = k == at ? x[j * E + k] : y;
+          float factor = 1.f;
+          const uint32_t u = hist ? cnt[c] : 0u;
+          if (u) y = penalise(y, u, w, inv_rho, factor);
+          const uint32_t b = bias ? last[c] : 0u;
+          if (b) y = y + a->r.bias_values[b - 1];
+          if constexpr (OP == Op::kGrad) {
+            y = (c == tok ? g + grad(y) : grad(y)) * (factor * inv_tau);
+#pragma unroll
+            for (int k = 0; k < E; ++k) r[j * E + k] = k == at ? y : r[j * E + k];
+          } else {
+#pragma unroll
+            for (int k = 0; k < E; ++k) x[j * E + k] = k == at ? y : x[j * E + k];
           }
         }
+      }
+    }
+    if constexpr (OP == Op::kAdjust) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) x[k] = x[k] * inv_tau;
+    }
+    if (some_off) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        if constexpr (OP == Op::kGrad)
+          r[k] = choose(opened, k, r[k], 0.f);
+        else
+          x[k] = choose(opened, k, x[k], kNegInf);
+      }
+    }
+    if constexpr (OP != Op::kStats) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int c = (j * kThreads + tid) * E;
+        Vec<TO, E> o;
+#pragma unroll
+        for (int k = 0; k < E; ++k) o.v[k] = narrow<TO>(OP == Op::kGrad ? r[j * E + k] : x[j * E + k]);
         if (c + E <= n) {
-          store_vec<TO, E>(out + c, o);
+          store_vec<TO, E>(out, c, o);
         } else {
 #pragma unroll
           for (int k = 0; k < E; ++k)
-            if (c + k < n) out[c + k] = o.v[k];
+            if (c + k < n) entry(out, c)[k] = o.v[k];
         }
       }
     }
 
+    if (i + 1 < n_rows) {
+      request(row + 1);
+      w = read_row(row + 1, hist, bias);
+      ahead = hist && w.begin == pb && w.split == ps && w.end >= pe && w.end - pe <= kThreads;
+      if (ahead) token_ahead = tid < (int)(w.end - pe) ? (uint32_t)*entry(a->r.history + pe, tid) - (uint32_t)v0 : ~0u;
+    }
     if constexpr (OP == Op::kStats) {
+      float m = x[0], low = x[0];
+#pragma unroll
+      for (int k = 1; k < kPer; ++k) {
+        m = fmaxf(m, x[k]);
+        low = fminf(low, x[k]);
+      }
       m = wave_max(m);
       const float at = m == kNegInf ? 0.f : m;
       float s = 0.f, u = 0.f;
+      if (__any(!((low - at) * log2e_tau > kFloor))) {  // entries whose 2^t is 0, t perhaps -inf (or a NaN)
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) {
-        const float q = x[k] - at;
-        const float p = exp_hw(q);
-        s += p;
-        u = fmaf(p, fmaxf(q, kFloor), u);
+        for (int k = 0; k < kPer; ++k) {
+          const float t = (x[k] - at) * log2e_tau;
+          const float p = exp2_hw(t);
+          s += p;
+          u = fmaf(p, fmaxf(t, kFloor), u);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+          const float t = (x[k] - at) * log2e_tau;
+          const float p = exp2_hw(t);
+          s += p;
+          u = fmaf(p, t, u);
+        }
       }
       s = wave_sum(s);
       u = wave_sum(u);
-      if ((threadIdx.x & 63) == 0) wstat[threadIdx.x >> 6] = {m, s, u};
-      const int tok = w.tok;
-      if (tok >= 0 && tok < n && tok / E % kThreads == (int)threadIdx.x) {
+      const int par = i & 1;
+      if ((tid & 63) == 0) wstat[par][tid >> 6] = {m, s, u};
+      if (tok >= 0 && tok < n && tok / E % kThreads == tid) {
 #pragma unroll
         for (int k = 0; k < kPer; ++k)
-          if (tok / E / kThreads * E + tok % E == k) tok_x = x[k];
+          if ((k / E * kThreads + tid) * E + k % E == tok) tok_x[par] = x[k];
       }
       __syncthreads();
-      if (threadIdx.x == 0) {
-        float top = wstat[0].m;
-#pragma unroll
-        for (int v = 1; v < kWaves; ++v) top = fmaxf(top, wstat[v].m);
-        Partial p = {top, 0.f, 0.f, tok >= 0 && tok < n ? tok_x : 0.f};
-#pragma unroll
-        for (int v = 0; v < kWaves; ++v) {
-          const Stat t = shift(wstat[v], top);
-          p.s += t.s;
-          p.u += t.u;
-        }
-        ((Partial*)a.part)[row * n_chunks + chunk] = p;
+      if (tid < 64) {  // lane l merges wave l % kWaves' with the others'
+        const Stat mine = wstat[par][tid % kWaves];
+        float top = fmaxf(mine.m, ror<4>(mine.m));
+        top = fmaxf(top, ror<2>(top));
+        top = fmaxf(top, ror<1>(top));
+        Stat t = shift(mine, top, log2e_tau);
+        t.s += ror<4>(t.s);
+        t.s += ror<2>(t.s);
+        t.s += ror<1>(t.s);
+        t.u += ror<4>(t.u);
+        t.u += ror<2>(t.u);
+        t.u += ror<1>(t.u);
+        if (tid == 0)
+          ((Partial*)a->part)[row * n_chunks + chunk] = {top, t.s, t.u, tok >= 0 && tok < n ? tok_x[par] : 0.f};
       }
+    } else if (SPARSE) {
+      __syncthreads();  // the next row changes what this one read from LDS
     }
-    // the next row changes what this one read from LDS
-    if (SPARSE || OP == Op::kStats) __syncthreads();
   }
 }
 
 // One wave per row: lane c holds chunk c's partial.
 __global__ __launch_bounds__(256) void rules_merge(const Partial* __restrict__ part, const int32_t* __restrict__ tokens,
-                                                   int64_t T, int V, int n_chunks, float* __restrict__ logp,
-                                                   float* __restrict__ entropy, float* __restrict__ lse) {
+                                                   int64_t T, int V, int n_chunks, float inv_tau,
+                                                   float* __restrict__ logp, float* __restrict__ entropy,
+                                                   float* __restrict__ lse) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (row >= T) return;
   Partial p = {kNegInf, 0.f, 0.f, 0.f};
   if (lane < n_chunks) p = part[row * n_chunks + lane];
   const float top = wave_max(p.m);
-  const Stat t = shift({p.m, p.s, p.u}, top);
+  const Stat t = shift({p.m, p.s, p.u}, top, kLog2e * inv_tau);
   const float S = wave_sum(t.s);
   const float U = wave_sum(t.u);
   const int tok = tokens[row];
   const bool valid = (unsigned)tok < (unsigned)V;
-  const float x = __shfl(p.ztok, valid ? tok / kChunk : 0);
+  const float y = __shfl(p.ztok, valid ? tok / kChunk : 0);
   if (lane == 0) {
     const bool none = top == kNegInf && S == 0.f;  // nothing allowed
     const float log_s = logf(S);
-    logp[row] = !valid ? __builtin_nanf("") : none ? kNegInf : (x - top) - log_s;
-    if (entropy) entropy[row] = none ? 0.f : log_s - U / S;
-    if (lse) lse[row] = none ? kNegInf : top + log_s;
+    logp[row] = !valid ? __builtin_nanf("") : none ? kNegInf : (y - top) * inv_tau - log_s;
+    if (entropy) entropy[row] = none ? 0.f : log_s - kLn2 * (U / S);
+    if (lse) lse[row] = none ? kNegInf : top * inv_tau + log_s;
   }
 }
 
 int rule_lds_bytes(const RuleArgs& a) {
-  return ((a.r.history ? 1 : 0) + (a.r.bias_ids ? 1 : 0)) * kChunk * 4;
+  return ((a.r.history ? 1 : 0) + (a.r.bias_ids ? 1 : 0)) * kWords * 4;
 }
 
 // `a` from row t0 on.
@@ -459,7 +632,8 @@ hipError_t launch_logits_logprobs(const RuleArgs& a, int dtype, float* logp, flo
   for (int64_t t0 = 0; t0 < a.T; t0 += step) {
     const int64_t rows = a.T - t0 < step ? a.T - t0 : step;
     rules_merge<<<(unsigned)((rows + 3) / 4), 256, 0, s>>>((const Partial*)a.part + t0 * n_chunks, a.tokens + t0, rows,
-                                                           a.V, n_chunks, logp + t0, entropy ? entropy + t0 : nullptr,
+                                                           a.V, n_chunks, a.inv_tau, logp + t0,
+                                                           entropy ? entropy + t0 : nullptr,
                                                            lse ? lse + t0 : nullptr);
     const hipError_t m = hipGetLastError();
     if (m != hipSuccess) return m;
