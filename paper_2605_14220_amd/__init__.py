@@ -531,17 +531,14 @@ def _launch(device, call, *args):
             _check(call(*args, _stream(device)))
 
 
-def _row_stride(t) -> int:
-    """Elements from row to row of a [rows, n] tensor (a lone row's stride means nothing)."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
-
-
-def _dense_rows(name, what, t):
-    """Refuses all but a matrix of dense rows that do not share elements."""
+def _dense_rows(name, what, t) -> int:
+    """Elements from row to row of a matrix of dense rows that do not share elements; refuses any other."""
     if t.dim() != 2:
         raise ValueError(f"tim.{name}: {what} must be a matrix")
-    if t.numel() and ((t.shape[1] > 1 and t.stride(1) != 1) or _row_stride(t) < t.shape[1]):
+    (n, m), (row, col) = t.shape, t.stride()
+    if n and m and ((m > 1 and col != 1) or (n > 1 and row < m)):
         raise ValueError(f"tim.{name}: {what} must have dense rows that do not overlap")
+    return row if n > 1 and m else max(m, 1)  # a lone row's stride means nothing
 
 
 class Mxfp4(NamedTuple):
@@ -569,7 +566,7 @@ def mxfp4_quantize(x: torch.Tensor, out: Mxfp4 | None = None) -> Mxfp4:
     lib = load_library()
     if x.dtype not in _DTYPES:
         raise TypeError("tim.mxfp4_quantize: x must be fp32, bf16 or fp16")
-    _dense_rows("mxfp4_quantize", "x", x)
+    ld = _dense_rows("mxfp4_quantize", "x", x)
     rows, d = x.shape
     if d < MXFP4_BLOCK or d % MXFP4_BLOCK:
         raise ValueError("tim.mxfp4_quantize: d must be a multiple of 32")
@@ -579,7 +576,7 @@ def mxfp4_quantize(x: torch.Tensor, out: Mxfp4 | None = None) -> Mxfp4:
     elif _mxfp4_shape("mxfp4_quantize", out) != (rows, d):
         raise ValueError("tim.mxfp4_quantize: out must hold [rows, d]")
     _on_one_gpu("mxfp4_quantize", x.device, x, *out)
-    _launch(x.device, lib.tim_mxfp4_quantize, _ptr(x), _DTYPES[x.dtype], rows, d, _row_stride(x), _ptr(out.codes),
+    _launch(x.device, lib.tim_mxfp4_quantize, _ptr(x), _DTYPES[x.dtype], rows, d, ld, _ptr(out.codes),
             _ptr(out.scales))
     return out
 
@@ -621,10 +618,10 @@ def mxfp4_logits(hidden: Mxfp4, w_vocab: Mxfp4, temperature: float = 1.0, dtype:
         raise ValueError("tim.mxfp4_logits: out must be [T, V]")
     if out.dtype not in _DTYPES:
         raise TypeError("tim.mxfp4_logits: logits are fp32, bf16 or fp16")
-    _dense_rows("mxfp4_logits", "out", out)
+    ld = _dense_rows("mxfp4_logits", "out", out)
     _on_one_gpu("mxfp4_logits", dev, *hidden, *w_vocab, out)
     _launch(dev, lib.tim_mxfp4_logits, _ptr(hidden.codes), _ptr(hidden.scales), _ptr(w_vocab.codes),
-            _ptr(w_vocab.scales), T, d, V, float(temperature), _ptr(out), _DTYPES[out.dtype], _row_stride(out))
+            _ptr(w_vocab.scales), T, d, V, float(temperature), _ptr(out), _DTYPES[out.dtype], ld)
     return out
 
 
@@ -653,8 +650,18 @@ class LogitRules:
     mask: torch.Tensor | None = None
     mask_rows: torch.Tensor | None = None
 
+    def __setattr__(self, field, value):
+        object.__setattr__(self, field, value)
+        object.__setattr__(self, "_built", None)
+
     def _struct(self, name, T, V, device) -> _LogitRules:
-        s = _LogitRules()
+        """The C struct for T rows of V logits on the device. It is checked and filled once and kept until a field is
+        set or a tensor's storage is another one; what the tensors hold may change in between."""
+        if self._built is not None:
+            s, held, rows, words, on = self._built
+            if rows == T and words * 32 >= V and on == device and all(t.data_ptr() == p for t, p in held):
+                return s
+        s, held, words = _LogitRules(), [], MAX_VOCAB
 
         def take(field, dtype, n=None):
             t = getattr(self, field)
@@ -669,6 +676,7 @@ class LogitRules:
             if not t.is_contiguous():
                 raise ValueError(f"tim.{name}: {field} must be contiguous")
             setattr(s, field, t.data_ptr())
+            held.append((t, t.data_ptr()))
 
         if self.history is not None:
             if self.hist_begin is None or self.hist_end is None:
@@ -690,27 +698,30 @@ class LogitRules:
         if self.mask is not None:
             if self.mask.dtype != torch.int32:
                 raise TypeError(f"tim.{name}: mask must be torch.int32")
-            _dense_rows(name, "mask", self.mask)
+            ld = _dense_rows(name, "mask", self.mask)
             if self.mask.device != device:
                 raise ValueError(f"tim.{name}: tensors must be on one GPU")
-            if self.mask.shape[1] < (V + 31) // 32:
+            words = self.mask.shape[1]
+            if words * 32 < V:
                 raise ValueError(f"tim.{name}: mask must have ceil(V / 32) words a row")
             if self.mask_rows is None and self.mask.shape[0] != T:
                 raise ValueError(f"tim.{name}: without mask_rows there is one mask a row")
-            s.mask, s.n_masks, s.mask_ld = self.mask.data_ptr(), self.mask.shape[0], _row_stride(self.mask)
+            s.mask, s.n_masks, s.mask_ld = self.mask.data_ptr(), self.mask.shape[0], ld
+            held.append((self.mask, s.mask))
             take("mask_rows", torch.int32, T)
+        object.__setattr__(self, "_built", (s, held, T, words, device))
         return s
 
 
 def _changed(name, logits, rules):
-    """(T, V, C rules or None) of the operators on changed logits."""
+    """(T, V, row stride, C rules or None) of the operators on changed logits."""
     if logits.dtype not in _DTYPES:
         raise TypeError(f"tim.{name}: logits must be fp32, bf16 or fp16")
-    _dense_rows(name, "logits", logits)
+    ld = _dense_rows(name, "logits", logits)
     if not logits.is_cuda:
         raise ValueError("tim: tensors must be on the GPU")
     T, V = logits.shape
-    return T, V, None if rules is None else ctypes.byref(rules._struct(name, T, V, logits.device))
+    return T, V, ld, None if rules is None else ctypes.byref(rules._struct(name, T, V, logits.device))
 
 
 def _row_vector(name, what, t, T, dtype):
@@ -728,15 +739,17 @@ def logits_adjust(logits: torch.Tensor, rules: LogitRules | None = None, tempera
     """The logits [T, V] (fp32, bf16 or fp16, dense rows) as a sampler reads them: penalties, bias, temperature and
     mask applied, each entry rounded once to the logits' type. out may be logits itself (in place)."""
     lib = load_library()
-    T, V, r = _changed("logits_adjust", logits, rules)
+    T, V, ld, r = _changed("logits_adjust", logits, rules)
     if out is None:
         out = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
-    if out.shape != (T, V) or out.dtype != logits.dtype:
-        raise ValueError("tim.logits_adjust: out must be like logits")
-    _dense_rows("logits_adjust", "out", out)
-    _on_one_gpu("logits_adjust", logits.device, logits, out)
-    _launch(logits.device, lib.tim_logits_adjust, _ptr(logits), _DTYPES[logits.dtype], T, V, _row_stride(logits), r,
-            float(temperature), _ptr(out), _row_stride(out))
+        out_ld = max(V, 1)
+    else:
+        if out.shape != (T, V) or out.dtype != logits.dtype:
+            raise ValueError("tim.logits_adjust: out must be like logits")
+        out_ld = _dense_rows("logits_adjust", "out", out)
+        _on_one_gpu("logits_adjust", logits.device, out)
+    _launch(logits.device, lib.tim_logits_adjust, _ptr(logits), _DTYPES[logits.dtype], T, V, ld, r, float(temperature),
+            _ptr(out), out_ld)
     return out
 
 
@@ -751,25 +764,29 @@ def logits_logprobs(logits: torch.Tensor, tokens: torch.Tensor, rules: LogitRule
     """Log-probabilities (and entropies, log-normalisers) of tokens int32 [T] under the changed logits of
     logits_adjust, from the logits themselves. Returns (logp, entropy or None, lse or None), fp32 [T] each."""
     lib = load_library()
-    T, V, r = _changed("logits_logprobs", logits, rules)
+    T, V, ld, r = _changed("logits_logprobs", logits, rules)
     dev = logits.device
     _row_vector("logits_logprobs", "tokens", tokens, T, torch.int32)
     if out is None:
-        lp = torch.empty(T, dtype=torch.float32, device=dev)
-        ent = torch.empty(T, dtype=torch.float32, device=dev) if entropy else None
-        ls = torch.empty(T, dtype=torch.float32, device=dev) if lse else None
+        rows = iter(torch.empty((1 + bool(entropy) + bool(lse), T), dtype=torch.float32, device=dev).unbind(0))
+        lp = next(rows)
+        ent = next(rows) if entropy else None
+        ls = next(rows) if lse else None
+        _on_one_gpu("logits_logprobs", dev, tokens)
     else:
         lp, ent, ls = out
         for what, t in (("logp", lp), ("entropy", ent), ("lse", ls)):
             _row_vector("logits_logprobs", what, t, T, torch.float32)
+        _on_one_gpu("logits_logprobs", dev, tokens, lp, ent, ls)
     if T == 0:
         return lp, ent, ls
     if workspace is None:
         workspace = torch.empty(logits_logprobs_workspace_size(T, V), dtype=torch.uint8, device=dev)
-    _require_gpu(workspace)
-    _on_one_gpu("logits_logprobs", dev, tokens, lp, ent, ls, workspace)
-    _launch(dev, lib.tim_logits_logprobs, _ptr(logits), _DTYPES[logits.dtype], T, V, _row_stride(logits), _ptr(tokens),
-            r, float(temperature), _ptr(lp), _ptr(ent), _ptr(ls), _ptr(workspace),
+    else:
+        _require_gpu(workspace)
+        _on_one_gpu("logits_logprobs", dev, workspace)
+    _launch(dev, lib.tim_logits_logprobs, _ptr(logits), _DTYPES[logits.dtype], T, V, ld, _ptr(tokens), r,
+            float(temperature), _ptr(lp), _ptr(ent), _ptr(ls), _ptr(workspace),
             workspace.numel() * workspace.element_size())
     return lp, ent, ls
 
@@ -782,7 +799,7 @@ def logits_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: to
     the changes. lse (and entropy, when grad_entropy is given) are logits_logprobs' outputs for the same inputs.
     dtype (the logits' by default) is the gradient's type; out may be logits itself where the types agree."""
     lib = load_library()
-    T, V, r = _changed("logits_logprobs_backward", logits, rules)
+    T, V, ld, r = _changed("logits_logprobs_backward", logits, rules)
     dev = logits.device
     _row_vector("logits_logprobs_backward", "tokens", tokens, T, torch.int32)
     for what, t in (("lse", lse), ("grad_logp", grad_logp), ("entropy", entropy), ("grad_entropy", grad_entropy)):
@@ -795,9 +812,9 @@ def logits_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: to
         raise TypeError("tim.logits_logprobs_backward: the gradient is fp32, bf16 or fp16")
     if out.shape != (T, V):
         raise ValueError("tim.logits_logprobs_backward: out must be [T, V]")
-    _dense_rows("logits_logprobs_backward", "out", out)
+    out_ld = _dense_rows("logits_logprobs_backward", "out", out)
     _on_one_gpu("logits_logprobs_backward", dev, tokens, lse, grad_logp, entropy, grad_entropy, out)
-    _launch(dev, lib.tim_logits_logprobs_backward, _ptr(logits), _DTYPES[logits.dtype], T, V, _row_stride(logits),
-            _ptr(tokens), r, float(temperature), _ptr(lse), _ptr(entropy), _ptr(grad_logp), _ptr(grad_entropy),
-            _ptr(out), _DTYPES[out.dtype], _row_stride(out))
+    _launch(dev, lib.tim_logits_logprobs_backward, _ptr(logits), _DTYPES[logits.dtype], T, V, ld, _ptr(tokens), r,
+            float(temperature), _ptr(lse), _ptr(entropy), _ptr(grad_logp), _ptr(grad_entropy), _ptr(out),
+            _DTYPES[out.dtype], out_ld)
     return out

@@ -212,3 +212,26 @@ def test_binding_refuses(call, error):
 def test_binding_refuses_rules(rules, error):
     with pytest.raises(error):
         tim.LogitRules(**rules)._struct("logits_adjust", 2, 40, torch.device("cpu"))
+
+
+def test_rules_are_filled_again_when_a_field_or_its_storage_changes():
+    cpu = torch.device("cpu")
+    r = tim.LogitRules(repetition=torch.ones(3), mask=torch.zeros(3, 2, dtype=torch.int32))
+    s = r._struct("logits_adjust", 3, 40, cpu)
+    assert r._struct("logits_adjust", 3, 64, cpu) is s and s.repetition == r.repetition.data_ptr()
+    r.repetition.mul_(2.0)  # contents may change
+    assert r._struct("logits_adjust", 3, 40, cpu) is s
+    with pytest.raises(ValueError):
+        r._struct("logits_adjust", 3, 65, cpu)   # the masks are too short
+    with pytest.raises(ValueError):
+        r._struct("logits_adjust", 4, 40, cpu)
+    r.repetition = torch.full((3,), 3.0)
+    t = r._struct("logits_adjust", 3, 40, cpu)
+    assert t is not s and t.repetition == r.repetition.data_ptr()
+    r.repetition.data = torch.full((3,), 4.0)
+    assert r._struct("logits_adjust", 3, 40, cpu).repetition == r.repetition.data_ptr()
+    r.repetition.data = torch.ones(3, dtype=torch.float64)
+    with pytest.raises(TypeError):
+        r._struct("logits_adjust", 3, 40, cpu)
+    r.repetition = None
+    assert r._struct("logits_adjust", 3, 40, cpu).repetition is None
