@@ -243,3 +243,43 @@ def test_every_end_of_a_row(T, d):
     hv = hv * torch.exp2(hs.double() - 127).repeat_interleave(32, 1)
     # sums of multiples of 1/8 below 36 * 2 * d < 2^21 units: exact in fp32
     assert torch.equal(tim.mxfp4_logits(h, w).double(), hv @ wv.T)
+
+
+@pytest.mark.parametrize("T,d", [(2, 640), (40, 1024), (100, 512), (300, 1152)])
+def test_nan_blocks_in_every_tile(T, d):
+    """As above with rows of a whole scale group and more, the NaN in the first, a middle and the last block."""
+    h, _ = _random(T, d, 13, 2)
+    w, _ = _random(300, d, 14, 2)
+    clean = tim.mxfp4_logits(h, w)
+    h.scales[1, 0] = 255
+    w.scales[77, d // 64] = 255
+    w.scales[299, d // 32 - 1] = 255
+    z = tim.mxfp4_logits(h, w)
+    bad = torch.zeros_like(z, dtype=torch.bool)
+    bad[1] = True
+    bad[:, [77, 299]] = True
+    assert torch.equal(torch.isnan(z), bad)
+    assert torch.equal(z[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("T", [3, 50, 100, 300])
+def test_scales_at_both_ends(T):
+    """One block of 2^60, the others of the smallest scale, against 2^-60: the small ones vanish, the rest is exact."""
+    d, V = 768, 200
+    codes = np.full((T, d), 2, np.uint8)  # 1.0 everywhere
+    hs = np.zeros((T, d // 32), np.uint8)
+    hs[:, 13] = 187
+    wc = np.full((V, d), 10, np.uint8)    # -1.0
+    ws = np.full((V, d // 32), 67, np.uint8)
+    h = tim.Mxfp4(torch.as_tensor(oracle.mxfp4_pack(codes)).cuda(), torch.as_tensor(hs).cuda())
+    w = tim.Mxfp4(torch.as_tensor(oracle.mxfp4_pack(wc)).cuda(), torch.as_tensor(ws).cuda())
+    assert (tim.mxfp4_logits(h, w) == -32.0).all()  # 32 products of 2^60 * -2^-60; the others sum to 736 * 2^-187
+
+
+def test_one_wide_row():
+    """A long d, one row: offsets along a row and the scale groups at their largest common size."""
+    d = 65536 + 128
+    h, hv = _random(1, d, 15, 0)
+    w, wv = _random(5, d, 16, 0)
+    # 36 * d * 4 units < 2^24: exact
+    assert torch.equal(tim.mxfp4_logits(h, w).double(), hv @ wv.T)

@@ -527,3 +527,101 @@ def test_rows_past_32_bit_offsets():
     for a, b in zip(whole, alone):
         assert torch.equal(a[T - 3:], b)
     assert torch.equal(tim.logits_adjust(z, None, 0.5)[T - 3:], tim.logits_adjust(z[T - 3:].clone(), None, 0.5))
+
+
+def _packed_rules(T, V, seed, masks):
+    """Histories of many short responses in one stream, some rows out of order, as tensors only."""
+    g = torch.Generator().manual_seed(seed)
+    n = T + 100
+    resp = torch.randint(1, 30, (T,), generator=g)
+    start = torch.cumsum(resp, 0) - resp
+    row = torch.arange(T)
+    first = torch.searchsorted(start, row, right=True) - 1
+    begin = start[first]
+    end = row.clone()
+    odd = torch.rand(T, generator=g) < 0.03
+    end[odd] = begin[odd] + torch.randint(0, 40, (int(odd.sum()),), generator=g)
+    split = begin + torch.randint(0, 3, (T,), generator=g)[first]
+    kw = dict(history=torch.randint(0, V, (n,), dtype=torch.int32, generator=g), hist_begin=begin, hist_split=split,
+              hist_end=end, repetition=0.5 + torch.rand(T, generator=g), frequency=torch.rand(T, generator=g),
+              presence=torch.rand(T, generator=g), bias_ids=torch.randint(0, V, (50,), dtype=torch.int32, generator=g),
+              bias_values=torch.randn(50, generator=g), bias_begin=first % 40, bias_end=first % 40 + first % 7)
+    if masks:
+        kw["mask"] = torch.randint(-2 ** 31, 2 ** 31, (T, (V + 31) // 32), dtype=torch.int64, generator=g).to(torch.int32)
+    return {k: v.cuda() for k, v in kw.items()}
+
+
+def _slice(kw, a, b):
+    rows = ("hist_begin", "hist_split", "hist_end", "repetition", "frequency", "presence", "bias_begin", "bias_end", "mask")
+    return tim.LogitRules(**{k: v[a:b].contiguous() if k in rows else v for k, v in kw.items()})
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_many_rows_to_a_workgroup(dtype):
+    """Rows enough for sixteen to a workgroup give the bits of calls with one row to each."""
+    T, V = 70001, 67
+    kw = _packed_rules(T, V, 31, True)
+    z = torch.randn(T, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(DTYPES[dtype])
+    tok = torch.randint(-1, V, (T,), device="cuda", dtype=torch.int32)
+    g = torch.randn(T, device="cuda")
+    g[::11] = 0.0
+    adj = tim.logits_adjust(z, _slice(kw, 0, T), 0.8)
+    lp, H, lse = tim.logits_logprobs(z, tok, _slice(kw, 0, T), 0.8, lse=True)
+    dz = tim.logits_logprobs_backward(z, tok, lse, g, _slice(kw, 0, T), 0.8)
+    for a in range(0, T, 4000):
+        b = min(T, a + 4000)
+        r = _slice(kw, a, b)
+        assert torch.equal(tim.logits_adjust(z[a:b], r, 0.8), adj[a:b])
+        for x, y in zip(tim.logits_logprobs(z[a:b], tok[a:b], r, 0.8, lse=True), (lp, H, lse)):
+            assert torch.equal(x.view(torch.int32), y[a:b].view(torch.int32))
+        assert torch.equal(tim.logits_logprobs_backward(z[a:b], tok[a:b], lse[a:b], g[a:b], r, 0.8), dz[a:b])
+
+
+def test_more_rows_than_a_launch():
+    """More rows than one launch takes (2^22 of one chunk), each with a mask of its own: the last rows against the same
+    rows alone."""
+    T, V = (1 << 22) + 5000, 5
+    kw = _packed_rules(T, V, 32, True)
+    z = torch.randn(T, V, device="cuda")
+    tok = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32)
+    g = torch.randn(T, device="cuda")
+    adj = tim.logits_adjust(z, _slice(kw, 0, T))
+    whole = tim.logits_logprobs(z, tok, _slice(kw, 0, T), lse=True)
+    dz = tim.logits_logprobs_backward(z, tok, whole[2], g, _slice(kw, 0, T))
+    for a, b in ((0, 100), ((1 << 22) - 50, (1 << 22) + 50), (T - 100, T)):
+        r = _slice(kw, a, b)
+        assert torch.equal(tim.logits_adjust(z[a:b], r), adj[a:b])
+        for x, y in zip(tim.logits_logprobs(z[a:b], tok[a:b], r, lse=True), whole):
+            assert torch.equal(x.view(torch.int32), y[a:b].view(torch.int32))
+        assert torch.equal(tim.logits_logprobs_backward(z[a:b], tok[a:b], whole[2][a:b], g[a:b], r), dz[a:b])
+
+
+def test_a_bias_for_the_whole_vocabulary():
+    """A list of every id, twice: the second entry of each wins."""
+    V = 20001
+    case = Case(2, V, 33, history=20)
+    ids = torch.cat([torch.randperm(V, generator=torch.Generator().manual_seed(k)) for k in (1, 2)]).to(torch.int32)
+    vals = torch.randn(2 * V, generator=torch.Generator().manual_seed(3))
+    case.lib.bias_ids, case.lib.bias_values = ids.cuda(), vals.cuda()
+    case.lib.bias_begin = torch.tensor([0, 7], device="cuda")
+    case.lib.bias_end = torch.tensor([2 * V, V + 7], device="cuda")
+    for r, (b, e) in zip(case.rules, ((0, 2 * V), (7, V + 7))):
+        r["bias"] = list(zip(ids[b:e].tolist(), vals[b:e].tolist()))
+    check_adjust(case, 0.7)
+    check_logprobs(case, 0.7)
+    check_backward(case, 0.7, True)
+
+
+def test_empty_rules():
+    """A rule set without anything, or with empty arrays, changes nothing but the temperature."""
+    z = torch.randn(3, 100, device="cuda")
+    none = torch.zeros(3, dtype=torch.int64, device="cuda")
+    empty = tim.LogitRules(history=torch.empty(0, dtype=torch.int32, device="cuda"), hist_begin=none, hist_end=none,
+                           repetition=torch.full((3,), 2.0, device="cuda"),
+                           bias_ids=torch.empty(0, dtype=torch.int32, device="cuda"),
+                           bias_values=torch.empty(0, device="cuda"), bias_begin=none, bias_end=none,
+                           mask=torch.empty((0, 4), dtype=torch.int32, device="cuda"),
+                           mask_rows=torch.zeros(3, dtype=torch.int32, device="cuda"))
+    want = tim.logits_adjust(z, None, 0.5)
+    assert torch.equal(tim.logits_adjust(z, empty, 0.5), want) and torch.equal(want, z * 2.0)
+    assert torch.equal(tim.logits_adjust(z, tim.LogitRules(), 0.5), want)
