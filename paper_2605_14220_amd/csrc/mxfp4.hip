@@ -17,7 +17,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kGroup = 8;       // elements of one lane: a quarter of a block
-constexpr int kGroupsEach = 4;  // groups per thread
+// Groups per thread: 151936 rows of 4096 bf16 elements quantised in 254 us with two (272 with four, 288 with eight),
+// dequantised in 276 with four (288, 292).
+constexpr int kGroupsIn = 2, kGroupsOut = 4;
 constexpr int64_t kLaunchBlocks = (int64_t)1 << 23;  // a grid holds fewer than 2^32 threads
 
 template <class T>
@@ -45,7 +47,7 @@ __device__ __forceinline__ uint32_t quantise_group(const float (&x)[kGroup], uin
     return 0;
   }
   scale = ex > 2 ? ex - 2 : 0;
-  const int e = 127 - (int)scale;
+  [[maybe_unused]] const int e = 127 - (int)scale;
   uint32_t c = 0;
 #if defined(__HIP_DEVICE_COMPILE__)
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, ldexpf(x[0], e), ldexpf(x[1], e), 1.f, 0);
@@ -62,9 +64,9 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void quantise(const T* __restrict__ x, int64_t groups, int64_t first,
                                                      int64_t per_row, int64_t ld, uint8_t* __restrict__ codes,
                                                      uint8_t* __restrict__ scales) {
-  const int64_t g0 = first + (int64_t)blockIdx.x * (kThreads * kGroupsEach) + threadIdx.x;
+  const int64_t g0 = first + (int64_t)blockIdx.x * (kThreads * kGroupsIn) + threadIdx.x;
 #pragma unroll
-  for (int j = 0; j < kGroupsEach; ++j) {
+  for (int j = 0; j < kGroupsIn; ++j) {
     const int64_t g = g0 + j * kThreads;
     // a block's four lanes are on the same side of the end, which is a multiple of 4
     if (g >= groups) continue;
@@ -85,9 +87,9 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void dequantise(const uint8_t* __restrict__ codes,
                                                        const uint8_t* __restrict__ scales, int64_t groups,
                                                        int64_t first, T* __restrict__ out) {
-  const int64_t g0 = first + (int64_t)blockIdx.x * (kThreads * kGroupsEach) + threadIdx.x;
+  const int64_t g0 = first + (int64_t)blockIdx.x * (kThreads * kGroupsOut) + threadIdx.x;
 #pragma unroll
-  for (int j = 0; j < kGroupsEach; ++j) {
+  for (int j = 0; j < kGroupsOut; ++j) {
     const int64_t g = g0 + j * kThreads;
     if (g >= groups) continue;
     uint32_t c;
@@ -111,10 +113,10 @@ hipError_t quantise_as(const void* x, int64_t rows, int d, int64_t ld, uint8_t* 
                        hipStream_t s) {
   const int64_t groups = rows * d / kGroup;
   const int64_t per_row = ld == d ? groups : d / kGroup;
-  const int64_t blocks = (groups + kThreads * kGroupsEach - 1) / (kThreads * kGroupsEach);
+  const int64_t blocks = (groups + kThreads * kGroupsIn - 1) / (kThreads * kGroupsIn);
   for (int64_t b = 0; b < blocks; b += kLaunchBlocks) {
     const unsigned grid = (unsigned)(blocks - b < kLaunchBlocks ? blocks - b : kLaunchBlocks);
-    quantise<T><<<grid, kThreads, 0, s>>>((const T*)x, groups, b * kThreads * kGroupsEach, per_row, ld, codes, scales);
+    quantise<T><<<grid, kThreads, 0, s>>>((const T*)x, groups, b * kThreads * kGroupsIn, per_row, ld, codes, scales);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -124,10 +126,10 @@ hipError_t quantise_as(const void* x, int64_t rows, int d, int64_t ld, uint8_t* 
 template <class T>
 hipError_t dequantise_as(const uint8_t* codes, const uint8_t* scales, int64_t rows, int d, void* out, hipStream_t s) {
   const int64_t groups = rows * d / kGroup;
-  const int64_t blocks = (groups + kThreads * kGroupsEach - 1) / (kThreads * kGroupsEach);
+  const int64_t blocks = (groups + kThreads * kGroupsOut - 1) / (kThreads * kGroupsOut);
   for (int64_t b = 0; b < blocks; b += kLaunchBlocks) {
     const unsigned grid = (unsigned)(blocks - b < kLaunchBlocks ? blocks - b : kLaunchBlocks);
-    dequantise<T><<<grid, kThreads, 0, s>>>(codes, scales, groups, b * kThreads * kGroupsEach, (T*)out);
+    dequantise<T><<<grid, kThreads, 0, s>>>(codes, scales, groups, b * kThreads * kGroupsOut, (T*)out);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

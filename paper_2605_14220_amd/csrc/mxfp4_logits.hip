@@ -475,8 +475,6 @@ hipError_t launch_short(const Mxfp4LogitsArgs& a, hipStream_t s) {
   return hipSuccess;
 }
 
-constexpr int64_t kCacheBytes = (int64_t)256 << 20;  // the memory-side cache
-
 template <class T>
 hipError_t product_as(const Mxfp4LogitsArgs& a, hipStream_t s) {
   if (a.d < kMinD) return launch_short<T>(a, s);

@@ -136,7 +136,10 @@ struct RuleArgs {
   void* out;              // adjust, backward: [T, out_ld]
   int64_t out_ld;
   const float *lse, *entropy, *grad_logp, *grad_entropy;  // backward
+  int32_t past_caches;    // out is larger than the caches
 };
+
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;  // the memory-side cache
 
 // An fp32 value rounded once to T. To fp16 the compiler would merge a multiply
 // before it into one mixed-precision instruction that rounds the exact product

@@ -625,3 +625,23 @@ def test_empty_rules():
     want = tim.logits_adjust(z, None, 0.5)
     assert torch.equal(tim.logits_adjust(z, empty, 0.5), want) and torch.equal(want, z * 2.0)
     assert torch.equal(tim.logits_adjust(z, tim.LogitRules(), 0.5), want)
+
+
+@pytest.mark.parametrize("dtype,grad,T,V", [("f32", "f32", 570, 120001), ("bf16", "f32", 570, 120003),
+                                            ("f32", "bf16", 1200, 120001), ("f16", "f16", 1150, 120002)])
+def test_outputs_larger_than_the_caches(dtype, grad, T, V):
+    """Outputs of more than 256 MB in rows of odd lengths: the same bits as the rows a few at a time."""
+    kw = _packed_rules(T, V, 34, False)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    z = torch.randn(T, V, device="cuda", generator=gen).to(DTYPES[dtype])
+    tok = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32, generator=gen)
+    g, e = (torch.randn(T, device="cuda", generator=gen) for _ in range(2))
+    r = _slice(kw, 0, T)
+    _, H, lse = tim.logits_logprobs(z, tok, r, 0.9, lse=True)
+    dz = tim.logits_logprobs_backward(z, tok, lse, g, r, 0.9, entropy=H, grad_entropy=e, dtype=DTYPES[grad])
+    adj = tim.logits_adjust(z, r, 0.9)
+    for a, b in ((0, 5), (T // 2, T // 2 + 3), (T - 7, T)):
+        r = _slice(kw, a, b)
+        assert torch.equal(tim.logits_adjust(z[a:b], r, 0.9), adj[a:b])
+        assert torch.equal(tim.logits_logprobs_backward(z[a:b], tok[a:b], lse[a:b], g[a:b], r, 0.9, entropy=H[a:b],
+                                                        grad_entropy=e[a:b], dtype=DTYPES[grad]), dz[a:b])
