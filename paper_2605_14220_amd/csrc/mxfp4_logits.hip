@@ -43,10 +43,14 @@ constexpr int kMinD = 512;        // a row holds a whole group
 constexpr int kGroupFp4 = 16;
 
 // A workgroup of WV x WT waves, each NA x NB blocks of 16 x 16, and PER_CU
-// workgroups on a CU.
-template <int WV_, int WT_, int NA_, int NB_, int PER_CU_>
+// workgroups on a CU. ONCE: one tile takes all hidden rows, so W is read once
+// and its loads pass the caches by (1 row of d = 2048 and V = 151936 31.5 us
+// against 34.8, 64 of d = 4096 79 against 84, 200 129 against 136); where tiles
+// share W they find it in L2 (2000 rows 774 us against 895).
+template <int WV_, int WT_, int NA_, int NB_, int PER_CU_, bool ONCE_>
 struct Fp4Tile {
   static constexpr int WV = WV_, WT = WT_, NA = NA_, NB = NB_, PER_CU = PER_CU_;
+  static constexpr int kAuxW = ONCE_ ? 2 : 0;  // the cache policy of W's loads: 2, non-temporal
   static constexpr int NW = WV * WT;
   static constexpr int TA = WV * NA * 16;  // vocabulary entries
   static constexpr int TB = WT * NB * 16;  // hidden rows
@@ -200,8 +204,12 @@ __device__ __forceinline__ void fp4_load(unsigned char* buf, const Fp4Source& o,
   const int code = tail ? o.code_tail : o.code;
   const bool first = q < TL::LA;
   const int b = first ? block(q, TL::CA) : block(q - TL::LA, TL::CB);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(first ? o.ac : o.bc, (lds_void*)(buf + (first ? 0 : TL::kCodesB) + b * 1024),
-                                           16, (uint32_t)(code + b * 8 * o.rowc), stage * kStageCodes, 0, 0);
+  const uint32_t at = (uint32_t)(code + b * 8 * o.rowc);
+  if (first)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(o.ac, (lds_void*)(buf + b * 1024), 16, at, stage * kStageCodes, 0, TL::kAuxW);
+  else
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(o.bc, (lds_void*)(buf + TL::kCodesB + b * 1024), 16, at,
+                                             stage * kStageCodes, 0, 0);
 #endif
 }
 
@@ -478,14 +486,14 @@ hipError_t launch_short(const Mxfp4LogitsArgs& a, hipStream_t s) {
 template <class T>
 hipError_t product_as(const Mxfp4LogitsArgs& a, hipStream_t s) {
   if (a.d < kMinD) return launch_short<T>(a, s);
-  if (a.T <= 16) return launch_tiles<Fp4Tile<4, 1, 2, 1, 3>, T>(a, s);
-  if (a.T <= 32) return launch_tiles<Fp4Tile<4, 1, 2, 2, 3>, T>(a, s);
-  if (a.T <= 64) return launch_tiles<Fp4Tile<4, 1, 2, 4, 2>, T>(a, s);
-  using Small = Fp4Tile<4, 1, 2, 8, 2>;
-  using Large = Fp4Tile<2, 4, 8, 4, 1>;
-  if (a.T <= Small::TB || fp4_small_tiles(a.T, a.V, device_cu_count())) return launch_tiles<Small, T>(a, s);
-  if (a.T * a.V * (int64_t)sizeof(T) > kCacheBytes) return launch_tiles<Large, T, true>(a, s);
-  return launch_tiles<Large, T>(a, s);
+  if (a.T <= 16) return launch_tiles<Fp4Tile<4, 1, 2, 1, 3, true>, T>(a, s);
+  if (a.T <= 32) return launch_tiles<Fp4Tile<4, 1, 2, 2, 3, true>, T>(a, s);
+  if (a.T <= 64) return launch_tiles<Fp4Tile<4, 1, 2, 4, 2, true>, T>(a, s);
+  if (a.T <= 128) return launch_tiles<Fp4Tile<4, 1, 2, 8, 2, true>, T>(a, s);
+  if (fp4_small_tiles(a.T, a.V, device_cu_count())) return launch_tiles<Fp4Tile<4, 1, 2, 8, 2, false>, T>(a, s);
+  if (a.T * a.V * (int64_t)sizeof(T) > kCacheBytes) return launch_tiles<Fp4Tile<2, 4, 8, 4, 1, false>, T, true>(a, s);
+  if (a.T <= 256) return launch_tiles<Fp4Tile<2, 4, 8, 4, 1, true>, T>(a, s);
+  return launch_tiles<Fp4Tile<2, 4, 8, 4, 1, false>, T>(a, s);
 }
 
 }  // namespace
