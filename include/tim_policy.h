@@ -109,7 +109,8 @@ tim_status tim_mxfp4_logits(const uint8_t* h_codes, const uint8_t* h_scales, con
  * Every pointer may be NULL: no history (then the penalties are not applied),
  * no bias, no mask; of the penalties, NULL leaves its step out. Offsets are
  * clamped into their arrays and put in order (split to at least begin, end to
- * at least split); tokens and bias ids outside [0, V) are ignored. */
+ * at least split); tokens and bias ids outside [0, V) are ignored. A token may
+ * occur up to 2^31 - 1 times in a row's output. */
 typedef struct {
   const int32_t* history;     /* [history_len] tokens */
   int64_t history_len;

@@ -654,12 +654,21 @@ class LogitRules:
         object.__setattr__(self, field, value)
         object.__setattr__(self, "_built", None)
 
+    def __getstate__(self):
+        return {f.name: getattr(self, f.name) for f in dataclasses.fields(self)}
+
+    def __setstate__(self, state):
+        for field, value in state.items():
+            setattr(self, field, value)
+
     def _struct(self, name, T, V, device) -> _LogitRules:
         """The C struct for T rows of V logits on the device. It is checked and filled once and kept until a field is
-        set or a tensor's storage is another one; what the tensors hold may change in between."""
+        set or a tensor's storage or layout is another one; what the tensors hold may change in between."""
         if self._built is not None:
-            s, held, rows, words, on = self._built
-            if rows == T and words * 32 >= V and on == device and all(t.data_ptr() == p for t, p in held):
+            s, held, rows, words, on, mask_stride = self._built
+            if (rows == T and words * 32 >= V and on == device
+                    and all(t.data_ptr() == p and t.numel() == n for t, p, n in held)
+                    and (self.mask is None or (self.mask.shape[1] == words and self.mask.stride() == mask_stride))):
                 return s
         s, held, words = _LogitRules(), [], MAX_VOCAB
 
@@ -676,7 +685,7 @@ class LogitRules:
             if not t.is_contiguous():
                 raise ValueError(f"tim.{name}: {field} must be contiguous")
             setattr(s, field, t.data_ptr())
-            held.append((t, t.data_ptr()))
+            held.append((t, t.data_ptr(), t.numel()))
 
         if self.history is not None:
             if self.hist_begin is None or self.hist_end is None:
@@ -707,9 +716,9 @@ class LogitRules:
             if self.mask_rows is None and self.mask.shape[0] != T:
                 raise ValueError(f"tim.{name}: without mask_rows there is one mask a row")
             s.mask, s.n_masks, s.mask_ld = self.mask.data_ptr(), self.mask.shape[0], ld
-            held.append((self.mask, s.mask))
+            held.append((self.mask, self.mask.data_ptr(), self.mask.numel()))
             take("mask_rows", torch.int32, T)
-        object.__setattr__(self, "_built", (s, held, T, words, device))
+        object.__setattr__(self, "_built", (s, held, T, words, device, None if self.mask is None else self.mask.stride()))
         return s
 
 
@@ -737,7 +746,8 @@ def _row_vector(name, what, t, T, dtype):
 def logits_adjust(logits: torch.Tensor, rules: LogitRules | None = None, temperature: float = 1.0,
                   out: torch.Tensor | None = None) -> torch.Tensor:
     """The logits [T, V] (fp32, bf16 or fp16, dense rows) as a sampler reads them: penalties, bias, temperature and
-    mask applied, each entry rounded once to the logits' type. out may be logits itself (in place)."""
+    mask applied, each entry rounded once to the logits' type. out may be logits itself (in place), but no other
+    overlap of the two is allowed."""
     lib = load_library()
     T, V, ld, r = _changed("logits_adjust", logits, rules)
     if out is None:
@@ -797,7 +807,7 @@ def logits_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: to
                              dtype: torch.dtype | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient [T, V] of sum_t grad_logp[t] logp[t] + grad_entropy[t] entropy[t] with respect to the logits, through
     the changes. lse (and entropy, when grad_entropy is given) are logits_logprobs' outputs for the same inputs.
-    dtype (the logits' by default) is the gradient's type; out may be logits itself where the types agree."""
+    dtype (the logits' by default) is the gradient's type; out may be logits itself where the types agree, but no other overlap is allowed."""
     lib = load_library()
     T, V, ld, r = _changed("logits_logprobs_backward", logits, rules)
     dev = logits.device

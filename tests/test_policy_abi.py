@@ -1,8 +1,10 @@
 """The entry points of include/tim_policy.h on the host: exported, sized by the documented formula, and refusing every
 bad argument with the documented status before anything is enqueued. No call here reaches a launch."""
 
+import copy
 import ctypes
 import os
+import pickle
 import re
 import subprocess
 
@@ -235,3 +237,30 @@ def test_rules_are_filled_again_when_a_field_or_its_storage_changes():
         r._struct("logits_adjust", 3, 40, cpu)
     r.repetition = None
     assert r._struct("logits_adjust", 3, 40, cpu).repetition is None
+
+
+def test_rules_are_filled_again_when_a_tensor_is_cut_in_place():
+    cpu = torch.device("cpu")
+    r = tim.LogitRules(history=torch.zeros(9, dtype=torch.int32), hist_begin=torch.zeros(2, dtype=torch.int64),
+                       hist_end=torch.zeros(2, dtype=torch.int64), mask=torch.zeros(8, 2, dtype=torch.int32),
+                       mask_rows=torch.zeros(2, dtype=torch.int32))
+    s = r._struct("logits_adjust", 2, 40, cpu)
+    assert (s.history_len, s.n_masks, s.mask_ld) == (9, 8, 2)
+    r.history.data = r.history[:5]
+    r.mask.data = r.mask[::2]
+    s = r._struct("logits_adjust", 2, 40, cpu)
+    assert (s.history_len, s.n_masks, s.mask_ld) == (5, 4, 4)
+    r.hist_end.resize_(1)
+    with pytest.raises(ValueError):
+        r._struct("logits_adjust", 2, 40, cpu)
+
+
+@pytest.mark.parametrize("copied", [copy.copy, copy.deepcopy, lambda r: pickle.loads(pickle.dumps(r))])
+def test_rules_are_copied_after_a_call(copied):
+    cpu = torch.device("cpu")
+    r = tim.LogitRules(repetition=torch.ones(3), mask=torch.zeros(3, 2, dtype=torch.int32))
+    r._struct("logits_adjust", 3, 40, cpu)
+    c = copied(r)
+    s = c._struct("logits_adjust", 3, 40, cpu)
+    assert s.repetition == c.repetition.data_ptr() and s.mask == c.mask.data_ptr()
+    assert torch.equal(c.repetition, r.repetition) and c.presence is None
