@@ -718,7 +718,8 @@ class LogitRules:
             s.mask, s.n_masks, s.mask_ld = self.mask.data_ptr(), self.mask.shape[0], ld
             held.append((self.mask, self.mask.data_ptr(), self.mask.numel()))
             take("mask_rows", torch.int32, T)
-        object.__setattr__(self, "_built", (s, held, T, words, device, None if self.mask is None else self.mask.stride()))
+        stride = None if self.mask is None else self.mask.stride()
+        object.__setattr__(self, "_built", (s, held, T, words, device, stride))
         return s
 
 
@@ -807,7 +808,8 @@ def logits_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: to
                              dtype: torch.dtype | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient [T, V] of sum_t grad_logp[t] logp[t] + grad_entropy[t] entropy[t] with respect to the logits, through
     the changes. lse (and entropy, when grad_entropy is given) are logits_logprobs' outputs for the same inputs.
-    dtype (the logits' by default) is the gradient's type; out may be logits itself where the types agree, but no other overlap is allowed."""
+    dtype (the logits' by default) is the gradient's type; out may be logits itself where the types agree,
+    but no other overlap is allowed."""
     lib = load_library()
     T, V, ld, r = _changed("logits_logprobs_backward", logits, rules)
     dev = logits.device
