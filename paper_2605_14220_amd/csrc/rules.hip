@@ -23,7 +23,11 @@
 // entries are, and it walks those by themselves, picking each out of its
 // registers; with the penalties' code inside the pass over the row, once per
 // entry of a load, 4096 rows of 151936 logits with up to 1280 tokens of history
-// took 574 us against 533.
+// took 574 us against 533 (before other steps made both faster).
+//
+// Reads reach 7 TB/s (4096 rows of 151936 fp32 logits without rules 355 us). With histories, and for 16-bit logits, the
+// vector instructions of the row loop bound the statistics (456 us fp32, 390 us bf16, 270 us bf16 without rules),
+// so whole chunks, all but the last of a row, take a path without bounds per load (bf16 450 us with them).
 
 #include <hip/hip_runtime.h>
 
@@ -155,8 +159,9 @@ __device__ __forceinline__ void count_token(uint32_t* cnt, uint32_t* touched, ui
 }
 
 // Tokens history[from .. to), the prompt's before split. Two loads a thread are
-// in flight at a time (more take registers from the rows': with eight 4096 rows
-// of 151936 logits took 602 us, with two 533).
+// in flight at a time: more take registers from the rows' (with two 64 rows of
+// 151936 logits take 17.7 us, with four 19.3, with eight 20.9; 4096 rows 495,
+// 495 and 525).
 __device__ __forceinline__ void count_tokens(uint32_t* cnt, uint32_t* touched, const int32_t* __restrict__ history,
                                              int64_t from, int64_t split, int64_t to, int v0, int n) {
   constexpr int kStep = 2 * kThreads;
@@ -251,7 +256,8 @@ __device__ __forceinline__ float choose(uint32_t bits, int k, float x, float z) 
 // LDS words of a history or a bias list: one per entry, and their bitmap.
 constexpr int kWords = kChunk + kChunk / 32;
 
-// Three workgroups a CU (80 registers): two (90 registers) took 8-20% longer, four spill.
+// Three workgroups a CU (80 registers): with two 4096 rows of 151936 logits take 560 us against 500 and 64 rows 19.9
+// against 17.7 (the gradients the same); four spill.
 template <Op OP, class TI, class TO, bool SPARSE>
 __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args, int n_chunks, int rows_per_group) {
   const ArgsPtr a = kernel_args();  // args
@@ -261,6 +267,8 @@ __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args,
   extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   __shared__ Stat wstat[2][kWaves];  // by row in turn, so that a row need not wait for the last one's merge
   __shared__ float tok_x[2];
+  // of the group's rows, stored at the end: a wait for the next row's loads would be one for the store too
+  __shared__ Partial parts[OP == Op::kStats && SPARSE ? kMaxGroup : 1];
 
   const int chunk = (int)(blockIdx.x % (unsigned)n_chunks);
   const int64_t r0 = (int64_t)(blockIdx.x / (unsigned)n_chunks) * rows_per_group;
@@ -278,6 +286,11 @@ __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args,
   auto request = [&](int64_t row) {
     const ArgsPtr a = kernel_args();
     const TI* z = (const TI*)a->logits + row * a->ld + v0;
+    if (n == kChunk) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) in[j] = load_vec<TI, E>(z, (j * kThreads + tid) * E);
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int c = (j * kThreads + tid) * E;
@@ -466,29 +479,54 @@ __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args,
           x[k] = choose(opened, k, x[k], kNegInf);
       }
     }
-    if constexpr (OP != Op::kStats) {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int c = (j * kThreads + tid) * E;
-        Vec<TO, E> o;
-#pragma unroll
-        for (int k = 0; k < E; ++k) o.v[k] = narrow<TO>(OP == Op::kGrad ? r[j * E + k] : x[j * E + k]);
-        if (c + E <= n) {
-          store_vec<TO, E>(out, c, o, past);
-        } else {
-#pragma unroll
-          for (int k = 0; k < E; ++k)
-            if (c + k < n) entry(out, c)[k] = o.v[k];
-        }
-      }
-    }
-
+    // The next row is requested before this one is stored: memory operations end in order, and loads behind the stores
+    // would wait for them (the gradient of 4096 rows of 151936 bf16 logits 582 us against 556).
     if (i + 1 < n_rows) {
       request(row + 1);
       w = read_row(row + 1, hist, bias);
       ahead = hist && w.begin == pb && w.split == ps && w.end >= pe && w.end - pe <= kThreads;
       if (ahead) token_ahead = tid < (int)(w.end - pe) ? (uint32_t)*entry(a->r.history + pe, tid) - (uint32_t)v0 : ~0u;
     }
+    if constexpr (OP != Op::kStats) {
+      auto rounded = [&](int j) {
+        Vec<TO, E> o;
+#pragma unroll
+        for (int k = 0; k < E; ++k) o.v[k] = narrow<TO>(OP == Op::kGrad ? r[j * E + k] : x[j * E + k]);
+        return o;
+      };
+      // The loads have to be there, the stores behind them need not be done. Where both are in a straight line the
+      // compiler's wait is that one.
+      auto arrived = [&] {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          i32x4 q;
+          __builtin_memcpy(&q, &in[j], 16);
+          asm volatile("" : "+v"(q));
+          __builtin_memcpy(&in[j], &q, 16);
+        }
+        if constexpr (SPARSE) asm volatile("" : "+v"(token_ahead));
+      };
+      if (n == kChunk) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) store_vec<TO, E>(out, (j * kThreads + tid) * E, rounded(j), past);
+        arrived();
+      } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          const int c = (j * kThreads + tid) * E;
+          const Vec<TO, E> o = rounded(j);
+          if (c + E <= n) {
+            store_vec<TO, E>(out, c, o, past);
+          } else {
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+              if (c + k < n) entry(out, c)[k] = o.v[k];
+          }
+        }
+        arrived();
+      }
+    }
+
     if constexpr (OP == Op::kStats) {
       float m = x[0], low = x[0];
 #pragma unroll
@@ -539,11 +577,16 @@ __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args,
         t.u += ror<2>(t.u);
         t.u += ror<1>(t.u);
         if (tid == 0)
-          ((Partial*)a->part)[row * n_chunks + chunk] = {top, t.s, t.u, tok >= 0 && tok < n ? tok_x[par] : 0.f};
+          (SPARSE ? parts[i] : ((Partial*)a->part)[row * n_chunks + chunk]) =
+              Partial{top, t.s, t.u, tok >= 0 && tok < n ? tok_x[par] : 0.f};
       }
     } else if (SPARSE) {
       __syncthreads();  // the next row changes what this one read from LDS
     }
+  }
+  if constexpr (OP == Op::kStats && SPARSE) {
+    __syncthreads();
+    if (tid < n_rows) ((Partial*)a->part)[(r0 + tid) * n_chunks + chunk] = parts[tid];
   }
 }
 
@@ -621,8 +664,8 @@ hipError_t launch_rules(const RuleArgs& a, hipStream_t s) {
     b.past_caches = a.T * a.V * (int64_t)sizeof(TO) > kCacheBytes;
     // Rows of one workgroup: histories that extend one another are counted once for the group, and the next row's
     // logits are on their way while a row is worked on, but only where the workgroups fill the CUs many times over.
-    // At 4096 workgroups: 4096 rows of 151936 logits 533 us (one row each 605), 200 rows of a decode step 58 us (as
-    // many rows as give 1024 workgroups 73).
+    // At 4096 workgroups: 4096 rows of 151936 logits 500 us (one row each 600), the gradient of 2047 rows 346 us (at
+    // 1024 workgroups 396, at 8192 359).
     int group = 1;
     if (b.r.history) {
       const int64_t fill = rows * n_chunks / 4096;
