@@ -283,3 +283,15 @@ def test_one_wide_row():
     w, wv = _random(5, d, 16, 0)
     # 36 * d * 4 units < 2^24: exact
     assert torch.equal(tim.mxfp4_logits(h, w).double(), hv @ wv.T)
+
+
+@pytest.mark.parametrize("T,d,dtype", [(129, 640, torch.float32), (200, 512, torch.bfloat16), (256, 1152, torch.float32)])
+def test_one_large_tile_of_rows(T, d, dtype):
+    """All rows in one tile of 256 of them, W read once: the same bits as the rows a few at a time."""
+    print(f"case T={T} d={d}", flush=True)
+    h, _ = _random(T, d, 15, 3)
+    w, _ = _random(150001, d, 16, 3)
+    z = tim.mxfp4_logits(h, w, 0.9, dtype=dtype)
+    for a, b in ((0, 64), (T - 40, T), (T // 2, T // 2 + 3)):
+        part = tim.Mxfp4(h.codes[a:b].contiguous(), h.scales[a:b].contiguous())
+        assert torch.equal(tim.mxfp4_logits(part, w, 0.9, dtype=dtype), z[a:b])
