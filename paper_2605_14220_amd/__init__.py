@@ -625,6 +625,11 @@ def mxfp4_logits(hidden: Mxfp4, w_vocab: Mxfp4, temperature: float = 1.0, dtype:
     return out
 
 
+def _matrix_layout(t: torch.Tensor) -> tuple:
+    """Where a tensor lies and how."""
+    return t.data_ptr(), t.dtype, t.shape, t.stride()
+
+
 @dataclasses.dataclass
 class LogitRules:
     """What changes the logits of T rows before sampling (tim_logit_rules in include/tim_policy.h); leave out what
@@ -663,13 +668,15 @@ class LogitRules:
 
     def _struct(self, name, T, V, device) -> _LogitRules:
         """The C struct for T rows of V logits on the device. It is checked and filled once and kept until a field is
-        set or a tensor's storage or layout is another one; what the tensors hold may change in between."""
+        set or a tensor's storage, size, strides or type are others; what the tensors hold may change in between."""
         if self._built is not None:
-            s, held, rows, words, on, mask_stride = self._built
-            if (rows == T and words * 32 >= V and on == device
-                    and all(t.data_ptr() == p and t.numel() == n for t, p, n in held)
-                    and (self.mask is None or (self.mask.shape[1] == words and self.mask.stride() == mask_stride))):
-                return s
+            s, held, rows, words, on, mask = self._built
+            if rows == T and words * 32 >= V and on == device and (mask is None or _matrix_layout(self.mask) == mask):
+                for t, ptr, n, dtype in held:
+                    if t.data_ptr() != ptr or t.nbytes != n or t.dtype is not dtype or not t.is_contiguous():
+                        break
+                else:
+                    return s
         s, held, words = _LogitRules(), [], MAX_VOCAB
 
         def take(field, dtype, n=None):
@@ -685,7 +692,7 @@ class LogitRules:
             if not t.is_contiguous():
                 raise ValueError(f"tim.{name}: {field} must be contiguous")
             setattr(s, field, t.data_ptr())
-            held.append((t, t.data_ptr(), t.numel()))
+            held.append((t, t.data_ptr(), t.nbytes, dtype))
 
         if self.history is not None:
             if self.hist_begin is None or self.hist_end is None:
@@ -716,10 +723,9 @@ class LogitRules:
             if self.mask_rows is None and self.mask.shape[0] != T:
                 raise ValueError(f"tim.{name}: without mask_rows there is one mask a row")
             s.mask, s.n_masks, s.mask_ld = self.mask.data_ptr(), self.mask.shape[0], ld
-            held.append((self.mask, self.mask.data_ptr(), self.mask.numel()))
             take("mask_rows", torch.int32, T)
-        stride = None if self.mask is None else self.mask.stride()
-        object.__setattr__(self, "_built", (s, held, T, words, device, stride))
+        mask = None if self.mask is None else _matrix_layout(self.mask)
+        object.__setattr__(self, "_built", (s, held, T, words, device, mask))
         return s
 
 

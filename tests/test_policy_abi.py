@@ -255,6 +255,39 @@ def test_rules_are_filled_again_when_a_tensor_is_cut_in_place():
         r._struct("logits_adjust", 2, 40, cpu)
 
 
+@pytest.mark.parametrize("relaid,error", [
+    (lambda t, spare: setattr(t, "data", spare[::2]), ValueError),             # every other element, the same address and count
+    (lambda t, spare: t.as_strided_((4,), (0,)), ValueError),                  # one element four times
+    (lambda t, spare: setattr(t, "data", t.data.view(torch.int32)), TypeError),  # the same bytes as another type
+])
+@pytest.mark.parametrize("mutated", ["repetition", "presence"])
+def test_rules_refuse_a_tensor_laid_out_anew_in_place(relaid, error, mutated):
+    """A used rule set refuses what a fresh one refuses: the address and the element count do not show the change."""
+    cpu = torch.device("cpu")
+    spare = torch.arange(8, dtype=torch.float32)
+    r = tim.LogitRules(frequency=torch.ones(4), **{mutated: spare[:4]})
+    s = r._struct("logits_adjust", 4, 40, cpu)
+    t = getattr(r, mutated)
+    relaid(t, spare)
+    assert t.data_ptr() == getattr(s, mutated) and t.numel() == 4
+    for rules in (r, tim.LogitRules(frequency=torch.ones(4), **{mutated: t})):
+        with pytest.raises(error):
+            rules._struct("logits_adjust", 4, 40, cpu)
+
+
+def test_masks_laid_out_anew_in_place():
+    cpu = torch.device("cpu")
+    words = torch.zeros(4, 4, dtype=torch.int32)
+    r = tim.LogitRules(mask=words, mask_rows=torch.zeros(3, dtype=torch.int32))
+    assert r._struct("logits_adjust", 3, 128, cpu).mask_ld == 4
+    r.mask.data = torch.as_strided(words, (2, 8), (8, 1))  # as many elements at the same address
+    s = r._struct("logits_adjust", 3, 128, cpu)
+    assert (s.n_masks, s.mask_ld) == (2, 8)
+    r.mask.data = r.mask.view(torch.float32)
+    with pytest.raises(TypeError):
+        r._struct("logits_adjust", 3, 128, cpu)
+
+
 @pytest.mark.parametrize("copied", [copy.copy, copy.deepcopy, lambda r: pickle.loads(pickle.dumps(r))])
 def test_rules_are_copied_after_a_call(copied):
     cpu = torch.device("cpu")
