@@ -105,6 +105,15 @@ __device__ __forceinline__ void store_logits(T* row, int v, int V, const f32x4& 
   }
 }
 
+// Between a wave's lanes that hand data on through LDS. The hardware takes a
+// wave's LDS accesses in order, so this is no instruction: it keeps the
+// compiler, which sees each lane by itself, from moving one across it.
+__device__ __forceinline__ void lanes_ordered() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // A wave's logits leave through LDS, 16 hidden rows at a time, so that a store
 // writes runs of NA * 16 logits of a row: straight from the accumulators it
 // would write 64 bytes in each of 16 rows. NT: past the caches, for logits too
@@ -138,6 +147,7 @@ __device__ __forceinline__ void store_tile(unsigned char* lds, const f32x4 (&acc
                                                 4 * sizeof(T)),
                        z, sizeof(z));
     }
+    lanes_ordered();
 #pragma unroll
     for (int r = lane / O::kLanes; r < 16; r += kRows) {
       const int64_t t = t0 + j * 16 + r;
@@ -157,6 +167,7 @@ __device__ __forceinline__ void store_tile(unsigned char* lds, const f32x4 (&acc
           if (v + e < V) out[e] = z[e];
       }
     }
+    lanes_ordered();  // the next rows take the same place
   }
 }
 
@@ -362,6 +373,7 @@ __global__ __launch_bounds__(TL::NW * 64, TL::PER_CU * TL::NW / 4) void fp4_logi
     for (int q = 0; q < L; ++q) fp4_load<TL>(lds + s * SB, o, st, st >= whole, wave, q);
   }
   wait_vmem<(NBUF - 1) * L>();  // group 0 and stage 0 landed
+  asm volatile("" ::: "memory");  // and no read of them is moved up
 #pragma unroll
   for (int q = 0; q < TL::LX; ++q) {
     i32x4* p = fp4_turned<TL>(lds, 0, q, wave, lane);

@@ -73,3 +73,21 @@ def test_column_sums_issue_few_instructions_a_row(assembly, kernel, rows):
     assert loops, "no loop over that many rows' loads"
     print(f"{kernel}: {len(loops[0])} instructions for {rows} rows")
     assert len(loops[0]) <= 11 * rows
+
+
+def test_logits_turned_in_lds_are_handed_on_in_order(assembly):
+    """The 4-bit head's logits go from lane to lane through LDS: behind the last product, between a wave's writes and
+    the reads of them, and before the next rows' writes, stands a mark that keeps the compiler's order."""
+    lines = assembly("mxfp4_logits")
+    kernels = 0
+    for i, l in enumerate(lines):
+        if not re.match(r"_Z\S*fp4_logitsI\S*:", l):
+            continue
+        kernels += 1
+        end = next(j for j in range(i, len(lines)) if lines[j].startswith(".Lfunc_end"))
+        last = max(j for j in range(i, end) if "v_mfma" in lines[j])
+        marks = [m[0] for x in lines[last:end] if (m := re.search(r"ds_write|ds_read|wave barrier", x))]
+        turn = marks[marks.index("ds_write"):]  # reads before it are the k-loop's last operands
+        assert "ds_read" in turn and "wave barrier" in turn
+        assert all({a, b} != {"ds_write", "ds_read"} for a, b in zip(turn, turn[1:])), (l, turn)
+    assert kernels >= 24
