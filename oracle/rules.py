@@ -59,7 +59,8 @@ def change_logits(z, rules, temperature: float = 1.0) -> tuple[np.ndarray, np.nd
 
 
 def _softmax(x):
-    """(p, log p with 0 where p = 0, lse) of each row; a row of -inf has p = 0 and lse = -inf."""
+    """(p, log p, lse) of each row; a row of -inf has p = 0 and lse = -inf. log p is taken from the row's maximum, as an
+    lse of a magnitude near the largest numbers holds no log sum."""
     m = x.max(axis=1, keepdims=True)
     none = np.isneginf(m[:, 0])
     with np.errstate(invalid="ignore"):
@@ -67,8 +68,13 @@ def _softmax(x):
         s = e.sum(axis=1, keepdims=True)
         lse = np.where(none, -np.inf, m[:, 0] + np.log(np.where(none, 1.0, s[:, 0])))
         p = e / np.where(none[:, None], 1.0, s)
-        logp = np.where(p > 0, x - np.where(none, 0.0, lse)[:, None], np.where(np.isnan(p), np.nan, 0.0))
+        logp = np.where(none[:, None], -np.inf, x - m - np.log(np.where(none[:, None], 1.0, s)))
     return p, logp, lse
+
+
+def _at_positive(p, a):
+    """a where p > 0 (or NaN), else 0: the factor of a product p a."""
+    return np.where(p == 0, 0.0, a)
 
 
 def changed_logprobs(z, tokens, rules, temperature: float = 1.0):
@@ -80,9 +86,8 @@ def changed_logprobs(z, tokens, rules, temperature: float = 1.0):
     ok = (tok >= 0) & (tok < V)
     logp = np.full(T, np.nan)
     for i in np.nonzero(ok)[0]:
-        none = np.isneginf(lse[i])
-        logp[i] = -np.inf if none else x[i, tok[i]] - lse[i]
-    return logp, -(p * logp_all).sum(axis=1), lse
+        logp[i] = logp_all[i, tok[i]]
+    return logp, -(p * _at_positive(p, logp_all)).sum(axis=1), lse
 
 
 def changed_logprobs_grad(z, tokens, rules, grad_logp, grad_entropy=None, temperature: float = 1.0) -> np.ndarray:
@@ -90,6 +95,7 @@ def changed_logprobs_grad(z, tokens, rules, grad_logp, grad_entropy=None, temper
     x, slope = change_logits(z, rules, temperature)
     T, V = x.shape
     p, logp_all, _ = _softmax(x)
+    logp_all = _at_positive(p, logp_all)
     H = -(p * logp_all).sum(axis=1)
     tok = np.asarray(tokens)
     ok = (tok >= 0) & (tok < V)

@@ -189,3 +189,20 @@ def test_pins_reject_mistakes(module, old, new, monkeypatch):
         except Exception:
             failed += 1
     assert failed
+
+
+@pytest.mark.parametrize("offset", [0.0, 1e6, -1e12, -3.4028234663852886e38, 3.4028234663852886e38])
+def test_offsets_common_to_a_row_do_not_enter(offset):
+    """n equal logits: p = 1 / n, H = log n, gradient g ([v = token] - 1 / n), whatever lse can hold."""
+    n = 37
+    z = np.full((2, n), offset)
+    allowed = np.arange(n) < 11
+    rules = [{}, {"allowed": allowed}]
+    lp, H, _ = oracle.changed_logprobs(z, [3, 4], rules, 0.7)
+    assert np.allclose(lp, [-math.log(n), -math.log(11)]) and np.allclose(H, [math.log(n), math.log(11)])
+    g = oracle.changed_logprobs_grad(z, [3, 4], rules, [1.0, -2.0], [5.0, 5.0], 0.7)
+    want = np.zeros((2, n))
+    want[0], want[1, :11] = -1 / n, 2 / 11
+    want[0, 3] += 1.0
+    want[1, 4] -= 2.0
+    assert np.allclose(g, want / 0.7, rtol=1e-12, atol=1e-12)
