@@ -154,7 +154,9 @@ size_t tim_logits_logprobs_workspace_size(int64_t T, int32_t V);
  * An entry at -inf (masked, or of a logit or bias of -inf) has p = 0 and adds
  * nothing to the entropy. Where nothing is left (every x is -inf) lse = -inf,
  * entropy = 0 and logp = -inf. A token outside [0, V) yields logp = NaN. NaN
- * or +inf in an entry that is not masked propagates to the row's outputs.
+ * or +inf in an entry that is not masked propagates to the row's outputs. lse is
+ * infinite where its value lies past fp32's range (entries near the largest or
+ * lowest number over a temperature below 1); logp and entropy are not touched.
  *
  * logits, dtype, ld, rules, temperature as tim_logits_adjust; tokens int32
  * [T]; logp fp32 [T] (required), entropy, lse fp32 [T] or NULL. x is not
@@ -173,8 +175,13 @@ tim_status tim_logits_logprobs(const void* logits, int32_t dtype, int64_t T, int
  * (or 0), H = entropy[i], p_v = exp(x_v - lse[i]), p_v log p_v = 0 where
  * p_v = 0, and slope_v = dx_v / dz_v: (float)(1 / temperature), times
  * 1 / repetition (z > 0) or repetition (z <= 0) for entries in the history, 0
- * for masked ones. A row with g = e = 0 (padding) and a row with lse = -inf
- * (nothing allowed) get zeros.
+ * for masked ones. A row with g = e = 0 (padding) and a row with nothing allowed
+ * get zeros.
+ *
+ * p_v goes by lse where |lse| < 1024, with lse's rounding in it: relatively less
+ * than 2^-14. Rows beyond, whose lse says too little of them (at fp32's lowest
+ * number it holds no log V, and it may be infinite), have their maximum and sum
+ * formed anew from the logits, in one workgroup each: right, but slower.
  *
  * lse, entropy  fp32 [T] from tim_logits_logprobs for the same inputs
  *         (entropy may be NULL when grad_entropy is).

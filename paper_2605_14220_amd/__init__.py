@@ -813,7 +813,8 @@ def logits_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: to
                              entropy: torch.Tensor | None = None, grad_entropy: torch.Tensor | None = None,
                              dtype: torch.dtype | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient [T, V] of sum_t grad_logp[t] logp[t] + grad_entropy[t] entropy[t] with respect to the logits, through
-    the changes. lse (and entropy, when grad_entropy is given) are logits_logprobs' outputs for the same inputs.
+    the changes. lse (and entropy, when grad_entropy is given) are logits_logprobs' outputs for the same inputs; rows of
+    |lse| >= 1024, where it is too coarse, take their normaliser from the logits and longer.
     dtype (the logits' by default) is the gradient's type; out may be logits itself where the types agree,
     but no other overlap is allowed."""
     lib = load_library()

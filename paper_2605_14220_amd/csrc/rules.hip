@@ -7,7 +7,8 @@
 //   logprobs: per chunk m = max y, and with t = (y - m) log2(e) / tau the sums
 //             s = sum 2^t, u = sum 2^t t; a merge over the chunks gives
 //             lse = M / tau + log S, H = log S - ln 2 U / S
-//   backward: dz = slope (g [v = tok] - p (g + e (log p + H))), p = e^(x-lse)
+//   backward: dz = slope (g [v = tok] - p (g + e (log p + H))), p = e^(x-lse),
+//             and where lse is too coarse for it the row's M and log S anew
 //
 // All three are one pass over the logits (read once; adjust and backward write
 // as many) and bound by HBM. A workgroup takes one chunk of TIM_RULE_CHUNK
@@ -255,6 +256,107 @@ __device__ __forceinline__ float choose(uint32_t bits, int k, float x, float z) 
 
 // LDS words of a history or a bias list: one per entry, and their bitmap.
 constexpr int kWords = kChunk + kChunk / 32;
+__device__ __forceinline__ void clear_words(uint32_t* words, int tid) {
+  for (int c = tid * 4; c < kWords; c += kThreads * 4) *(uint4*)(words + c) = uint4{0, 0, 0, 0};
+}
+
+// The entries of a bias list that fall into a chunk's n from v0 on: the last one of each id.
+__device__ __forceinline__ void mark_biases(uint32_t* last, const int32_t* ids, int64_t from, int64_t to, int v0, int n,
+                                            int tid) {
+  for (int64_t k = from + tid; k < to; k += kThreads) {
+    const uint32_t id = (uint32_t)ids[k] - (uint32_t)v0;
+    if (id < (uint32_t)n) {
+      atomicOr(&last[kChunk + (id >> 5)], 1u << (id & 31));
+      atomicMax(&last[id], (uint32_t)k + 1u);
+    }
+  }
+}
+
+// |lse| from which a row's gradient does not go by it. p = e^(x - lse) is
+// relatively as far off as fp32's lse is absolutely, |lse| 2^-24: less than
+// 2^-14 short of this, but at fp32's lowest value lse holds no log n any more,
+// and over a temperature below 1 it is infinite.
+constexpr float kFarLse = 1024.f;
+
+// The whole gradient of such a row in one workgroup, which first forms the
+// row's maximum y and log S as the statistics do: p = e^((y - top) / tau - log
+// S). One workgroup, so that the gradient may lie where the logits do. A model's
+// rows hardly come here: 150 rows of 50257 fp16 logits with histories, all of
+// them far, take 123 us against 17, 2047 of 151936 fp32 logits 1640 against 350.
+template <class TI, class TO, bool SPARSE>
+__device__ __forceinline__ void far_row(int64_t row, uint32_t* lds, Stat* wstat) {
+  const ArgsPtr a = kernel_args();
+  const int tid = threadIdx.x;
+  const bool hist = SPARSE && a->r.history != nullptr;
+  const bool bias = SPARSE && a->r.bias_ids != nullptr;
+  uint32_t* cnt = lds;
+  uint32_t* last = lds + (hist ? kWords : 0);
+  const Row w = read_row(row, hist, bias);
+  const int token = scalar(a->tokens, row);
+  const float g = (unsigned)token < (unsigned)a->V ? scalar(a->grad_logp, row) : 0.f;
+  const float e = a->grad_entropy ? scalar(a->grad_entropy, row) : 0.f;
+  const float ent = a->grad_entropy ? scalar(a->entropy, row) : 0.f;
+  const float inv_tau = a->inv_tau, log2e_tau = kLog2e * inv_tau;
+  const float inv_rho = 1.f / w.rho;
+  const TI* z = (const TI*)a->logits + row * a->ld;
+  TO* out = (TO*)a->out + row * a->out_ld;
+  const uint32_t* mask = a->r.mask + w.mask * a->r.mask_ld;
+  // each(v, open, y, factor of the slope) for the thread's entries of every chunk
+  auto walk = [&](auto&& each) {
+    for (int v0 = 0; v0 < a->V; v0 += kChunk) {
+      const int n = a->V - v0 < kChunk ? a->V - v0 : kChunk;
+      if constexpr (SPARSE) {
+        __syncthreads();  // the last chunk's words have been read
+        if (hist) clear_words(cnt, tid);
+        if (bias) clear_words(last, tid);
+        __syncthreads();
+        if (hist) count_tokens(cnt, cnt + kChunk, a->r.history, w.begin, w.split, w.end, v0, n);
+        if (bias) mark_biases(last, a->r.bias_ids, w.bias0, w.bias1, v0, n, tid);
+        __syncthreads();
+      }
+      for (int c = tid; c < n; c += kThreads) {
+        const int v = v0 + c;
+        float y = widen(z[v]), factor = 1.f;
+        if constexpr (SPARSE) {
+          const uint32_t u = hist ? cnt[c] : 0u;
+          if (u) y = penalise(y, u, w, inv_rho, factor);
+          const uint32_t b = bias ? last[c] : 0u;
+          if (b) y = y + a->r.bias_values[b - 1];
+        }
+        each(v, w.mask < 0 || (mask[v >> 5] >> (v & 31) & 1u), y, factor);
+      }
+    }
+  };
+  float m = kNegInf, s = 0.f;  // of the thread's entries; a NaN or +inf makes s NaN
+  walk([&](int, bool open, float y, float) {
+    if (!open || y == kNegInf) return;
+    const float top = fmaxf(m, y);
+    s = s * exp2_hw((m - top) * log2e_tau) + exp2_hw((y - top) * log2e_tau);
+    m = top;
+  });
+  const float wave_top = wave_max(m);
+  s = wave_sum(shift({m, s, 0.f}, wave_top, log2e_tau).s);
+  if ((tid & 63) == 0) wstat[tid >> 6] = {wave_top, s, 0.f};
+  __syncthreads();
+  float top = kNegInf, S = 0.f;
+#pragma unroll
+  for (int j = 0; j < kWaves; ++j) top = fmaxf(top, wstat[j].m);
+#pragma unroll
+  for (int j = 0; j < kWaves; ++j) S += shift(wstat[j], top, log2e_tau).s;
+  const bool none = top == kNegInf && S == 0.f;  // nothing allowed
+  const float log_s = logf(S);
+  walk([&](int v, bool open, float y, float factor) {
+    float r = 0.f;
+    if (open && !none) {
+      const float q = (y - top) * inv_tau - log_s;
+      const float p = exp2_hw(q * kLog2e);
+      r = e == 0.f ? -p * g : -p * (g + e * (fmaxf(q, kFloor) + ent));
+      r = (v == token ? g + r : r) * (factor * inv_tau);
+    }
+    out[v] = narrow<TO>(r);
+  });
+  __syncthreads();  // wstat and the words have been read
+}
 
 // Three workgroups a CU (80 registers): with two 4096 rows of 151936 logits take 560 us against 500 and 64 rows 19.9
 // against 17.7 (the gradients the same); four spill.
@@ -303,9 +405,7 @@ __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args,
     }
   };
   request(r0);
-  auto clear = [&](uint32_t* words) {
-    for (int c = tid * 4; c < kWords; c += kThreads * 4) *(uint4*)(words + c) = uint4{0, 0, 0, 0};
-  };
+  auto clear = [&](uint32_t* words) { clear_words(words, tid); };
   if (hist) clear(cnt);
   if (bias) clear(last);
   if constexpr (SPARSE) __syncthreads();
@@ -317,6 +417,7 @@ __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args,
   // requested with the row.
   bool ahead = false;
   uint32_t token_ahead = ~0u;
+  uint32_t far = 0;  // backward: bit i: row i of the group is left to the end, where no register holds its state
 
   for (int i = 0; i < n_rows; ++i) {
     // Opaque copies: the entries' bounds and offsets are worked out where they are used, not once for all rows and
@@ -340,8 +441,12 @@ __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args,
           e = scalar(a->grad_entropy, row);
           ent = scalar(a->entropy, row);
         }
-        if ((g == 0.f && e == 0.f) || lse == kNegInf) {
-          for (int c = tid; c < n; c += kThreads) *entry(out, c) = (TO)0.f;
+        const bool zero = g == 0.f && e == 0.f;
+        if (zero || fabsf(lse) >= kFarLse) {
+          if (zero)
+            for (int c = tid; c < n; c += kThreads) *entry(out, c) = (TO)0.f;
+          else
+            far |= 1u << i;
           if (i + 1 < n_rows) {
             request(row + 1);
             w = read_row(row + 1, hist, bias);
@@ -388,13 +493,7 @@ __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args,
           clear(last);
           __syncthreads();
         }
-        for (int64_t k = b + tid; k < t; k += kThreads) {
-          const uint32_t id = (uint32_t)a->r.bias_ids[k] - (uint32_t)v0;
-          if (id < (uint32_t)n) {
-            atomicOr(&last[kChunk + (id >> 5)], 1u << (id & 31));
-            atomicMax(&last[id], (uint32_t)k + 1u);
-          }
-        }
+        mark_biases(last, a->r.bias_ids, b, t, v0, n, tid);
         qb = b;
         qe = t;
       }
@@ -582,6 +681,13 @@ __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args,
       }
     } else if (SPARSE) {
       __syncthreads();  // the next row changes what this one read from LDS
+    }
+  }
+  if constexpr (OP == Op::kGrad) {
+    for (; far; far &= far - 1) {  // a row's chunks share its work out by the rows; a launch's rows fit 32 bits
+      const int64_t row = r0 + __builtin_ctz(far);
+      const unsigned chunks = (unsigned)(kernel_args()->V + kChunk - 1) / kChunk;
+      if ((unsigned)row % chunks == (unsigned)v0 / kChunk) far_row<TI, TO, SPARSE>(row, lds, wstat[0]);
     }
   }
   if constexpr (OP == Op::kStats && SPARSE) {

@@ -645,3 +645,143 @@ def test_outputs_larger_than_the_caches(dtype, grad, T, V):
         assert torch.equal(tim.logits_adjust(z[a:b], r, 0.9), adj[a:b])
         assert torch.equal(tim.logits_logprobs_backward(z[a:b], tok[a:b], lse[a:b], g[a:b], r, 0.9, entropy=H[a:b],
                                                         grad_entropy=e[a:b], dtype=DTYPES[grad]), dz[a:b])
+
+
+# Rows far from 0. lse holds its row's normaliser to |lse| 2^-24 only, so from |lse| = 1024 on the gradient forms it anew
+# from the logits, as their largest y and log S. Without penalties and biases y is exact there, and p off by what S and
+# the exponentials are: S is a sum of V / 512 < 42 terms a thread, each step an exponential, a product and an addition,
+# then 17 additions and the logarithm, its exponentials within (2 + 2 |t|) u and a p-weighted mean of |t| below
+# ln V + 1 < 12: at most (3 * 42 + 17 + 8 + 26) u < 180 u. With penalties and biases every y is within 6 u M of its exact
+# value, and so is the softmax average of them. Short of 1024 the given lse's half step enters p instead.
+
+
+def check_far_backward(case, tau, entropy, grad=None, **kw):
+    rng = np.random.default_rng(case.T + 7)
+    g = rng.standard_normal(case.T).astype(np.float32)
+    e = rng.standard_normal(case.T).astype(np.float32) if entropy else None
+    inv = float(np.float32(1.0 / np.float64(np.float32(tau))))
+    z64 = case.z.double().cpu().numpy()
+    _, H, lse64 = oracle.changed_logprobs(z64, case.tokens, case.rules, 1.0 / inv)
+    with np.errstate(over="ignore"):
+        lse = lse64.astype(np.float32)  # infinite past fp32's range
+    as_gpu = lambda x: None if x is None else torch.as_tensor(x.astype(np.float32)).cuda()  # noqa: E731
+    x, slope = oracle.change_logits(z64, case.rules, 1.0 / inv)
+    ref = oracle.changed_logprobs_grad(z64, case.tokens, case.rules, g, e, 1.0 / inv)
+    changed = any(r.get("prompt") or r.get("output") or r.get("bias") for r in case.rules)
+    _, top = fp32_steps(case, case.z, tau)
+    got = tim.logits_logprobs_backward(case.z, case.tok, as_gpu(lse), as_gpu(g), case.lib, tau, entropy=as_gpu(H),
+                                       grad_entropy=as_gpu(e), dtype=grad, **kw)
+    D = 12 * U * top * inv if changed else np.zeros(case.T)
+    D = (D + np.where(np.abs(lse64) < 1024.5, np.abs(lse64), 0) * U + 180 * U)[:, None]
+    none = np.isneginf(x).all(1)[:, None]
+    with np.errstate(invalid="ignore", divide="ignore"):
+        m = x.max(1, keepdims=True)
+        q = np.where(np.isfinite(x) & ~none, x - m - np.log(np.exp(x - m).sum(1, keepdims=True)), 0.0)
+    p = np.where(np.isfinite(x) & ~none, np.exp(q), 0.0)
+    a = np.abs(g)[:, None] + (0.0 if e is None else np.abs(e)[:, None]) * (np.abs(q) + np.abs(H)[:, None] + 1)
+    onehot = np.zeros_like(z64)
+    ok = (case.tokens >= 0) & (case.tokens < case.V)
+    onehot[np.nonzero(ok)[0], case.tokens[ok]] = 1.0
+    bound = slope * (p * a * (D + (4 * np.abs(q) + 12) * U) + 4 * U * np.abs(g)[:, None] * onehot) + 4 * U * np.abs(ref)
+    bound += slope * a * 2.0 ** -126
+    bound += torch.finfo(got.dtype).eps / 2 * (np.abs(ref) + bound) + TINY[got.dtype]
+    err = np.abs(got.double().cpu().numpy() - ref)
+    assert np.isfinite(err).all()
+    print(f"[parity] far grad: max|err| {err.max():.2e}, {np.max(err / bound):.3f} of the bound")
+    assert (err <= bound).all(), np.argwhere(err > bound)[:5]
+    return got, g
+
+
+@pytest.mark.parametrize("tau", [1.0, 0.7, 0.3])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_gradient_of_rows_of_lowest_values(dtype, tau):
+    """Rows of the type's lowest and largest value: p is 1 / n, also where lse holds no log n or is past fp32's range."""
+    V, n = 20003, 20003 - 9000
+    case = Case(6, V, 41, dtype=DTYPES[dtype], history=None, masks=2)
+    allowed = np.ones(V, bool)
+    allowed[100:9100] = False
+    for m, bits in ((0, allowed), (1, np.zeros(V, bool))):
+        case.lib.mask[m] = torch.as_tensor(np.packbits(np.pad(bits, (0, case.lib.mask.shape[1] * 32 - V)),
+                                                       bitorder="little").view(np.int32)).cuda()
+    lowest = torch.finfo(DTYPES[dtype]).min
+    case.z[0] = lowest
+    case.z[1] = lowest
+    case.z[2] = -lowest
+    case.z[3] = lowest
+    case.z[3, 9500:9510] = lowest / 2      # ten entries left
+    case.z[4] = -math.inf                  # nothing left
+    case.z[5] = lowest                     # nothing allowed
+    case.lib.mask_rows[:] = torch.tensor([0, -1, 0, 0, 0, 1], dtype=torch.int32)
+    for r, m in zip(case.rules, (allowed, None, allowed, allowed, allowed, np.zeros(V, bool))):
+        r.pop("allowed", None)
+        if m is not None:
+            r["allowed"] = m
+    case.tokens[:] = [5, 30, 20002, 9501, 3, 4]
+    case.tok = torch.as_tensor(case.tokens).cuda()
+    lp, H, lse = (x.double().cpu() for x in tim.logits_logprobs(case.z, case.tok, case.lib, tau, lse=True))
+    assert lp[0].item() == pytest.approx(-math.log(n), abs=1e-5) and H[0].item() == pytest.approx(math.log(n), abs=1e-4)
+    for entropy in (False, True):
+        got, g = check_far_backward(case, tau, entropy, grad=torch.float32)
+        if not entropy:  # each row's gradient sums to 0, each of its entries within the bound above of p g / tau
+            for i in range(4):
+                assert abs(got[i].double().sum().item()) <= 600 * U * abs(g[i]) / tau
+        assert (got[4:] == 0).all() and (got[0, 100:9100] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,grad", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("f16", "f32"), ("f16", "f16")])
+@pytest.mark.parametrize("V", [1, 700, 8193, 20003])
+def test_gradient_of_rows_far_from_zero(dtype, grad, V):
+    """Offsets common to a row, on both sides of where lse becomes too coarse: the gradient does not feel them."""
+    offsets = [0.0, 900.0, 1020.0, -1020.0, 1030.0, -1030.0, 5000.0, -20000.0]
+    if dtype != "f16":
+        offsets += [1e5, -1e6, 3e7, -1e12]
+    print(f"case {dtype} -> {grad} V={V}", flush=True)
+    case = Case(len(offsets), V, 42, dtype=DTYPES[dtype], history=None, masks=3, pad=1)
+    case.z += torch.tensor(offsets, device="cuda")[:, None].to(case.z.dtype)
+    for entropy in (False, True):
+        check_far_backward(case, 0.9, entropy, grad=DTYPES[grad])
+
+
+@pytest.mark.parametrize("bias", [0, 30])
+@pytest.mark.parametrize("V", [500, 20003])
+def test_gradient_of_changed_rows_far_from_zero(V, bias):
+    """Penalties, biases and masks on rows at an offset, whose changes are of its size."""
+    case = Case(9, V, 43, history=60, bias=bias, masks=5)
+    case.z[::2] += 3000.0
+    case.z[1::4] -= 3000.0
+    for entropy in (False, True):
+        check_far_backward(case, 1.0, entropy)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_far_rows_beside_others_in_a_workgroup(dtype):
+    """Far, padded, empty and ordinary rows in turn, several to a workgroup, their histories extending one another: each
+    row has the bits it has alone, in place too."""
+    T, V = 4200, 17001
+    kw = _packed_rules(T, V, 44, True)
+    kw["mask"][10::97] = 0
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    z = torch.randn(T, V, device="cuda", generator=gen)
+    z[::5] += 4000.0
+    z[2::7] -= 4000.0
+    z = z.to(DTYPES[dtype])
+    tok = torch.randint(-1, V, (T,), device="cuda", dtype=torch.int32, generator=gen)
+    g, e = (torch.randn(T, device="cuda", generator=gen) for _ in range(2))
+    g[::11] = 0.0
+    e[::11] = 0.0
+    r = _slice(kw, 0, T)
+    _, H, lse = tim.logits_logprobs(z, tok, r, 0.9, lse=True)
+    assert (lse.abs() > 1024).sum() > T // 4 and torch.isinf(lse).sum() > T // 100
+    dz = tim.logits_logprobs_backward(z, tok, lse, g, r, 0.9, entropy=H, grad_entropy=e)
+    assert torch.isfinite(dz).all()
+    for a in (0, 1, 2, 5, 10, 11, 2000, 2005, 2100, T - 3):
+        one = tim.logits_logprobs_backward(z[a:a + 1], tok[a:a + 1], lse[a:a + 1], g[a:a + 1], _slice(kw, a, a + 1), 0.9,
+                                           entropy=H[a:a + 1], grad_entropy=e[a:a + 1])
+        assert torch.equal(one, dz[a:a + 1]), a
+    for a in range(0, T, 600):
+        part = _slice(kw, a, a + 600)
+        assert torch.equal(tim.logits_logprobs_backward(z[a:a + 600], tok[a:a + 600], lse[a:a + 600], g[a:a + 600], part,
+                                                        0.9, entropy=H[a:a + 600], grad_entropy=e[a:a + 600]),
+                           dz[a:a + 600]), a
+    tim.logits_logprobs_backward(z, tok, lse, g, r, 0.9, entropy=H, grad_entropy=e, out=z)
+    assert torch.equal(z, dz)
