@@ -36,7 +36,6 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStageCodes = 128;  // bytes of a row's codes in a stage (two k-steps)
 constexpr int kGroupScales = 16;  // bytes of a row's scales in a group (two stages)
-constexpr int kMinD = 512;        // a row holds a whole group
 // Vocabulary tiles per group in the workgroup -> tile order. What a round of workgroups writes is runs of this many
 // tiles in the rows of a few: 2000 rows at d = 4096, V = 151936 780 us against 811 for 8 and 850 for 4 (8000 rows:
 // 2948, 2897 and 2985; one or two row tiles the same).
@@ -497,15 +496,18 @@ hipError_t launch_short(const Mxfp4LogitsArgs& a, hipStream_t s) {
 
 template <class T>
 hipError_t product_as(const Mxfp4LogitsArgs& a, hipStream_t s) {
-  if (a.d < kMinD) return launch_short<T>(a, s);
-  if (a.T <= 16) return launch_tiles<Fp4Tile<4, 1, 2, 1, 3, true>, T>(a, s);
-  if (a.T <= 32) return launch_tiles<Fp4Tile<4, 1, 2, 2, 3, true>, T>(a, s);
-  if (a.T <= 64) return launch_tiles<Fp4Tile<4, 1, 2, 4, 2, true>, T>(a, s);
-  if (a.T <= 128) return launch_tiles<Fp4Tile<4, 1, 2, 8, 2, true>, T>(a, s);
-  if (fp4_small_tiles(a.T, a.V, device_cu_count())) return launch_tiles<Fp4Tile<4, 1, 2, 8, 2, false>, T>(a, s);
-  if (a.T * a.V * (int64_t)sizeof(T) > kCacheBytes) return launch_tiles<Fp4Tile<2, 4, 8, 4, 1, false>, T, true>(a, s);
-  if (a.T <= 256) return launch_tiles<Fp4Tile<2, 4, 8, 4, 1, true>, T>(a, s);
-  return launch_tiles<Fp4Tile<2, 4, 8, 4, 1, false>, T>(a, s);
+  switch (fp4_kernel(a.T, a.d, a.V, sizeof(T), device_cu_count())) {
+    case Fp4Kernel::kShort: return launch_short<T>(a, s);
+    case Fp4Kernel::kRows16: return launch_tiles<Fp4Tile<4, 1, 2, 1, 3, true>, T>(a, s);
+    case Fp4Kernel::kRows32: return launch_tiles<Fp4Tile<4, 1, 2, 2, 3, true>, T>(a, s);
+    case Fp4Kernel::kRows64: return launch_tiles<Fp4Tile<4, 1, 2, 4, 2, true>, T>(a, s);
+    case Fp4Kernel::kRows128: return launch_tiles<Fp4Tile<4, 1, 2, 8, 2, true>, T>(a, s);
+    case Fp4Kernel::kSmall: return launch_tiles<Fp4Tile<4, 1, 2, 8, 2, false>, T>(a, s);
+    case Fp4Kernel::kLargePast: return launch_tiles<Fp4Tile<2, 4, 8, 4, 1, false>, T, true>(a, s);
+    case Fp4Kernel::kLargeOnce: return launch_tiles<Fp4Tile<2, 4, 8, 4, 1, true>, T>(a, s);
+    case Fp4Kernel::kLarge: return launch_tiles<Fp4Tile<2, 4, 8, 4, 1, false>, T>(a, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace

@@ -136,4 +136,24 @@ inline bool fp4_small_tiles(int64_t T, int64_t V, int64_t cus) {
   return 5 * ((small + 2 * cus - 1) / (2 * cus)) < 8 * ((large + cus - 1) / cus);
 }
 
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;  // the memory-side cache
+constexpr int kFp4MinD = 512;                        // the tiled 4-bit product's: a row holds a group of scales
+
+// The 4-bit head's kernel for T rows of d elements, V vocabulary entries and
+// logits of `esize` bytes: short rows from memory; one tile of 16 to 128 rows
+// for all of them; beyond, small or large tiles, the large ones with their
+// logits past the caches where those are larger, and W too where one tile takes
+// all rows.
+enum class Fp4Kernel { kShort, kRows16, kRows32, kRows64, kRows128, kSmall, kLargePast, kLargeOnce, kLarge };
+inline Fp4Kernel fp4_kernel(int64_t T, int32_t d, int64_t V, int64_t esize, int64_t cus) {
+  if (d < kFp4MinD) return Fp4Kernel::kShort;
+  if (T <= 16) return Fp4Kernel::kRows16;
+  if (T <= 32) return Fp4Kernel::kRows32;
+  if (T <= 64) return Fp4Kernel::kRows64;
+  if (T <= 128) return Fp4Kernel::kRows128;
+  if (fp4_small_tiles(T, V, cus)) return Fp4Kernel::kSmall;
+  if (T * V * esize > kCacheBytes) return Fp4Kernel::kLargePast;
+  return T <= 256 ? Fp4Kernel::kLargeOnce : Fp4Kernel::kLarge;
+}
+
 }  // namespace tim

@@ -139,8 +139,6 @@ struct RuleArgs {
   int32_t past_caches;    // out is larger than the caches
 };
 
-constexpr int64_t kCacheBytes = (int64_t)256 << 20;  // the memory-side cache
-
 // An fp32 value rounded once to T. To fp16 the compiler would merge a multiply
 // before it into one mixed-precision instruction that rounds the exact product
 // to fp16, other bits than the fp32 product's; the empty asm keeps the two

@@ -18,6 +18,9 @@ extern "C" int stream_shape(int64_t rows, int d, int n_ht, int cus) {
   return 10 * s.row_blocks + s.group;
 }
 extern "C" int norm_fused(int64_t T, int d) { return tim::norm_fused(T, d); }
+extern "C" int fp4_kernel(int64_t T, int d, int64_t V, int64_t esize, int64_t cus) {
+  return (int)tim::fp4_kernel(T, d, V, esize, cus);
+}
 """
 
 
@@ -33,6 +36,7 @@ def _lib():
     lib.response_blocks.argtypes = [ctypes.c_int] + [ctypes.c_int64] * 3
     lib.stream_shape.argtypes = [ctypes.c_int64] + [ctypes.c_int] * 3
     lib.norm_fused.argtypes = [ctypes.c_int64, ctypes.c_int]
+    lib.fp4_kernel.argtypes = [ctypes.c_int64, ctypes.c_int] + [ctypes.c_int64] * 3
     return lib
 
 
@@ -51,3 +55,11 @@ def stream_shape(rows, d, V, cus=256):
 
 def norm_fused(T, d):
     return bool(_lib().norm_fused(T, d))
+
+
+FP4_KERNELS = ("short", "rows16", "rows32", "rows64", "rows128", "small", "large_past", "large_once", "large")
+
+
+def fp4_kernel(T, d, V, esize, cus=256):
+    """The kernel of the 4-bit head's product, by its name in FP4_KERNELS."""
+    return FP4_KERNELS[_lib().fp4_kernel(T, d, V, esize, cus)]

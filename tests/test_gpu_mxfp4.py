@@ -14,6 +14,7 @@ import torch
 
 import oracle
 import paper_2605_14220_amd as tim
+from plan_shim import fp4_kernel
 from tim_testutil import require_gpu
 
 pytestmark = pytest.mark.gpu
@@ -295,3 +296,60 @@ def test_one_large_tile_of_rows(T, d, dtype):
     for a, b in ((0, 64), (T - 40, T), (T // 2, T // 2 + 3)):
         part = tim.Mxfp4(h.codes[a:b].contiguous(), h.scales[a:b].contiguous())
         assert torch.equal(tim.mxfp4_logits(part, w, 0.9, dtype=dtype), z[a:b])
+
+
+# ------------------------------------------------------------------ every kernel of the product, by the rule's own name
+
+KERNELS = {  # (T, V, type): rows and vocabulary end inside a tile
+    "rows16": [(9, 331, torch.float32)], "rows32": [(30, 331, torch.bfloat16)], "rows64": [(50, 331, torch.float32)],
+    "rows128": [(100, 331, torch.float16)], "small": [(300, 331, torch.float32)],
+    "large_once": [(200, 50257, torch.float32), (131, 50257, torch.bfloat16)],
+    "large": [(500, 32001, torch.float32), (499, 32003, torch.bfloat16), (500, 32001, torch.float16)],
+    "large_past": [(500, 140001, torch.float32), (999, 140003, torch.bfloat16), (1000, 140001, torch.float16)],
+}
+
+
+def _on_gpu(rows, d, seed):
+    """Random codes, scales of 126 to 128, and the values they stand for."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    codes = torch.randint(0, 256, (rows, d // 2), dtype=torch.uint8, device="cuda", generator=g)
+    scales = torch.randint(126, 129, (rows, d // 32), dtype=torch.int32, device="cuda", generator=g).to(torch.uint8)
+    table = torch.as_tensor(oracle.mxfp4_code_values()).cuda()
+    v = table[torch.stack((codes & 15, codes >> 4), 2).view(rows, d).int()]
+    return tim.Mxfp4(codes, scales), v * torch.exp2(scales.double() - 127).repeat_interleave(32, 1)
+
+
+@pytest.mark.parametrize("d", [512, 640, 768, 896, 1024, 1152, 1408, 2048])
+@pytest.mark.parametrize("kernel,T,V,dtype", [(k, *c) for k, cases in KERNELS.items() for c in cases])
+def test_every_kernel_at_every_end_of_a_row(kernel, T, V, dtype, d):
+    """Exact logits where rows of one scale group and of several end after each of its k-steps, then the same bits
+    around NaN blocks at the first, a middle and the last block of rows and entries in different tiles."""
+    esize = torch.empty((), dtype=dtype).element_size()
+    assert fp4_kernel(T, d, V, esize, torch.cuda.get_device_properties(0).multi_processor_count) == kernel
+    print(f"case {kernel} T={T} d={d} V={V} {dtype}", flush=True)
+    h, hv = _on_gpu(T, d, d)
+    w, wv = _on_gpu(V, d, d + 1)
+    # sums of multiples of 1/16 below 36 * 4 * d < 2^23 units: exact in fp32, rounded once on the way out
+    z = tim.mxfp4_logits(h, w, dtype=dtype)
+    assert torch.equal(z, (hv @ wv.T).to(dtype))
+    rows, entries, blocks = (0, T // 2, T - 1), (1, V // 2, V - 1), (0, d // 64, d // 32 - 1)
+    for r, v, b in zip(rows, entries, blocks):
+        h.scales[r, b] = 255
+        w.scales[v, d // 32 - 1 - b] = 255
+    y = tim.mxfp4_logits(h, w, dtype=dtype)
+    bad = torch.zeros_like(z, dtype=torch.bool)
+    bad[list(rows)] = True
+    bad[:, list(entries)] = True
+    assert torch.equal(torch.isnan(y), bad)
+    assert torch.equal(torch.where(bad, 0.0, y), torch.where(bad, 0.0, z))
+
+
+def test_more_short_rows_than_a_launch():
+    """More rows than one launch of the kernel for short rows takes (65535 blocks of 16): the rows about its end."""
+    T, d, V = 65535 * 16 + 50, 384, 3
+    h, _ = _on_gpu(T, d, 1)
+    w, wv = _on_gpu(V, d, 2)
+    z = tim.mxfp4_logits(h, w)
+    for a, b in ((0, 40), (65535 * 16 - 20, 65535 * 16 + 20), (T - 33, T)):
+        part = tim.Mxfp4(h.codes[a:b], h.scales[a:b])
+        assert torch.equal(z[a:b].double(), tim.mxfp4_dequantize(part, torch.float32).double() @ wv.T)
