@@ -101,6 +101,14 @@ tim_status tim_mxfp4_logits(const uint8_t* h_codes, const uint8_t* h_scales, con
  * each step one fp32 operation. A masked entry is excluded whatever its logit
  * holds (NaN and infinities too).
  *
+ * Engines differ in where the bias enters; this order, the bias on the logits
+ * that the penalties leave, is the library's choice, and with a repetition
+ * penalty the other one is another distribution. An engine that adds its biases
+ * first is had by two calls: tim_logits_adjust with the bias list alone, at
+ * temperature 1 and in fp32, and then any call of this section with the other
+ * rules on its output. The gradient with respect to that output is the one with
+ * respect to the logits.
+ *
  * Histories may overlap and share a stream: decode rows point at their
  * requests' tokens, the rows of a packed training stream each at the tokens
  * before their own. Consecutive rows of the same begin and split whose end

@@ -640,7 +640,8 @@ class LogitRules:
     tokens in the history, frequency is subtracted per occurrence in the generated part, presence once (fp32 [T]).
     bias_ids int32 [M] and bias_values fp32 [M]; row i adds the entries bias_begin[i]:bias_end[i] (int64 [T]; of an
     id listed twice the last). mask int32 [n, >= ceil(V / 32)], bit v % 32 of word v // 32 set where v is allowed;
-    row i takes mask mask_rows[i] (int32 [T], outside [0, n): none) or, without mask_rows, mask i."""
+    row i takes mask mask_rows[i] (int32 [T], outside [0, n): none) or, without mask_rows, mask i. The bias comes after
+    the penalties; for an engine that adds it before them, logits_adjust with a rule set of the bias alone goes first."""
     history: torch.Tensor | None = None
     hist_begin: torch.Tensor | None = None
     hist_split: torch.Tensor | None = None

@@ -785,3 +785,23 @@ def test_far_rows_beside_others_in_a_workgroup(dtype):
                            dz[a:a + 600]), a
     tim.logits_logprobs_backward(z, tok, lse, g, r, 0.9, entropy=H, grad_entropy=e, out=z)
     assert torch.equal(z, dz)
+
+
+def test_biases_before_the_penalties_by_two_calls():
+    """The other order of bias and penalties: a call with the bias alone, the rest on its fp32 output."""
+    case = Case(7, 9001, 45, history=80, bias=30, masks=4, scale=1.0)
+    bias = tim.LogitRules(**{f: getattr(case.lib, f) for f in ("bias_ids", "bias_values", "bias_begin", "bias_end")})
+    first = tim.logits_adjust(case.z, bias)
+    want = case.z.cpu().numpy().copy()
+    for row, r in zip(want, case.rules):
+        for t, b in dict(r.pop("bias", ())).items():
+            if 0 <= t < case.V:
+                row[t] = row[t] + np.float32(b)
+    assert torch.equal(first.cpu(), torch.as_tensor(want))
+    one = tim.logits_adjust(case.z, case.lib, 0.7)
+    case.z = first
+    for f in ("bias_ids", "bias_values", "bias_begin", "bias_end"):
+        setattr(case.lib, f, None)
+    assert not torch.equal(check_adjust(case, 0.7), one.cpu())
+    check_logprobs(case, 0.7)
+    check_backward(case, 0.7, True)
