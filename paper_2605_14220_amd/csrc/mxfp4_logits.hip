@@ -17,8 +17,11 @@
 // that a lane reads the four bytes of its block column with one ds_read_b32
 // and the MFMA picks the k-step's by its byte select.
 //
-// Few rows are bound by the stream of W; many by the MFMAs, the LDS reads
-// that feed them, and the fp32 logits going out.
+// Few rows are bound by the stream of W. Many are bound by the k-loop of the
+// 256 x 256 tile: at V = 151936 2000 rows take 439, 753 and 1325 us for d =
+// 2048, 4096 and 8192, in 18.6 rounds of tiles 2.0 us a stage, of which the
+// MFMAs need 1.3 (two buffers fit, so every boundary waits for all loads), and
+// 7.8 us a tile besides, its first loads and its logits.
 
 #include <hip/hip_runtime.h>
 
@@ -37,15 +40,16 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 constexpr int kStageCodes = 128;  // bytes of a row's codes in a stage (two k-steps)
 constexpr int kGroupScales = 16;  // bytes of a row's scales in a group (two stages)
 // Vocabulary tiles per group in the workgroup -> tile order. What a round of workgroups writes is runs of this many
-// tiles in the rows of a few: 2000 rows at d = 4096, V = 151936 780 us against 811 for 8 and 850 for 4 (8000 rows:
-// 2948, 2897 and 2985; one or two row tiles the same).
+// tiles in the rows of a few: 2000 rows at d = 4096, V = 151936 753 us against 789 for 8 and 830 for 4, 1000 rows 405,
+// 431 and 431 (8000 rows 2857, 2848 and 2921; one or two row tiles the same).
 constexpr int kGroupFp4 = 16;
 
 // A workgroup of WV x WT waves, each NA x NB blocks of 16 x 16, and PER_CU
 // workgroups on a CU. ONCE: one tile takes all hidden rows, so W is read once
-// and its loads pass the caches by (1 row of d = 2048 and V = 151936 31.5 us
-// against 34.8, 64 of d = 4096 79 against 84, 200 129 against 136); where tiles
-// share W they find it in L2 (2000 rows 774 us against 895).
+// and its loads pass the caches by (1 row of d = 2048 and V = 151936 31.1 us
+// against 34.6, 64 of d = 4096 79 against 83, 128 and 200 the same; a W of less
+// than the caches, called for again at once, would be found there: 28.5 against
+// 26.7); where tiles share W they find it in L2 (2000 rows 753 us against 899).
 template <int WV_, int WT_, int NA_, int NB_, int PER_CU_, bool ONCE_>
 struct Fp4Tile {
   static constexpr int WV = WV_, WT = WT_, NA = NA_, NB = NB_, PER_CU = PER_CU_;
@@ -116,8 +120,8 @@ __device__ __forceinline__ void lanes_ordered() {
 // A wave's logits leave through LDS, 16 hidden rows at a time, so that a store
 // writes runs of NA * 16 logits of a row: straight from the accumulators it
 // would write 64 bytes in each of 16 rows. NT: past the caches, for logits too
-// large to be found there again (2000 rows at d = 4096, V = 151936, 1.2 GB: 0.80
-// ms against 0.86; with the scattered stores 0.96 against 0.89).
+// large to be found there again (2000 rows at d = 4096, V = 151936, 1.2 GB: 753
+// us against 780; with the scattered stores, before other steps, 960 against 890).
 typedef i32x4 i32x4_by2 __attribute__((aligned(2)));  // logits are aligned to their element
 typedef i32x4 i32x4_by4 __attribute__((aligned(4)));
 template <class TL, class T>
@@ -436,7 +440,10 @@ __global__ __launch_bounds__(TL::NW * 64, TL::PER_CU * TL::NW / 4) void fp4_logi
 }
 
 // Rows shorter than a group of scales: one wave per block of 16 x 16, operands
-// from memory.
+// from memory. For few rows that is near W's stream (1 row of d = 384 and V =
+// 151936 8.7 us, 6.4 at the copy's rate); W is read again for every 16 rows and
+// logits leave in 64-byte runs, so many rows are far from it (2000 rows of d =
+// 256 672 us and of d = 384 740, where rows of 512 take 258 in tiles).
 template <class T>
 __global__ __launch_bounds__(256) void fp4_logits_short(const Mxfp4LogitsArgs a) {
   const int lane = threadIdx.x & 63;

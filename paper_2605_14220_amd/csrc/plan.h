@@ -126,10 +126,11 @@ inline bool norm_fused(int64_t T, int32_t d) {
 
 // The 4-bit head's tile for more than 128 rows: 128 x 128, two workgroups a CU,
 // or 256 x 256, one. A round of the small ones does half the work of a large
-// one's in 0.60-0.67 of its time (d = 1536, V = 50257, 512 rows: 16 us a round
-// against 23; d = 4096, V = 151936, 1000 rows: 30 against 45), so they pay where
+// one's in 0.53-0.66 of its time (d = 1536, V = 50257, 512 rows: 11 us a round
+// against 21; d = 4096, V = 151936, 1000 rows: 27 against 40), so they pay where
 // they take less than 8/5 of the rounds: 333 rows at d = 1536, V = 50257 (3
-// against 2) 34 us against 45; 256 rows there (2 against 1) 31 against 26.
+// against 2) 33 us against 37; 256 rows there (2 against 1) 29 against 26, 512
+// rows (4 against 2) 45 against 42.
 inline bool fp4_small_tiles(int64_t T, int64_t V, int64_t cus) {
   if (cus < 1) return false;
   const int64_t small = (T + 127) / 128 * ((V + 127) / 128), large = (T + 255) / 256 * ((V + 255) / 256);

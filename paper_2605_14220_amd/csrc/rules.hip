@@ -26,9 +26,9 @@
 // entry of a load, 4096 rows of 151936 logits with up to 1280 tokens of history
 // took 574 us against 533 (before other steps made both faster).
 //
-// Reads reach 7 TB/s (4096 rows of 151936 fp32 logits without rules 355 us). With histories, and for 16-bit logits, the
-// vector instructions of the row loop bound the statistics (456 us fp32, 390 us bf16, 270 us bf16 without rules),
-// so whole chunks, all but the last of a row, take a path without bounds per load (bf16 450 us with them).
+// Reads reach 7 TB/s (4096 rows of 151936 fp32 logits without rules 349 us). With histories, and for 16-bit logits, the
+// vector instructions of the row loop bound the statistics (442 us fp32, 386 us bf16, 251 us bf16 without rules),
+// so whole chunks, all but the last of a row, take a path without bounds per load (with them 458, 447 and 296 us).
 
 #include <hip/hip_runtime.h>
 
@@ -74,8 +74,8 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef i32x2 i32x2_by2 __attribute__((aligned(2)));
 typedef i32x4 i32x4_by2 __attribute__((aligned(2)));
-// Streaming loads: the pass does not read its logits again (4096 rows of 151936
-// fp32 logits 526 us against 495, 64 rows 20.5 against 17.7).
+// Streaming loads: the pass does not read its logits again (log-probs of 4096
+// rows of 151936 fp32 logits 442 us against 459, 64 rows 16.1 against 18.4).
 template <class T, int N>
 __device__ __forceinline__ Vec<T, N> load_vec(const T* p, int c) {
   static_assert(sizeof(Vec<T, N>) == 16, "one load");
@@ -161,8 +161,8 @@ __device__ __forceinline__ void count_token(uint32_t* cnt, uint32_t* touched, ui
 
 // Tokens history[from .. to), the prompt's before split. Two loads a thread are
 // in flight at a time: more take registers from the rows' (with two 64 rows of
-// 151936 logits take 17.7 us, with four 19.3, with eight 20.9; 4096 rows 495,
-// 495 and 525).
+// 151936 logits take 16.1 us, with four 17.2, with eight 17.8; 4096 rows 442,
+// 448 and 477).
 __device__ __forceinline__ void count_tokens(uint32_t* cnt, uint32_t* touched, const int32_t* __restrict__ history,
                                              int64_t from, int64_t split, int64_t to, int v0, int n) {
   constexpr int kStep = 2 * kThreads;
@@ -182,7 +182,8 @@ __device__ __forceinline__ void count_tokens(uint32_t* cnt, uint32_t* touched, c
 }
 
 // p[i] for an index that is the same in every lane, through the scalar cache:
-// no kernel here writes what these arrays hold.
+// no kernel writes these arrays while it reads them, and what an earlier launch
+// wrote (the merge lse and entropy) is seen from the start of the next.
 template <class T>
 __device__ __forceinline__ T scalar(const T* p, int64_t i) {
   typedef const __attribute__((address_space(4))) T* constant;
@@ -358,8 +359,8 @@ __device__ __forceinline__ void far_row(int64_t row, uint32_t* lds, Stat* wstat)
   __syncthreads();  // wstat and the words have been read
 }
 
-// Three workgroups a CU (80 registers): with two 4096 rows of 151936 logits take 560 us against 500 and 64 rows 19.9
-// against 17.7 (the gradients the same); four spill.
+// Three workgroups a CU (80 registers): with two 4096 rows of 151936 logits take 546 us against 442, 64 rows 18.6
+// against 16.1, the gradient of 2047 rows 361 against 337; four spill.
 template <Op OP, class TI, class TO, bool SPARSE>
 __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args, int n_chunks, int rows_per_group) {
   const ArgsPtr a = kernel_args();  // args
@@ -579,7 +580,7 @@ __global__ __launch_bounds__(kThreads, 6) void rules_kernel(const RuleArgs args,
       }
     }
     // The next row is requested before this one is stored: memory operations end in order, and loads behind the stores
-    // would wait for them (the gradient of 4096 rows of 151936 bf16 logits 582 us against 556).
+    // would wait for them (the gradient of 2047 rows of 151936 fp32 logits 343 us against 337; of bf16 logits the same).
     if (i + 1 < n_rows) {
       request(row + 1);
       w = read_row(row + 1, hist, bias);
@@ -770,8 +771,8 @@ hipError_t launch_rules(const RuleArgs& a, hipStream_t s) {
     b.past_caches = a.T * a.V * (int64_t)sizeof(TO) > kCacheBytes;
     // Rows of one workgroup: histories that extend one another are counted once for the group, and the next row's
     // logits are on their way while a row is worked on, but only where the workgroups fill the CUs many times over.
-    // At 4096 workgroups: 4096 rows of 151936 logits 500 us (one row each 600), the gradient of 2047 rows 346 us (at
-    // 1024 workgroups 396, at 8192 359).
+    // At 4096 workgroups: log-probs of 4096 rows of 151936 logits 442 us (at 1024 workgroups 450, at 8192 437, one row
+    // each 557), the gradient of 2047 rows 337 us (at 1024 410, at 8192 357, one row each 327).
     int group = 1;
     if (b.r.history) {
       const int64_t fill = rows * n_chunks / 4096;
