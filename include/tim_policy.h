@@ -186,8 +186,8 @@ tim_status tim_logits_logprobs(const void* logits, int32_t dtype, int64_t T, int
  * for masked ones. A row with g = e = 0 (padding) and a row with nothing allowed
  * get zeros.
  *
- * p_v goes by lse where |lse| < 1024, with lse's rounding in it: relatively less
- * than 2^-14. Rows beyond, whose lse says too little of them (at fp32's lowest
+ * p_v goes by lse where |lse| < 1024 and carries its error, relatively 2^-14 or
+ * little more. Rows beyond, whose lse says too little of them (at fp32's lowest
  * number it holds no log V, and it may be infinite), have their maximum and sum
  * formed anew from the logits, in one workgroup each: right, but slower.
  *

@@ -274,9 +274,9 @@ __device__ __forceinline__ void mark_biases(uint32_t* last, const int32_t* ids, 
 }
 
 // |lse| from which a row's gradient does not go by it. p = e^(x - lse) is
-// relatively as far off as fp32's lse is absolutely, |lse| 2^-24: less than
-// 2^-14 short of this, but at fp32's lowest value lse holds no log n any more,
-// and over a temperature below 1 it is infinite.
+// relatively as far off as fp32's lse is absolutely, by two roundings: 2^-14
+// short of this, but at fp32's lowest value lse holds no log n any more, and
+// over a temperature below 1 it is infinite.
 constexpr float kFarLse = 1024.f;
 
 // The whole gradient of such a row in one workgroup, which first forms the

@@ -805,3 +805,47 @@ def test_biases_before_the_penalties_by_two_calls():
     assert not torch.equal(check_adjust(case, 0.7), one.cpu())
     check_logprobs(case, 0.7)
     check_backward(case, 0.7, True)
+
+
+def test_far_rows_captured_and_on_two_streams():
+    """A captured gradient whose rows become far and near between replays, and two at once, give the eager bits."""
+    T, V = 40, 17001
+    kw = _packed_rules(T, V, 46, True)
+    rules, gen = _slice(kw, 0, T), torch.Generator(device="cuda").manual_seed(4)
+    base = torch.randn(T, V, device="cuda", generator=gen)
+    z, tok = base.clone(), torch.randint(0, V, (T,), device="cuda", dtype=torch.int32, generator=gen)
+    g, e = (torch.randn(T, device="cuda", generator=gen) for _ in range(2))
+    out = tuple(torch.empty(T, device="cuda") for _ in range(3))
+    ws = torch.empty(tim.logits_logprobs_workspace_size(T, V), dtype=torch.uint8, device="cuda")
+    dz = torch.empty_like(z)
+
+    def step(z, out, ws, dz):
+        tim.logits_logprobs(z, tok, rules, 0.8, workspace=ws, out=out)
+        tim.logits_logprobs_backward(z, tok, out[2], g, rules, 0.8, entropy=out[1], grad_entropy=e, out=dz)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(z, out, ws, dz)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(z, out, ws, dz)
+    other = [(torch.empty_like(z), tuple(torch.empty_like(t) for t in out), torch.empty_like(ws), torch.empty_like(dz))
+             for _ in range(3)]
+    for k in range(4):
+        z.copy_(base + 5000.0 * ((torch.arange(T, device="cuda") + k) % 3 - 1)[:, None])
+        for a in other:
+            a[0].copy_(z)
+        step(*other[0])
+        want = other[0][3].clone()
+        torch.cuda.synchronize()
+        graph.replay()
+        assert torch.equal(dz, want), k
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        for s, a in zip(streams, other[1:]):
+            with torch.cuda.stream(s):
+                step(*a)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a[3], want) for a in other[1:]), k
