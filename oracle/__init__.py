@@ -20,6 +20,8 @@ Parity status (each function's own docstring names its pins):
 * ``mxfp4_*``  pinned (the values by hand, brute force, ties, an element loop).
 * ``change_logits``, ``changed_logprobs``, ``changed_logprobs_grad``  pinned
   (hand-made rows, float64 autograd, finite differences, ``logprobs``).
+* ``embedding``, ``embedding_backward``, ``adapters_add``, ``adapters_backward``
+  pinned (hand-made rows, float64 autograd, magnitudes by hand).
 """
 
 from .logprobs import bf16_to_f64, logits, logprobs  # noqa: F401
@@ -30,3 +32,4 @@ from .mxfp4 import (mxfp4_code_values, mxfp4_logits, mxfp4_pack, mxfp4_quantize,
 from .ppo import ppo_loss  # noqa: F401
 from .rmsnorm import f64_to_bf16_bits, rmsnorm, rmsnorm_grads, round_bf16  # noqa: F401
 from .rules import change_logits, changed_logprobs, changed_logprobs_grad  # noqa: F401
+from .vocab import adapters_add, adapters_backward, embedding, embedding_backward  # noqa: F401

@@ -64,6 +64,12 @@ class _LogitRules(ctypes.Structure):
                 ("mask_ld", ctypes.c_int64), ("mask_rows", ctypes.c_void_p)]
 
 
+class _Adapters(ctypes.Structure):
+    """tim_adapters"""
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("n", ctypes.c_int32), ("r", ctypes.c_int32), ("d", ctypes.c_int32), ("N", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -135,6 +141,26 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.tim_mxfp4_logits.restype = c.c_int
     lib.tim_mxfp4_logits.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int64, c.c_int32, c.c_int32,
                                      c.c_float, c.c_void_p, c.c_int32, c.c_int64, c.c_void_p]
+    lib.tim_embedding.restype = c.c_int
+    lib.tim_embedding.argtypes = [c.c_void_p, c.c_int32, c.c_int32, c.c_int32, c.c_int64, c.c_void_p, c.c_int64, c.c_float,
+                                  c.c_void_p, c.c_int32, c.c_int64, c.c_void_p]
+    lib.tim_embedding_backward_workspace_size.restype = c.c_size_t
+    lib.tim_embedding_backward_workspace_size.argtypes = [c.c_int64, c.c_int32, c.c_int32]
+    lib.tim_embedding_backward.restype = c.c_int
+    lib.tim_embedding_backward.argtypes = [c.c_void_p, c.c_int32, c.c_int64, c.c_int32, c.c_int64, c.c_void_p, c.c_int32,
+                                           c.c_float, c.c_void_p, c.c_int64, c.c_int32, c.c_void_p, c.c_size_t,
+                                           c.c_void_p]
+    adapters = c.POINTER(_Adapters)
+    for f in (lib.tim_adapters_add_workspace_size, lib.tim_adapters_backward_workspace_size):
+        f.restype = c.c_size_t
+        f.argtypes = [c.c_int64, c.c_int32, c.c_int32, c.c_int32, c.c_int32]
+    lib.tim_adapters_add.restype = c.c_int
+    lib.tim_adapters_add.argtypes = [adapters, c.c_void_p, c.c_int64, c.c_void_p, c.c_int64, c.c_void_p, c.c_int64,
+                                     c.c_void_p, c.c_int32, c.c_int64, c.c_void_p, c.c_size_t, c.c_void_p]
+    lib.tim_adapters_backward.restype = c.c_int
+    lib.tim_adapters_backward.argtypes = [adapters, c.c_void_p, c.c_int64, c.c_void_p, c.c_int64, c.c_void_p, c.c_int32,
+                                          c.c_int64, c.c_void_p, c.c_int32, c.c_int64, c.c_int32, c.c_void_p, c.c_void_p,
+                                          c.c_int32, c.c_void_p, c.c_size_t, c.c_void_p]
     rules = c.POINTER(_LogitRules)
     lib.tim_logits_adjust.restype = c.c_int
     lib.tim_logits_adjust.argtypes = [c.c_void_p, c.c_int32, c.c_int64, c.c_int32, c.c_int64, rules, c.c_float,
@@ -838,3 +864,218 @@ def logits_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: to
             float(temperature), _ptr(lse), _ptr(entropy), _ptr(grad_logp), _ptr(grad_entropy), _ptr(out),
             _DTYPES[out.dtype], out_ld)
     return out
+
+
+# ------------------------------------------------------------------ what stands beside the head
+# (include/tim_vocab.h)
+
+
+def _scratch(name, workspace, size, device) -> torch.Tensor:
+    """The caller's workspace, or a new one of the size."""
+    if workspace is None:
+        return torch.empty(size, dtype=torch.uint8, device=device)
+    _require_gpu(workspace)
+    _on_one_gpu(name, device, workspace)
+    return workspace
+
+
+def _int32(name, *sizes):
+    """Sizes that the C interface takes as 32-bit integers."""
+    if any(not 0 <= n < 1 << 31 for n in sizes):
+        raise ValueError(f"tim.{name}: a size is out of range")
+
+
+def embedding(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, dtype: torch.dtype | None = None,
+              out: torch.Tensor | None = None) -> torch.Tensor:
+    """scale * table[tokens]: rows [T, d] of table [V, d] (fp32, bf16 or fp16, dense rows) for tokens int32 [T], each
+    element formed in fp32 and rounded once to dtype (the table's by default); zeros for a token outside [0, V)
+    (padding). out, if given, may have padded rows."""
+    lib = load_library()
+    if table.dtype not in _DTYPES:
+        raise TypeError("tim.embedding: the table must be fp32, bf16 or fp16")
+    ld = _dense_rows("embedding", "table", table)
+    V, d = table.shape
+    _int32("embedding", V, d)
+    if tokens.dim() != 1:
+        raise ValueError("tim.embedding: tokens must be [T]")
+    T = tokens.shape[0]
+    _row_vector("embedding", "tokens", tokens, T, torch.int32)
+    if out is None:
+        out = torch.empty((T, d), dtype=table.dtype if dtype is None else dtype, device=table.device)
+    elif dtype is not None and out.dtype != dtype:
+        raise ValueError("tim.embedding: out must have the dtype asked for")
+    if out.dtype not in _DTYPES:
+        raise TypeError("tim.embedding: rows are fp32, bf16 or fp16")
+    if out.shape != (T, d):
+        raise ValueError("tim.embedding: out must be [T, d]")
+    out_ld = _dense_rows("embedding", "out", out)
+    _on_one_gpu("embedding", table.device, table, tokens, out)
+    _launch(table.device, lib.tim_embedding, _ptr(table), _DTYPES[table.dtype], V, d, ld, _ptr(tokens), T, float(scale),
+            _ptr(out), _DTYPES[out.dtype], out_ld)
+    return out
+
+
+def embedding_backward_workspace_size(T: int, V: int, d: int) -> int:
+    """Bytes of workspace tim_embedding_backward needs (0 for T == 0 or invalid shapes)."""
+    return int(load_library().tim_embedding_backward_workspace_size(int(T), int(V), int(d)))
+
+
+def embedding_backward(grad: torch.Tensor, tokens: torch.Tensor, V: int, scale: float = 1.0,
+                       grad_table: torch.Tensor | None = None, accumulate: bool = False,
+                       workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient fp32 [V, d] of the embedding's table from that of its rows, grad [T, d] (fp32, bf16 or fp16, dense
+    rows). With accumulate the sums are added to grad_table (the grad_w of logprobs_backward for a tied head) in the rows
+    of the tokens that occur; otherwise every row is written. Deterministic."""
+    lib = load_library()
+    if grad.dtype not in _DTYPES:
+        raise TypeError("tim.embedding_backward: grad must be fp32, bf16 or fp16")
+    ld = _dense_rows("embedding_backward", "grad", grad)
+    T, d = grad.shape
+    V = int(V)
+    _int32("embedding_backward", V, d)
+    _row_vector("embedding_backward", "tokens", tokens, T, torch.int32)
+    dev = grad.device
+    if grad_table is None:
+        if accumulate:
+            raise ValueError("tim.embedding_backward: accumulate needs the grad_table buffer")
+        grad_table = torch.empty((V, d), dtype=torch.float32, device=dev)
+    if grad_table.dtype != torch.float32:
+        raise TypeError("tim.embedding_backward: grad_table must be fp32")
+    if grad_table.shape != (V, d):
+        raise ValueError("tim.embedding_backward: grad_table must be [V, d]")
+    table_ld = _dense_rows("embedding_backward", "grad_table", grad_table)
+    ws = _scratch("embedding_backward", workspace, int(lib.tim_embedding_backward_workspace_size(T, V, d)), dev)
+    _on_one_gpu("embedding_backward", dev, grad, tokens, grad_table)
+    _launch(dev, lib.tim_embedding_backward, _ptr(grad), _DTYPES[grad.dtype], T, d, ld, _ptr(tokens), V, float(scale),
+            _ptr(grad_table), table_ld, 1 if accumulate else 0, _ptr(ws), ws.numel() * ws.element_size())
+    return grad_table
+
+
+class Adapters(NamedTuple):
+    """Low-rank adapters of a projection from d to N elements: adapter k adds scales[k] (x a[k]^T) b[k]^T. a [n, r, d] and
+    b [n, N, r] of one type (bf16 or fp16), contiguous; scales fp32 [n], None for ones."""
+    a: torch.Tensor
+    b: torch.Tensor
+    scales: torch.Tensor | None = None
+
+
+def _adapters(name, ad, x, rows) -> tuple[_Adapters, int, int]:
+    """(C struct, T, row stride of x) of the adapters and the rows they apply to."""
+    if ad.a.dtype not in (torch.bfloat16, torch.float16) or ad.b.dtype != ad.a.dtype or x.dtype != ad.a.dtype:
+        raise TypeError(f"tim.{name}: a, b and x must be bf16, or all fp16")
+    if ad.a.dim() != 3 or ad.b.dim() != 3 or ad.a.shape[0] != ad.b.shape[0] or ad.a.shape[1] != ad.b.shape[2]:
+        raise ValueError(f"tim.{name}: a [n, r, d] and b [n, N, r]")
+    x_ld = _dense_rows(name, "x", x)
+    n, r, d = ad.a.shape
+    if x.shape[1] != d:
+        raise ValueError(f"tim.{name}: x must be [T, d]")
+    _int32(name, n, r, d, ad.b.shape[1])
+    T = x.shape[0]
+    _row_vector(name, "rows", rows, T, torch.int32)
+    if ad.scales is not None:
+        if ad.scales.dtype != torch.float32:
+            raise TypeError(f"tim.{name}: scales must be fp32")
+        if ad.scales.shape != (n,):
+            raise ValueError(f"tim.{name}: scales must be [n]")
+    _require_gpu(ad.a, ad.b, ad.scales)
+    _on_one_gpu(name, x.device, x, rows, ad.a, ad.b, ad.scales)
+    return _Adapters(_ptr(ad.a), _ptr(ad.b), _ptr(ad.scales), _DTYPES[x.dtype], n, r, d, ad.b.shape[1]), T, x_ld
+
+
+def adapters_add_workspace_size(T: int, d: int, N: int, n: int, r: int) -> int:
+    """Bytes of workspace tim_adapters_add needs (0 for T == 0 or invalid shapes)."""
+    return int(load_library().tim_adapters_add_workspace_size(int(T), int(d), int(N), int(n), int(r)))
+
+
+def adapters_add(base: torch.Tensor | None, x: torch.Tensor, rows: torch.Tensor, adapters: Adapters,
+                 dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
+                 workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """base [T, N] (a shared projection's output, the head's logits among them; None: zeros) plus the adapter of each row
+    of x [T, d]: row t's is adapters rows[t] (int32 [T]), none where that is outside [0, n). fp32 sums, rounded once to
+    base's type (to dtype without a base, x's by default). out may be base itself (in place), but no other overlap is
+    allowed."""
+    lib = load_library()
+    ad, T, x_ld = _adapters("adapters_add", adapters, x, rows)
+    dev = x.device
+    base_ld = ad.N
+    if base is not None:
+        if base.shape != (T, ad.N):
+            raise ValueError("tim.adapters_add: base must be [T, N]")
+        base_ld = _dense_rows("adapters_add", "base", base)
+        _on_one_gpu("adapters_add", dev, base)
+        if dtype is not None and dtype != base.dtype:
+            raise ValueError("tim.adapters_add: the output has base's type")
+        dtype = base.dtype
+    if out is None:
+        out = torch.empty((T, ad.N), dtype=x.dtype if dtype is None else dtype, device=dev)
+    elif out.shape != (T, ad.N) or (dtype is not None and out.dtype != dtype):
+        raise ValueError("tim.adapters_add: out must be [T, N] of the output's type")
+    if out.dtype not in _DTYPES:
+        raise TypeError("tim.adapters_add: the output is fp32, bf16 or fp16")
+    out_ld = _dense_rows("adapters_add", "out", out)
+    _on_one_gpu("adapters_add", dev, out)
+    ws = _scratch("adapters_add", workspace, int(lib.tim_adapters_add_workspace_size(T, ad.d, ad.N, ad.n, ad.r)), dev)
+    _launch(dev, lib.tim_adapters_add, ctypes.byref(ad), _ptr(x), x_ld, _ptr(rows), T, _ptr(base), base_ld, _ptr(out),
+            _DTYPES[out.dtype], out_ld, _ptr(ws), ws.numel() * ws.element_size())
+    return out
+
+
+def adapters_backward_workspace_size(T: int, d: int, N: int, n: int, r: int) -> int:
+    """Bytes of workspace tim_adapters_backward needs (0 for T == 0 or invalid shapes)."""
+    return int(load_library().tim_adapters_backward_workspace_size(int(T), int(d), int(N), int(n), int(r)))
+
+
+def adapters_backward(grad: torch.Tensor, x: torch.Tensor, rows: torch.Tensor, adapters: Adapters, want_x: bool = True,
+                      want_a: bool = True, want_b: bool = True, dtype: torch.dtype | None = None,
+                      grad_x: torch.Tensor | None = None, accumulate_x: bool = False,
+                      grad_a: torch.Tensor | None = None, grad_b: torch.Tensor | None = None, accumulate: bool = False,
+                      workspace: torch.Tensor | None = None):
+    """(grad_x [T, d] or None, grad_a fp32 [n, r, d] or None, grad_b fp32 [n, N, r] or None) through adapters_add, from
+    the gradient [T, N] of its output (fp32, bf16 or fp16, dense rows). grad_x is of dtype (x's by default); with
+    accumulate_x it is added to the grad_x given, with accumulate grad_a and grad_b to theirs. Rows without an adapter and
+    adapters without rows get zeros, or nothing added."""
+    lib = load_library()
+    name = "adapters_backward"
+    ad, T, x_ld = _adapters(name, adapters, x, rows)
+    dev = x.device
+    if grad.dtype not in _DTYPES:
+        raise TypeError(f"tim.{name}: grad must be fp32, bf16 or fp16")
+    if grad.shape != (T, ad.N):
+        raise ValueError(f"tim.{name}: grad must be [T, N]")
+    grad_ld = _dense_rows(name, "grad", grad)
+    _on_one_gpu(name, dev, grad)
+    gx_ld, gx_type = ad.d, 0
+    if want_x:
+        if grad_x is None:
+            if accumulate_x:
+                raise ValueError(f"tim.{name}: accumulate_x needs the grad_x buffer")
+            grad_x = torch.empty((T, ad.d), dtype=x.dtype if dtype is None else dtype, device=dev)
+        elif dtype is not None and grad_x.dtype != dtype:
+            raise ValueError(f"tim.{name}: grad_x must have the dtype asked for")
+        if grad_x.dtype not in _DTYPES:
+            raise TypeError(f"tim.{name}: grad_x is fp32, bf16 or fp16")
+        if grad_x.shape != (T, ad.d):
+            raise ValueError(f"tim.{name}: grad_x must be [T, d]")
+        gx_ld, gx_type = _dense_rows(name, "grad_x", grad_x), _DTYPES[grad_x.dtype]
+        _on_one_gpu(name, dev, grad_x)
+    weights = []
+    for want, what, t, shape in ((want_a, "grad_a", grad_a, (ad.n, ad.r, ad.d)),
+                                 (want_b, "grad_b", grad_b, (ad.n, ad.N, ad.r))):
+        if want and t is None:
+            if accumulate:
+                raise ValueError(f"tim.{name}: accumulate needs the {what} buffer")
+            t = torch.empty(shape, dtype=torch.float32, device=dev)
+        if want:
+            if t.dtype != torch.float32:
+                raise TypeError(f"tim.{name}: {what} must be fp32")
+            if t.shape != shape:
+                raise ValueError(f"tim.{name}: {what} must be {list(shape)}")
+            _require_gpu(t)
+            _on_one_gpu(name, dev, t)
+        weights.append(t if want else None)
+    ws = _scratch(name, workspace, int(lib.tim_adapters_backward_workspace_size(T, ad.d, ad.N, ad.n, ad.r)), dev)
+    grad_x = grad_x if want_x else None
+    _launch(dev, lib.tim_adapters_backward, ctypes.byref(ad), _ptr(x), x_ld, _ptr(rows), T, _ptr(grad),
+            _DTYPES[grad.dtype], grad_ld, _ptr(grad_x), gx_type, gx_ld, 1 if accumulate_x else 0, _ptr(weights[0]),
+            _ptr(weights[1]), 1 if accumulate else 0, _ptr(ws), ws.numel() * ws.element_size())
+    return grad_x, weights[0], weights[1]

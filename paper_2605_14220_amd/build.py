@@ -18,7 +18,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libtim.so")
 SOURCES = ["lmhead.hip", "lmgrad.hip", "rmsnorm.hip", "mismatch.hip", "seqstats.hip", "ppo.hip", "tim_api.hip",
-           "mxfp4.hip", "mxfp4_logits.hip", "rules.hip", "policy_api.hip"]
+           "mxfp4.hip", "mxfp4_logits.hip", "rules.hip", "policy_api.hip", "grouping.hip", "embedding.hip", "adapters.hip",
+           "vocab_api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

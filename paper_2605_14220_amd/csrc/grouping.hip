@@ -1,0 +1,402 @@
+// Stable sort of row indices by key, least significant digit first, and the
+// lists of runs. Up to kGroupSmall rows are one workgroup's work in LDS; more
+// are sorted in one or two passes of two launches each (counts per block, then
+// places), blocks in row order, then listed.
+//
+// Within a wave 64 consecutive items find the ones of their own digit by one
+// ballot per bit, so equal digits keep their order without atomics.
+
+#include <hip/hip_runtime.h>
+
+#include "grouping.h"
+
+namespace tim {
+namespace {
+
+constexpr int kSmallThreads = 1024;
+constexpr int kSmallWaves = kSmallThreads / 64;
+constexpr int kSortThreads = 256;
+constexpr int kSortWaves = kSortThreads / 64;
+
+// Keeps the compiler from moving LDS accesses of a wave across it; the hardware
+// takes a wave's LDS accesses in order.
+__device__ __forceinline__ void lanes_in_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// The lanes whose digit (of `bits` bits) is this lane's, among those of `active`.
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, uint64_t active) {
+  uint64_t peers = active;
+  for (int b = 0; b < bits; ++b) {
+    const bool set = (digit >> b) & 1;
+    const uint64_t m = __ballot(set);
+    peers &= set ? m : ~m;
+  }
+  return peers;
+}
+__device__ __forceinline__ int lanes_below(uint64_t m) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+
+__device__ __forceinline__ uint32_t key_of(const int32_t* keys, int64_t i, int32_t n) {
+  const uint32_t k = (uint32_t)keys[i];
+  return k < (uint32_t)n ? k : (uint32_t)n;
+}
+
+// Counts a wave's items of consecutive steps per digit: `count` is the wave's own.
+__device__ __forceinline__ void count_step(uint32_t digit, int bits, bool there, volatile uint32_t* count) {
+  const uint64_t peers = same_digit(digit, bits, __ballot(there));
+  if (there && lanes_below(peers) == 0) count[digit] += __popcll(peers);
+  lanes_in_order();
+}
+// The item's place: `place` holds the wave's next place of each digit.
+__device__ __forceinline__ uint32_t place_step(uint32_t digit, int bits, bool there, volatile uint32_t* place) {
+  const uint64_t peers = same_digit(digit, bits, __ballot(there));
+  const int below = lanes_below(peers);
+  const uint32_t at = there ? place[digit] : 0;
+  lanes_in_order();
+  if (there && below == 0) place[digit] = at + __popcll(peers);
+  lanes_in_order();
+  return at + below;
+}
+
+// Lists the run or the join that place p of the sorted keys starts or ends, if
+// any. first: the first place of p's key.
+struct Lists {
+  int32_t n, lists;
+  int32_t C[kMaxRunLists];
+  Run* runs[kMaxRunLists];
+  Join* joins[kMaxRunLists];
+};
+template <class Keys, class Append>
+__device__ __forceinline__ void list_place(const Lists& L, Keys key_at, int32_t T, int32_t p, bool there, uint32_t key,
+                                           int32_t first, Append append) {
+  for (int l = 0; l < L.lists; ++l) {
+    const int C = L.C[l];
+    const bool starts = there && (p - first) % C == 0;
+    Run r = {p, 0, (int32_t)key, -1};
+    bool ends = false;  // the last run of several
+    if (starts) {
+      // the first place in (p, p + C] that is not of the key
+      int lo = p + 1, hi = p + C < T ? p + C : T;
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (key_at(mid) == key) lo = mid + 1; else hi = mid;
+      }
+      r.count = lo - p;
+      const bool last = !(lo < T && key_at(lo) == key);
+      if (p != first || !last) r.slot = run_slot(p, C, last);
+      ends = last && p != first;
+    }
+    const int at = append(2 * l, starts);
+    if (starts) L.runs[l][at] = r;
+    const int j = append(2 * l + 1, ends);
+    if (ends) L.joins[l][j] = {first, p + r.count, (int32_t)key, 0};
+  }
+}
+
+// The inclusive maximum over the wave's lanes up to this one.
+__device__ __forceinline__ int32_t wave_scan_max(int32_t x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int32_t y = __shfl_up(x, o);
+    if (lane >= o && y > x) x = y;
+  }
+  return x;
+}
+
+// ------------------------------------------------------------- few rows
+
+// One workgroup: items are key * 4096 + row index, 32 bits for keys below 2^20.
+__global__ __launch_bounds__(kSmallThreads) void group_small(const int32_t* keys, int32_t T, int passes, int digit_bits,
+                                                             int32_t limit, Lists L, int32_t* order, uint8_t* seen,
+                                                             int32_t* counters) {
+  __shared__ uint32_t item[2][kGroupSmall];
+  __shared__ uint32_t place[kSmallWaves][256];
+  __shared__ uint32_t wave_total[4];
+  __shared__ int32_t wave_first[kSmallWaves];
+  __shared__ int32_t carry;
+  __shared__ int32_t counted[2 * kMaxRunLists];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int bins = 1 << digit_bits;
+  // each wave takes consecutive items, a multiple of 64
+  const int per_wave = ((T + kSmallWaves - 1) / kSmallWaves + 63) / 64 * 64;
+  const int from = wave * per_wave, to = from + per_wave < T ? from + per_wave : T;
+  if (tid < 2 * kMaxRunLists) counted[tid] = 0;
+  for (int i = tid; i < T; i += kSmallThreads) item[0][i] = key_of(keys, i, L.n) << 12 | i;
+  int cur = 0;
+  for (int pass = 0; pass < passes; ++pass, cur ^= 1) {
+    const int shift = 12 + pass * digit_bits;
+    for (int b = lane; b < bins; b += 64) place[wave][b] = 0;
+    __syncthreads();
+    for (int i = from; i < to; i += 64) {
+      const bool there = i + lane < to;
+      const uint32_t x = there ? item[cur][i + lane] : 0;
+      count_step((x >> shift) & (bins - 1), digit_bits, there, place[wave]);
+    }
+    __syncthreads();
+    // places: digits in order, the waves' items of one digit in wave order
+    uint32_t sum = 0, incl = 0;
+    if (tid < 256) {
+      if (tid < bins)
+        for (int w = 0; w < kSmallWaves; ++w) {
+          const uint32_t c = place[w][tid];
+          place[w][tid] = sum;
+          sum += c;
+        }
+      incl = sum;
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) {
+        const uint32_t y = __shfl_up(incl, o);
+        if (lane >= o) incl += y;
+      }
+      if (lane == 63) wave_total[wave] = incl;
+    }
+    __syncthreads();
+    if (tid < bins) {
+      uint32_t before = incl - sum;
+      for (int w = 0; w < wave; ++w) before += wave_total[w];
+      for (int w = 0; w < kSmallWaves; ++w) place[w][tid] += before;
+    }
+    __syncthreads();
+    for (int i = from; i < to; i += 64) {
+      const bool there = i + lane < to;
+      const uint32_t x = there ? item[cur][i + lane] : 0;
+      const uint32_t at = place_step((x >> shift) & (bins - 1), digit_bits, there, place[wave]);
+      if (there) item[cur ^ 1][at] = x;
+    }
+    __syncthreads();
+  }
+  const uint32_t* sorted = item[cur];
+  auto key_at = [&](int p) { return sorted[p] >> 12; };
+  auto append = [&](int c, bool add) {
+    const uint64_t m = __ballot(add);
+    int base = 0;
+    if (m != 0 && lane == 0) base = atomicAdd(&counted[c], (int)__popcll(m));
+    return __shfl(base, 0) + lanes_below(m);
+  };
+  if (tid == 0) carry = 0;
+  for (int base = 0; base < T; base += kSmallThreads) {
+    const int p = base + tid;
+    const uint32_t x = p < T ? sorted[p] : 0xffffffffu;
+    const uint32_t key = x >> 12;
+    const bool head = p < T && (p == 0 || key_at(p - 1) != key);
+    int first = wave_scan_max(head ? p : 0, lane);
+    if (lane == 63) wave_first[wave] = first;
+    __syncthreads();
+    int before = carry;
+    for (int w = 0; w < wave; ++w) before = wave_first[w] > before ? wave_first[w] : before;
+    first = first > before ? first : before;
+    const bool there = p < T && (int32_t)key < limit;
+    if (p < T) order[p] = x & 4095;
+    if (head && there && seen && (int32_t)key < L.n) seen[key] = 1;
+    list_place(L, key_at, T, p, there, key, first, append);
+    __syncthreads();
+    if (tid == kSmallThreads - 1) carry = first;
+  }
+  __syncthreads();
+  if (tid < 2 * kMaxRunLists) counters[tid] = counted[tid];
+}
+
+// ------------------------------------------------------------ many rows
+
+// One pass's input: the keys themselves (first pass), or key and row pairs.
+struct Source {
+  const int32_t* keys;
+  const uint2* pairs;
+  int64_t T;
+  int32_t n, per_block, shift, bits;
+};
+__device__ __forceinline__ uint2 item_of(const Source& s, int64_t i) {
+  return s.pairs ? s.pairs[i] : uint2{key_of(s.keys, i, s.n), (uint32_t)i};
+}
+
+// hist[block][digit]: items of each digit; the first launch of a grouping also
+// clears the counters.
+__global__ __launch_bounds__(kSortThreads) void sort_count(Source s, uint32_t* hist, int32_t* counters) {
+  __shared__ uint32_t count[kSortWaves][1024];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int bins = 1 << s.bits;
+  if (counters && blockIdx.x == 0 && threadIdx.x < 2 * kMaxRunLists) counters[threadIdx.x] = 0;
+  for (int b = lane; b < bins; b += 64) count[wave][b] = 0;
+  __syncthreads();
+  const int64_t base = (int64_t)blockIdx.x * s.per_block;
+  const int64_t to = base + s.per_block < s.T ? base + s.per_block : s.T;
+  for (int64_t i = base + wave * 64; i < to; i += kSortThreads) {
+    const bool there = i + lane < to;
+    const uint32_t x = there ? item_of(s, i + lane).x : 0;
+    count_step((x >> s.shift) & (bins - 1), s.bits, there, count[wave]);
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < bins; b += kSortThreads)
+    hist[((size_t)blockIdx.x << s.bits) + b] = count[0][b] + count[1][b] + count[2][b] + count[3][b];
+}
+
+// The items in the pass's order: pairs, or (last pass) rows and keys apart.
+__global__ __launch_bounds__(kSortThreads) void sort_place(Source s, const uint32_t* hist, uint2* pairs, int32_t* order,
+                                                           uint32_t* keys) {
+  __shared__ uint32_t place[kSortWaves][1024];
+  __shared__ uint32_t wave_total[kSortWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int bins = 1 << s.bits;
+  for (int b = lane; b < bins; b += 64) place[wave][b] = 0;
+  __syncthreads();
+  // a wave takes consecutive quarters here, so that its items precede the next wave's
+  const int64_t base = (int64_t)blockIdx.x * s.per_block + (int64_t)wave * (s.per_block / kSortWaves);
+  const int64_t end = base + s.per_block / kSortWaves;
+  const int64_t to = end < s.T ? end : s.T;
+  for (int64_t i = base; i < to; i += 64) {
+    const bool there = i + lane < to;
+    const uint32_t x = there ? item_of(s, i + lane).x : 0;
+    count_step((x >> s.shift) & (bins - 1), s.bits, there, place[wave]);
+  }
+  __syncthreads();
+  // four consecutive digits a thread: items of smaller digits, and of the same one in earlier blocks
+  const int per = bins > kSortThreads ? bins / kSortThreads : 1;
+  uint32_t all[4] = {}, mine[4] = {}, sum = 0;
+  if (threadIdx.x * per < (unsigned)bins) {
+    for (unsigned k = 0; k < gridDim.x; ++k) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < per) {
+          const uint32_t c = hist[((size_t)k << s.bits) + threadIdx.x * per + e];
+          all[e] += c;
+          if (k < blockIdx.x) mine[e] += c;
+        }
+    }
+    sum = all[0] + all[1] + all[2] + all[3];
+  }
+  uint32_t incl = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const uint32_t y = __shfl_up(incl, o);
+    if (lane >= o) incl += y;
+  }
+  if (lane == 63) wave_total[wave] = incl;
+  __syncthreads();
+  uint32_t before = incl - sum;
+  for (int w = 0; w < wave; ++w) before += wave_total[w];
+  if (threadIdx.x * per < (unsigned)bins) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < per) {
+        uint32_t at = before + mine[e];
+        before += all[e];
+        for (int w = 0; w < kSortWaves; ++w) {
+          const uint32_t c = place[w][threadIdx.x * per + e];
+          place[w][threadIdx.x * per + e] = at;
+          at += c;
+        }
+      }
+  }
+  __syncthreads();
+  for (int64_t i = base; i < to; i += 64) {
+    const bool there = i + lane < to;
+    const uint2 x = there ? item_of(s, i + lane) : uint2{0, 0};
+    const uint32_t at = place_step((x.x >> s.shift) & (bins - 1), s.bits, there, place[wave]);
+    if (there) {
+      if (pairs) {
+        pairs[at] = x;
+      } else {
+        order[at] = (int32_t)x.y;
+        keys[at] = x.x;
+      }
+    }
+  }
+}
+
+constexpr int kListThreads = 256;
+__global__ __launch_bounds__(kListThreads) void list_runs(const uint32_t* keys, int32_t T, int32_t limit, Lists L,
+                                                          uint8_t* seen, int32_t* counters) {
+  __shared__ int32_t wave_first[kListThreads / 64];
+  __shared__ int32_t carry;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t base = blockIdx.x * kListThreads, p = base + tid;
+  auto key_at = [&](int q) { return keys[q]; };
+  if (wave == 0) {
+    // the first place of the key at the block's start: 64 probes at a time
+    const uint32_t key = keys[base];
+    int lo = 0, hi = base;  // the answer is in [lo, hi]
+    while (lo < hi) {
+      const int step = (hi - lo + 63) / 64;
+      const int q = lo + lane * step;
+      const uint64_t at_or_after = __ballot(q >= hi || keys[q] >= key);
+      // the first probe at or after the answer, and the one before it
+      const int f = at_or_after ? __builtin_ctzll(at_or_after) : 64;
+      const int new_hi = f == 64 ? hi : (lo + f * step < hi ? lo + f * step : hi);
+      if (f > 0) lo = lo + (f - 1) * step + 1;
+      hi = new_hi;
+    }
+    if (lane == 0) carry = lo;
+  }
+  const uint32_t key = p < T ? keys[p] : 0xffffffffu;
+  const bool head = p < T && (p == 0 || keys[p - 1] != key);
+  int first = wave_scan_max(head ? p : 0, lane);
+  if (lane == 63) wave_first[wave] = first;
+  __syncthreads();
+  int before = carry;
+  for (int w = 0; w < wave; ++w) before = wave_first[w] > before ? wave_first[w] : before;
+  first = first > before ? first : before;
+  const bool there = p < T && (int32_t)key < limit;
+  if (head && there && seen && (int32_t)key < L.n) seen[key] = 1;
+  auto append = [&](int c, bool add) {
+    const uint64_t m = __ballot(add);
+    int at = 0;
+    if (m != 0 && lane == 0) at = atomicAdd(&counters[c], (int)__popcll(m));
+    return __shfl(at, 0) + lanes_below(m);
+  };
+  list_place(L, key_at, T, p, there, key, first, append);
+}
+
+__global__ __launch_bounds__(256) void clear_bytes(uint8_t* p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i * 4 < n; i += (int64_t)gridDim.x * 256)
+    ((uint32_t*)p)[i] = 0;
+}
+
+}  // namespace
+
+#define TIM_TRY(call)                  \
+  do {                                 \
+    call;                              \
+    const hipError_t e_ = hipGetLastError(); \
+    if (e_ != hipSuccess) return e_;   \
+  } while (0)
+
+hipError_t launch_grouping(const Grouping& g, const int32_t* keys, bool keep_rest, uint8_t* seen, void* ws,
+                           hipStream_t s) {
+  char* w = (char*)ws;
+  int32_t* counters = (int32_t*)(w + g.counters);
+  int32_t* order = (int32_t*)(w + g.order);
+  Lists L = {};
+  L.n = g.n;
+  L.lists = g.lists;
+  for (int l = 0; l < g.lists; ++l) {
+    L.C[l] = g.C[l];
+    L.runs[l] = (Run*)(w + g.runs[l]);
+    L.joins[l] = (Join*)(w + g.joins[l]);
+  }
+  const int32_t limit = keep_rest ? g.n + 1 : g.n;
+  // whole words: seen has room for a multiple of 4 keys
+  if (seen) TIM_TRY((clear_bytes<<<256, 256, 0, s>>>(seen, g.n)));
+  if (g.T <= kGroupSmall) {
+    TIM_TRY((group_small<<<1, kSmallThreads, 0, s>>>(keys, (int32_t)g.T, g.passes, g.digit, limit, L, order, seen,
+                                                     counters)));
+    return hipSuccess;
+  }
+  uint32_t* sorted = (uint32_t*)(w + g.keys);
+  uint2* pairs = (uint2*)(w + g.pairs);
+  uint32_t* hist = (uint32_t*)(w + g.hist);
+  for (int pass = 0; pass < g.passes; ++pass) {
+    const bool last = pass + 1 == g.passes;
+    const Source src = {keys, pass == 0 ? nullptr : pairs, g.T, g.n, g.per_block, pass * g.digit, g.digit};
+    TIM_TRY((sort_count<<<g.blocks, kSortThreads, 0, s>>>(src, hist, pass == 0 ? counters : nullptr)));
+    TIM_TRY((sort_place<<<g.blocks, kSortThreads, 0, s>>>(src, hist, last ? nullptr : pairs, order, sorted)));
+  }
+  TIM_TRY((list_runs<<<(unsigned)((g.T + kListThreads - 1) / kListThreads), kListThreads, 0, s>>>(
+      sorted, (int32_t)g.T, limit, L, seen, counters)));
+  return hipSuccess;
+}
+
+}  // namespace tim

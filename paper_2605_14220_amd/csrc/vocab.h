@@ -1,0 +1,204 @@
+// Internal launch interface and host-side checks of the tim_vocab.h entry
+// points. The checks are pure C++, so every error path runs without a GPU.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstddef>
+#include <cstdint>
+
+#include "grouping.h"
+#include "policy.h"
+#include "tim_vocab.h"
+
+namespace tim {
+
+inline bool valid_width(int64_t d) { return d >= 1 && d <= TIM_MAX_WIDTH; }
+inline bool valid_keys(int64_t V) { return V >= 1 && V <= TIM_MAX_VOCAB; }
+inline bool grouped_rows(int64_t T) { return T >= 0 && T <= TIM_MAX_GROUPED_ROWS; }
+inline bool valid_flag(int32_t f) { return f == 0 || f == 1; }
+
+inline tim_status validate_embedding(const void* table, int32_t dtype, int32_t V, int32_t d, int64_t ld,
+                                     const int32_t* tokens, int64_t T, float scale, const void* out, int32_t out_dtype,
+                                     int64_t out_ld) {
+  if (T < 0 || !valid_keys(V) || !valid_width(d) || ld < d || out_ld < d) return TIM_ERR_SHAPE;
+  if (!valid_dtype(dtype) || !valid_dtype(out_dtype) || !std::isfinite(scale)) return TIM_ERR_VALUE;
+  if (T == 0) return TIM_OK;
+  if (!table || !tokens || !out) return TIM_ERR_NULL;
+  if (!aligned_to(table, dtype_bytes(dtype)) || !aligned_to(tokens, 4) || !aligned_to(out, dtype_bytes(out_dtype)))
+    return TIM_ERR_VALUE;
+  return TIM_OK;
+}
+
+// The embedding gradient's workspace: the grouping, a byte per token that
+// occurs, the partial sums of tokens with several runs.
+struct EmbedPlan {
+  Grouping g;
+  size_t seen, part, bytes;
+};
+inline EmbedPlan plan_embedding_backward(int64_t T, int32_t V, int32_t d) {
+  const int C[1] = {TIM_EMBED_RUN};
+  EmbedPlan p = {plan_grouping(T, V, 1, C), 0, 0, 0};
+  size_t at = p.g.bytes;
+  p.seen = at, at += group_align((size_t)V);
+  p.part = at, at += T > TIM_EMBED_RUN ? group_align((size_t)run_slots(T, TIM_EMBED_RUN) * d * 4) : 0;
+  p.bytes = at;
+  return p;
+}
+
+inline tim_status validate_embedding_backward(const void* grad_out, int32_t dtype, int64_t T, int32_t d, int64_t ld,
+                                              const int32_t* tokens, int32_t V, float scale, const float* grad_table,
+                                              int64_t grad_ld, int32_t accumulate, const void* ws, size_t ws_bytes) {
+  if (!grouped_rows(T) || !valid_keys(V) || !valid_width(d) || ld < d || grad_ld < d) return TIM_ERR_SHAPE;
+  if (!valid_dtype(dtype) || !std::isfinite(scale) || !valid_flag(accumulate)) return TIM_ERR_VALUE;
+  if (!grad_table) return TIM_ERR_NULL;
+  if (!aligned_to(grad_table, 4)) return TIM_ERR_VALUE;
+  if (T == 0) return TIM_OK;
+  if (!grad_out || !tokens) return TIM_ERR_NULL;
+  if (!aligned_to(grad_out, dtype_bytes(dtype)) || !aligned_to(tokens, 4)) return TIM_ERR_VALUE;
+  if (!ws || !aligned16(ws) || ws_bytes < plan_embedding_backward(T, V, d).bytes) return TIM_ERR_WORKSPACE;
+  return TIM_OK;
+}
+
+struct EmbedArgs {
+  const void* table;
+  int32_t V, d;
+  int64_t ld;
+  const int32_t* tokens;
+  int64_t T;
+  float scale;
+  void* out;
+  int64_t out_ld;
+};
+hipError_t launch_embedding(const EmbedArgs& a, int dtype, int out_dtype, hipStream_t s);
+
+struct EmbedGradArgs {
+  const void* grad_out;
+  int64_t T, ld;
+  int32_t V, d;
+  const int32_t* tokens;
+  float scale;
+  float* grad_table;
+  int64_t grad_ld;
+  int32_t accumulate;
+};
+hipError_t launch_embedding_backward(const EmbedGradArgs& a, int dtype, void* ws, hipStream_t s);
+
+// ------------------------------------------------------------------ adapters
+
+constexpr int kAdapterRun = 64;     // rows of one adapter that a workgroup takes together
+constexpr int kShrinkChunk = 1024;  // elements of d (of N in the backward: kGradChunk) whose products one workgroup sums
+constexpr int kGradChunk = 1024;
+constexpr int kGradRows = 512;      // rows of one adapter whose outer products one workgroup sums
+
+inline int rank_padded(int r) { return (r + 15) / 16 * 16; }
+inline int chunks_of(int64_t n, int chunk) { return (int)((n + chunk - 1) / chunk); }
+
+// Workspaces: the grouping, then fp32 [chunks, T, rank_padded] of partial sums
+// of x a^T, and for the backward those of grad b, both sums, and the partial
+// weight gradients of adapters with several runs of kGradRows rows.
+struct AdapterPlan {
+  Grouping g;
+  int rp, x_chunks, g_chunks;
+  size_t u_part, v_part, u, v, a_part, b_part, seen, bytes;
+};
+inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r, bool backward) {
+  const int C[2] = {kAdapterRun, kGradRows};
+  AdapterPlan p = {};
+  p.g = plan_grouping(T, n, backward ? 2 : 1, C);
+  p.rp = rank_padded(r);
+  p.x_chunks = chunks_of(d, kShrinkChunk);
+  p.g_chunks = chunks_of(N, kGradChunk);
+  size_t at = p.g.bytes;
+  const size_t rows = group_align((size_t)T * p.rp * 4);
+  p.u_part = at, at += rows * p.x_chunks;
+  if (backward) {
+    p.v_part = at, at += rows * p.g_chunks;
+    p.u = at, at += rows;
+    p.v = at, at += rows;
+    const size_t slots = T > kGradRows ? (size_t)run_slots(T, kGradRows) * r * 4 : 0;
+    p.a_part = at, at += group_align(slots * d);
+    p.b_part = at, at += group_align(slots * N);
+    p.seen = at, at += group_align((size_t)n);
+  }
+  p.bytes = at;
+  return p;
+}
+
+inline bool valid_adapter_shape(int64_t T, int64_t d, int64_t N, int64_t n, int64_t r) {
+  return grouped_rows(T) && valid_width(d) && valid_width(N) && valid_keys(n) && r >= 1 && r <= TIM_MAX_RANK;
+}
+
+// The adapters and the rows they apply to.
+inline tim_status validate_adapters(const tim_adapters* ad, const void* x, int64_t x_ld, const int32_t* rows,
+                                    int64_t T) {
+  if (!ad) return TIM_ERR_NULL;
+  if (!valid_adapter_shape(T, ad->d, ad->N, ad->n, ad->r) || x_ld < ad->d) return TIM_ERR_SHAPE;
+  if (ad->dtype != TIM_BF16 && ad->dtype != TIM_F16) return TIM_ERR_VALUE;
+  if (T == 0) return TIM_OK;
+  if (!ad->a || !ad->b || !x || !rows) return TIM_ERR_NULL;
+  if (!aligned_to(ad->a, 2) || !aligned_to(ad->b, 2) || !aligned_to(ad->scales, 4) || !aligned_to(x, 2) ||
+      !aligned_to(rows, 4))
+    return TIM_ERR_VALUE;
+  return TIM_OK;
+}
+
+inline tim_status validate_adapters_add(const tim_adapters* ad, const void* x, int64_t x_ld, const int32_t* rows,
+                                        int64_t T, const void* base, int64_t base_ld, const void* out,
+                                        int32_t out_dtype, int64_t out_ld, const void* ws, size_t ws_bytes) {
+  const tim_status s = validate_adapters(ad, x, x_ld, rows, T);
+  if (s != TIM_OK) return s;
+  if ((base && base_ld < ad->N) || out_ld < ad->N) return TIM_ERR_SHAPE;
+  if (!valid_dtype(out_dtype)) return TIM_ERR_VALUE;
+  if (T == 0) return TIM_OK;
+  if (!out) return TIM_ERR_NULL;
+  if (base == out && base_ld != out_ld) return TIM_ERR_SHAPE;
+  if (!aligned_to(base, dtype_bytes(out_dtype)) || !aligned_to(out, dtype_bytes(out_dtype))) return TIM_ERR_VALUE;
+  if (!ws || !aligned16(ws) || ws_bytes < plan_adapters(T, ad->d, ad->N, ad->n, ad->r, false).bytes)
+    return TIM_ERR_WORKSPACE;
+  return TIM_OK;
+}
+
+inline tim_status validate_adapters_backward(const tim_adapters* ad, const void* x, int64_t x_ld, const int32_t* rows,
+                                             int64_t T, const void* grad, int32_t grad_dtype, int64_t grad_ld,
+                                             const void* grad_x, int32_t gx_dtype, int64_t gx_ld, int32_t accumulate_x,
+                                             const float* grad_a, const float* grad_b, int32_t accumulate_ab,
+                                             const void* ws, size_t ws_bytes) {
+  const tim_status s = validate_adapters(ad, x, x_ld, rows, T);
+  if (s != TIM_OK) return s;
+  if (grad_ld < ad->N || (grad_x && gx_ld < ad->d)) return TIM_ERR_SHAPE;
+  if (!valid_dtype(grad_dtype) || !valid_flag(accumulate_x) || !valid_flag(accumulate_ab)) return TIM_ERR_VALUE;
+  if (grad_x && (!valid_dtype(gx_dtype) || !aligned_to(grad_x, dtype_bytes(gx_dtype)))) return TIM_ERR_VALUE;
+  if (!aligned_to(grad_a, 4) || !aligned_to(grad_b, 4)) return TIM_ERR_VALUE;
+  if (T == 0) return TIM_OK;
+  if (!grad) return TIM_ERR_NULL;
+  if (!aligned_to(grad, dtype_bytes(grad_dtype))) return TIM_ERR_VALUE;
+  if (!ws || !aligned16(ws) || ws_bytes < plan_adapters(T, ad->d, ad->N, ad->n, ad->r, true).bytes)
+    return TIM_ERR_WORKSPACE;
+  return TIM_OK;
+}
+
+hipError_t launch_adapters_add(const tim_adapters& ad, const void* x, int64_t x_ld, const int32_t* rows, int64_t T,
+                               const void* base, int64_t base_ld, void* out, int out_dtype, int64_t out_ld, void* ws,
+                               hipStream_t s);
+
+struct AdapterGradArgs {
+  const void* x;
+  int64_t x_ld;
+  const int32_t* rows;
+  int64_t T;
+  const void* grad;
+  int64_t grad_ld;
+  void* grad_x;
+  int64_t gx_ld;
+  int32_t accumulate_x;
+  float *grad_a, *grad_b;
+  int32_t accumulate_ab;
+};
+hipError_t launch_adapters_backward(const tim_adapters& ad, const AdapterGradArgs& a, int grad_dtype, int gx_dtype,
+                                    void* ws, hipStream_t s);
+// p[r * ld + c] = 0 for r < rows, c < d.
+hipError_t launch_zero_rows(float* p, int64_t rows, int64_t d, int64_t ld, hipStream_t s);
+
+}  // namespace tim

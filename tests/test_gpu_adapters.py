@@ -1,0 +1,260 @@
+"""GPU parity of low-rank adapters and their gradients (tim_adapters_*) against the fp64 oracle.
+
+Whole numbers. Small whole numbers keep every sum exact in fp32 in any order, so outputs are compared for equality with
+the exact result rounded once: that pins the grouping, every index and the ends of odd sizes, in every rank's kernel.
+
+Other numbers. Sums of k terms in fp32 are off by at most k 2^-23 of their terms' magnitudes (one rounding of at most 2^-23
+a term, whatever the order, for the matrix instructions may truncate). With S the oracle's sum of magnitudes:
+  out     d + r + 3 additions and multiplications behind an element: (d + r + 3) 2^-23 S, then eps / 2 of the output type
+  grad_x  N + r + 3: the same with N
+  grad_a  N + rows + 3,  grad_b  d + rows + 3, fp32 outputs
+times (1 + 2^-8) for the products of those factors (the counts stay below 2^14)."""
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2605_14220_amd as tim
+from tim_testutil import require_gpu
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    require_gpu()
+
+
+def _np(t):
+    return None if t is None else t.detach().double().cpu().numpy()
+
+
+def _padded(t, pad):
+    if not pad:
+        return t
+    rows, cols = t.shape
+    big = torch.full((rows * (cols + pad) + 1,), 77.0, dtype=t.dtype, device=t.device)
+    view = big[1:].view(rows, cols + pad)[:, :cols]
+    view.copy_(t)
+    return view
+
+
+def _rows(T, n, kind, g):
+    if kind == "one":
+        return torch.full((T,), n - 1, dtype=torch.int32)
+    if kind == "runs":
+        return (torch.arange(T) * 3 // max(T, 1) % n).to(torch.int32)
+    if kind == "none":
+        return torch.full((T,), -1, dtype=torch.int32)
+    r = torch.randint(-1, n, (T,), generator=g)
+    odd = torch.tensor([n, 2 ** 31 - 1, -2 ** 31])
+    return torch.where(r < 0, odd[torch.randint(0, 3, (T,), generator=g)], r).to(torch.int32)
+
+
+# T, d, N, n, r, rows, padding of strides
+SIZES = [(1, 1, 1, 1, 1, "one", 0), (1, 2048, 1000, 4, 16, "one", 0), (2, 33, 7, 3, 2, "mixed", 0),
+         (16, 64, 64, 2, 16, "mixed", 0), (17, 100, 65, 2, 9, "mixed", 3), (48, 130, 300, 32, 16, "mixed", 0),
+         (63, 40, 257, 1, 17, "one", 0), (64, 1024, 256, 1, 32, "one", 1), (65, 1025, 255, 1, 33, "one", 0),
+         (130, 257, 1031, 2, 64, "runs", 0), (200, 96, 64, 5, 65, "mixed", 2), (37, 72, 130, 2, 100, "mixed", 0),
+         (70, 40, 90, 2, 256, "mixed", 0), (333, 500, 130, 3, 8, "runs", 0), (700, 64, 70, 2, 5, "mixed", 0),
+         (1500, 40, 66, 1, 12, "one", 0), (5000, 24, 33, 7, 3, "mixed", 0), (100, 48, 40, 3, 4, "none", 0),
+         (4097, 20, 16, 1000, 2, "mixed", 0), (40, 3000, 20, 2, 1, "mixed", 0)]
+
+
+def _whole(T, d, N, n, r, kind, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+
+    def ints(*shape, top=2, keep=1.0):
+        z = torch.randint(-top, top + 1, shape, generator=g).float()
+        return z * (torch.rand(shape, generator=g) < keep)
+
+    # few nonzero elements, so that sums of products of three stay far below 2^24
+    x = ints(T, d, keep=min(1.0, 40 / d))
+    a, b = ints(n, r, d), ints(n, N, r, keep=min(1.0, 16 / r))
+    grad = ints(T, N, keep=min(1.0, 40 / N))
+    scales = 2.0 ** torch.randint(-1, 3, (n,), generator=g).float()
+    rows = _rows(T, n, kind, g)
+    return [t.to(dtype) for t in (x, a, b, grad)] + [scales, rows]
+
+
+@pytest.mark.parametrize("case", range(len(SIZES)))
+@pytest.mark.parametrize("dtype,out", [(BF16, F32), (F16, F16), (BF16, BF16), (F16, F32)])
+def test_whole_numbers(case, dtype, out):
+    T, d, N, n, r, kind, pad = SIZES[case]
+    x, a, b, grad, scales, rows = _whole(T, d, N, n, r, kind, dtype, 7 * case)
+    g = torch.Generator().manual_seed(case)
+    base = torch.randint(-100, 101, (T, N), generator=g).to(out)
+    dev = [t.cuda() for t in (a, b, scales)]
+    ad = tim.Adapters(*dev)
+    xd, rd = _padded(x.cuda(), pad), rows.cuda()
+    print(SIZES[case], dtype, out, flush=True)
+
+    want, size = oracle.adapters_add(_np(base), _np(x), rows.numpy(), _np(a), _np(b), _np(scales))
+    assert size.max() < 2 ** 24
+    bd = _padded(base.cuda(), pad)
+    got = tim.adapters_add(bd, xd, rd, ad)
+    assert torch.equal(got.cpu(), torch.as_tensor(want).to(out))
+    got = tim.adapters_add(bd, xd, rd, ad, out=bd)  # in place
+    assert got is bd and torch.equal(bd.cpu(), torch.as_tensor(want).to(out))
+    if pad:
+        assert (bd._base[1:].view(T, N + pad)[:, N:] == 77).all()
+    want, _ = oracle.adapters_add(None, _np(x), rows.numpy(), _np(a), _np(b), None)
+    got = tim.adapters_add(None, xd, rd, tim.Adapters(dev[0], dev[1]), dtype=out)
+    assert torch.equal(got.cpu(), torch.as_tensor(want).to(out))
+
+    (wx, wa, wb), sizes = oracle.adapters_backward(_np(grad), _np(x), rows.numpy(), _np(a), _np(b), _np(scales))
+    assert all(s.max() < 2 ** 24 for s in sizes)
+    gd = _padded(grad.to(out).cuda(), pad)
+    gx, ga, gb = tim.adapters_backward(gd, xd, rd, ad, dtype=out)
+    assert torch.equal(gx.cpu(), torch.as_tensor(wx).to(out))
+    assert torch.equal(ga.cpu().double(), torch.as_tensor(wa))
+    assert torch.equal(gb.cpu().double(), torch.as_tensor(wb))
+    # accumulated, into rows with gaps
+    old = torch.randint(-9, 10, (T, d), generator=g).float()
+    acc = _padded(old.to(out).cuda(), pad)
+    pa, pb = torch.ones_like(ga), torch.ones_like(gb)
+    tim.adapters_backward(gd, xd, rd, ad, grad_x=acc, accumulate_x=True, grad_a=pa, grad_b=pb, accumulate=True)
+    assert torch.equal(acc.cpu(), (torch.as_tensor(wx) + old).to(out))
+    assert torch.equal(pa.cpu().double(), torch.as_tensor(wa) + 1) and torch.equal(pb.cpu().double(), torch.as_tensor(wb) + 1)
+
+
+NUMBERS = [(5, 4096, 700, 3, 16, "mixed"), (200, 300, 257, 4, 9, "mixed"), (90, 1500, 1100, 2, 64, "runs"),
+           (600, 128, 80, 1, 40, "one"), (21, 60, 3000, 2, 130, "mixed")]
+
+
+@pytest.mark.parametrize("case", range(len(NUMBERS)))
+@pytest.mark.parametrize("dtype,out", [(BF16, F32), (F16, F32), (BF16, BF16), (F16, F16)])
+def test_numbers(case, dtype, out):
+    T, d, N, n, r, kind = NUMBERS[case]
+    g = torch.Generator().manual_seed(case)
+    x = (torch.randn(T, d, generator=g) * torch.exp(torch.randn(T, 1, generator=g))).to(dtype)
+    a = (torch.randn(n, r, d, generator=g) / d ** 0.5).to(dtype)
+    b = (torch.randn(n, N, r, generator=g) * 0.02).to(dtype)
+    scales = torch.rand(n, generator=g) + 0.5
+    rows = _rows(T, n, kind, g)
+    base = (2.5 * torch.randn(T, N, generator=g)).to(out)
+    grad = (0.1 * torch.randn(T, N, generator=g)).to(out)
+    ad = tim.Adapters(a.cuda(), b.cuda(), scales.cuda())
+    eps = torch.finfo(out).eps / 2
+    tiny = 2.0 ** -25 if out == F16 else 0.0  # half the step of fp16's subnormal numbers
+
+    def check(name, got, want, size, terms, eps):
+        err, bound = np.abs(_np(got) - want), terms * 2.0 ** -23 * size * (1 + 2.0 ** -8) + eps * np.abs(want) * (
+            1 + 2.0 ** -8) + tiny * (eps > 2.0 ** -24)
+        print(f"{name}: max err / bound {np.max(err / np.maximum(bound, 1e-300)):.3f}")
+        assert (err <= bound).all()
+
+    want, size = oracle.adapters_add(_np(base), _np(x), rows.numpy(), _np(a), _np(b), _np(scales))
+    check("out", tim.adapters_add(base.cuda(), x.cuda(), rows.cuda(), ad), want, size, d + r + 3, eps)
+    want, size = oracle.adapters_backward(_np(grad), _np(x), rows.numpy(), _np(a), _np(b), _np(scales))
+    got = tim.adapters_backward(grad.cuda(), x.cuda(), rows.cuda(), ad, dtype=out)
+    check("grad_x", got[0], want[0], size[0], N + r + 3, eps)
+    check("grad_a", got[1], want[1], size[1], N + T + 3, 2.0 ** -24)
+    check("grad_b", got[2], want[2], size[2], d + T + 3, 2.0 ** -24)
+
+
+def test_gradients_are_the_derivative():
+    """Against central differences of sum(out * c) with whole numbers: out is linear in each of x, a and b, so the
+    differences are exact."""
+    T, d, N, n, r = 11, 5, 6, 2, 3
+    x, a, b, c, scales, rows = [t.cuda() for t in _whole(T, d, N, n, r, "mixed", BF16, 1)]
+
+    def loss(x, a, b):
+        return (tim.adapters_add(None, x, rows, tim.Adapters(a, b, scales), dtype=F32).double() * c.double()).sum().item()
+
+    grads = tim.adapters_backward(c.float(), x, rows, tim.Adapters(a, b, scales), dtype=F32)
+    for i, t in enumerate((x, a, b)):
+        flat = grads[i].flatten()
+        for k in range(t.numel()):
+            args = [[x, a, b][j].clone() for j in range(3)]
+            args[i].view(-1)[k] += 1
+            up = loss(*args)
+            args[i].view(-1)[k] -= 2
+            assert (up - loss(*args)) / 2 == flat[k].item()
+
+
+def test_a_row_depends_on_itself_only():
+    """out and grad_x bit for bit, in batches of other sizes, other neighbours and other places."""
+    d, N, n, r = 2100, 1500, 5, 24
+    g = torch.Generator().manual_seed(2)
+    a = (torch.randn(n, r, d, generator=g) / d ** 0.5).to(BF16).cuda()
+    b = (torch.randn(n, N, r, generator=g) * 0.1).to(BF16).cuda()
+    ad = tim.Adapters(a, b, torch.rand(n, generator=g).cuda())
+    x, base, grad = torch.randn(1, d, generator=g).to(BF16), torch.randn(1, N, generator=g), torch.randn(1, N, generator=g)
+    one = torch.tensor([3], dtype=torch.int32).cuda()
+    y0 = tim.adapters_add(base.cuda(), x.cuda(), one, ad)
+    x0 = tim.adapters_backward(grad.cuda(), x.cuda(), one, ad, dtype=F32)[0]
+    for T in (2, 17, 65, 500, 4100):
+        at = T * 2 // 3
+        X, Y, G = torch.randn(T, d, generator=g).to(BF16), torch.randn(T, N, generator=g), torch.randn(T, N, generator=g)
+        X[at], Y[at], G[at] = x[0], base[0], grad[0]
+        rows = torch.randint(-1, n, (T,), generator=g, dtype=torch.int32)
+        rows[at] = 3
+        X, Y, G, rows = X.cuda(), Y.cuda(), G.cuda(), rows.cuda()
+        assert torch.equal(tim.adapters_add(Y, X, rows, ad)[at], y0[0])
+        assert torch.equal(tim.adapters_backward(G, X, rows, ad, dtype=F32)[0][at], x0[0])
+
+
+def test_nan_and_infinity_stay_in_their_rows():
+    T, d, N, n, r = 40, 70, 90, 3, 5
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn(T, d, generator=g).to(BF16).cuda()
+    a, b = torch.randn(n, r, d, generator=g).to(BF16).cuda(), torch.randn(n, N, r, generator=g).to(BF16).cuda()
+    rows = (torch.arange(T) % 4 - 1).to(torch.int32).cuda()  # -1 .. 2
+    base = torch.randn(T, N, generator=g).cuda()
+    grad = torch.randn(T, N, generator=g).cuda()
+    ad = tim.Adapters(a, b)
+    good = tim.adapters_add(base, x, rows, ad)
+    gx = tim.adapters_backward(grad, x, rows, ad, dtype=F32)[0]
+    x[6, 3] = float("nan")   # adapter 1
+    x[10, 0] = float("inf")  # adapter 1
+    grad[13, 2] = float("nan")  # adapter 0
+    x[4], grad[4] = float("nan"), float("inf")  # no adapter
+    got = tim.adapters_add(base, x, rows, ad)
+    bad = torch.zeros(T, dtype=torch.bool)
+    bad[6] = bad[10] = True
+    assert torch.equal((~torch.isfinite(got)).any(1).cpu(), bad)
+    assert torch.equal(got[~bad.cuda()], good[~bad.cuda()])
+    hx, ha, hb = tim.adapters_backward(grad, x, rows, ad, dtype=F32)
+    keep = torch.arange(T).cuda() != 13
+    assert torch.isnan(hx[13]).all() and torch.equal(hx[keep], gx[keep])
+    assert torch.isfinite(ha[2]).all() and torch.isfinite(hb[2]).all()  # other adapters
+    # an adapter that holds NaN reaches its own rows only
+    a[0] = float("nan")
+    got = tim.adapters_add(base, x, rows, ad)
+    assert torch.isnan(got[rows == 0]).all() and torch.equal(got[rows == 2], good[rows == 2])
+
+
+def test_rows_without_adapter_keep_the_bits_of_base():
+    base = torch.tensor([[-0.0, float("nan"), float("inf"), 1e-45, 3.0]], device="cuda")
+    x = torch.full((1, 4), float("nan"), dtype=BF16, device="cuda")
+    ad = tim.Adapters(torch.ones(2, 3, 4, dtype=BF16, device="cuda"), torch.ones(2, 5, 3, dtype=BF16, device="cuda"))
+    for k in (-1, 2):
+        got = tim.adapters_add(base, x, torch.tensor([k], dtype=torch.int32, device="cuda"), ad)
+        assert torch.equal(got.view(torch.int32), base.view(torch.int32))
+
+
+def test_parts_of_the_backward():
+    x, a, b, grad, scales, rows = [t.cuda() for t in _whole(90, 50, 60, 2, 6, "mixed", BF16, 3)]
+    ad = tim.Adapters(a, b, scales)
+    full = tim.adapters_backward(grad, x, rows, ad)
+    for want in range(8):
+        flags = [bool(want >> i & 1) for i in range(3)]
+        got = tim.adapters_backward(grad, x, rows, ad, want_x=flags[0], want_a=flags[1], want_b=flags[2])
+        for f, t, u in zip(flags, got, full):
+            assert torch.equal(t, u) if f else t is None
+
+
+def test_no_rows():
+    ad = tim.Adapters(torch.ones(2, 3, 4, dtype=BF16, device="cuda"), torch.ones(2, 5, 3, dtype=BF16, device="cuda"))
+    x = torch.empty(0, 4, dtype=BF16, device="cuda")
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert tim.adapters_add(torch.empty(0, 5, device="cuda"), x, none, ad).shape == (0, 5)
+    old = torch.ones(2, 3, 4, device="cuda")
+    gx, ga, gb = tim.adapters_backward(torch.empty(0, 5, device="cuda"), x, none, ad, grad_a=old)
+    assert gx.shape == (0, 4) and (ga == 0).all() and (gb == 0).all()
+    tim.adapters_backward(torch.empty(0, 5, device="cuda"), x, none, ad, grad_a=old.fill_(1), grad_b=gb, accumulate=True)
+    assert (old == 1).all()
