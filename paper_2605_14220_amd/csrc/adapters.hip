@@ -145,56 +145,6 @@ __global__ __launch_bounds__(kThreads) void shrink(ShrinkArgs a, RunList l) {
   store_sums<JB>(acc, lds, a.part + ((int64_t)blockIdx.y * a.T + run.first) * a.rp, a.rp, j0, run.count, lane, wave);
 }
 
-struct ContractArgs {
-  const void* grad;
-  int64_t ld, T;
-  const void* w;  // [n, N, r]
-  int32_t n, r, rp, N;
-  float* part;    // [chunks, T, rp]
-};
-
-// v_part[chunk][place][j] = sum over the chunk's columns of grad[row][c] b[c][j].
-template <class T, class G, int JB>
-__global__ __launch_bounds__(kThreads) void contract(ContractArgs a, RunList l) {
-  __shared__ f32x4 lds[kWaves - 1][JB][4][64];
-  if ((int)blockIdx.x >= *l.n_runs) return;
-  const Run run = l.runs[blockIdx.x];
-  if (run.key >= a.n) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
-  const int j0 = blockIdx.z * JB * 16;
-  const T* w = (const T*)a.w + (int64_t)run.key * a.N * a.r;
-  const G* row[4];
-  const int blocks = (run.count + 15) / 16;
-#pragma unroll
-  for (int rb = 0; rb < 4; ++rb) {
-    const int t = rb * 16 + m;
-    row[rb] = (const G*)a.grad + l.order[run.first + (t < run.count ? t : run.count - 1)] * a.ld;
-  }
-  f32x4 acc[JB][4] = {};
-  const int from = blockIdx.y * kGradChunk + wave * (kGradChunk / kWaves);
-  const int to = from + kGradChunk / kWaves < a.N ? from + kGradChunk / kWaves : a.N;
-  for (int c0 = from; c0 < to; c0 += 16) {
-    const int c = c0 + g * 4, n = a.N - c;
-    f32x4 wf[JB];
-#pragma unroll
-    for (int jb = 0; jb < JB; ++jb) {
-      const int j = j0 + jb * 16 + m;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) wf[jb][s] = j < a.r && s < n ? (float)w[(int64_t)(c + s) * a.r + j] : 0.f;
-    }
-#pragma unroll
-    for (int rb = 0; rb < 4; ++rb)
-      if (rb < blocks) {
-        const f32x4 gf = load4(row[rb] + c, n);
-#pragma unroll
-        for (int jb = 0; jb < JB; ++jb)
-#pragma unroll
-          for (int s = 0; s < 4; ++s) acc[jb][rb] = mfma(wf[jb][s], gf[s], acc[jb][rb]);
-      }
-  }
-  store_sums<JB>(acc, lds, a.part + ((int64_t)blockIdx.y * a.T + run.first) * a.rp, a.rp, j0, run.count, lane, wave);
-}
-
 // out[place][j] = scale of the place's adapter * the sum of its chunks in order.
 __global__ __launch_bounds__(kThreads) void sum_chunks(const float* part, int64_t T, int rp, int chunks, int n,
                                                        const float* scales, float* out, RunList l) {
@@ -331,67 +281,258 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
   }
 }
 
-struct OuterArgs {
+struct PassArgs {
   const void* src;  // [T, N]
-  int64_t ld;
+  int64_t ld, T;
   const float* w;   // [T, rp] by place
+  const void* b;    // [n, N, r], the contraction's
+  float* part;      // [chunks, T, rp], the contraction's sums
   int32_t n, r, rp, N;
-  float* out;       // [n, N, r], or [n, r, N] where FLAT
-  float* part;      // [slots] of the same
+  float* out;       // [n, N, r], or [n, r, N] without the contraction
+  float* out_part;  // [slots] of the same
   int32_t accumulate;
 };
 
-// The sum over a run of rows of src[row][c] w[place][j], for 256 columns.
-template <class S, bool FLAT, int JB>
-__global__ __launch_bounds__(kThreads) void outer(OuterArgs a, RunList l) {
+// One pass over the columns of src = grad: for a run of one adapter's rows and
+// CT * 256 columns
+//   out[c][j]      sum over the rows of src[row][c] w[place][j]
+//   part[place][j] sum over the columns of src[row][c] b[c][j]    (CONTRACT)
+// and without the contraction the first alone, [j][c], of src = x.
+//
+// 64 rows of 256 columns at a time lie in LDS, read from memory once, and are
+// read from there along the rows for one product and along the columns for the
+// other. A wave takes 64 columns of the first and 16 rows of the second.
+//
+// FAST, where all is bf16: both on the bf16 matrix instructions, w as the sum of
+// three bf16 numbers, which holds all of its 24 bits. Otherwise on the fp32 ones.
+constexpr int kPassRows = 64, kPassCols = 256;
+template <class S, class W, bool CONTRACT, int JB, int CT>
+struct Pass {
+  static constexpr bool FAST = std::is_same_v<S, __bf16> && std::is_same_v<W, __bf16>;
+  typedef std::conditional_t<FAST, __bf16, float> E;  // of the tile and of w in LDS
+  static constexpr int kTerms = FAST ? 3 : 1;
+  static constexpr int kPad = 16 / (int)sizeof(E);
+  static constexpr int kRow = kPassCols + kPad;  // elements from row to row of the tile
+  static constexpr int kW = kPassRows + kPad;    // of w, [term][j][row]
+  static constexpr int kB = CT * kPassCols + 8;  // of b, [j][c]
+  static constexpr int kLoads = kPassRows * kPassCols * (int)sizeof(S) / 16 / kThreads;  // 16 bytes a thread
+  static constexpr int kV = 16 / (int)sizeof(S);
+};
+template <class S, class W, bool CONTRACT, int JB, int CT>
+__global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
+  typedef Pass<S, W, CONTRACT, JB, CT> P;
+  typedef typename P::E E;
+  typedef S sv __attribute__((ext_vector_type(P::kV)));
+  typedef E ev __attribute__((ext_vector_type(P::kV)));
+  __shared__ __attribute__((aligned(16))) E tile[kPassRows * P::kRow];
+  __shared__ __attribute__((aligned(16))) E wt[P::kTerms * JB * 16 * P::kW];
+  __shared__ __attribute__((aligned(16))) W bt[CONTRACT ? JB * 16 * P::kB : 1];
+  __shared__ int32_t rows[kMaxPassRows];
   if ((int)blockIdx.x >= *l.n_runs) return;
   const Run run = l.runs[blockIdx.x];
   if (run.key >= a.n) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
-  const int c0 = (blockIdx.y * kWaves + wave) * 64, j0 = blockIdx.z * JB * 16;
-  if (c0 >= a.N) return;
-  const int c = c0 + 4 * m;
-  f32x4 acc[JB][4] = {};
-  for (int t0 = 0; t0 < run.count; t0 += 4) {
-    const int t = t0 + g;
-    const bool there = t < run.count;
-    const int place = run.first + (there ? t : 0);
-    const f32x4 sf = there && c < a.N ? load4((const S*)a.src + l.order[place] * a.ld + c, a.N - c) : f32x4{};
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane % 16, g = lane / 16;
+  const int c_first = blockIdx.y * CT * kPassCols, j0 = blockIdx.z * JB * 16;
+  const int tiles = (a.N - c_first + kPassCols - 1) / kPassCols < CT ? (a.N - c_first + kPassCols - 1) / kPassCols : CT;
+  const int32_t* order = l.order + run.first;
+  const float* w = a.w + (int64_t)run.first * a.rp + j0;
+
+  for (int t = tid; t < run.count; t += kThreads) rows[t] = order[t];
+  if constexpr (CONTRACT) {
+    // a thread takes 8 ranks of a column; the loads first, then their way into LDS
+    constexpr int kEach = JB * 16 * CT * kPassCols / 8 / kThreads;
+    const W* b = (const W*)a.b + ((int64_t)run.key * a.N + c_first) * a.r + j0;
+    x8<W> x[kEach];
 #pragma unroll
-    for (int jb = 0; jb < JB; ++jb) {
-      const int j = j0 + jb * 16 + m;
-      const float wf = there && j < a.r ? a.w[(int64_t)place * a.rp + j] : 0.f;
+    for (int k = 0; k < kEach; ++k) {
+      const int i = tid + k * kThreads, j = i % (JB * 2) * 8, c = i / (JB * 2);
+      x[k] = c_first + c < a.N ? load_some<x8<W>, 8>(b + (int64_t)c * a.r + j, a.r - j0 - j) : x8<W>{};
+    }
 #pragma unroll
-      for (int nb = 0; nb < 4; ++nb)
-        acc[jb][nb] = FLAT ? mfma(sf[nb], wf, acc[jb][nb]) : mfma(wf, sf[nb], acc[jb][nb]);
+    for (int k = 0; k < kEach; ++k) {
+      const int i = tid + k * kThreads, j = i % (JB * 2) * 8, c = i / (JB * 2);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bt[(j + e) * P::kB + c] = x[k][e];
     }
   }
-  const bool only = run.slot < 0, add = only && a.accumulate;
-  float* out = only ? a.out + (int64_t)run.key * a.r * a.N : a.part + (int64_t)run.slot * a.r * a.N;
+  __syncthreads();  // rows
+
+  // the tile's loads: thread t takes column group t % kAcross of the rows t / kAcross + k * kDown
+  constexpr int kAcross = kPassCols / P::kV, kDown = kThreads / kAcross;
+  sv held[P::kLoads];
+  f32x4 held_w[JB];
+  const int lc = tid % kAcross * P::kV, lr = tid / kAcross;
+  auto load_tile = [&](int t0, int ct) {
+    const int c = c_first + ct * kPassCols + lc;
 #pragma unroll
-  for (int jb = 0; jb < JB; ++jb)
+    for (int k = 0; k < P::kLoads; ++k) {
+      const int t = t0 + lr + k * kDown;
+      held[k] = t < run.count ? load_some<sv, P::kV>((const S*)a.src + rows[t] * a.ld + c, a.N - c) : sv{};
+    }
+    if (ct == 0) {
+      const int t = t0 + lane;
 #pragma unroll
-    for (int nb = 0; nb < 4; ++nb)
+      for (int jb = 0; jb < JB; ++jb) {
+        const int j = jb * 16 + wave * 4;
+        held_w[jb] = a.w && t < run.count && j0 + j < a.rp ? *(const f32x4*)(w + (int64_t)t * a.rp + j) : f32x4{};
+      }
+    }
+  };
+  auto store_tile = [&](int ct) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = j0 + jb * 16 + (FLAT ? m : 4 * g + i), cc = FLAT ? c0 + 4 * (4 * g + i) + nb : c + nb;
-        if (j < a.r && cc < a.N) {
-          float* p = out + (FLAT ? (int64_t)j * a.N + cc : (int64_t)cc * a.r + j);
-          *p = add ? *p + acc[jb][nb][i] : acc[jb][nb][i];
+    for (int k = 0; k < P::kLoads; ++k) {
+      ev x;
+#pragma unroll
+      for (int e = 0; e < P::kV; ++e) x[e] = (E)held[k][e];
+      *(ev*)(tile + (lr + k * kDown) * P::kRow + lc) = x;
+    }
+    if (ct == 0) {
+#pragma unroll
+      for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = (jb * 16 + wave * 4 + e) * P::kW + lane;
+          const float x = held_w[jb][e];
+          if constexpr (P::FAST) {
+            const __bf16 hi = (__bf16)x;
+            const bool finite = __builtin_isfinite((float)hi);
+            const float r1 = finite ? x - (float)hi : 0.f;
+            const __bf16 mid = (__bf16)r1;
+            wt[at] = hi;
+            wt[JB * 16 * P::kW + at] = mid;
+            wt[2 * JB * 16 * P::kW + at] = (__bf16)(r1 - (float)mid);
+          } else {
+            wt[at] = x;
+          }
         }
+    }
+  };
+
+  f32x4 acc[CT][JB][4] = {};  // out
+  f32x4 sum[JB];              // part
+  load_tile(0, 0);
+  for (int t0 = 0; t0 < run.count; t0 += kPassRows) {
+#pragma unroll
+    for (int jb = 0; jb < JB; ++jb) sum[jb] = f32x4{};
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      if (ct >= tiles) break;
+      __syncthreads();
+      store_tile(ct);
+      __syncthreads();
+      if (ct + 1 < tiles)
+        load_tile(t0, ct + 1);
+      else if (t0 + kPassRows < run.count)
+        load_tile(t0 + kPassRows, 0);
+      if constexpr (P::FAST) {
+#pragma unroll
+        for (int ks = 0; ks < kPassRows / 32; ++ks) {
+          x4<E> x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            x[e] = *(const x4<E>*)(tile + (ks * 32 + g * 8 + e) * P::kRow + wave * 64 + 4 * m);
+          bf16x8 f[4];
+#pragma unroll
+          for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[nb][e] = x[e][nb];
+#pragma unroll
+          for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+              const bf16x8 wf = *(const bf16x8*)(wt + ((q * JB + jb) * 16 + m) * P::kW + ks * 32 + g * 8);
+#pragma unroll
+              for (int nb = 0; nb < 4; ++nb)
+                acc[ct][jb][nb] = CONTRACT ? mfma(wf, f[nb], acc[ct][jb][nb]) : mfma(f[nb], wf, acc[ct][jb][nb]);
+            }
+        }
+        if constexpr (CONTRACT) {
+#pragma unroll
+          for (int ks = 0; ks < kPassCols / 32; ++ks) {
+            const bf16x8 x = *(const bf16x8*)(tile + (wave * 16 + m) * P::kRow + ks * 32 + g * 8);
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+              sum[jb] = mfma(*(const bf16x8*)(bt + (jb * 16 + m) * P::kB + ct * kPassCols + ks * 32 + g * 8), x, sum[jb]);
+          }
+        }
+      } else {
+#pragma unroll 4
+        for (int q = 0; q < kPassRows / 4; ++q) {
+          const f32x4 x = *(const f32x4*)(tile + (q * 4 + g) * P::kRow + wave * 64 + 4 * m);
+#pragma unroll
+          for (int jb = 0; jb < JB; ++jb) {
+            const float wf = wt[(jb * 16 + m) * P::kW + q * 4 + g];
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb)
+              acc[ct][jb][nb] = CONTRACT ? mfma(wf, x[nb], acc[ct][jb][nb]) : mfma(x[nb], wf, acc[ct][jb][nb]);
+          }
+        }
+        if constexpr (CONTRACT) {
+#pragma unroll 4
+          for (int ks = 0; ks < kPassCols / 16; ++ks) {
+            const f32x4 x = *(const f32x4*)(tile + (wave * 16 + m) * P::kRow + ks * 16 + g * 4);
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb) {
+              const x4<W> bf = *(const x4<W>*)(bt + (jb * 16 + m) * P::kB + ct * kPassCols + ks * 16 + g * 4);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sum[jb] = mfma((float)bf[e], x[e], sum[jb]);
+            }
+          }
+        }
+      }
+    }
+    if constexpr (CONTRACT) {
+      const int t = t0 + wave * 16 + m;
+      float* p = a.part + ((int64_t)blockIdx.y * a.T + run.first + t) * a.rp + j0 + g * 4;
+#pragma unroll
+      for (int jb = 0; jb < JB; ++jb)
+        if (t < run.count && j0 + jb * 16 < a.rp) *(f32x4*)(p + jb * 16) = sum[jb];
+    }
+  }
+
+  if (!a.out) return;
+  const bool only = run.slot < 0, add = only && a.accumulate;
+  float* out = only ? a.out + (int64_t)run.key * a.r * a.N : a.out_part + (int64_t)run.slot * a.r * a.N;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        // four elements next to each other in memory: of the rank, or of the columns
+        const int c0 = c_first + ct * kPassCols + wave * 64;
+        const int j = j0 + jb * 16 + (CONTRACT ? 4 * g : m), c = c0 + (CONTRACT ? 4 * m + q : 16 * g + 4 * q);
+        if (j >= a.r || c >= a.N) continue;
+        const f32x4 y = CONTRACT ? acc[ct][jb][q]
+                                 : f32x4{acc[ct][jb][0][q], acc[ct][jb][1][q], acc[ct][jb][2][q], acc[ct][jb][3][q]};
+        float* p = out + (CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c);
+        const int left = CONTRACT ? a.r - j : a.N - c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < left) p[e] = add ? p[e] + y[e] : y[e];
       }
 }
 
 // Adapters of several runs of rows: the runs' sums in order.
-__global__ __launch_bounds__(kThreads) void join_outer(const float* part, float* out, int64_t size, int n, int accumulate,
-                                                       RunList l) {
+__global__ __launch_bounds__(kThreads) void join_outer(const float* part, float* out, int64_t size, int n, int C,
+                                                       int accumulate, RunList l) {
   if ((int)blockIdx.x >= *l.n_joins) return;
   const Join j = l.joins[blockIdx.x];
   if (j.key >= n) return;
   for (int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x; i < size; i += (int64_t)gridDim.y * kThreads) {
     float s = 0.f;
-    for (int p = j.first; p < j.end; p += kGradRows)
-      s += part[run_slot(p, kGradRows, p + kGradRows >= j.end) * size + i];
+    constexpr int kAhead = 8;  // loads in flight, added in order
+    for (int p = j.first; p < j.end; p += kAhead * C) {
+      float x[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int q = p + k * C;
+        x[k] = q < j.end ? part[run_slot(q, C, q + C >= j.end) * size + i] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (p + k * C < j.end) s += x[k];
+    }
     float* q = out + j.key * size + i;
     *q = accumulate ? *q + s : s;
   }
@@ -423,17 +564,6 @@ hipError_t run_shrink(const ShrinkArgs& a, const RunList& l, int chunks, hipStre
     TIM_LAUNCH((shrink<T, 4><<<dim3(runs, chunks, (a.rp + 63) / 64), kThreads, 0, s>>>(a, l)));
   return hipSuccess;
 }
-template <class T, class G>
-hipError_t run_contract(const ContractArgs& a, const RunList& l, int chunks, hipStream_t s) {
-  const unsigned runs = (unsigned)l.max_runs;
-  if (a.rp <= 16)
-    TIM_LAUNCH((contract<T, G, 1><<<dim3(runs, chunks), kThreads, 0, s>>>(a, l)));
-  else if (a.rp <= 32)
-    TIM_LAUNCH((contract<T, G, 2><<<dim3(runs, chunks), kThreads, 0, s>>>(a, l)));
-  else
-    TIM_LAUNCH((contract<T, G, 4><<<dim3(runs, chunks, (a.rp + 63) / 64), kThreads, 0, s>>>(a, l)));
-  return hipSuccess;
-}
 template <class T, class O, bool FLAT>
 hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
   const dim3 grid((unsigned)l.max_runs, (unsigned)((a.N + kWaves * 64 - 1) / (kWaves * 64)));
@@ -455,25 +585,32 @@ hipError_t run_expand(const ExpandArgs& a, int dtype, const RunList& l, hipStrea
     default: return run_expand<T, _Float16, FLAT>(a, l, s);
   }
 }
-template <class S, bool FLAT>
-hipError_t run_outer(const OuterArgs& a, const RunList& l, hipStream_t s) {
-  const unsigned runs = (unsigned)l.max_runs, tiles = (unsigned)((a.N + kWaves * 64 - 1) / (kWaves * 64));
-  if (a.rp <= 16)
-    TIM_LAUNCH((outer<S, FLAT, 1><<<dim3(runs, tiles), kThreads, 0, s>>>(a, l)));
-  else if (a.rp <= 32)
-    TIM_LAUNCH((outer<S, FLAT, 2><<<dim3(runs, tiles), kThreads, 0, s>>>(a, l)));
-  else
-    TIM_LAUNCH((outer<S, FLAT, 4><<<dim3(runs, tiles, (a.rp + 63) / 64), kThreads, 0, s>>>(a, l)));
+template <class S, class W, bool CONTRACT, int JB, int CT>
+hipError_t run_pass(const PassArgs& a, const RunList& l, hipStream_t s) {
+  const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, CT * kPassCols), (unsigned)((a.rp + 63) / 64));
+  TIM_LAUNCH((pass<S, W, CONTRACT, JB, CT><<<grid, kThreads, 0, s>>>(a, l)));
   return hipSuccess;
 }
-template <class S, bool FLAT>
-hipError_t weight_gradient(const OuterArgs& a, const RunList& l, int64_t T, const uint8_t* seen, hipStream_t s) {
+template <class S, class W, bool CONTRACT>
+hipError_t run_pass(const PassArgs& a, int tiles, const RunList& l, hipStream_t s) {
+  if (a.rp <= 16) {
+    if constexpr (CONTRACT)
+      if (tiles == 4) return run_pass<S, W, CONTRACT, 1, 4>(a, l, s);
+    return run_pass<S, W, CONTRACT, 1, 1>(a, l, s);
+  }
+  if (a.rp <= 32) {
+    if constexpr (CONTRACT)
+      if (tiles == 2) return run_pass<S, W, CONTRACT, 2, 2>(a, l, s);
+    return run_pass<S, W, CONTRACT, 2, 1>(a, l, s);
+  }
+  return run_pass<S, W, CONTRACT, 4, 1>(a, l, s);
+}
+// What follows a pass: the runs' sums joined, zeros for the adapters without rows.
+hipError_t finish_gradient(const PassArgs& a, int C, const RunList& l, const uint8_t* seen, hipStream_t s) {
   const int64_t size = (int64_t)a.r * a.N;
   const unsigned across = (unsigned)(size < 256 * 1024 ? (size + 255) / 256 : 1024);
-  hipError_t e = run_outer<S, FLAT>(a, l, s);
-  if (e != hipSuccess) return e;
-  if (T > kGradRows)
-    TIM_LAUNCH((join_outer<<<dim3((unsigned)l.max_joins, across), kThreads, 0, s>>>(a.part, a.out, size, a.n,
+  if (a.T > C)
+    TIM_LAUNCH((join_outer<<<dim3((unsigned)l.max_joins, across), kThreads, 0, s>>>(a.out_part, a.out, size, a.n, C,
                                                                                     a.accumulate, l)));
   if (!a.accumulate)
     TIM_LAUNCH((zero_adapters<<<dim3((unsigned)(a.n < 1024 ? a.n : 1024), across), kThreads, 0, s>>>(a.out, size, a.n,
@@ -497,7 +634,7 @@ hipError_t add_typed(const tim_adapters& ad, const void* x, int64_t x_ld, int64_
 template <class T, class G>
 hipError_t backward_typed(const tim_adapters& ad, const AdapterGradArgs& a, int gx_dtype, const AdapterPlan& p, char* ws,
                           hipStream_t s) {
-  const RunList l = run_list(p.g, ws, 0), rows = run_list(p.g, ws, 1);
+  const RunList l = run_list(p.g, ws, 0), la = run_list(p.g, ws, 1), lb = run_list(p.g, ws, 2);
   float *u = (float*)(ws + p.u), *v = (float*)(ws + p.v);
   const uint8_t* seen = (const uint8_t*)(ws + p.seen);
   hipError_t e;
@@ -507,32 +644,32 @@ hipError_t backward_typed(const tim_adapters& ad, const AdapterGradArgs& a, int 
     if (e != hipSuccess) return e;
     TIM_LAUNCH((sum_chunks<<<(unsigned)l.max_runs, kThreads, 0, s>>>(sa.part, a.T, p.rp, p.x_chunks, ad.n, ad.scales, u,
                                                                      l)));
+  } else {
+    u = nullptr;
   }
-  if (a.grad_x || a.grad_a) {
-    const ContractArgs ca = {a.grad, a.grad_ld, a.T, ad.b, ad.n, ad.r, p.rp, ad.N, (float*)(ws + p.v_part)};
-    e = run_contract<T, G>(ca, l, p.g_chunks, s);
+  const PassArgs pb = {a.grad, a.grad_ld, a.T,      u,    ad.b, (float*)(ws + p.v_part),   ad.n,
+                       ad.r,   p.rp,      ad.N,     a.grad_b, (float*)(ws + p.b_part), a.accumulate_ab};
+  e = run_pass<G, T, true>(pb, p.tiles, lb, s);
+  if (e != hipSuccess) return e;
+  if (a.grad_b) {
+    e = finish_gradient(pb, p.g.C[2], lb, seen, s);
     if (e != hipSuccess) return e;
-    TIM_LAUNCH((sum_chunks<<<(unsigned)l.max_runs, kThreads, 0, s>>>(ca.part, a.T, p.rp, p.g_chunks, ad.n, ad.scales, v,
-                                                                     l)));
   }
+  if (!a.grad_x && !a.grad_a) return hipSuccess;
+  TIM_LAUNCH((sum_chunks<<<(unsigned)l.max_runs, kThreads, 0, s>>>(pb.part, a.T, p.rp, p.g_chunks, ad.n, ad.scales, v,
+                                                                   l)));
   if (a.grad_x) {
     const ExpandArgs ea = {v, a.T, 1, ad.n, ad.r, p.rp, ad.d, nullptr, ad.a, a.accumulate_x ? a.grad_x : nullptr,
                            a.gx_ld, a.grad_x, a.gx_ld};
     e = run_expand<T, true>(ea, gx_dtype, l, s);
     if (e != hipSuccess) return e;
   }
-  if (a.grad_a) {
-    const OuterArgs oa = {a.x, a.x_ld, v, ad.n, ad.r, p.rp, ad.d, a.grad_a, (float*)(ws + p.a_part), a.accumulate_ab};
-    e = weight_gradient<T, true>(oa, rows, a.T, seen, s);
-    if (e != hipSuccess) return e;
-  }
-  if (a.grad_b) {
-    const OuterArgs oa = {a.grad, a.grad_ld, u, ad.n, ad.r, p.rp, ad.N, a.grad_b, (float*)(ws + p.b_part),
-                          a.accumulate_ab};
-    e = weight_gradient<G, false>(oa, rows, a.T, seen, s);
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  if (!a.grad_a) return hipSuccess;
+  const PassArgs pa = {a.x,  a.x_ld, a.T,  v,        nullptr,                    nullptr,        ad.n,
+                       ad.r, p.rp,   ad.d, a.grad_a, (float*)(ws + p.a_part), a.accumulate_ab};
+  e = run_pass<T, T, false>(pa, 1, la, s);
+  if (e != hipSuccess) return e;
+  return finish_gradient(pa, p.g.C[1], la, seen, s);
 }
 template <class T>
 hipError_t backward_grad(const tim_adapters& ad, const AdapterGradArgs& a, int grad_dtype, int gx_dtype,

@@ -33,7 +33,7 @@ __host__ __device__ inline int32_t run_slot(int32_t first, int C, bool last) { r
 inline int64_t run_slots(int64_t T, int C) { return (T + C - 1) / C * 2; }
 
 constexpr int kGroupSmall = 4096;  // rows that one workgroup sorts in LDS
-constexpr int kMaxRunLists = 2;
+constexpr int kMaxRunLists = 3;
 
 // Sizes and workspace of a grouping of T rows by keys in [0, n); keys outside
 // are those of key n, whose runs are listed only with keep_rest.

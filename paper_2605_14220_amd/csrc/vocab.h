@@ -88,28 +88,38 @@ hipError_t launch_embedding_backward(const EmbedGradArgs& a, int dtype, void* ws
 // ------------------------------------------------------------------ adapters
 
 constexpr int kAdapterRun = 64;     // rows of one adapter that a workgroup takes together
-constexpr int kShrinkChunk = 1024;  // elements of d (of N in the backward: kGradChunk) whose products one workgroup sums
-constexpr int kGradChunk = 1024;
-constexpr int kGradRows = 512;      // rows of one adapter whose outer products one workgroup sums
+constexpr int kShrinkChunk = 1024;  // elements of d whose products one workgroup sums
 
 inline int rank_padded(int r) { return (r + 15) / 16 * 16; }
 inline int chunks_of(int64_t n, int chunk) { return (int)((n + chunk - 1) / chunk); }
 
+// Tiles of 256 columns that a workgroup of the pass over grad takes, by N and
+// the rank alone (the sums of grad b are over that many columns).
+inline int pass_tiles(int64_t N, int rp) { return N < 32768 || rp > 32 ? 1 : rp > 16 ? 2 : 4; }
+// Rows of one adapter that it takes.
+constexpr int kMaxPassRows = 512;
+inline int pass_rows(int64_t T, int64_t column_groups) {
+  int rows = kMaxPassRows;
+  while (rows > 128 && (T + rows - 1) / rows * column_groups < 512) rows /= 2;
+  return rows;
+}
+
 // Workspaces: the grouping, then fp32 [chunks, T, rank_padded] of partial sums
 // of x a^T, and for the backward those of grad b, both sums, and the partial
-// weight gradients of adapters with several runs of kGradRows rows.
+// weight gradients of adapters with several runs of rows.
 struct AdapterPlan {
-  Grouping g;
-  int rp, x_chunks, g_chunks;
+  Grouping g;  // runs of kAdapterRun rows; the backward's for grad_a and for grad_b
+  int rp, x_chunks, tiles, g_chunks;
   size_t u_part, v_part, u, v, a_part, b_part, seen, bytes;
 };
 inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r, bool backward) {
-  const int C[2] = {kAdapterRun, kGradRows};
   AdapterPlan p = {};
-  p.g = plan_grouping(T, n, backward ? 2 : 1, C);
   p.rp = rank_padded(r);
   p.x_chunks = chunks_of(d, kShrinkChunk);
-  p.g_chunks = chunks_of(N, kGradChunk);
+  p.tiles = pass_tiles(N, p.rp);
+  p.g_chunks = chunks_of(N, p.tiles * 256);
+  const int C[3] = {kAdapterRun, pass_rows(T, chunks_of(d, 256)), pass_rows(T, p.g_chunks)};
+  p.g = plan_grouping(T, n, backward ? 3 : 1, C);
   size_t at = p.g.bytes;
   const size_t rows = group_align((size_t)T * p.rp * 4);
   p.u_part = at, at += rows * p.x_chunks;
@@ -117,9 +127,8 @@ inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int
     p.v_part = at, at += rows * p.g_chunks;
     p.u = at, at += rows;
     p.v = at, at += rows;
-    const size_t slots = T > kGradRows ? (size_t)run_slots(T, kGradRows) * r * 4 : 0;
-    p.a_part = at, at += group_align(slots * d);
-    p.b_part = at, at += group_align(slots * N);
+    p.a_part = at, at += T > C[1] ? group_align((size_t)run_slots(T, C[1]) * r * d * 4) : 0;
+    p.b_part = at, at += T > C[2] ? group_align((size_t)run_slots(T, C[2]) * r * N * 4) : 0;
     p.seen = at, at += group_align((size_t)n);
   }
   p.bytes = at;

@@ -61,7 +61,8 @@ SIZES = [(1, 1, 1, 1, 1, "one", 0), (1, 2048, 1000, 4, 16, "one", 0), (2, 33, 7,
          (130, 257, 1031, 2, 64, "runs", 0), (200, 96, 64, 5, 65, "mixed", 2), (37, 72, 130, 2, 100, "mixed", 0),
          (70, 40, 90, 2, 256, "mixed", 0), (333, 500, 130, 3, 8, "runs", 0), (700, 64, 70, 2, 5, "mixed", 0),
          (1500, 40, 66, 1, 12, "one", 0), (5000, 24, 33, 7, 3, "mixed", 0), (100, 48, 40, 3, 4, "none", 0),
-         (4097, 20, 16, 1000, 2, "mixed", 0), (40, 3000, 20, 2, 1, "mixed", 0)]
+         (4097, 20, 16, 1000, 2, "mixed", 0), (40, 3001, 20, 2, 1, "mixed", 0),
+         (70, 24, 33001, 2, 16, "mixed", 1), (150, 24, 32768, 2, 20, "runs", 0)]
 
 
 def _whole(T, d, N, n, r, kind, dtype, seed):
