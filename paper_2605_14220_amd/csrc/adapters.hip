@@ -65,19 +65,27 @@ __device__ __forceinline__ V load_some(const T* p, int n) {
   }
   return r;
 }
+// The same where all N elements are known to lie in the array: without the
+// branches, so that many loads are in flight at once. WHOLE picks one by a
+// condition that is the same in every lane.
+template <bool WHOLE, class V, int N, class T>
+__device__ __forceinline__ V load_n(const T* p, int n) {
+  if constexpr (WHOLE) {
+    V r;
+    __builtin_memcpy(&r, p, N * sizeof(T));
+    return r;
+  } else {
+    return load_some<V, N>(p, n);
+  }
+}
 template <class T>
 using x4 = T __attribute__((ext_vector_type(4)));
-template <class T>
-__device__ __forceinline__ f32x4 load4(const T* p, int n) {
-  const x4<T> r = load_some<x4<T>, 4>(p, n);
-  return f32x4{(float)r[0], (float)r[1], (float)r[2], (float)r[3]};
-}
-
 // A wave's results of JB blocks of 16 ranks for RB blocks of 16 rows, summed
-// over the workgroup's waves in wave order and stored as part[place][rank].
+// over the workgroup's waves in wave order and stored as part[place][rank], zeros
+// for the ranks from r on.
 template <int JB>
-__device__ __forceinline__ void store_sums(f32x4 (&acc)[JB][4], f32x4 (*lds)[JB][4][64], float* part, int rp, int j0,
-                                           int count, int lane, int wave) {
+__device__ __forceinline__ void store_sums(f32x4 (&acc)[JB][4], f32x4 (*lds)[JB][4][64], float* part, int r, int rp,
+                                           int j0, int count, int lane, int wave) {
   if (wave > 0) {
 #pragma unroll
     for (int jb = 0; jb < JB; ++jb)
@@ -94,6 +102,9 @@ __device__ __forceinline__ void store_sums(f32x4 (&acc)[JB][4], f32x4 (*lds)[JB]
 #pragma unroll
       for (int w = 0; w < kWaves - 1; ++w) s += lds[w][jb][rb][lane];
       const int t = rb * 16 + lane % 16, j = j0 + jb * 16 + lane / 16 * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e >= r) s[e] = 0.f;
       if (t < count && j < rp) *(f32x4*)(part + (int64_t)t * rp + j) = s;
     }
 }
@@ -123,42 +134,62 @@ __global__ __launch_bounds__(kThreads) void shrink(ShrinkArgs a, RunList l) {
     const int t = rb * 16 + m;
     xr[rb] = (const T*)a.x + l.order[run.first + (t < run.count ? t : run.count - 1)] * a.x_ld;
   }
-  f32x4 acc[JB][4] = {};
-  const int from = blockIdx.y * kShrinkChunk + wave * (kShrinkChunk / kWaves);
-  const int to = from + kShrinkChunk / kWaves < a.d ? from + kShrinkChunk / kWaves : a.d;
-  for (int k0 = from; k0 < to; k0 += 32) {
-    const int k = k0 + g * 8, n = a.d - k;
-    x8<T> wf[JB];
+  const T* wr[JB];
 #pragma unroll
-    for (int jb = 0; jb < JB; ++jb) {
-      const int j = j0 + jb * 16 + m;
-      wf[jb] = j < a.r ? load_some<x8<T>, 8>(w + (int64_t)j * a.d + k, n) : x8<T>{};
-    }
+  for (int jb = 0; jb < JB; ++jb) {
+    const int j = j0 + jb * 16 + m;
+    wr[jb] = w + (int64_t)(j < a.r ? j : a.r - 1) * a.d;
+  }
+  f32x4 acc[JB][4] = {};
+  constexpr int kEach = kShrinkChunk / kWaves;
+  const int from = blockIdx.y * kShrinkChunk + wave * kEach;
+  auto step = [&](auto whole, int k0) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    const int k = k0 + g * 8, n = a.d - k;
+    x8<T> wf[JB], xf[4];
+#pragma unroll
+    for (int jb = 0; jb < JB; ++jb) wf[jb] = load_n<WHOLE, x8<T>, 8>(wr[jb] + k, n);
 #pragma unroll
     for (int rb = 0; rb < 4; ++rb)
-      if (rb < blocks) {
-        const x8<T> xf = load_some<x8<T>, 8>(xr[rb] + k, n);
+      if (rb < blocks) xf[rb] = load_n<WHOLE, x8<T>, 8>(xr[rb] + k, n);
 #pragma unroll
-        for (int jb = 0; jb < JB; ++jb) acc[jb][rb] = mfma(wf[jb], xf, acc[jb][rb]);
-      }
+    for (int rb = 0; rb < 4; ++rb)
+      if (rb < blocks)
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) acc[jb][rb] = mfma(wf[jb], xf[rb], acc[jb][rb]);
+  };
+  if (from + kEach <= a.d) {
+#pragma unroll 4
+    for (int k0 = 0; k0 < kEach; k0 += 32) step(std::true_type{}, from + k0);
+  } else {
+    for (int k0 = from; k0 < a.d && k0 < from + kEach; k0 += 32) step(std::false_type{}, k0);
   }
-  store_sums<JB>(acc, lds, a.part + ((int64_t)blockIdx.y * a.T + run.first) * a.rp, a.rp, j0, run.count, lane, wave);
+  store_sums<JB>(acc, lds, a.part + ((int64_t)blockIdx.y * a.T + run.first) * a.rp, a.r, a.rp, j0, run.count, lane, wave);
 }
 
-// out[place][j] = scale of the place's adapter * the sum of its chunks in order.
+// out[place][j] = scale of the place's adapter * the sum of its chunks: 64
+// consecutive elements a workgroup, a sixteenth of the chunks a group of 16
+// lanes, each in order, then the groups in order.
 __global__ __launch_bounds__(kThreads) void sum_chunks(const float* part, int64_t T, int rp, int chunks, int n,
                                                        const float* scales, float* out, RunList l) {
+  __shared__ f32x4 lds[16][16];
   if ((int)blockIdx.x >= *l.n_runs) return;
   const Run run = l.runs[blockIdx.x];
-  if (run.key >= n) return;
-  const float scale = scales ? scales[run.key] : 1.f;
-  const int64_t at = (int64_t)run.first * rp;
-  for (int i = threadIdx.x; i < run.count * rp; i += kThreads) {
-    float s = 0.f;
+  const int i = (blockIdx.y * 16 + threadIdx.x % 16) * 4, group = threadIdx.x / 16;
+  if (run.key >= n || (int)blockIdx.y * 64 >= run.count * rp) return;
+  const int per = (chunks + 15) / 16, from = group * per, to = from + per < chunks ? from + per : chunks;
+  const float* p = part + (int64_t)run.first * rp + i;
+  f32x4 s = {};
+  if (i < run.count * rp) {
 #pragma unroll 8
-    for (int c = 0; c < chunks; ++c) s += part[(int64_t)c * T * rp + at + i];
-    out[at + i] = scale * s;
+    for (int c = from; c < to; ++c) s += *(const f32x4*)(p + (int64_t)c * T * rp);
   }
+  lds[group][threadIdx.x % 16] = s;
+  __syncthreads();
+  if (group > 0 || i >= run.count * rp) return;
+#pragma unroll
+  for (int k = 1; k < 16; ++k) s += lds[k][threadIdx.x];
+  *(f32x4*)(out + (int64_t)run.first * rp + i) = s * (scales ? scales[run.key] : 1.f);
 }
 
 struct ExpandArgs {
@@ -173,111 +204,159 @@ struct ExpandArgs {
   int64_t out_ld;
 };
 
-// out[row][c] = base[row][c] + sum_j u[place][j] w[c][j] for 256 columns of a
-// run. The matrix instructions' results pass through LDS, so that rows are read
-// and written 256 bytes at a time.
-template <class T, class O, bool FLAT, int JB>
+// out[row][c] = base[row][c] + sum_j u[place][j] w[c][j] for NT * 256 columns of
+// a run, 64 columns a wave and tile. The weights of all tiles are requested
+// first; base is requested one block of 16 rows ahead. The matrix instructions'
+// results pass through LDS, so that rows are read and written 256 bytes at a time.
+template <class T, class O, bool FLAT, int JB, int NT>
 __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
   constexpr int kU = JB * 16 + 4;    // a row of u, apart in the banks
   constexpr int kTile = 64 + 4;      // a row of a wave's 16 x 64 results
   constexpr bool kHold = JB <= 4;    // the columns' weights stay in registers for all rows
   __shared__ float u[64 * kU];
   __shared__ float tile[kWaves][16 * kTile];
+  __shared__ int32_t rows[64];
   if ((int)blockIdx.x >= *l.n_runs) return;
   const Run run = l.runs[blockIdx.x];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
-  const int c0 = (blockIdx.y * kWaves + wave) * 64;
+  const int c_first = blockIdx.y * NT * kWaves * 64;
   const int32_t* order = l.order + run.first;
   if (run.key >= a.n) {  // no adapter
     for (int t = wave; t < run.count; t += kWaves) {
       const int64_t row = order[t];
-      for (int c = (int)blockIdx.y * kWaves * 64 + lane; c < a.N && c < ((int)blockIdx.y + 1) * kWaves * 64; c += 64)
+      for (int c = c_first + lane; c < a.N && c < c_first + NT * kWaves * 64; c += 64)
         ((O*)a.out)[row * a.out_ld + c] = a.base ? ((const O*)a.base)[row * a.base_ld + c] : (O)0.f;
     }
     return;
   }
+  const T* w = (const T*)a.w + (int64_t)run.key * a.r * a.N;
+  // raw[nb][s]: the weight of rank jb * 16 + 4 g + s in column c0 + 16 nb + m; FLAT: raw[s][nb] in column c0 + 4 m + nb.
+  // Without FLAT the four ranks may reach into the next columns' weights (up to 15 columns on): zeros take their place.
+  auto weights = [&](auto whole, int c0, int jb, x4<T>(&raw)[4]) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    const int j = jb * 16 + g * 4;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (FLAT) {
+        const int c = c0 + 4 * m;
+        raw[q] = load_n<WHOLE, x4<T>, 4>(w + (int64_t)(j + q < a.r ? j + q : a.r - 1) * a.N + c, a.N - c);
+        if (a.r != a.rp && j + q >= a.r) raw[q] = x4<T>{};
+      } else {
+        const int c = c0 + q * 16 + m;
+        if (WHOLE || c < a.N)
+          raw[q] = load_n<WHOLE, x4<T>, 4>(w + (int64_t)c * a.r + j, a.r - j);
+        else
+          raw[q] = x4<T>{};
+        if (a.r != a.rp)
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+            if (j + s >= a.r) raw[q][s] = (T)0.f;
+      }
+    }
+  };
+  const bool whole = c_first + NT * kWaves * 64 + (FLAT ? 0 : 16) <= a.N;  // of all the workgroup's columns
+  x4<T> held[kHold ? NT : 1][kHold ? JB : 1][4];
+  auto hold = [&](auto whole) {
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+      for (int jb = 0; jb < JB; ++jb) weights(whole, c_first + (ct * kWaves + wave) * 64, jb, held[ct][jb]);
+  };
+  if constexpr (kHold) {
+    if (whole)
+      hold(std::true_type{});
+    else
+      hold(std::false_type{});
+  }
+  if (threadIdx.x < 64) rows[threadIdx.x] = order[(int)threadIdx.x < run.count ? threadIdx.x : run.count - 1];
   const float scale = a.scales ? a.scales[run.key] : 1.f;
   for (int i = threadIdx.x; i < 64 * a.rp / 4; i += kThreads) {
     const int t = i / (a.rp / 4), j = i % (a.rp / 4) * 4;
     f32x4 s = {};
     if (t < run.count) {
-      for (int c = 0; c < a.chunks; ++c) s += *(const f32x4*)(a.u + ((int64_t)c * a.T + run.first + t) * a.rp + j);
+      const float* p = a.u + ((int64_t)run.first + t) * a.rp + j;
+#pragma unroll 4
+      for (int c = 0; c < a.chunks; ++c) s += *(const f32x4*)(p + (int64_t)c * a.T * a.rp);
       s *= scale;
     }
     *(f32x4*)(u + t * kU + j) = s;
   }
   __syncthreads();
-  if (c0 >= a.N) return;
-  const T* w = (const T*)a.w + (int64_t)run.key * a.r * a.N;
-  // wf[nb][s]: the weight of rank jb * 16 + 4 g + s in column c0 + 16 nb + m, or (FLAT) c0 + 4 m + nb
-  auto weights = [&](int jb, f32x4(&wf)[4]) {
-    const int j = jb * 16 + g * 4;
-    if constexpr (FLAT) {
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const f32x4 x = j + s < a.r ? load4(w + (int64_t)(j + s) * a.N + c0 + 4 * m, a.N - c0 - 4 * m) : f32x4{};
-#pragma unroll
-        for (int nb = 0; nb < 4; ++nb) wf[nb][s] = x[nb];
-      }
-    } else {
-#pragma unroll
-      for (int nb = 0; nb < 4; ++nb) {
-        const int c = c0 + nb * 16 + m;
-        wf[nb] = c < a.N ? load4(w + (int64_t)c * a.r + j, a.r - j) : f32x4{};
-      }
-    }
-  };
-  f32x4 held[kHold ? JB : 1][4];
-  if constexpr (kHold)
-#pragma unroll
-    for (int jb = 0; jb < JB; ++jb) weights(jb, held[jb]);
   float* const my = tile[wave];
   const int blocks = (run.count + 15) / 16;
-  for (int rb = 0; rb < blocks; ++rb) {
-    f32x4 acc[4] = {};
+  // what lane (m, g) reads and writes of a block: row 4 q + g, columns 4 m .. 4 m + 3
+  x4<O> old[4];
+  auto load_base = [&](int c0, int rb) {
+    const int c = c0 + 4 * m;
+    if (whole) {
 #pragma unroll
-    for (int jb = 0; jb < JB; ++jb) {
-      if (jb * 16 >= a.rp) break;
-      if constexpr (!kHold) weights(jb, held[0]);
-      const f32x4 uf = *(const f32x4*)(u + (rb * 16 + m) * kU + jb * 16 + g * 4);
+      for (int q = 0; q < 4; ++q)
+        old[q] = load_n<true, x4<O>, 4>((const O*)a.base + rows[rb * 16 + q * 4 + g] * a.base_ld + c, 4);
+    } else {
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(held[kHold ? jb : 0][nb][s], uf[s], acc[nb]);
+      for (int q = 0; q < 4; ++q)
+        old[q] = load_some<x4<O>, 4>((const O*)a.base + rows[rb * 16 + q * 4 + g] * a.base_ld + c, a.N - c);
     }
-    // lane: row m of the block, columns of the instruction's rows 4 g + i
+  };
+  if (a.base) load_base(c_first + wave * 64, 0);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if constexpr (FLAT)
-        *(f32x4*)(my + m * kTile + 16 * g + 4 * q) = f32x4{acc[0][q], acc[1][q], acc[2][q], acc[3][q]};
-      else
-        *(f32x4*)(my + m * kTile + 16 * q + 4 * g) = acc[q];
-    }
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");
+  for (int ct = 0; ct < NT; ++ct) {
+    const int c0 = c_first + (ct * kWaves + wave) * 64;
+    if (c0 >= a.N) break;
+    for (int rb = 0; rb < blocks; ++rb) {
+      f32x4 acc[4] = {};
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int t = rb * 16 + q * 4 + g, c = c0 + 4 * m, n = a.N - c;
-      if (t >= run.count || n <= 0) continue;
-      const int64_t row = order[t];
-      f32x4 y = *(const f32x4*)(my + (q * 4 + g) * kTile + 4 * m);
-      if (a.base) y += load4((const O*)a.base + row * a.base_ld + c, n);
-      O* dst = (O*)a.out + row * a.out_ld + c;
-      if (n >= 4) {
-        O z[4];
+      for (int jb = 0; jb < JB; ++jb) {
+        if (jb * 16 >= a.rp) break;
+        if constexpr (!kHold) weights(std::false_type{}, c0, jb, held[0][0]);
+        const f32x4 uf = *(const f32x4*)(u + (rb * 16 + m) * kU + jb * 16 + g * 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = narrow<O>(y[e]);
-        __builtin_memcpy(dst, z, sizeof(z));
-      } else {
+        for (int s = 0; s < 4; ++s)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < n) dst[e] = narrow<O>(y[e]);
+          for (int nb = 0; nb < 4; ++nb) {
+            const x4<T>(&h)[4] = held[kHold ? ct : 0][kHold ? jb : 0];
+            acc[nb] = mfma((float)(FLAT ? h[s][nb] : h[nb][s]), uf[s], acc[nb]);
+          }
+      }
+      // lane: row m of the block, columns of the instruction's rows 4 g + i
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if constexpr (FLAT)
+          *(f32x4*)(my + m * kTile + 16 * g + 4 * q) = f32x4{acc[0][q], acc[1][q], acc[2][q], acc[3][q]};
+        else
+          *(f32x4*)(my + m * kTile + 16 * q + 4 * g) = acc[q];
+      }
+      lanes_in_order();
+      f32x4 y[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        y[q] = *(const f32x4*)(my + (q * 4 + g) * kTile + 4 * m);
+        if (a.base) y[q] += f32x4{(float)old[q][0], (float)old[q][1], (float)old[q][2], (float)old[q][3]};
+      }
+      lanes_in_order();
+      if (a.base) {
+        if (rb + 1 < blocks)
+          load_base(c0, rb + 1);
+        else if (ct + 1 < NT)
+          load_base(c0 + kWaves * 64, 0);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int t = rb * 16 + q * 4 + g, c = c0 + 4 * m, n = a.N - c;
+        if (t >= run.count || n <= 0) continue;
+        O* dst = (O*)a.out + rows[t] * a.out_ld + c;
+        x4<O> z;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = narrow<O>(y[q][e]);
+        if (n >= 4) {
+          __builtin_memcpy(dst, &z, sizeof(z));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < n) dst[e] = z[e];
+        }
       }
     }
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");
   }
 }
 
@@ -337,7 +416,9 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   const int32_t* order = l.order + run.first;
   const float* w = a.w + (int64_t)run.first * a.rp + j0;
 
-  for (int t = tid; t < run.count; t += kThreads) rows[t] = order[t];
+  // rows past the run's end, up to a whole tile, are read as its last one
+  for (int t = tid; t < (run.count + kPassRows - 1) / kPassRows * kPassRows; t += kThreads)
+    rows[t] = order[t < run.count ? t : run.count - 1];
   if constexpr (CONTRACT) {
     // a thread takes 8 ranks of a column; the loads first, then their way into LDS
     constexpr int kEach = JB * 16 * CT * kPassCols / 8 / kThreads;
@@ -364,10 +445,14 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   const int lc = tid % kAcross * P::kV, lr = tid / kAcross;
   auto load_tile = [&](int t0, int ct) {
     const int c = c_first + ct * kPassCols + lc;
+    const S* src = (const S*)a.src + c;
+    if (c_first + (ct + 1) * kPassCols <= a.N) {
 #pragma unroll
-    for (int k = 0; k < P::kLoads; ++k) {
-      const int t = t0 + lr + k * kDown;
-      held[k] = t < run.count ? load_some<sv, P::kV>((const S*)a.src + rows[t] * a.ld + c, a.N - c) : sv{};
+      for (int k = 0; k < P::kLoads; ++k) held[k] = load_n<true, sv, P::kV>(src + rows[t0 + lr + k * kDown] * a.ld, 0);
+    } else {
+#pragma unroll
+      for (int k = 0; k < P::kLoads; ++k)
+        held[k] = load_some<sv, P::kV>(src + rows[t0 + lr + k * kDown] * a.ld, a.N - c);
     }
     if (ct == 0) {
       const int t = t0 + lane;
@@ -378,7 +463,12 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
       }
     }
   };
-  auto store_tile = [&](int ct) {
+  auto store_tile = [&](int t0, int ct) {
+    if (t0 + kPassRows > run.count) {  // rows past the run's end
+#pragma unroll
+      for (int k = 0; k < P::kLoads; ++k)
+        if (t0 + lr + k * kDown >= run.count) held[k] = sv{};
+    }
 #pragma unroll
     for (int k = 0; k < P::kLoads; ++k) {
       ev x;
@@ -418,7 +508,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
     for (int ct = 0; ct < CT; ++ct) {
       if (ct >= tiles) break;
       __syncthreads();
-      store_tile(ct);
+      store_tile(t0, ct);
       __syncthreads();
       if (ct + 1 < tiles)
         load_tile(t0, ct + 1);
@@ -513,36 +603,50 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
       }
 }
 
-// Adapters of several runs of rows: the runs' sums in order.
-__global__ __launch_bounds__(kThreads) void join_outer(const float* part, float* out, int64_t size, int n, int C,
-                                                       int accumulate, RunList l) {
-  if ((int)blockIdx.x >= *l.n_joins) return;
-  const Join j = l.joins[blockIdx.x];
-  if (j.key >= n) return;
-  for (int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x; i < size; i += (int64_t)gridDim.y * kThreads) {
+// What follows the passes: of adapters with several runs of rows the runs' sums
+// in order, and zeros for the adapters without rows. blockIdx.z: of grad_a, of grad_b.
+struct FinishArgs {
+  const float* part[2];
+  float* out[2];
+  int64_t size[2];  // r * d, r * N
+  int32_t C[2];
+  RunList l[2];
+  int32_t n, joins, accumulate;
+  const uint8_t* seen;
+};
+__global__ __launch_bounds__(kThreads) void finish(FinishArgs a) {
+  const int z = blockIdx.z;
+  const int64_t size = a.size[z], step = (int64_t)gridDim.y * kThreads;
+  float* out = a.out[z];
+  if (!out) return;
+  if ((int)blockIdx.x >= a.joins) {
+    for (int k = blockIdx.x - a.joins; k < a.n; k += gridDim.x - a.joins) {
+      if (a.seen[k]) continue;
+      for (int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x; i < size; i += step) out[k * size + i] = 0.f;
+    }
+    return;
+  }
+  if ((int)blockIdx.x >= *a.l[z].n_joins) return;
+  const Join j = a.l[z].joins[blockIdx.x];
+  if (j.key >= a.n) return;
+  const int C = a.C[z], runs = (j.end - j.first + C - 1) / C;
+  // the key's runs are two slots apart, the last one's is the odd one
+  const float* part = a.part[z] + (int64_t)run_slot(j.first, C, false) * size;
+  for (int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x; i < size; i += step) {
     float s = 0.f;
     constexpr int kAhead = 8;  // loads in flight, added in order
-    for (int p = j.first; p < j.end; p += kAhead * C) {
+    for (int k0 = 0; k0 < runs; k0 += kAhead) {
       float x[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const int q = p + k * C;
-        x[k] = q < j.end ? part[run_slot(q, C, q + C >= j.end) * size + i] : 0.f;
+        const int q = k0 + k < runs ? k0 + k : runs - 1;
+        x[k] = part[(int64_t)(2 * q + (q == runs - 1)) * size + i];
       }
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (p + k * C < j.end) s += x[k];
+      for (int k = 0; k < kAhead; ++k) s += k0 + k < runs ? x[k] : 0.f;
     }
     float* q = out + j.key * size + i;
-    *q = accumulate ? *q + s : s;
-  }
-}
-
-__global__ __launch_bounds__(kThreads) void zero_adapters(float* p, int64_t size, int n, const uint8_t* seen) {
-  for (int k = blockIdx.x; k < n; k += gridDim.x) {
-    if (seen[k]) continue;
-    for (int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x; i < size; i += (int64_t)gridDim.y * kThreads)
-      p[k * size + i] = 0.f;
+    *q = a.accumulate ? *q + s : s;
   }
 }
 
@@ -564,18 +668,19 @@ hipError_t run_shrink(const ShrinkArgs& a, const RunList& l, int chunks, hipStre
     TIM_LAUNCH((shrink<T, 4><<<dim3(runs, chunks, (a.rp + 63) / 64), kThreads, 0, s>>>(a, l)));
   return hipSuccess;
 }
+template <class T, class O, bool FLAT, int JB, int NT>
+hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
+  const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, NT * kWaves * 64));
+  TIM_LAUNCH((expand<T, O, FLAT, JB, NT><<<grid, kThreads, 0, s>>>(a, l)));
+  return hipSuccess;
+}
 template <class T, class O, bool FLAT>
 hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
-  const dim3 grid((unsigned)l.max_runs, (unsigned)((a.N + kWaves * 64 - 1) / (kWaves * 64)));
-  if (a.rp <= 16)
-    TIM_LAUNCH((expand<T, O, FLAT, 1><<<grid, kThreads, 0, s>>>(a, l)));
-  else if (a.rp <= 32)
-    TIM_LAUNCH((expand<T, O, FLAT, 2><<<grid, kThreads, 0, s>>>(a, l)));
-  else if (a.rp <= 64)
-    TIM_LAUNCH((expand<T, O, FLAT, 4><<<grid, kThreads, 0, s>>>(a, l)));
-  else
-    TIM_LAUNCH((expand<T, O, FLAT, 16><<<grid, kThreads, 0, s>>>(a, l)));
-  return hipSuccess;
+  const bool many = l.max_runs * chunks_of(a.N, 4 * kWaves * 64) >= 512;
+  if (a.rp <= 16) return many ? run_expand<T, O, FLAT, 1, 4>(a, l, s) : run_expand<T, O, FLAT, 1, 1>(a, l, s);
+  if (a.rp <= 32) return many ? run_expand<T, O, FLAT, 2, 2>(a, l, s) : run_expand<T, O, FLAT, 2, 1>(a, l, s);
+  if (a.rp <= 64) return run_expand<T, O, FLAT, 4, 1>(a, l, s);
+  return run_expand<T, O, FLAT, 16, 1>(a, l, s);
 }
 template <class T, bool FLAT>
 hipError_t run_expand(const ExpandArgs& a, int dtype, const RunList& l, hipStream_t s) {
@@ -605,19 +710,6 @@ hipError_t run_pass(const PassArgs& a, int tiles, const RunList& l, hipStream_t 
   }
   return run_pass<S, W, CONTRACT, 4, 1>(a, l, s);
 }
-// What follows a pass: the runs' sums joined, zeros for the adapters without rows.
-hipError_t finish_gradient(const PassArgs& a, int C, const RunList& l, const uint8_t* seen, hipStream_t s) {
-  const int64_t size = (int64_t)a.r * a.N;
-  const unsigned across = (unsigned)(size < 256 * 1024 ? (size + 255) / 256 : 1024);
-  if (a.T > C)
-    TIM_LAUNCH((join_outer<<<dim3((unsigned)l.max_joins, across), kThreads, 0, s>>>(a.out_part, a.out, size, a.n, C,
-                                                                                    a.accumulate, l)));
-  if (!a.accumulate)
-    TIM_LAUNCH((zero_adapters<<<dim3((unsigned)(a.n < 1024 ? a.n : 1024), across), kThreads, 0, s>>>(a.out, size, a.n,
-                                                                                                     seen)));
-  return hipSuccess;
-}
-
 template <class T>
 hipError_t add_typed(const tim_adapters& ad, const void* x, int64_t x_ld, int64_t n_rows, const void* base,
                      int64_t base_ld, void* out, int out_dtype, int64_t out_ld, const AdapterPlan& p, char* ws,
@@ -636,13 +728,12 @@ hipError_t backward_typed(const tim_adapters& ad, const AdapterGradArgs& a, int 
                           hipStream_t s) {
   const RunList l = run_list(p.g, ws, 0), la = run_list(p.g, ws, 1), lb = run_list(p.g, ws, 2);
   float *u = (float*)(ws + p.u), *v = (float*)(ws + p.v);
-  const uint8_t* seen = (const uint8_t*)(ws + p.seen);
   hipError_t e;
   if (a.grad_b) {
     const ShrinkArgs sa = {a.x, a.x_ld, a.T, ad.a, ad.n, ad.r, p.rp, ad.d, (float*)(ws + p.u_part)};
     e = run_shrink<T>(sa, l, p.x_chunks, s);
     if (e != hipSuccess) return e;
-    TIM_LAUNCH((sum_chunks<<<(unsigned)l.max_runs, kThreads, 0, s>>>(sa.part, a.T, p.rp, p.x_chunks, ad.n, ad.scales, u,
+    TIM_LAUNCH((sum_chunks<<<dim3((unsigned)l.max_runs, p.rp), kThreads, 0, s>>>(sa.part, a.T, p.rp, p.x_chunks, ad.n, ad.scales, u,
                                                                      l)));
   } else {
     u = nullptr;
@@ -651,25 +742,38 @@ hipError_t backward_typed(const tim_adapters& ad, const AdapterGradArgs& a, int 
                        ad.r,   p.rp,      ad.N,     a.grad_b, (float*)(ws + p.b_part), a.accumulate_ab};
   e = run_pass<G, T, true>(pb, p.tiles, lb, s);
   if (e != hipSuccess) return e;
-  if (a.grad_b) {
-    e = finish_gradient(pb, p.g.C[2], lb, seen, s);
-    if (e != hipSuccess) return e;
-  }
-  if (!a.grad_x && !a.grad_a) return hipSuccess;
-  TIM_LAUNCH((sum_chunks<<<(unsigned)l.max_runs, kThreads, 0, s>>>(pb.part, a.T, p.rp, p.g_chunks, ad.n, ad.scales, v,
-                                                                   l)));
+  if (a.grad_x || a.grad_a)
+    TIM_LAUNCH((sum_chunks<<<dim3((unsigned)l.max_runs, p.rp), kThreads, 0, s>>>(pb.part, a.T, p.rp, p.g_chunks, ad.n,
+                                                                                 ad.scales, v, l)));
   if (a.grad_x) {
     const ExpandArgs ea = {v, a.T, 1, ad.n, ad.r, p.rp, ad.d, nullptr, ad.a, a.accumulate_x ? a.grad_x : nullptr,
                            a.gx_ld, a.grad_x, a.gx_ld};
     e = run_expand<T, true>(ea, gx_dtype, l, s);
     if (e != hipSuccess) return e;
   }
-  if (!a.grad_a) return hipSuccess;
-  const PassArgs pa = {a.x,  a.x_ld, a.T,  v,        nullptr,                    nullptr,        ad.n,
-                       ad.r, p.rp,   ad.d, a.grad_a, (float*)(ws + p.a_part), a.accumulate_ab};
-  e = run_pass<T, T, false>(pa, 1, la, s);
-  if (e != hipSuccess) return e;
-  return finish_gradient(pa, p.g.C[1], la, seen, s);
+  float* a_part = (float*)(ws + p.a_part);
+  if (a.grad_a) {
+    const PassArgs pa = {a.x,  a.x_ld, a.T,  v,        nullptr, nullptr,        ad.n,
+                         ad.r, p.rp,   ad.d, a.grad_a, a_part,  a.accumulate_ab};
+    e = run_pass<T, T, false>(pa, 1, la, s);
+    if (e != hipSuccess) return e;
+  }
+  if (!a.grad_a && !a.grad_b) return hipSuccess;
+  FinishArgs f = {{a_part, pb.out_part},
+                  {a.grad_a, a.grad_b},
+                  {(int64_t)ad.r * ad.d, (int64_t)ad.r * ad.N},
+                  {p.g.C[1], p.g.C[2]},
+                  {la, lb},
+                  ad.n,
+                  0,
+                  a.accumulate_ab,
+                  (const uint8_t*)(ws + p.seen)};
+  f.joins = (int)(la.max_joins > lb.max_joins ? la.max_joins : lb.max_joins);
+  const int zeros = a.accumulate_ab ? 0 : ad.n < 1024 ? ad.n : 1024;
+  const int64_t most = f.size[0] > f.size[1] ? f.size[0] : f.size[1];
+  const unsigned across = (unsigned)(most < 512 * kThreads ? (most + kThreads - 1) / kThreads : 512);
+  if (f.joins + zeros > 0) TIM_LAUNCH((finish<<<dim3(f.joins + zeros, across, 2), kThreads, 0, s>>>(f)));
+  return hipSuccess;
 }
 template <class T>
 hipError_t backward_grad(const tim_adapters& ad, const AdapterGradArgs& a, int grad_dtype, int gx_dtype,

@@ -81,7 +81,7 @@ inline Grouping plan_grouping(int64_t T, int32_t n, int lists, const int* C) {
   for (int l = 0; l < lists; ++l) {
     g.C[l] = C[l];
     g.max_runs[l] = T / C[l] + distinct;
-    g.max_joins[l] = T / (C[l] + 1) + 1;
+    g.max_joins[l] = T / (C[l] + 1) < distinct ? T / (C[l] + 1) : distinct;
     g.runs[l] = at, at += group_align((size_t)g.max_runs[l] * sizeof(Run));
     g.joins[l] = at, at += group_align((size_t)g.max_joins[l] * sizeof(Join));
   }
@@ -103,6 +103,14 @@ inline RunList run_list(const Grouping& g, const void* ws, int l) {
   const int32_t* c = (const int32_t*)(w + g.counters);
   return {(const int32_t*)(w + g.order), (const Run*)(w + g.runs[l]), (const Join*)(w + g.joins[l]), c + 2 * l,
           c + 2 * l + 1, g.max_runs[l], g.max_joins[l]};
+}
+
+// Keeps the compiler from moving LDS accesses of a wave across it; the hardware
+// takes a wave's LDS accesses in order.
+__device__ __forceinline__ void lanes_in_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // seen (may be null): a byte per key in [0, n), set to 1 for the keys that

@@ -18,14 +18,6 @@ constexpr int kSmallWaves = kSmallThreads / 64;
 constexpr int kSortThreads = 256;
 constexpr int kSortWaves = kSortThreads / 64;
 
-// Keeps the compiler from moving LDS accesses of a wave across it; the hardware
-// takes a wave's LDS accesses in order.
-__device__ __forceinline__ void lanes_in_order() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_wave_barrier();
-  asm volatile("" ::: "memory");
-}
-
 // The lanes whose digit (of `bits` bits) is this lane's, among those of `active`.
 __device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, uint64_t active) {
   uint64_t peers = active;
