@@ -121,9 +121,8 @@ struct ShrinkArgs {
 template <class T, int JB>
 __global__ __launch_bounds__(kThreads) void shrink(ShrinkArgs a, RunList l) {
   __shared__ f32x4 lds[kWaves - 1][JB][4][64];
-  if ((int)blockIdx.x >= *l.n_runs) return;
-  const Run run = l.runs[blockIdx.x];
-  if (run.key >= a.n) return;
+  const Run run = own_run(l);
+  if (run.count == 0 || run.key >= a.n) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
   const int j0 = blockIdx.z * JB * 16;
   const T* w = (const T*)a.w + (int64_t)run.key * a.r * a.d;
@@ -167,22 +166,35 @@ __global__ __launch_bounds__(kThreads) void shrink(ShrinkArgs a, RunList l) {
   store_sums<JB>(acc, lds, a.part + ((int64_t)blockIdx.y * a.T + run.first) * a.rp, a.r, a.rp, j0, run.count, lane, wave);
 }
 
-// out[place][j] = scale of the place's adapter * the sum of its chunks: 64
-// consecutive elements a workgroup, a sixteenth of the chunks a group of 16
-// lanes, each in order, then the groups in order.
-__global__ __launch_bounds__(kThreads) void sum_chunks(const float* part, int64_t T, int rp, int chunks, int n,
+// out[place][j] = scale of the place's adapter * the sum of its chunks: in order
+// over `inner` chunks, then a sixteenth of these sums a group of 16 lanes, each
+// in order, then the groups in order. 64 consecutive elements a workgroup.
+__global__ __launch_bounds__(kThreads) void sum_chunks(const float* part, int64_t T, int rp, int chunks, int inner, int n,
                                                        const float* scales, float* out, RunList l) {
   __shared__ f32x4 lds[16][16];
-  if ((int)blockIdx.x >= *l.n_runs) return;
-  const Run run = l.runs[blockIdx.x];
+  const Run run = own_run(l);
+  if (run.count == 0) return;
   const int i = (blockIdx.y * 16 + threadIdx.x % 16) * 4, group = threadIdx.x / 16;
   if (run.key >= n || (int)blockIdx.y * 64 >= run.count * rp) return;
-  const int per = (chunks + 15) / 16, from = group * per, to = from + per < chunks ? from + per : chunks;
+  const int outer = (chunks + inner - 1) / inner, per = (outer + 15) / 16 * inner;
+  const int from = group * per, to = from + per < chunks ? from + per : chunks;
   const float* p = part + (int64_t)run.first * rp + i;
+  const int64_t step = T * rp;
   f32x4 s = {};
   if (i < run.count * rp) {
+    if (inner == 1) {
 #pragma unroll 8
-    for (int c = from; c < to; ++c) s += *(const f32x4*)(p + (int64_t)c * T * rp);
+      for (int c = from; c < to; ++c) s += *(const f32x4*)(p + c * step);
+    } else {
+#pragma unroll 2
+      for (int c = from; c < to; c += inner) {
+        f32x4 q = *(const f32x4*)(p + c * step);
+#pragma unroll
+        for (int k = 1; k < kChunkQuad; ++k)
+          if (k < inner && c + k < to) q += *(const f32x4*)(p + (c + k) * step);
+        s += q;
+      }
+    }
   }
   lds[group][threadIdx.x % 16] = s;
   __syncthreads();
@@ -204,118 +216,129 @@ struct ExpandArgs {
   int64_t out_ld;
 };
 
-// out[row][c] = base[row][c] + sum_j u[place][j] w[c][j] for NT * 256 columns of
-// a run, 64 columns a wave and tile. The weights of all tiles are requested
-// first; base is requested one block of 16 rows ahead. The matrix instructions'
-// results pass through LDS, so that rows are read and written 256 bytes at a time.
+// out[row][c] = base[row][c] + sum_j u[place][j] w[c][j] for the rows of a run and
+// NT tiles of 64 columns a wave. The waves work by themselves: u and the first
+// tile's weights and rows of base are requested together, later ones a step
+// (16 rows of a tile) ahead, before the step's stores. The matrix instructions'
+// results pass through LDS, so that rows are read and written 64 columns at a time.
 template <class T, class O, bool FLAT, int JB, int NT>
 __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
-  constexpr int kU = JB * 16 + 4;    // a row of u, apart in the banks
-  constexpr int kTile = 64 + 4;      // a row of a wave's 16 x 64 results
-  constexpr bool kHold = JB <= 4;    // the columns' weights stay in registers for all rows
-  __shared__ float u[64 * kU];
+  constexpr int kTile = 64 + 4;    // a row of the 16 x 64 results
+  constexpr bool kHold = JB <= 4;  // u and a tile's weights stay in registers for all rows
   __shared__ float tile[kWaves][16 * kTile];
-  __shared__ int32_t rows[64];
-  if ((int)blockIdx.x >= *l.n_runs) return;
-  const Run run = l.runs[blockIdx.x];
+  const Run run = own_run(l);
+  if (run.count == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
-  const int c_first = blockIdx.y * NT * kWaves * 64;
-  const int32_t* order = l.order + run.first;
+  const int c_first = (blockIdx.y * kWaves + wave) * NT * 64;
+  if (c_first >= a.N) return;
+  const int my_row = l.order[run.first + (lane < run.count ? lane : run.count - 1)];  // of the run's row `lane`
+  const O* base = (const O*)a.base;
   if (run.key >= a.n) {  // no adapter
-    for (int t = wave; t < run.count; t += kWaves) {
-      const int64_t row = order[t];
-      for (int c = c_first + lane; c < a.N && c < c_first + NT * kWaves * 64; c += 64)
-        ((O*)a.out)[row * a.out_ld + c] = a.base ? ((const O*)a.base)[row * a.base_ld + c] : (O)0.f;
+    for (int t = 0; t < run.count; ++t) {
+      const int64_t row = __shfl(my_row, t);
+      for (int c = c_first + lane; c < a.N && c < c_first + NT * 64; c += 64)
+        ((O*)a.out)[row * a.out_ld + c] = base ? base[row * a.base_ld + c] : (O)0.f;
     }
     return;
   }
+  const int blocks = (run.count + 15) / 16, tiles = (a.N - c_first + 63) / 64 < NT ? (a.N - c_first + 63) / 64 : NT;
   const T* w = (const T*)a.w + (int64_t)run.key * a.r * a.N;
   // raw[nb][s]: the weight of rank jb * 16 + 4 g + s in column c0 + 16 nb + m; FLAT: raw[s][nb] in column c0 + 4 m + nb.
   // Without FLAT the four ranks may reach into the next columns' weights (up to 15 columns on): zeros take their place.
-  auto weights = [&](auto whole, int c0, int jb, x4<T>(&raw)[4]) {
-    constexpr bool WHOLE = decltype(whole)::value;
+  auto weights = [&](int c0, int jb, x4<T>(&raw)[4]) {
     const int j = jb * 16 + g * 4;
+    if (c0 + 64 + (FLAT ? 0 : 16) <= a.N) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if constexpr (FLAT) {
-        const int c = c0 + 4 * m;
-        raw[q] = load_n<WHOLE, x4<T>, 4>(w + (int64_t)(j + q < a.r ? j + q : a.r - 1) * a.N + c, a.N - c);
-        if (a.r != a.rp && j + q >= a.r) raw[q] = x4<T>{};
-      } else {
-        const int c = c0 + q * 16 + m;
-        if (WHOLE || c < a.N)
-          raw[q] = load_n<WHOLE, x4<T>, 4>(w + (int64_t)c * a.r + j, a.r - j);
-        else
-          raw[q] = x4<T>{};
-        if (a.r != a.rp)
+      for (int q = 0; q < 4; ++q)
+        raw[q] = FLAT ? load_n<true, x4<T>, 4>(w + (int64_t)(j + q < a.r ? j + q : a.r - 1) * a.N + c0 + 4 * m, 4)
+                      : load_n<true, x4<T>, 4>(w + (int64_t)(c0 + q * 16 + m) * a.r + j, 4);
+      if (a.r != a.rp) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
           for (int s = 0; s < 4; ++s)
-            if (j + s >= a.r) raw[q][s] = (T)0.f;
+            if (j + (FLAT ? q : s) >= a.r) raw[q][s] = (T)0.f;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = FLAT ? c0 + 4 * m : c0 + q * 16 + m;
+        raw[q] = x4<T>{};
+        if (FLAT && j + q < a.r) raw[q] = load_some<x4<T>, 4>(w + (int64_t)(j + q) * a.N + c, a.N - c);
+        if (!FLAT && c < a.N) raw[q] = load_some<x4<T>, 4>(w + (int64_t)c * a.r + j, a.r - j);
       }
     }
   };
-  const bool whole = c_first + NT * kWaves * 64 + (FLAT ? 0 : 16) <= a.N;  // of all the workgroup's columns
-  x4<T> held[kHold ? NT : 1][kHold ? JB : 1][4];
-  auto hold = [&](auto whole) {
-#pragma unroll
-    for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-      for (int jb = 0; jb < JB; ++jb) weights(whole, c_first + (ct * kWaves + wave) * 64, jb, held[ct][jb]);
-  };
-  if constexpr (kHold) {
-    if (whole)
-      hold(std::true_type{});
-    else
-      hold(std::false_type{});
-  }
-  if (threadIdx.x < 64) rows[threadIdx.x] = order[(int)threadIdx.x < run.count ? threadIdx.x : run.count - 1];
   const float scale = a.scales ? a.scales[run.key] : 1.f;
-  for (int i = threadIdx.x; i < 64 * a.rp / 4; i += kThreads) {
-    const int t = i / (a.rp / 4), j = i % (a.rp / 4) * 4;
-    f32x4 s = {};
-    if (t < run.count) {
-      const float* p = a.u + ((int64_t)run.first + t) * a.rp + j;
+  // row m of a block, ranks jb * 16 + 4 g on
+  auto load_u = [&](int rb, int jb) {
+    const int t = rb * 16 + m < run.count ? rb * 16 + m : run.count - 1;
+    const float* p = a.u + ((int64_t)run.first + t) * a.rp + jb * 16 + g * 4;
+    f32x4 s = *(const f32x4*)p;
 #pragma unroll 4
-      for (int c = 0; c < a.chunks; ++c) s += *(const f32x4*)(p + (int64_t)c * a.T * a.rp);
-      s *= scale;
-    }
-    *(f32x4*)(u + t * kU + j) = s;
-  }
-  __syncthreads();
-  float* const my = tile[wave];
-  const int blocks = (run.count + 15) / 16;
-  // what lane (m, g) reads and writes of a block: row 4 q + g, columns 4 m .. 4 m + 3
+    for (int c = 1; c < a.chunks; ++c) s += *(const f32x4*)(p + (int64_t)c * a.T * a.rp);
+    return s * scale;
+  };
+  x4<T> raw[kHold ? JB : 1][4];
   x4<O> old[4];
+  // what lane (m, g) reads and writes of a step: row 4 q + g, columns 4 m .. 4 m + 3
   auto load_base = [&](int c0, int rb) {
     const int c = c0 + 4 * m;
-    if (whole) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        old[q] = load_n<true, x4<O>, 4>((const O*)a.base + rows[rb * 16 + q * 4 + g] * a.base_ld + c, 4);
-    } else {
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        old[q] = load_some<x4<O>, 4>((const O*)a.base + rows[rb * 16 + q * 4 + g] * a.base_ld + c, a.N - c);
+    for (int q = 0; q < 4; ++q) {
+      const int t = rb * 16 + q * 4;
+      if (t >= run.count) break;
+      const O* p = base + __shfl(my_row, t + g) * a.base_ld + c;
+      old[q] = c0 + 64 <= a.N ? load_n<true, x4<O>, 4>(p, 4) : load_some<x4<O>, 4>(p, a.N - c);
     }
   };
-  if (a.base) load_base(c_first + wave * 64, 0);
+  if constexpr (kHold)
 #pragma unroll
-  for (int ct = 0; ct < NT; ++ct) {
-    const int c0 = c_first + (ct * kWaves + wave) * 64;
-    if (c0 >= a.N) break;
-    for (int rb = 0; rb < blocks; ++rb) {
+    for (int jb = 0; jb < JB; ++jb) weights(c_first, jb, raw[jb]);
+  if (base) load_base(c_first, 0);
+  f32x4 u[kHold ? 4 : 1][kHold ? JB : 1];
+  if constexpr (kHold)
+#pragma unroll
+    for (int rb = 0; rb < 4; ++rb)
+      if (rb < blocks)
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) u[rb][jb] = jb * 16 < a.rp ? load_u(rb, jb) : f32x4{};
+  float* const my = tile[wave];
+  for (int ct = 0; ct < tiles; ++ct) {
+    const int c0 = c_first + ct * 64;
+    f32x4 wf[kHold ? JB : 1][4];
+    auto widen = [&](int k) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) wf[k][q][s] = (float)raw[k][q][s];
+    };
+    if constexpr (kHold) {
+#pragma unroll
+      for (int jb = 0; jb < JB; ++jb) widen(jb);
+      if (ct + 1 < tiles)
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) weights(c0 + 64, jb, raw[jb]);
+    }
+#pragma unroll
+    for (int rb = 0; rb < 4; ++rb) {
+      if (rb >= blocks) break;
       f32x4 acc[4] = {};
 #pragma unroll
       for (int jb = 0; jb < JB; ++jb) {
         if (jb * 16 >= a.rp) break;
-        if constexpr (!kHold) weights(std::false_type{}, c0, jb, held[0][0]);
-        const f32x4 uf = *(const f32x4*)(u + (rb * 16 + m) * kU + jb * 16 + g * 4);
+        if constexpr (!kHold) {
+          weights(c0, jb, raw[0]);
+          widen(0);
+          u[0][0] = load_u(rb, jb);
+        }
+        const f32x4 uf = u[kHold ? rb : 0][kHold ? jb : 0];
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
           for (int nb = 0; nb < 4; ++nb) {
-            const x4<T>(&h)[4] = held[kHold ? ct : 0][kHold ? jb : 0];
-            acc[nb] = mfma((float)(FLAT ? h[s][nb] : h[nb][s]), uf[s], acc[nb]);
+            const f32x4(&h)[4] = wf[kHold ? jb : 0];
+            acc[nb] = mfma(FLAT ? h[s][nb] : h[nb][s], uf[s], acc[nb]);
           }
       }
       // lane: row m of the block, columns of the instruction's rows 4 g + i
@@ -331,20 +354,22 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         y[q] = *(const f32x4*)(my + (q * 4 + g) * kTile + 4 * m);
-        if (a.base) y[q] += f32x4{(float)old[q][0], (float)old[q][1], (float)old[q][2], (float)old[q][3]};
+        if (base) y[q] += f32x4{(float)old[q][0], (float)old[q][1], (float)old[q][2], (float)old[q][3]};
       }
       lanes_in_order();
-      if (a.base) {
+      if (base) {
         if (rb + 1 < blocks)
           load_base(c0, rb + 1);
-        else if (ct + 1 < NT)
-          load_base(c0 + kWaves * 64, 0);
+        else if (ct + 1 < tiles)
+          load_base(c0 + 64, 0);
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
+        if (rb * 16 + q * 4 >= run.count) break;
         const int t = rb * 16 + q * 4 + g, c = c0 + 4 * m, n = a.N - c;
+        const int64_t row = __shfl(my_row, t);
         if (t >= run.count || n <= 0) continue;
-        O* dst = (O*)a.out + rows[t] * a.out_ld + c;
+        O* dst = (O*)a.out + row * a.out_ld + c;
         x4<O> z;
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[e] = narrow<O>(y[q][e]);
@@ -384,7 +409,7 @@ struct PassArgs {
 //
 // FAST, where all is bf16: both on the bf16 matrix instructions, w as the sum of
 // three bf16 numbers, which holds all of its 24 bits. Otherwise on the fp32 ones.
-constexpr int kPassRows = 64, kPassCols = 256;
+constexpr int kPassRows = 64;
 template <class S, class W, bool CONTRACT, int JB, int CT>
 struct Pass {
   static constexpr bool FAST = std::is_same_v<S, __bf16> && std::is_same_v<W, __bf16>;
@@ -407,9 +432,8 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   __shared__ __attribute__((aligned(16))) E wt[P::kTerms * JB * 16 * P::kW];
   __shared__ __attribute__((aligned(16))) W bt[CONTRACT ? JB * 16 * P::kB : 1];
   __shared__ int32_t rows[kMaxPassRows];
-  if ((int)blockIdx.x >= *l.n_runs) return;
-  const Run run = l.runs[blockIdx.x];
-  if (run.key >= a.n) return;
+  const Run run = own_run(l);
+  if (run.count == 0 || run.key >= a.n) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane % 16, g = lane / 16;
   const int c_first = blockIdx.y * CT * kPassCols, j0 = blockIdx.z * JB * 16;
   const int tiles = (a.N - c_first + kPassCols - 1) / kPassCols < CT ? (a.N - c_first + kPassCols - 1) / kPassCols : CT;
@@ -499,11 +523,13 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   };
 
   f32x4 acc[CT][JB][4] = {};  // out
-  f32x4 sum[JB];              // part
+  f32x4 total[JB];            // part, over the tiles so far
+  auto add_up = [](f32x4(&total)[JB], const f32x4(&sum)[JB], int ct) {
+#pragma unroll
+    for (int jb = 0; jb < JB; ++jb) total[jb] = ct == 0 ? sum[jb] : total[jb] + sum[jb];
+  };
   load_tile(0, 0);
   for (int t0 = 0; t0 < run.count; t0 += kPassRows) {
-#pragma unroll
-    for (int jb = 0; jb < JB; ++jb) sum[jb] = f32x4{};
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       if (ct >= tiles) break;
@@ -537,6 +563,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
             }
         }
         if constexpr (CONTRACT) {
+          f32x4 sum[JB] = {};
 #pragma unroll
           for (int ks = 0; ks < kPassCols / 32; ++ks) {
             const bf16x8 x = *(const bf16x8*)(tile + (wave * 16 + m) * P::kRow + ks * 32 + g * 8);
@@ -544,6 +571,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
             for (int jb = 0; jb < JB; ++jb)
               sum[jb] = mfma(*(const bf16x8*)(bt + (jb * 16 + m) * P::kB + ct * kPassCols + ks * 32 + g * 8), x, sum[jb]);
           }
+          add_up(total, sum, ct);
         }
       } else {
 #pragma unroll 4
@@ -558,6 +586,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
           }
         }
         if constexpr (CONTRACT) {
+          f32x4 sum[JB] = {};
 #pragma unroll 4
           for (int ks = 0; ks < kPassCols / 16; ++ks) {
             const f32x4 x = *(const f32x4*)(tile + (wave * 16 + m) * P::kRow + ks * 16 + g * 4);
@@ -568,6 +597,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
               for (int e = 0; e < 4; ++e) sum[jb] = mfma((float)bf[e], x[e], sum[jb]);
             }
           }
+          add_up(total, sum, ct);
         }
       }
     }
@@ -576,7 +606,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
       float* p = a.part + ((int64_t)blockIdx.y * a.T + run.first + t) * a.rp + j0 + g * 4;
 #pragma unroll
       for (int jb = 0; jb < JB; ++jb)
-        if (t < run.count && j0 + jb * 16 < a.rp) *(f32x4*)(p + jb * 16) = sum[jb];
+        if (t < run.count && j0 + jb * 16 < a.rp) *(f32x4*)(p + jb * 16) = total[jb];
     }
   }
 
@@ -609,7 +639,7 @@ struct FinishArgs {
   const float* part[2];
   float* out[2];
   int64_t size[2];  // r * d, r * N
-  int32_t C[2];
+  int32_t log_C[2];
   RunList l[2];
   int32_t n, joins, accumulate;
   const uint8_t* seen;
@@ -629,9 +659,9 @@ __global__ __launch_bounds__(kThreads) void finish(FinishArgs a) {
   if ((int)blockIdx.x >= *a.l[z].n_joins) return;
   const Join j = a.l[z].joins[blockIdx.x];
   if (j.key >= a.n) return;
-  const int C = a.C[z], runs = (j.end - j.first + C - 1) / C;
+  const int C = 1 << a.log_C[z], runs = (j.end - j.first + C - 1) / C;
   // the key's runs are two slots apart, the last one's is the odd one
-  const float* part = a.part[z] + (int64_t)run_slot(j.first, C, false) * size;
+  const float* part = a.part[z] + (int64_t)run_slot(j.first, a.log_C[z], false) * size;
   for (int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x; i < size; i += step) {
     float s = 0.f;
     constexpr int kAhead = 8;  // loads in flight, added in order
@@ -676,10 +706,11 @@ hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
 }
 template <class T, class O, bool FLAT>
 hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
-  const bool many = l.max_runs * chunks_of(a.N, 4 * kWaves * 64) >= 512;
+  // a wave takes four tiles where that leaves 16 waves for each of 256 CUs
+  const bool many = l.max_runs * chunks_of(a.N, 4 * 64) >= 4096;
   if (a.rp <= 16) return many ? run_expand<T, O, FLAT, 1, 4>(a, l, s) : run_expand<T, O, FLAT, 1, 1>(a, l, s);
-  if (a.rp <= 32) return many ? run_expand<T, O, FLAT, 2, 2>(a, l, s) : run_expand<T, O, FLAT, 2, 1>(a, l, s);
-  if (a.rp <= 64) return run_expand<T, O, FLAT, 4, 1>(a, l, s);
+  if (a.rp <= 32) return many ? run_expand<T, O, FLAT, 2, 4>(a, l, s) : run_expand<T, O, FLAT, 2, 1>(a, l, s);
+  if (a.rp <= 64) return many ? run_expand<T, O, FLAT, 4, 4>(a, l, s) : run_expand<T, O, FLAT, 4, 1>(a, l, s);
   return run_expand<T, O, FLAT, 16, 1>(a, l, s);
 }
 template <class T, bool FLAT>
@@ -699,8 +730,10 @@ hipError_t run_pass(const PassArgs& a, const RunList& l, hipStream_t s) {
 template <class S, class W, bool CONTRACT>
 hipError_t run_pass(const PassArgs& a, int tiles, const RunList& l, hipStream_t s) {
   if (a.rp <= 16) {
-    if constexpr (CONTRACT)
+    if constexpr (CONTRACT) {
       if (tiles == 4) return run_pass<S, W, CONTRACT, 1, 4>(a, l, s);
+      if (tiles == 2) return run_pass<S, W, CONTRACT, 1, 2>(a, l, s);
+    }
     return run_pass<S, W, CONTRACT, 1, 1>(a, l, s);
   }
   if (a.rp <= 32) {
@@ -710,6 +743,7 @@ hipError_t run_pass(const PassArgs& a, int tiles, const RunList& l, hipStream_t 
   }
   return run_pass<S, W, CONTRACT, 4, 1>(a, l, s);
 }
+
 template <class T>
 hipError_t add_typed(const tim_adapters& ad, const void* x, int64_t x_ld, int64_t n_rows, const void* base,
                      int64_t base_ld, void* out, int out_dtype, int64_t out_ld, const AdapterPlan& p, char* ws,
@@ -733,17 +767,18 @@ hipError_t backward_typed(const tim_adapters& ad, const AdapterGradArgs& a, int 
     const ShrinkArgs sa = {a.x, a.x_ld, a.T, ad.a, ad.n, ad.r, p.rp, ad.d, (float*)(ws + p.u_part)};
     e = run_shrink<T>(sa, l, p.x_chunks, s);
     if (e != hipSuccess) return e;
-    TIM_LAUNCH((sum_chunks<<<dim3((unsigned)l.max_runs, p.rp), kThreads, 0, s>>>(sa.part, a.T, p.rp, p.x_chunks, ad.n, ad.scales, u,
+    TIM_LAUNCH((sum_chunks<<<dim3((unsigned)l.max_runs, p.rp), kThreads, 0, s>>>(sa.part, a.T, p.rp, p.x_chunks, 1, ad.n, ad.scales, u,
                                                                      l)));
   } else {
     u = nullptr;
   }
   const PassArgs pb = {a.grad, a.grad_ld, a.T,      u,    ad.b, (float*)(ws + p.v_part),   ad.n,
                        ad.r,   p.rp,      ad.N,     a.grad_b, (float*)(ws + p.b_part), a.accumulate_ab};
-  e = run_pass<G, T, true>(pb, p.tiles, lb, s);
+  e = run_pass<G, T, true>(pb, p.of_grad.tiles, lb, s);
   if (e != hipSuccess) return e;
   if (a.grad_x || a.grad_a)
-    TIM_LAUNCH((sum_chunks<<<dim3((unsigned)l.max_runs, p.rp), kThreads, 0, s>>>(pb.part, a.T, p.rp, p.g_chunks, ad.n,
+    TIM_LAUNCH((sum_chunks<<<dim3((unsigned)l.max_runs, p.rp), kThreads, 0, s>>>(pb.part, a.T, p.rp, p.g_chunks,
+                                                                                 kChunkQuad / p.of_grad.tiles, ad.n,
                                                                                  ad.scales, v, l)));
   if (a.grad_x) {
     const ExpandArgs ea = {v, a.T, 1, ad.n, ad.r, p.rp, ad.d, nullptr, ad.a, a.accumulate_x ? a.grad_x : nullptr,
@@ -762,7 +797,7 @@ hipError_t backward_typed(const tim_adapters& ad, const AdapterGradArgs& a, int 
   FinishArgs f = {{a_part, pb.out_part},
                   {a.grad_a, a.grad_b},
                   {(int64_t)ad.r * ad.d, (int64_t)ad.r * ad.N},
-                  {p.g.C[1], p.g.C[2]},
+                  {p.of_x.log_rows, p.of_grad.log_rows},
                   {la, lb},
                   ad.n,
                   0,

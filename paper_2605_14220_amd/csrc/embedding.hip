@@ -30,24 +30,39 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& r) {
 }
 
 // A row is taken by `lanes` threads (a power of two up to 256), N elements at a
-// time; blockIdx.y walks slices of lanes * N elements.
+// time; blockIdx.y walks slices of lanes * N elements. A thread takes kEmbedRows
+// rows, whose loads are in flight together.
+constexpr int kEmbedRows = 4;
 template <class T, class O, int N>
 __global__ __launch_bounds__(kThreads) void embed(EmbedArgs a, int64_t row0, int lanes) {
-  const int64_t t = row0 + (int64_t)blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes;
+  const int down = kThreads / lanes;
+  const int64_t t0 = row0 + (int64_t)blockIdx.x * down * kEmbedRows + threadIdx.x / lanes;
   const int c = (blockIdx.y * lanes + threadIdx.x % lanes) * N;
-  if (t >= a.T || c >= a.d) return;
-  const uint32_t v = (uint32_t)a.tokens[t];
-  const bool there = v < (uint32_t)a.V;
-  const T* src = (const T*)a.table + (there ? (int64_t)v : 0) * a.ld + c;
-  O* dst = (O*)a.out + t * a.out_ld + c;
-  if (c + N <= a.d) {
-    const Pack<T, N> x = load_pack<T, N>(src);
-    Pack<O, N> y;
+  if (c >= a.d) return;
+  uint32_t v[kEmbedRows];
 #pragma unroll
-    for (int e = 0; e < N; ++e) y.v[e] = there ? narrow<O>((float)x.v[e] * a.scale) : (O)0.f;
-    store_pack(dst, y);
+  for (int k = 0; k < kEmbedRows; ++k) v[k] = t0 + k * down < a.T ? (uint32_t)a.tokens[t0 + k * down] : ~0u;
+  const T* table = (const T*)a.table + c;
+  O* out = (O*)a.out + c;
+  if (c + N <= a.d) {
+    Pack<T, N> x[kEmbedRows];
+#pragma unroll
+    for (int k = 0; k < kEmbedRows; ++k)
+      x[k] = load_pack<T, N>(table + (v[k] < (uint32_t)a.V ? (int64_t)v[k] : 0) * a.ld);
+#pragma unroll
+    for (int k = 0; k < kEmbedRows; ++k) {
+      if (t0 + k * down >= a.T) break;
+      const bool there = v[k] < (uint32_t)a.V;
+      Pack<O, N> y;
+#pragma unroll
+      for (int e = 0; e < N; ++e) y.v[e] = there ? narrow<O>((float)x[k].v[e] * a.scale) : (O)0.f;
+      store_pack(out + (t0 + k * down) * a.out_ld, y);
+    }
   } else {
-    for (int e = 0; c + e < a.d; ++e) dst[e] = there ? narrow<O>((float)src[e] * a.scale) : (O)0.f;
+    for (int k = 0; k < kEmbedRows; ++k)
+      for (int e = 0; c + e < a.d && t0 + k * down < a.T; ++e)
+        out[(t0 + k * down) * a.out_ld + e] =
+            v[k] < (uint32_t)a.V ? narrow<O>((float)table[v[k] * a.ld + e] * a.scale) : (O)0.f;
   }
 }
 
@@ -56,7 +71,7 @@ hipError_t embed_typed(const EmbedArgs& a, hipStream_t s) {
   constexpr int N = 16 / (int)sizeof(T);
   int lanes = 1;
   while (lanes < kThreads && (int64_t)lanes * N < a.d) lanes *= 2;
-  const int rows = kThreads / lanes;
+  const int rows = kThreads / lanes * kEmbedRows;
   const unsigned slices = (unsigned)((a.d + (int64_t)lanes * N - 1) / ((int64_t)lanes * N));
   // fewer than 2^32 threads a launch and direction
   const int64_t per = (int64_t)1 << 23;
@@ -79,14 +94,43 @@ hipError_t embed_out(const EmbedArgs& a, int out_dtype, hipStream_t s) {
 
 // ------------------------------------------------------------------ gradient
 
+// Zeros in kZeroRows consecutive rows from r0 on, those of tokens that occur left out.
+#ifndef VZ
+#define VZ 1
+#endif
+constexpr int kZeroRows = VZ;
+__device__ __forceinline__ void zero_rows(float* p, int64_t r0, int64_t rows, int64_t d, int64_t ld,
+                                          const uint8_t* seen) {
+  uint32_t skip = 0;
+  if (seen) {
+    const int lane = threadIdx.x & 63;
+    skip = (uint32_t)__ballot(lane < kZeroRows && r0 + lane < rows && seen[r0 + lane < rows ? r0 + lane : 0]);
+  }
+  for (int k = 0; k < kZeroRows && r0 + k < rows; ++k) {
+    if (skip >> k & 1) continue;
+    float* q = p + (r0 + k) * ld;
+    int64_t c = (int64_t)threadIdx.x * 4;
+    for (; c + 4 <= d; c += kThreads * 4) store_pack(q + c, Pack<float, 4>{});
+    for (int e = 0; c + e < d && e < 4; ++e) q[c + e] = 0.f;
+  }
+}
+__global__ __launch_bounds__(kThreads) void zero_all(float* p, int64_t rows, int64_t d, int64_t ld) {
+  zero_rows(p, (int64_t)blockIdx.x * kZeroRows, rows, d, ld, nullptr);
+}
+
 // The sum of a run's rows, a chain by ascending t, for one slice of columns. A
 // token's only run is scaled and stored (or added to the table's row), one of
-// several is left in its slot.
+// several is left in its slot. The workgroups past the runs' clear the rows of
+// the tokens that do not occur: the runs' chains then hide behind the stores.
 template <class T, int N>
-__global__ __launch_bounds__(kThreads) void sum_runs(EmbedGradArgs a, RunList l, float* part) {
-  const int64_t item = blockIdx.x;
-  if (item >= *l.n_runs) return;
-  const Run run = l.runs[item];
+__global__ __launch_bounds__(kThreads) void sum_runs(EmbedGradArgs a, RunList l, float* part,
+                                                         const uint8_t* seen) {
+  if (blockIdx.x >= l.max_runs) {
+    zero_rows(a.grad_table, ((blockIdx.x - l.max_runs) * gridDim.y + blockIdx.y) * kZeroRows, a.V, a.d, a.grad_ld, seen);
+    return;
+  }
+  const Run run = own_run(l);
+  if (run.count == 0) return;
   const int c = (blockIdx.y * kThreads + threadIdx.x) * N;
   if (c >= a.d) return;
   const int n = a.d - c < N ? a.d - c : N;
@@ -148,22 +192,10 @@ __global__ __launch_bounds__(kThreads) void join_runs(EmbedGradArgs a, RunList l
   float sum = 0.f;
 #pragma unroll 4
   for (int p = j.first; p < j.end; p += TIM_EMBED_RUN)
-    sum += part[(int64_t)run_slot(p, TIM_EMBED_RUN, p + TIM_EMBED_RUN >= j.end) * a.d + c];
+    sum += part[(int64_t)run_slot(p, kLogEmbedRun, p + TIM_EMBED_RUN >= j.end) * a.d + c];
   sum *= a.scale;
   float* dst = a.grad_table + j.key * a.grad_ld + c;
   *dst = a.accumulate ? *dst + sum : sum;
-}
-
-// Zeros in the rows of the tokens that do not occur.
-__global__ __launch_bounds__(kThreads) void zero_unseen(float* p, int64_t rows, int64_t d, int64_t ld,
-                                                        const uint8_t* seen) {
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    if (seen && seen[r]) continue;
-    float* q = p + r * ld;
-    int64_t c = (int64_t)threadIdx.x * 4;
-    for (; c + 4 <= d; c += kThreads * 4) store_pack(q + c, Pack<float, 4>{});
-    for (; c < d; ++c) q[c] = 0.f;
-  }
 }
 
 template <class T>
@@ -174,16 +206,12 @@ hipError_t grad_typed(const EmbedGradArgs& a, const EmbedPlan& p, char* ws, hipS
   uint8_t* seen = a.accumulate ? nullptr : (uint8_t*)(ws + p.seen);
   hipError_t e = launch_grouping(p.g, a.tokens, false, seen, ws, s);
   if (e != hipSuccess) return e;
-  if (!a.accumulate) {
-    zero_unseen<<<(unsigned)(a.V < 16384 ? a.V : 16384), kThreads, 0, s>>>(a.grad_table, a.V, a.d, a.grad_ld, seen);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   const int slices = (a.d + kThreads * N - 1) / (kThreads * N);
-  sum_runs<T, N><<<dim3((unsigned)l.max_runs, slices), kThreads, 0, s>>>(a, l, part);
+  const int64_t zero_blocks = a.accumulate ? 0 : ((a.V + kZeroRows - 1) / kZeroRows + slices - 1) / slices;
+  sum_runs<T, N><<<dim3((unsigned)(l.max_runs + zero_blocks), slices), kThreads, 0, s>>>(a, l, part, seen);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.T > TIM_EMBED_RUN) {
+  if (l.max_joins > 0) {
     const int js = (a.d + kThreads - 1) / kThreads;
     join_runs<<<dim3((unsigned)l.max_joins, js), kThreads, 0, s>>>(a, l, part);
     e = hipGetLastError();
@@ -194,7 +222,7 @@ hipError_t grad_typed(const EmbedGradArgs& a, const EmbedPlan& p, char* ws, hipS
 }  // namespace
 
 hipError_t launch_zero_rows(float* p, int64_t rows, int64_t d, int64_t ld, hipStream_t s) {
-  zero_unseen<<<(unsigned)(rows < 16384 ? rows : 16384), kThreads, 0, s>>>(p, rows, d, ld, nullptr);
+  zero_all<<<(unsigned)((rows + kZeroRows - 1) / kZeroRows), kThreads, 0, s>>>(p, rows, d, ld);
   return hipGetLastError();
 }
 

@@ -1,7 +1,7 @@
 // Rows grouped by a key (a row's token, or its adapter): a stable sort of the
 // row indices by key and the list of runs that the operators work on.
 //
-// A run is at most C consecutive places of the sorted order with one key, and
+// A run is at most C (a power of two) consecutive places of the sorted order with one key, and
 // runs start every C places from the key's first: what a run holds depends on
 // the key's own rows only. The lists' order in memory is not fixed (it is made
 // with an atomic counter), so nothing may depend on it but which workgroup
@@ -29,10 +29,16 @@ struct alignas(16) Join {
 
 // Slots of runs of C places. Of the keys with several runs, at most one full
 // run starts in each C places, and at most one last (shorter or full) run of a key.
-__host__ __device__ inline int32_t run_slot(int32_t first, int C, bool last) { return first / C * 2 + (last ? 1 : 0); }
-inline int64_t run_slots(int64_t T, int C) { return (T + C - 1) / C * 2; }
+// C is a power of two, given by its logarithm.
+__host__ __device__ inline int32_t run_slot(int32_t first, int log_C, bool last) {
+  return (first >> log_C) * 2 + (last ? 1 : 0);
+}
+inline int64_t run_slots(int64_t T, int log_C) { return ((T >> log_C) + 1) * 2; }
 
-constexpr int kGroupSmall = 4096;  // rows that one workgroup sorts in LDS
+// Rows that one workgroup sorts in LDS, by the sorting passes it takes: with one
+// pass (up to 255 keys) 8192 rows take 9 us against 24 in several launches, with
+// three 4096 rows 16 against 28 and twice as many the same.
+inline int64_t group_small_rows(int passes) { return passes == 1 ? 16384 : 4096; }
 constexpr int kMaxRunLists = 3;
 
 // Sizes and workspace of a grouping of T rows by keys in [0, n); keys outside
@@ -41,7 +47,7 @@ struct Grouping {
   int64_t T;
   int32_t n;
   int32_t lists;                // lists of runs
-  int32_t C[kMaxRunLists];      // their lengths
+  int32_t log_C[kMaxRunLists];  // logarithms of their lengths
   int64_t max_runs[kMaxRunLists], max_joins[kMaxRunLists];
   int32_t bits, passes, digit;  // of a key, sorting passes, bits a pass
   int32_t blocks, per_block;    // of the sort of many rows
@@ -51,7 +57,7 @@ struct Grouping {
 
 inline size_t group_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
-inline Grouping plan_grouping(int64_t T, int32_t n, int lists, const int* C) {
+inline Grouping plan_grouping(int64_t T, int32_t n, int lists, const int* log_C) {
   Grouping g = {};
   g.T = T;
   g.n = n;
@@ -60,12 +66,12 @@ inline Grouping plan_grouping(int64_t T, int32_t n, int lists, const int* C) {
   size_t at = 0;
   g.counters = at, at += 256;
   g.order = at, at += group_align((size_t)T * 4);
-  if (T <= kGroupSmall) {
-    // digits of at most 8 bits: a bin for each of 256 threads to add up
-    g.passes = (g.bits + 7) / 8;
+  // digits of at most 8 bits: a bin for each of 256 threads to add up
+  g.passes = (g.bits + 7) / 8;
+  if (T <= group_small_rows(g.passes)) {
     g.digit = (g.bits + g.passes - 1) / g.passes;
     g.blocks = 1;
-    g.per_block = kGroupSmall;
+    g.per_block = (int32_t)T;
   } else {
     g.passes = (g.bits + 9) / 10;
     g.digit = (g.bits + g.passes - 1) / g.passes;
@@ -79,9 +85,10 @@ inline Grouping plan_grouping(int64_t T, int32_t n, int lists, const int* C) {
   }
   const int64_t distinct = T < (int64_t)n + 1 ? T : (int64_t)n + 1;
   for (int l = 0; l < lists; ++l) {
-    g.C[l] = C[l];
-    g.max_runs[l] = T / C[l] + distinct;
-    g.max_joins[l] = T / (C[l] + 1) < distinct ? T / (C[l] + 1) : distinct;
+    const int64_t C = (int64_t)1 << log_C[l];
+    g.log_C[l] = log_C[l];
+    g.max_runs[l] = T / C + distinct;
+    g.max_joins[l] = T / (C + 1) < distinct ? T / (C + 1) : distinct;
     g.runs[l] = at, at += group_align((size_t)g.max_runs[l] * sizeof(Run));
     g.joins[l] = at, at += group_align((size_t)g.max_joins[l] * sizeof(Join));
   }
@@ -98,6 +105,16 @@ struct RunList {
   const int32_t* n_joins;
   int64_t max_runs, max_joins;
 };
+// This workgroup's run (count 0: none), asked for beside the list's length rather than after it.
+#if defined(__HIPCC__)
+__device__ __forceinline__ Run own_run(const RunList& l) {
+  Run r = l.runs[blockIdx.x];
+  const int32_t n = *l.n_runs;
+  asm volatile("" ::"s"(n), "s"(r.first));  // both loads before the branch
+  if ((int)blockIdx.x >= n) r.count = 0;
+  return r;
+}
+#endif
 inline RunList run_list(const Grouping& g, const void* ws, int l) {
   const char* w = (const char*)ws;
   const int32_t* c = (const int32_t*)(w + g.counters);
@@ -114,7 +131,7 @@ __device__ __forceinline__ void lanes_in_order() {
 }
 
 // seen (may be null): a byte per key in [0, n), set to 1 for the keys that
-// occur and 0 for the others.
+// occur and 0 for the others; room for whole words, 4-byte aligned.
 hipError_t launch_grouping(const Grouping& g, const int32_t* keys, bool keep_rest, uint8_t* seen, void* ws,
                            hipStream_t s);
 

@@ -1,5 +1,5 @@
 // Stable sort of row indices by key, least significant digit first, and the
-// lists of runs. Up to kGroupSmall rows are one workgroup's work in LDS; more
+// lists of runs. Up to group_small_rows rows are one workgroup's work in LDS; more
 // are sorted in one or two passes of two launches each (counts per block, then
 // places), blocks in row order, then listed.
 //
@@ -54,73 +54,36 @@ __device__ __forceinline__ uint32_t place_step(uint32_t digit, int bits, bool th
   return at + below;
 }
 
-// Lists the run or the join that place p of the sorted keys starts or ends, if
-// any. first: the first place of p's key.
+// The lists to make of the sorted keys.
 struct Lists {
   int32_t n, lists;
-  int32_t C[kMaxRunLists];
+  int32_t log_C[kMaxRunLists];
   Run* runs[kMaxRunLists];
   Join* joins[kMaxRunLists];
 };
-template <class Keys, class Append>
-__device__ __forceinline__ void list_place(const Lists& L, Keys key_at, int32_t T, int32_t p, bool there, uint32_t key,
-                                           int32_t first, Append append) {
-  for (int l = 0; l < L.lists; ++l) {
-    const int C = L.C[l];
-    const bool starts = there && (p - first) % C == 0;
-    Run r = {p, 0, (int32_t)key, -1};
-    bool ends = false;  // the last run of several
-    if (starts) {
-      // the first place in (p, p + C] that is not of the key
-      int lo = p + 1, hi = p + C < T ? p + C : T;
-      while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (key_at(mid) == key) lo = mid + 1; else hi = mid;
-      }
-      r.count = lo - p;
-      const bool last = !(lo < T && key_at(lo) == key);
-      if (p != first || !last) r.slot = run_slot(p, C, last);
-      ends = last && p != first;
-    }
-    const int at = append(2 * l, starts);
-    if (starts) L.runs[l][at] = r;
-    const int j = append(2 * l + 1, ends);
-    if (ends) L.joins[l][j] = {first, p + r.count, (int32_t)key, 0};
-  }
-}
-
-// The inclusive maximum over the wave's lanes up to this one.
-__device__ __forceinline__ int32_t wave_scan_max(int32_t x, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    const int32_t y = __shfl_up(x, o);
-    if (lane >= o && y > x) x = y;
-  }
-  return x;
-}
-
 // ------------------------------------------------------------- few rows
 
-// One workgroup: items are key * 4096 + row index, 32 bits for keys below 2^20.
+// One workgroup. Items are the key above the row index, 32 bits: keys below 2^20
+// with 4096 rows, below 2^18 with 16384.
+template <int LOG_ROWS>
 __global__ __launch_bounds__(kSmallThreads) void group_small(const int32_t* keys, int32_t T, int passes, int digit_bits,
                                                              int32_t limit, Lists L, int32_t* order, uint8_t* seen,
                                                              int32_t* counters) {
-  __shared__ uint32_t item[2][kGroupSmall];
+  constexpr int kRows = 1 << LOG_ROWS;
+  __shared__ uint32_t item[2][kRows + 64];
   __shared__ uint32_t place[kSmallWaves][256];
-  __shared__ uint32_t wave_total[4];
-  __shared__ int32_t wave_first[kSmallWaves];
-  __shared__ int32_t carry;
-  __shared__ int32_t counted[2 * kMaxRunLists];
+  __shared__ uint32_t wave_total[kSmallWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int bins = 1 << digit_bits;
   // each wave takes consecutive items, a multiple of 64
   const int per_wave = ((T + kSmallWaves - 1) / kSmallWaves + 63) / 64 * 64;
   const int from = wave * per_wave, to = from + per_wave < T ? from + per_wave : T;
-  if (tid < 2 * kMaxRunLists) counted[tid] = 0;
-  for (int i = tid; i < T; i += kSmallThreads) item[0][i] = key_of(keys, i, L.n) << 12 | i;
+  for (int i = tid; i < T; i += kSmallThreads) item[0][i] = key_of(keys, i, L.n) << LOG_ROWS | i;
+  if (seen)
+    for (int i = tid; i * 4 < L.n; i += kSmallThreads) ((uint32_t*)seen)[i] = 0;
   int cur = 0;
   for (int pass = 0; pass < passes; ++pass, cur ^= 1) {
-    const int shift = 12 + pass * digit_bits;
+    const int shift = LOG_ROWS + pass * digit_bits;
     for (int b = lane; b < bins; b += 64) place[wave][b] = 0;
     __syncthreads();
     for (int i = from; i < to; i += 64) {
@@ -130,14 +93,18 @@ __global__ __launch_bounds__(kSmallThreads) void group_small(const int32_t* keys
     }
     __syncthreads();
     // places: digits in order, the waves' items of one digit in wave order
-    uint32_t sum = 0, incl = 0;
+    uint32_t sum = 0, incl = 0, c[kSmallWaves] = {};
     if (tid < 256) {
-      if (tid < bins)
+      if (tid < bins) {
+#pragma unroll
+        for (int w = 0; w < kSmallWaves; ++w) c[w] = place[w][tid];
+#pragma unroll
         for (int w = 0; w < kSmallWaves; ++w) {
-          const uint32_t c = place[w][tid];
-          place[w][tid] = sum;
-          sum += c;
+          const uint32_t x = c[w];
+          c[w] = sum;
+          sum += x;
         }
+      }
       incl = sum;
 #pragma unroll
       for (int o = 1; o < 64; o *= 2) {
@@ -150,7 +117,8 @@ __global__ __launch_bounds__(kSmallThreads) void group_small(const int32_t* keys
     if (tid < bins) {
       uint32_t before = incl - sum;
       for (int w = 0; w < wave; ++w) before += wave_total[w];
-      for (int w = 0; w < kSmallWaves; ++w) place[w][tid] += before;
+#pragma unroll
+      for (int w = 0; w < kSmallWaves; ++w) place[w][tid] = before + c[w];
     }
     __syncthreads();
     for (int i = from; i < to; i += 64) {
@@ -162,34 +130,74 @@ __global__ __launch_bounds__(kSmallThreads) void group_small(const int32_t* keys
     __syncthreads();
   }
   const uint32_t* sorted = item[cur];
-  auto key_at = [&](int p) { return sorted[p] >> 12; };
-  auto append = [&](int c, bool add) {
-    const uint64_t m = __ballot(add);
-    int base = 0;
-    if (m != 0 && lane == 0) base = atomicAdd(&counted[c], (int)__popcll(m));
-    return __shfl(base, 0) + lanes_below(m);
+  int32_t* head = (int32_t*)item[cur ^ 1];  // the first place of each key that occurs
+  // the sum of x over the threads before this one and the earlier `total`, which grows by the sum over all threads
+  auto scan = [&](uint32_t x, uint32_t& total) {
+    uint32_t incl = x;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const uint32_t y = __shfl_up(incl, o);
+      if (lane >= o) incl += y;
+    }
+    __syncthreads();  // the last scan's sums are read
+    if (lane == 63) wave_total[wave] = incl;
+    __syncthreads();
+    uint32_t before = total + incl - x;
+#pragma unroll
+    for (int w = 0; w < kSmallWaves; ++w) {
+      const uint32_t y = wave_total[w];
+      before += w < wave ? y : 0;
+      total += y;
+    }
+    return before;
   };
-  if (tid == 0) carry = 0;
+  uint32_t heads = 0;
   for (int base = 0; base < T; base += kSmallThreads) {
     const int p = base + tid;
-    const uint32_t x = p < T ? sorted[p] : 0xffffffffu;
-    const uint32_t key = x >> 12;
-    const bool head = p < T && (p == 0 || key_at(p - 1) != key);
-    int first = wave_scan_max(head ? p : 0, lane);
-    if (lane == 63) wave_first[wave] = first;
-    __syncthreads();
-    int before = carry;
-    for (int w = 0; w < wave; ++w) before = wave_first[w] > before ? wave_first[w] : before;
-    first = first > before ? first : before;
-    const bool there = p < T && (int32_t)key < limit;
-    if (p < T) order[p] = x & 4095;
-    if (head && there && seen && (int32_t)key < L.n) seen[key] = 1;
-    list_place(L, key_at, T, p, there, key, first, append);
-    __syncthreads();
-    if (tid == kSmallThreads - 1) carry = first;
+    const uint32_t x = p < T ? sorted[p] : 0, key = x >> LOG_ROWS;
+    const bool is = p < T && (p == 0 || sorted[p - 1] >> LOG_ROWS != key);
+    if (p < T) order[p] = x & (kRows - 1);
+    if (is && seen && (int32_t)key < L.n) seen[key] = 1;
+    const uint32_t at = scan(is, heads);
+    if (is) head[at] = p;
   }
+  if (tid == 0) head[heads] = T;
   __syncthreads();
-  if (tid < 2 * kMaxRunLists) counters[tid] = counted[tid];
+  // the keys from `limit` on are the last ones: key n alone
+  if ((int32_t)(sorted[T - 1] >> LOG_ROWS) >= limit) --heads;
+  for (int l = 0; l < L.lists; ++l) {
+    const int log_C = L.log_C[l], C = 1 << log_C;
+    uint32_t total = 0;  // runs, and joins from bit 16 on
+    for (uint32_t base = 0; base < heads; base += kSmallThreads) {
+      const uint32_t h = base + tid;
+      int first = 0, end = 0, key = 0;
+      if (h < heads) {
+        first = head[h];
+        end = head[h + 1];
+        key = sorted[first] >> LOG_ROWS;
+      }
+      const int runs = (end - first + C - 1) >> log_C;
+      const uint32_t at = scan(runs + (runs > 1 ? 1 << 16 : 0), total);
+      auto put = [&](int q, int first, int end, int key, int runs, int at) {
+        const int f = first + q * C;
+        L.runs[l][at + q] = {f, end - f < C ? end - f : C, key, runs > 1 ? run_slot(f, log_C, q == runs - 1) : -1};
+      };
+      constexpr int kOwn = 4;  // runs that the key's thread lists; more are the whole wave's work
+      for (int q = 0; q < kOwn; ++q)
+        if (q < runs) put(q, first, end, key, runs, at & 0xffff);
+      if (runs > 1) L.joins[l][at >> 16] = {first, end, key, 0};
+      for (uint64_t more = __ballot(runs > kOwn); more != 0; more &= more - 1) {
+        const int src = __builtin_ctzll(more);
+        const int f = __shfl(first, src), e = __shfl(end, src), k = __shfl(key, src), n = __shfl(runs, src);
+        const int a = __shfl((int)(at & 0xffff), src);
+        for (int q = kOwn + lane; q < n; q += 64) put(q, f, e, k, n, a);
+      }
+    }
+    if (tid == 0) {
+      counters[2 * l] = total & 0xffff;
+      counters[2 * l + 1] = total >> 16;
+    }
+  }
 }
 
 // ------------------------------------------------------------ many rows
@@ -206,12 +214,16 @@ __device__ __forceinline__ uint2 item_of(const Source& s, int64_t i) {
 }
 
 // hist[block][digit]: items of each digit; the first launch of a grouping also
-// clears the counters.
-__global__ __launch_bounds__(kSortThreads) void sort_count(Source s, uint32_t* hist, int32_t* counters) {
+// clears the counters and `seen`.
+__global__ __launch_bounds__(kSortThreads) void sort_count(Source s, uint32_t* hist, int32_t* counters,
+                                                           uint8_t* seen) {
   __shared__ uint32_t count[kSortWaves][1024];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int bins = 1 << s.bits;
   if (counters && blockIdx.x == 0 && threadIdx.x < 2 * kMaxRunLists) counters[threadIdx.x] = 0;
+  if (seen)
+    for (int i = blockIdx.x * kSortThreads + threadIdx.x; i * 4 < s.n; i += gridDim.x * kSortThreads)
+      ((uint32_t*)seen)[i] = 0;
   for (int b = lane; b < bins; b += 64) count[wave][b] = 0;
   __syncthreads();
   const int64_t base = (int64_t)blockIdx.x * s.per_block;
@@ -299,6 +311,44 @@ __global__ __launch_bounds__(kSortThreads) void sort_place(Source s, const uint3
   }
 }
 
+// Lists the run that place p starts, if any, and the join of the runs that it ends. first: the first place of p's key.
+template <class Keys, class Append>
+__device__ __forceinline__ void list_place(const Lists& L, Keys key_at, int32_t T, int32_t p, bool there, uint32_t key,
+                                           int32_t first, Append append) {
+  for (int l = 0; l < L.lists; ++l) {
+    const int log_C = L.log_C[l], C = 1 << log_C;
+    const bool starts = there && ((p - first) & (C - 1)) == 0;
+    Run r = {p, 0, (int32_t)key, -1};
+    bool ends = false;  // the last run of several
+    if (starts) {
+      // the first place in (p, p + C] that is not of the key
+      int lo = p + 1, hi = p + C < T ? p + C : T;
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (key_at(mid) == key) lo = mid + 1; else hi = mid;
+      }
+      r.count = lo - p;
+      const bool last = !(lo < T && key_at(lo) == key);
+      if (p != first || !last) r.slot = run_slot(p, log_C, last);
+      ends = last && p != first;
+    }
+    const int at = append(2 * l, starts);
+    if (starts) L.runs[l][at] = r;
+    const int j = append(2 * l + 1, ends);
+    if (ends) L.joins[l][j] = {first, p + r.count, (int32_t)key, 0};
+  }
+}
+
+// The inclusive maximum over the wave's lanes up to this one.
+__device__ __forceinline__ int32_t wave_scan_max(int32_t x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int32_t y = __shfl_up(x, o);
+    if (lane >= o && y > x) x = y;
+  }
+  return x;
+}
+
 constexpr int kListThreads = 256;
 __global__ __launch_bounds__(kListThreads) void list_runs(const uint32_t* keys, int32_t T, int32_t limit, Lists L,
                                                           uint8_t* seen, int32_t* counters) {
@@ -342,11 +392,6 @@ __global__ __launch_bounds__(kListThreads) void list_runs(const uint32_t* keys, 
   list_place(L, key_at, T, p, there, key, first, append);
 }
 
-__global__ __launch_bounds__(256) void clear_bytes(uint8_t* p, int64_t n) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i * 4 < n; i += (int64_t)gridDim.x * 256)
-    ((uint32_t*)p)[i] = 0;
-}
-
 }  // namespace
 
 #define TIM_TRY(call)                  \
@@ -365,16 +410,18 @@ hipError_t launch_grouping(const Grouping& g, const int32_t* keys, bool keep_res
   L.n = g.n;
   L.lists = g.lists;
   for (int l = 0; l < g.lists; ++l) {
-    L.C[l] = g.C[l];
+    L.log_C[l] = g.log_C[l];
     L.runs[l] = (Run*)(w + g.runs[l]);
     L.joins[l] = (Join*)(w + g.joins[l]);
   }
   const int32_t limit = keep_rest ? g.n + 1 : g.n;
-  // whole words: seen has room for a multiple of 4 keys
-  if (seen) TIM_TRY((clear_bytes<<<256, 256, 0, s>>>(seen, g.n)));
-  if (g.T <= kGroupSmall) {
-    TIM_TRY((group_small<<<1, kSmallThreads, 0, s>>>(keys, (int32_t)g.T, g.passes, g.digit, limit, L, order, seen,
-                                                     counters)));
+  if (g.blocks == 1) {
+    if (g.T <= 4096)
+      TIM_TRY((group_small<12><<<1, kSmallThreads, 0, s>>>(keys, (int32_t)g.T, g.passes, g.digit, limit, L, order, seen,
+                                                           counters)));
+    else
+      TIM_TRY((group_small<14><<<1, kSmallThreads, 0, s>>>(keys, (int32_t)g.T, g.passes, g.digit, limit, L, order, seen,
+                                                           counters)));
     return hipSuccess;
   }
   uint32_t* sorted = (uint32_t*)(w + g.keys);
@@ -383,7 +430,8 @@ hipError_t launch_grouping(const Grouping& g, const int32_t* keys, bool keep_res
   for (int pass = 0; pass < g.passes; ++pass) {
     const bool last = pass + 1 == g.passes;
     const Source src = {keys, pass == 0 ? nullptr : pairs, g.T, g.n, g.per_block, pass * g.digit, g.digit};
-    TIM_TRY((sort_count<<<g.blocks, kSortThreads, 0, s>>>(src, hist, pass == 0 ? counters : nullptr)));
+    TIM_TRY((sort_count<<<g.blocks, kSortThreads, 0, s>>>(src, hist, pass == 0 ? counters : nullptr,
+                                                      pass == 0 ? seen : nullptr)));
     TIM_TRY((sort_place<<<g.blocks, kSortThreads, 0, s>>>(src, hist, last ? nullptr : pairs, order, sorted)));
   }
   TIM_TRY((list_runs<<<(unsigned)((g.T + kListThreads - 1) / kListThreads), kListThreads, 0, s>>>(

@@ -33,16 +33,18 @@ inline tim_status validate_embedding(const void* table, int32_t dtype, int32_t V
 
 // The embedding gradient's workspace: the grouping, a byte per token that
 // occurs, the partial sums of tokens with several runs.
+constexpr int kLogEmbedRun = 6;
+static_assert(TIM_EMBED_RUN == 1 << kLogEmbedRun, "the documented run");
 struct EmbedPlan {
   Grouping g;
   size_t seen, part, bytes;
 };
 inline EmbedPlan plan_embedding_backward(int64_t T, int32_t V, int32_t d) {
-  const int C[1] = {TIM_EMBED_RUN};
-  EmbedPlan p = {plan_grouping(T, V, 1, C), 0, 0, 0};
+  const int log_C[1] = {kLogEmbedRun};
+  EmbedPlan p = {plan_grouping(T, V, 1, log_C), 0, 0, 0};
   size_t at = p.g.bytes;
   p.seen = at, at += group_align((size_t)V);
-  p.part = at, at += T > TIM_EMBED_RUN ? group_align((size_t)run_slots(T, TIM_EMBED_RUN) * d * 4) : 0;
+  p.part = at, at += T > TIM_EMBED_RUN ? group_align((size_t)run_slots(T, kLogEmbedRun) * d * 4) : 0;
   p.bytes = at;
   return p;
 }
@@ -87,21 +89,30 @@ hipError_t launch_embedding_backward(const EmbedGradArgs& a, int dtype, void* ws
 
 // ------------------------------------------------------------------ adapters
 
-constexpr int kAdapterRun = 64;     // rows of one adapter that a workgroup takes together
+constexpr int kLogAdapterRun = 6;   // 64 rows of one adapter that a workgroup takes together
 constexpr int kShrinkChunk = 1024;  // elements of d whose products one workgroup sums
 
 inline int rank_padded(int r) { return (r + 15) / 16 * 16; }
 inline int chunks_of(int64_t n, int chunk) { return (int)((n + chunk - 1) / chunk); }
 
-// Tiles of 256 columns that a workgroup of the pass over grad takes, by N and
-// the rank alone (the sums of grad b are over that many columns).
-inline int pass_tiles(int64_t N, int rp) { return N < 32768 || rp > 32 ? 1 : rp > 16 ? 2 : 4; }
-// Rows of one adapter that it takes.
-constexpr int kMaxPassRows = 512;
-inline int pass_rows(int64_t T, int64_t column_groups) {
-  int rows = kMaxPassRows;
-  while (rows > 128 && (T + rows - 1) / rows * column_groups < 512) rows /= 2;
-  return rows;
+// The pass over grad sums grad b over chunks of 256 columns, and four chunks in
+// order, whatever a workgroup takes: `tiles` chunks (1, 2 or 4) of up to
+// 2^log_rows rows of one adapter. More tiles leave fewer partial sums of grad b,
+// more rows fewer of the weights' gradients; both have to leave work for 256 CUs.
+constexpr int kPassCols = 256, kChunkQuad = 4;
+constexpr int kLogMaxPassRows = 9, kMaxPassRows = 1 << kLogMaxPassRows;
+struct PassShape {
+  int tiles, log_rows;
+};
+inline PassShape pass_shape(int64_t T, int64_t N, int rp, bool contract) {
+  PassShape s = {1, kLogMaxPassRows};
+  auto workgroups = [&](int tiles, int log_rows) {
+    return ((T >> log_rows) + 1) * chunks_of(N, tiles * kPassCols);
+  };
+  while (contract && s.tiles < (rp <= 16 ? 4 : rp <= 32 ? 2 : 1) && workgroups(s.tiles * 2, s.log_rows) >= 512)
+    s.tiles *= 2;
+  while (s.log_rows > 7 && workgroups(s.tiles, s.log_rows) < 512) --s.log_rows;
+  return s;
 }
 
 // Workspaces: the grouping, then fp32 [chunks, T, rank_padded] of partial sums
@@ -109,17 +120,19 @@ inline int pass_rows(int64_t T, int64_t column_groups) {
 // weight gradients of adapters with several runs of rows.
 struct AdapterPlan {
   Grouping g;  // runs of kAdapterRun rows; the backward's for grad_a and for grad_b
-  int rp, x_chunks, tiles, g_chunks;
+  int rp, x_chunks, g_chunks;
+  PassShape of_x, of_grad;
   size_t u_part, v_part, u, v, a_part, b_part, seen, bytes;
 };
 inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r, bool backward) {
   AdapterPlan p = {};
   p.rp = rank_padded(r);
   p.x_chunks = chunks_of(d, kShrinkChunk);
-  p.tiles = pass_tiles(N, p.rp);
-  p.g_chunks = chunks_of(N, p.tiles * 256);
-  const int C[3] = {kAdapterRun, pass_rows(T, chunks_of(d, 256)), pass_rows(T, p.g_chunks)};
-  p.g = plan_grouping(T, n, backward ? 3 : 1, C);
+  p.of_x = pass_shape(T, d, p.rp, false);
+  p.of_grad = pass_shape(T, N, p.rp, true);
+  p.g_chunks = chunks_of(N, p.of_grad.tiles * kPassCols);
+  const int log_C[3] = {kLogAdapterRun, p.of_x.log_rows, p.of_grad.log_rows};
+  p.g = plan_grouping(T, n, backward ? 3 : 1, log_C);
   size_t at = p.g.bytes;
   const size_t rows = group_align((size_t)T * p.rp * 4);
   p.u_part = at, at += rows * p.x_chunks;
@@ -127,8 +140,8 @@ inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int
     p.v_part = at, at += rows * p.g_chunks;
     p.u = at, at += rows;
     p.v = at, at += rows;
-    p.a_part = at, at += T > C[1] ? group_align((size_t)run_slots(T, C[1]) * r * d * 4) : 0;
-    p.b_part = at, at += T > C[2] ? group_align((size_t)run_slots(T, C[2]) * r * N * 4) : 0;
+    p.a_part = at, at += p.g.max_joins[1] > 0 ? group_align((size_t)run_slots(T, log_C[1]) * r * d * 4) : 0;
+    p.b_part = at, at += p.g.max_joins[2] > 0 ? group_align((size_t)run_slots(T, log_C[2]) * r * N * 4) : 0;
     p.seen = at, at += group_align((size_t)n);
   }
   p.bytes = at;
