@@ -121,7 +121,8 @@ struct ShrinkArgs {
 template <class T, int JB>
 __global__ __launch_bounds__(kThreads) void shrink(ShrinkArgs a, RunList l) {
   __shared__ f32x4 lds[kWaves - 1][JB][4][64];
-  const Run run = own_run(l);
+  const Place at = place_of();
+  const Run run = run_of(l, at.item);
   if (run.count == 0 || run.key >= a.n) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
   const int j0 = blockIdx.z * JB * 16;
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(kThreads) void shrink(ShrinkArgs a, RunList l) {
   }
   f32x4 acc[JB][4] = {};
   constexpr int kEach = kShrinkChunk / kWaves;
-  const int from = blockIdx.y * kShrinkChunk + wave * kEach;
+  const int from = at.tile * kShrinkChunk + wave * kEach;
   auto step = [&](auto whole, int k0) {
     constexpr bool WHOLE = decltype(whole)::value;
     const int k = k0 + g * 8, n = a.d - k;
@@ -163,19 +164,20 @@ __global__ __launch_bounds__(kThreads) void shrink(ShrinkArgs a, RunList l) {
   } else {
     for (int k0 = from; k0 < a.d && k0 < from + kEach; k0 += 32) step(std::false_type{}, k0);
   }
-  store_sums<JB>(acc, lds, a.part + ((int64_t)blockIdx.y * a.T + run.first) * a.rp, a.r, a.rp, j0, run.count, lane, wave);
+  store_sums<JB>(acc, lds, a.part + ((int64_t)at.tile * a.T + run.first) * a.rp, a.r, a.rp, j0, run.count, lane, wave);
 }
 
 // out[place][j] = scale of the place's adapter * the sum of its chunks: in order
-// over `inner` chunks, then a sixteenth of these sums a group of 16 lanes, each
+// over `inner` chunks (1 or 2), then a sixteenth of these sums a group of 16 lanes, each
 // in order, then the groups in order. 64 consecutive elements a workgroup.
 __global__ __launch_bounds__(kThreads) void sum_chunks(const float* part, int64_t T, int rp, int chunks, int inner, int n,
                                                        const float* scales, float* out, RunList l) {
   __shared__ f32x4 lds[16][16];
-  const Run run = own_run(l);
+  const Place at = place_of();
+  const Run run = run_of(l, at.item);
   if (run.count == 0) return;
-  const int i = (blockIdx.y * 16 + threadIdx.x % 16) * 4, group = threadIdx.x / 16;
-  if (run.key >= n || (int)blockIdx.y * 64 >= run.count * rp) return;
+  const int i = ((int)at.tile * 16 + (int)threadIdx.x % 16) * 4, group = threadIdx.x / 16;
+  if (run.key >= n || (int)at.tile * 64 >= run.count * rp) return;
   const int outer = (chunks + inner - 1) / inner, per = (outer + 15) / 16 * inner;
   const int from = group * per, to = from + per < chunks ? from + per : chunks;
   const float* p = part + (int64_t)run.first * rp + i;
@@ -186,12 +188,10 @@ __global__ __launch_bounds__(kThreads) void sum_chunks(const float* part, int64_
 #pragma unroll 8
       for (int c = from; c < to; ++c) s += *(const f32x4*)(p + c * step);
     } else {
-#pragma unroll 2
-      for (int c = from; c < to; c += inner) {
+#pragma unroll 4
+      for (int c = from; c < to; c += 2) {
         f32x4 q = *(const f32x4*)(p + c * step);
-#pragma unroll
-        for (int k = 1; k < kChunkQuad; ++k)
-          if (k < inner && c + k < to) q += *(const f32x4*)(p + (c + k) * step);
+        if (c + 1 < to) q += *(const f32x4*)(p + (c + 1) * step);
         s += q;
       }
     }
@@ -226,10 +226,11 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
   constexpr int kTile = 64 + 4;    // a row of the 16 x 64 results
   constexpr bool kHold = JB <= 4;  // u and a tile's weights stay in registers for all rows
   __shared__ float tile[kWaves][16 * kTile];
-  const Run run = own_run(l);
+  const Place at = place_of();
+  const Run run = run_of(l, at.item);
   if (run.count == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
-  const int c_first = (blockIdx.y * kWaves + wave) * NT * 64;
+  const int c_first = (at.tile * kWaves + wave) * NT * 64;
   if (c_first >= a.N) return;
   const int my_row = l.order[run.first + (lane < run.count ? lane : run.count - 1)];  // of the run's row `lane`
   const O* base = (const O*)a.base;
@@ -432,10 +433,11 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   __shared__ __attribute__((aligned(16))) E wt[P::kTerms * JB * 16 * P::kW];
   __shared__ __attribute__((aligned(16))) W bt[CONTRACT ? JB * 16 * P::kB : 1];
   __shared__ int32_t rows[kMaxPassRows];
-  const Run run = own_run(l);
+  const Place at = place_of();
+  const Run run = run_of(l, at.item);
   if (run.count == 0 || run.key >= a.n) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane % 16, g = lane / 16;
-  const int c_first = blockIdx.y * CT * kPassCols, j0 = blockIdx.z * JB * 16;
+  const int c_first = at.tile * CT * kPassCols, j0 = blockIdx.z * JB * 16;
   const int tiles = (a.N - c_first + kPassCols - 1) / kPassCols < CT ? (a.N - c_first + kPassCols - 1) / kPassCols : CT;
   const int32_t* order = l.order + run.first;
   const float* w = a.w + (int64_t)run.first * a.rp + j0;
@@ -505,18 +507,18 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
       for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int at = (jb * 16 + wave * 4 + e) * P::kW + lane;
+          const int to = (jb * 16 + wave * 4 + e) * P::kW + lane;
           const float x = held_w[jb][e];
           if constexpr (P::FAST) {
             const __bf16 hi = (__bf16)x;
             const bool finite = __builtin_isfinite((float)hi);
             const float r1 = finite ? x - (float)hi : 0.f;
             const __bf16 mid = (__bf16)r1;
-            wt[at] = hi;
-            wt[JB * 16 * P::kW + at] = mid;
-            wt[2 * JB * 16 * P::kW + at] = (__bf16)(r1 - (float)mid);
+            wt[to] = hi;
+            wt[JB * 16 * P::kW + to] = mid;
+            wt[2 * JB * 16 * P::kW + to] = (__bf16)(r1 - (float)mid);
           } else {
-            wt[at] = x;
+            wt[to] = x;
           }
         }
     }
@@ -603,7 +605,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
     }
     if constexpr (CONTRACT) {
       const int t = t0 + wave * 16 + m;
-      float* p = a.part + ((int64_t)blockIdx.y * a.T + run.first + t) * a.rp + j0 + g * 4;
+      float* p = a.part + ((int64_t)at.tile * a.T + run.first + t) * a.rp + j0 + g * 4;
 #pragma unroll
       for (int jb = 0; jb < JB; ++jb)
         if (t < run.count && j0 + jb * 16 < a.rp) *(f32x4*)(p + jb * 16) = total[jb];
@@ -627,9 +629,15 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
                                  : f32x4{acc[ct][jb][0][q], acc[ct][jb][1][q], acc[ct][jb][2][q], acc[ct][jb][3][q]};
         float* p = out + (CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c);
         const int left = CONTRACT ? a.r - j : a.N - c;
+        if (left >= 4) {
+          f32x4 z = y;
+          if (add) z = load_n<true, f32x4, 4>(p, 4) + y;
+          __builtin_memcpy(p, &z, sizeof(z));
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < left) p[e] = add ? p[e] + y[e] : y[e];
+          for (int e = 0; e < 4; ++e)
+            if (e < left) p[e] = add ? p[e] + y[e] : y[e];
+        }
       }
 }
 
@@ -645,24 +653,25 @@ struct FinishArgs {
   const uint8_t* seen;
 };
 __global__ __launch_bounds__(kThreads) void finish(FinishArgs a) {
+  const Place at = place_of();
   const int z = blockIdx.z;
   const int64_t size = a.size[z], step = (int64_t)gridDim.y * kThreads;
   float* out = a.out[z];
   if (!out) return;
-  if ((int)blockIdx.x >= a.joins) {
-    for (int k = blockIdx.x - a.joins; k < a.n; k += gridDim.x - a.joins) {
+  if ((int)at.item >= a.joins) {
+    for (int k = (int)at.item - a.joins; k < a.n; k += gridDim.x - a.joins) {
       if (a.seen[k]) continue;
-      for (int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x; i < size; i += step) out[k * size + i] = 0.f;
+      for (int64_t i = (int64_t)at.tile * kThreads + threadIdx.x; i < size; i += step) out[k * size + i] = 0.f;
     }
     return;
   }
-  if ((int)blockIdx.x >= *a.l[z].n_joins) return;
-  const Join j = a.l[z].joins[blockIdx.x];
+  if ((int)at.item >= *a.l[z].n_joins) return;
+  const Join j = a.l[z].joins[at.item];
   if (j.key >= a.n) return;
   const int C = 1 << a.log_C[z], runs = (j.end - j.first + C - 1) / C;
   // the key's runs are two slots apart, the last one's is the odd one
   const float* part = a.part[z] + (int64_t)run_slot(j.first, a.log_C[z], false) * size;
-  for (int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x; i < size; i += step) {
+  for (int64_t i = (int64_t)at.tile * kThreads + threadIdx.x; i < size; i += step) {
     float s = 0.f;
     constexpr int kAhead = 8;  // loads in flight, added in order
     for (int k0 = 0; k0 < runs; k0 += kAhead) {
@@ -710,7 +719,7 @@ hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
   const bool many = l.max_runs * chunks_of(a.N, 4 * 64) >= 4096;
   if (a.rp <= 16) return many ? run_expand<T, O, FLAT, 1, 4>(a, l, s) : run_expand<T, O, FLAT, 1, 1>(a, l, s);
   if (a.rp <= 32) return many ? run_expand<T, O, FLAT, 2, 4>(a, l, s) : run_expand<T, O, FLAT, 2, 1>(a, l, s);
-  if (a.rp <= 64) return many ? run_expand<T, O, FLAT, 4, 4>(a, l, s) : run_expand<T, O, FLAT, 4, 1>(a, l, s);
+  if (a.rp <= 64) return run_expand<T, O, FLAT, 4, 1>(a, l, s);
   return run_expand<T, O, FLAT, 16, 1>(a, l, s);
 }
 template <class T, bool FLAT>
@@ -730,10 +739,8 @@ hipError_t run_pass(const PassArgs& a, const RunList& l, hipStream_t s) {
 template <class S, class W, bool CONTRACT>
 hipError_t run_pass(const PassArgs& a, int tiles, const RunList& l, hipStream_t s) {
   if (a.rp <= 16) {
-    if constexpr (CONTRACT) {
-      if (tiles == 4) return run_pass<S, W, CONTRACT, 1, 4>(a, l, s);
+    if constexpr (CONTRACT)
       if (tiles == 2) return run_pass<S, W, CONTRACT, 1, 2>(a, l, s);
-    }
     return run_pass<S, W, CONTRACT, 1, 1>(a, l, s);
   }
   if (a.rp <= 32) {
@@ -778,7 +785,7 @@ hipError_t backward_typed(const tim_adapters& ad, const AdapterGradArgs& a, int 
   if (e != hipSuccess) return e;
   if (a.grad_x || a.grad_a)
     TIM_LAUNCH((sum_chunks<<<dim3((unsigned)l.max_runs, p.rp), kThreads, 0, s>>>(pb.part, a.T, p.rp, p.g_chunks,
-                                                                                 kChunkQuad / p.of_grad.tiles, ad.n,
+                                                                                 kChunkPair / p.of_grad.tiles, ad.n,
                                                                                  ad.scales, v, l)));
   if (a.grad_x) {
     const ExpandArgs ea = {v, a.T, 1, ad.n, ad.r, p.rp, ad.d, nullptr, ad.a, a.accumulate_x ? a.grad_x : nullptr,

@@ -95,10 +95,7 @@ hipError_t embed_out(const EmbedArgs& a, int out_dtype, hipStream_t s) {
 // ------------------------------------------------------------------ gradient
 
 // Zeros in kZeroRows consecutive rows from r0 on, those of tokens that occur left out.
-#ifndef VZ
-#define VZ 1
-#endif
-constexpr int kZeroRows = VZ;
+constexpr int kZeroRows = 1;
 __device__ __forceinline__ void zero_rows(float* p, int64_t r0, int64_t rows, int64_t d, int64_t ld,
                                           const uint8_t* seen) {
   uint32_t skip = 0;
@@ -129,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void sum_runs(EmbedGradArgs a, RunList l,
     zero_rows(a.grad_table, ((blockIdx.x - l.max_runs) * gridDim.y + blockIdx.y) * kZeroRows, a.V, a.d, a.grad_ld, seen);
     return;
   }
-  const Run run = own_run(l);
+  const Run run = run_of(l, blockIdx.x);
   if (run.count == 0) return;
   const int c = (blockIdx.y * kThreads + threadIdx.x) * N;
   if (c >= a.d) return;

@@ -105,13 +105,25 @@ struct RunList {
   const int32_t* n_joins;
   int64_t max_runs, max_joins;
 };
-// This workgroup's run (count 0: none), asked for beside the list's length rather than after it.
 #if defined(__HIPCC__)
-__device__ __forceinline__ Run own_run(const RunList& l) {
-  Run r = l.runs[blockIdx.x];
+// The run (or other item) and the tile of it that a workgroup of a grid of
+// (items, tiles) takes: consecutive workgroups take consecutive tiles. They go to
+// the eight XCDs in turn; with the items first, of which a list leaves some
+// empty, 8 items with 4 runs among them would leave four XCDs without work (the
+// pass over grad of 2047 rows on a head of 151936 took 242 us so).
+struct Place {
+  uint32_t item, tile;
+};
+__device__ __forceinline__ Place place_of() {
+  const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
+  return {id / gridDim.y, id % gridDim.y};
+}
+// A run of the list (count 0: past its end), asked for beside the list's length rather than after it.
+__device__ __forceinline__ Run run_of(const RunList& l, uint32_t item) {
+  Run r = l.runs[item];
   const int32_t n = *l.n_runs;
   asm volatile("" ::"s"(n), "s"(r.first));  // both loads before the branch
-  if ((int)blockIdx.x >= n) r.count = 0;
+  if ((int)item >= n) r.count = 0;
   return r;
 }
 #endif

@@ -90,16 +90,16 @@ hipError_t launch_embedding_backward(const EmbedGradArgs& a, int dtype, void* ws
 // ------------------------------------------------------------------ adapters
 
 constexpr int kLogAdapterRun = 6;   // 64 rows of one adapter that a workgroup takes together
-constexpr int kShrinkChunk = 1024;  // elements of d whose products one workgroup sums
+constexpr int kShrinkChunk = 512;  // elements of d whose products one workgroup sums
 
 inline int rank_padded(int r) { return (r + 15) / 16 * 16; }
 inline int chunks_of(int64_t n, int chunk) { return (int)((n + chunk - 1) / chunk); }
 
-// The pass over grad sums grad b over chunks of 256 columns, and four chunks in
-// order, whatever a workgroup takes: `tiles` chunks (1, 2 or 4) of up to
+// The pass over grad sums grad b over chunks of 256 columns, and two chunks in
+// order, whatever a workgroup takes: `tiles` chunks (1 or 2) of up to
 // 2^log_rows rows of one adapter. More tiles leave fewer partial sums of grad b,
 // more rows fewer of the weights' gradients; both have to leave work for 256 CUs.
-constexpr int kPassCols = 256, kChunkQuad = 4;
+constexpr int kPassCols = 256, kChunkPair = 2;
 constexpr int kLogMaxPassRows = 9, kMaxPassRows = 1 << kLogMaxPassRows;
 struct PassShape {
   int tiles, log_rows;
@@ -109,7 +109,7 @@ inline PassShape pass_shape(int64_t T, int64_t N, int rp, bool contract) {
   auto workgroups = [&](int tiles, int log_rows) {
     return ((T >> log_rows) + 1) * chunks_of(N, tiles * kPassCols);
   };
-  while (contract && s.tiles < (rp <= 16 ? 4 : rp <= 32 ? 2 : 1) && workgroups(s.tiles * 2, s.log_rows) >= 512)
+  while (contract && s.tiles < (rp <= 32 ? 2 : 1) && workgroups(s.tiles * 2, s.log_rows) >= 512)
     s.tiles *= 2;
   while (s.log_rows > 7 && workgroups(s.tiles, s.log_rows) < 512) --s.log_rows;
   return s;
