@@ -1,0 +1,120 @@
+// Low-rank adapters of many requests beside a shared projection, and their
+// gradients, on gfx950. Rows are grouped by adapter (grouping.h); a workgroup
+// takes a run of up to 64 rows of one adapter:
+//
+//   shrink   u = x a^T          contraction over d, 1024 elements a workgroup
+//   expand   out = base + u b^T 256 columns a workgroup (backward: v a)
+//   contract v = grad b         contraction over N, 1024 elements a workgroup
+//   outer    sum_t src[t] w[t]  up to 512 rows of one adapter, 256 columns a workgroup
+//
+// x, a and b are 16 bits wide; their products with each other run on the 16-bit
+// matrix instructions. u and v stay in fp32, and so do the products that they
+// enter (16x16x4 fp32 MFMA): what a call moves, not what it computes, bounds it.
+
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "vocab.h"
+
+namespace tim {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+__device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+__device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+template <class T>
+using x8 = std::conditional_t<std::is_same_v<T, __bf16>, bf16x8, f16x8>;
+
+// N elements from p, the first n of them (the others zero); aligned to their
+// element only.
+template <class V, int N, class T>
+__device__ __forceinline__ V load_some(const T* p, int n) {
+  V r = {};
+  if (n >= N) {
+    __builtin_memcpy(&r, p, N * sizeof(T));
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < n) r[e] = p[e];
+  }
+  return r;
+}
+// The same where all N elements are known to lie in the array: without the
+// branches, so that many loads are in flight at once. WHOLE picks one by a
+// condition that is the same in every lane.
+template <bool WHOLE, class V, int N, class T>
+__device__ __forceinline__ V load_n(const T* p, int n) {
+  if constexpr (WHOLE) {
+    V r;
+    __builtin_memcpy(&r, p, N * sizeof(T));
+    return r;
+  } else {
+    return load_some<V, N>(p, n);
+  }
+}
+template <class T>
+using x4 = T __attribute__((ext_vector_type(4)));
+struct ExpandArgs {
+  const float* u;  // [chunks, T, rp], summed and scaled here
+  int64_t T;
+  int32_t chunks, n, r, rp, N;
+  const float* scales;
+  const void* w;   // [n, N, r], or [n, r, N] where FLAT
+  const void* base;
+  int64_t base_ld;
+  void* out;
+  int64_t out_ld;
+};
+
+struct PassArgs {
+  const void* src;  // [T, N]
+  int64_t ld, T;
+  const float* w;   // [T, rp]
+  const void* b;    // [n, N, r], the contraction's
+  float* part;      // [chunks, T, rp], the contraction's sums
+  int32_t n, r, rp, N;
+  float* out;       // [n, N, r], or [n, r, N] without the contraction
+  float* out_part;  // [slots] of the same
+  int32_t accumulate;
+};
+
+// The products over the runs of a list, see adapters_expand.hip and adapters_pass.hip.
+hipError_t launch_expand(const ExpandArgs& a, int dtype, int out_dtype, bool flat, const RunList& l, hipStream_t s);
+hipError_t launch_pass(const PassArgs& a, int src_dtype, int dtype, bool contract, int tiles, const RunList& l,
+                       hipStream_t s);
+
+#define TIM_LAUNCH(...)                      \
+  do {                                       \
+    __VA_ARGS__;                             \
+    const hipError_t e_ = hipGetLastError(); \
+    if (e_ != hipSuccess) return e_;         \
+  } while (0)
+
+}  // namespace tim

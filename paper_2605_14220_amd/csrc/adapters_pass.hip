@@ -1,0 +1,290 @@
+// Adapters: the pass over the rows that the backward makes once for both products that need it.
+
+#include <hip/hip_runtime.h>
+
+#include "adapters.h"
+
+namespace tim {
+namespace {
+
+// One pass over the columns of src = grad: for a run of one adapter's rows and
+// CT * 256 columns
+//   out[c][j]      sum over the rows of src[row][c] w[row][j]
+//   part[row][j] sum over the columns of src[row][c] b[c][j]    (CONTRACT)
+// and without the contraction the first alone, [j][c], of src = x.
+//
+// 64 rows of 256 columns at a time lie in LDS, read from memory once, and are
+// read from there along the rows for one product and along the columns for the
+// other. A wave takes 64 columns of the first and 16 rows of the second.
+//
+// FAST, where all is bf16: both on the bf16 matrix instructions, w as the sum of
+// three bf16 numbers, which holds all of its 24 bits. Otherwise on the fp32 ones.
+constexpr int kPassRows = 64;
+template <class S, class W, bool CONTRACT, int JB, int CT>
+struct Pass {
+  static constexpr bool FAST = std::is_same_v<S, __bf16> && std::is_same_v<W, __bf16>;
+  typedef std::conditional_t<FAST, __bf16, float> E;  // of the tile and of w in LDS
+  static constexpr int kTerms = FAST ? 3 : 1;
+  static constexpr int kPad = 16 / (int)sizeof(E);
+  static constexpr int kRow = kPassCols + kPad;  // elements from row to row of the tile
+  static constexpr int kW = kPassRows + kPad;    // of w, [term][j][row]
+  static constexpr int kB = CT * kPassCols + 8;  // of b, [j][c]
+  static constexpr int kLoads = kPassRows * kPassCols * (int)sizeof(S) / 16 / kThreads;  // 16 bytes a thread
+  static constexpr int kV = 16 / (int)sizeof(S);
+};
+template <class S, class W, bool CONTRACT, int JB, int CT>
+__global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
+  typedef Pass<S, W, CONTRACT, JB, CT> P;
+  typedef typename P::E E;
+  typedef S sv __attribute__((ext_vector_type(P::kV)));
+  typedef E ev __attribute__((ext_vector_type(P::kV)));
+  __shared__ __attribute__((aligned(16))) E tile[kPassRows * P::kRow];
+  __shared__ __attribute__((aligned(16))) E wt[P::kTerms * JB * 16 * P::kW];
+  __shared__ __attribute__((aligned(16))) W bt[CONTRACT ? JB * 16 * P::kB : 1];
+  __shared__ int32_t rows[kMaxPassRows];
+  const Place at = place_of();
+  const Run run = run_of(l, at.item);
+  if (run.count == 0 || run.key >= a.n) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane % 16, g = lane / 16;
+  const int c_first = at.tile * CT * kPassCols, j0 = blockIdx.z * JB * 16;
+  const int tiles = (a.N - c_first + kPassCols - 1) / kPassCols < CT ? (a.N - c_first + kPassCols - 1) / kPassCols : CT;
+  const int32_t* order = l.order + run.first;
+  const float* w = a.w + j0;
+
+  // rows past the run's end, up to a whole tile, are read as its last one
+  for (int t = tid; t < (run.count + kPassRows - 1) / kPassRows * kPassRows; t += kThreads)
+    rows[t] = order[t < run.count ? t : run.count - 1];
+  if constexpr (CONTRACT) {
+    // a thread takes 8 ranks of a column; the loads first, then their way into LDS
+    constexpr int kEach = JB * 16 * CT * kPassCols / 8 / kThreads;
+    const W* b = (const W*)a.b + ((int64_t)run.key * a.N + c_first) * a.r + j0;
+    x8<W> x[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int i = tid + k * kThreads, j = i % (JB * 2) * 8, c = i / (JB * 2);
+      x[k] = c_first + c < a.N ? load_some<x8<W>, 8>(b + (int64_t)c * a.r + j, a.r - j0 - j) : x8<W>{};
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int i = tid + k * kThreads, j = i % (JB * 2) * 8, c = i / (JB * 2);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bt[(j + e) * P::kB + c] = x[k][e];
+    }
+  }
+  __syncthreads();  // rows
+
+  // the tile's loads: thread t takes column group t % kAcross of the rows t / kAcross + k * kDown
+  constexpr int kAcross = kPassCols / P::kV, kDown = kThreads / kAcross;
+  sv held[P::kLoads];
+  f32x4 held_w[JB];
+  const int lc = tid % kAcross * P::kV, lr = tid / kAcross;
+  auto load_tile = [&](int t0, int ct) {
+    const int c = c_first + ct * kPassCols + lc;
+    const S* src = (const S*)a.src + c;
+    if (c_first + (ct + 1) * kPassCols <= a.N) {
+#pragma unroll
+      for (int k = 0; k < P::kLoads; ++k) held[k] = load_n<true, sv, P::kV>(src + rows[t0 + lr + k * kDown] * a.ld, 0);
+    } else {
+#pragma unroll
+      for (int k = 0; k < P::kLoads; ++k)
+        held[k] = load_some<sv, P::kV>(src + rows[t0 + lr + k * kDown] * a.ld, a.N - c);
+    }
+    if (ct == 0) {
+      const int t = t0 + lane;
+#pragma unroll
+      for (int jb = 0; jb < JB; ++jb) {
+        const int j = jb * 16 + wave * 4;
+        held_w[jb] = a.w && t < run.count && j0 + j < a.rp ? *(const f32x4*)(w + (int64_t)rows[t] * a.rp + j) : f32x4{};
+      }
+    }
+  };
+  auto store_tile = [&](int t0, int ct) {
+    if (t0 + kPassRows > run.count) {  // rows past the run's end
+#pragma unroll
+      for (int k = 0; k < P::kLoads; ++k)
+        if (t0 + lr + k * kDown >= run.count) held[k] = sv{};
+    }
+#pragma unroll
+    for (int k = 0; k < P::kLoads; ++k) {
+      ev x;
+#pragma unroll
+      for (int e = 0; e < P::kV; ++e) x[e] = (E)held[k][e];
+      *(ev*)(tile + (lr + k * kDown) * P::kRow + lc) = x;
+    }
+    if (ct == 0) {
+#pragma unroll
+      for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int to = (jb * 16 + wave * 4 + e) * P::kW + lane;
+          const float x = held_w[jb][e];
+          if constexpr (P::FAST) {
+            const __bf16 hi = (__bf16)x;
+            const bool finite = __builtin_isfinite((float)hi);
+            const float r1 = finite ? x - (float)hi : 0.f;
+            const __bf16 mid = (__bf16)r1;
+            wt[to] = hi;
+            wt[JB * 16 * P::kW + to] = mid;
+            wt[2 * JB * 16 * P::kW + to] = (__bf16)(r1 - (float)mid);
+          } else {
+            wt[to] = x;
+          }
+        }
+    }
+  };
+
+  f32x4 acc[CT][JB][4] = {};  // out
+  f32x4 total[JB];            // part, over the tiles so far
+  auto add_up = [](f32x4(&total)[JB], const f32x4(&sum)[JB], int ct) {
+#pragma unroll
+    for (int jb = 0; jb < JB; ++jb) total[jb] = ct == 0 ? sum[jb] : total[jb] + sum[jb];
+  };
+  load_tile(0, 0);
+  for (int t0 = 0; t0 < run.count; t0 += kPassRows) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      if (ct >= tiles) break;
+      __syncthreads();
+      store_tile(t0, ct);
+      __syncthreads();
+      if (ct + 1 < tiles)
+        load_tile(t0, ct + 1);
+      else if (t0 + kPassRows < run.count)
+        load_tile(t0 + kPassRows, 0);
+      if constexpr (P::FAST) {
+#pragma unroll
+        for (int ks = 0; ks < kPassRows / 32; ++ks) {
+          x4<E> x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            x[e] = *(const x4<E>*)(tile + (ks * 32 + g * 8 + e) * P::kRow + wave * 64 + 4 * m);
+          bf16x8 f[4];
+#pragma unroll
+          for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[nb][e] = x[e][nb];
+#pragma unroll
+          for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+              const bf16x8 wf = *(const bf16x8*)(wt + ((q * JB + jb) * 16 + m) * P::kW + ks * 32 + g * 8);
+#pragma unroll
+              for (int nb = 0; nb < 4; ++nb)
+                acc[ct][jb][nb] = CONTRACT ? mfma(wf, f[nb], acc[ct][jb][nb]) : mfma(f[nb], wf, acc[ct][jb][nb]);
+            }
+        }
+        if constexpr (CONTRACT) {
+          f32x4 sum[JB] = {};
+#pragma unroll
+          for (int ks = 0; ks < kPassCols / 32; ++ks) {
+            const bf16x8 x = *(const bf16x8*)(tile + (wave * 16 + m) * P::kRow + ks * 32 + g * 8);
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+              sum[jb] = mfma(*(const bf16x8*)(bt + (jb * 16 + m) * P::kB + ct * kPassCols + ks * 32 + g * 8), x, sum[jb]);
+          }
+          add_up(total, sum, ct);
+        }
+      } else {
+#pragma unroll 4
+        for (int q = 0; q < kPassRows / 4; ++q) {
+          const f32x4 x = *(const f32x4*)(tile + (q * 4 + g) * P::kRow + wave * 64 + 4 * m);
+#pragma unroll
+          for (int jb = 0; jb < JB; ++jb) {
+            const float wf = wt[(jb * 16 + m) * P::kW + q * 4 + g];
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb)
+              acc[ct][jb][nb] = CONTRACT ? mfma(wf, x[nb], acc[ct][jb][nb]) : mfma(x[nb], wf, acc[ct][jb][nb]);
+          }
+        }
+        if constexpr (CONTRACT) {
+          f32x4 sum[JB] = {};
+#pragma unroll 4
+          for (int ks = 0; ks < kPassCols / 16; ++ks) {
+            const f32x4 x = *(const f32x4*)(tile + (wave * 16 + m) * P::kRow + ks * 16 + g * 4);
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb) {
+              const x4<W> bf = *(const x4<W>*)(bt + (jb * 16 + m) * P::kB + ct * kPassCols + ks * 16 + g * 4);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sum[jb] = mfma((float)bf[e], x[e], sum[jb]);
+            }
+          }
+          add_up(total, sum, ct);
+        }
+      }
+    }
+    if constexpr (CONTRACT) {
+      const int t = t0 + wave * 16 + m;
+      if (t < run.count) {
+        float* p = a.part + ((int64_t)at.tile * a.T + rows[t]) * a.rp + j0 + g * 4;
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb)
+          if (j0 + jb * 16 < a.rp) *(f32x4*)(p + jb * 16) = total[jb];
+      }
+    }
+  }
+
+  if (!a.out) return;
+  const bool only = run.slot < 0, add = only && a.accumulate;
+  float* out = only ? a.out + (int64_t)run.key * a.r * a.N : a.out_part + (int64_t)run.slot * a.r * a.N;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        // four elements next to each other in memory: of the rank, or of the columns
+        const int c0 = c_first + ct * kPassCols + wave * 64;
+        const int j = j0 + jb * 16 + (CONTRACT ? 4 * g : m), c = c0 + (CONTRACT ? 4 * m + q : 16 * g + 4 * q);
+        if (j >= a.r || c >= a.N) continue;
+        const f32x4 y = CONTRACT ? acc[ct][jb][q]
+                                 : f32x4{acc[ct][jb][0][q], acc[ct][jb][1][q], acc[ct][jb][2][q], acc[ct][jb][3][q]};
+        float* p = out + (CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c);
+        const int left = CONTRACT ? a.r - j : a.N - c;
+        if (left >= 4) {
+          f32x4 z = y;
+          if (add) z = load_n<true, f32x4, 4>(p, 4) + y;
+          __builtin_memcpy(p, &z, sizeof(z));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < left) p[e] = add ? p[e] + y[e] : y[e];
+        }
+      }
+}
+
+template <class S, class W, bool CONTRACT, int JB, int CT>
+hipError_t run_pass(const PassArgs& a, const RunList& l, hipStream_t s) {
+  const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, CT * kPassCols), (unsigned)((a.rp + 63) / 64));
+  TIM_LAUNCH((pass<S, W, CONTRACT, JB, CT><<<grid, kThreads, 0, s>>>(a, l)));
+  return hipSuccess;
+}
+template <class S, class W, bool CONTRACT>
+hipError_t run_pass(const PassArgs& a, int tiles, const RunList& l, hipStream_t s) {
+  if (a.rp <= 16) {
+    if constexpr (CONTRACT)
+      if (tiles == 2) return run_pass<S, W, CONTRACT, 1, 2>(a, l, s);
+    return run_pass<S, W, CONTRACT, 1, 1>(a, l, s);
+  }
+  if (a.rp <= 32) return run_pass<S, W, CONTRACT, 2, 1>(a, l, s);
+  return run_pass<S, W, CONTRACT, 4, 1>(a, l, s);
+}
+
+template <class W>
+hipError_t run_pass(const PassArgs& a, int src_dtype, bool contract, int tiles, const RunList& l, hipStream_t s) {
+  if (!contract) return run_pass<W, W, false>(a, 1, l, s);
+  switch (src_dtype) {
+    case TIM_F32: return run_pass<float, W, true>(a, tiles, l, s);
+    case TIM_BF16: return run_pass<__bf16, W, true>(a, tiles, l, s);
+    default: return run_pass<_Float16, W, true>(a, tiles, l, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_pass(const PassArgs& a, int src_dtype, int dtype, bool contract, int tiles, const RunList& l,
+                       hipStream_t s) {
+  return dtype == TIM_BF16 ? run_pass<__bf16>(a, src_dtype, contract, tiles, l, s)
+                           : run_pass<_Float16>(a, src_dtype, contract, tiles, l, s);
+}
+
+}  // namespace tim

@@ -8,196 +8,17 @@
 
 #include <hip/hip_runtime.h>
 
-#include "grouping.h"
+#include "group_rows.h"
 
 namespace tim {
 namespace {
 
-constexpr int kSmallThreads = 1024;
-constexpr int kSmallWaves = kSmallThreads / 64;
 constexpr int kSortThreads = 256;
 constexpr int kSortWaves = kSortThreads / 64;
 
-// The lanes whose digit (of `bits` bits) is this lane's, among those of `active`.
-__device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, uint64_t active) {
-  uint64_t peers = active;
-  for (int b = 0; b < bits; ++b) {
-    const bool set = (digit >> b) & 1;
-    const uint64_t m = __ballot(set);
-    peers &= set ? m : ~m;
-  }
-  return peers;
-}
-__device__ __forceinline__ int lanes_below(uint64_t m) {
-  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-}
-
-__device__ __forceinline__ uint32_t key_of(const int32_t* keys, int64_t i, int32_t n) {
-  const uint32_t k = (uint32_t)keys[i];
-  return k < (uint32_t)n ? k : (uint32_t)n;
-}
-
-// Counts a wave's items of consecutive steps per digit: `count` is the wave's own.
-__device__ __forceinline__ void count_step(uint32_t digit, int bits, bool there, volatile uint32_t* count) {
-  const uint64_t peers = same_digit(digit, bits, __ballot(there));
-  if (there && lanes_below(peers) == 0) count[digit] += __popcll(peers);
-  lanes_in_order();
-}
-// The item's place: `place` holds the wave's next place of each digit.
-__device__ __forceinline__ uint32_t place_step(uint32_t digit, int bits, bool there, volatile uint32_t* place) {
-  const uint64_t peers = same_digit(digit, bits, __ballot(there));
-  const int below = lanes_below(peers);
-  const uint32_t at = there ? place[digit] : 0;
-  lanes_in_order();
-  if (there && below == 0) place[digit] = at + __popcll(peers);
-  lanes_in_order();
-  return at + below;
-}
-
-// The lists to make of the sorted keys.
-struct Lists {
-  int32_t n, lists;
-  int32_t log_C[kMaxRunLists];
-  Run* runs[kMaxRunLists];
-  Join* joins[kMaxRunLists];
-};
-// ------------------------------------------------------------- few rows
-
-// One workgroup. Items are the key above the row index, 32 bits: keys below 2^20
-// with 4096 rows, below 2^18 with 16384.
 template <int LOG_ROWS>
-__global__ __launch_bounds__(kSmallThreads) void group_small(const int32_t* keys, int32_t T, int passes, int digit_bits,
-                                                             int32_t limit, Lists L, int32_t* order, uint8_t* seen,
-                                                             int32_t* counters) {
-  constexpr int kRows = 1 << LOG_ROWS;
-  __shared__ uint32_t item[2][kRows + 64];
-  __shared__ uint32_t place[kSmallWaves][256];
-  __shared__ uint32_t wave_total[kSmallWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int bins = 1 << digit_bits;
-  // each wave takes consecutive items, a multiple of 64
-  const int per_wave = ((T + kSmallWaves - 1) / kSmallWaves + 63) / 64 * 64;
-  const int from = wave * per_wave, to = from + per_wave < T ? from + per_wave : T;
-  for (int i = tid; i < T; i += kSmallThreads) item[0][i] = key_of(keys, i, L.n) << LOG_ROWS | i;
-  if (seen)
-    for (int i = tid; i * 4 < L.n; i += kSmallThreads) ((uint32_t*)seen)[i] = 0;
-  int cur = 0;
-  for (int pass = 0; pass < passes; ++pass, cur ^= 1) {
-    const int shift = LOG_ROWS + pass * digit_bits;
-    for (int b = lane; b < bins; b += 64) place[wave][b] = 0;
-    __syncthreads();
-    for (int i = from; i < to; i += 64) {
-      const bool there = i + lane < to;
-      const uint32_t x = there ? item[cur][i + lane] : 0;
-      count_step((x >> shift) & (bins - 1), digit_bits, there, place[wave]);
-    }
-    __syncthreads();
-    // places: digits in order, the waves' items of one digit in wave order
-    uint32_t sum = 0, incl = 0, c[kSmallWaves] = {};
-    if (tid < 256) {
-      if (tid < bins) {
-#pragma unroll
-        for (int w = 0; w < kSmallWaves; ++w) c[w] = place[w][tid];
-#pragma unroll
-        for (int w = 0; w < kSmallWaves; ++w) {
-          const uint32_t x = c[w];
-          c[w] = sum;
-          sum += x;
-        }
-      }
-      incl = sum;
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) {
-        const uint32_t y = __shfl_up(incl, o);
-        if (lane >= o) incl += y;
-      }
-      if (lane == 63) wave_total[wave] = incl;
-    }
-    __syncthreads();
-    if (tid < bins) {
-      uint32_t before = incl - sum;
-      for (int w = 0; w < wave; ++w) before += wave_total[w];
-#pragma unroll
-      for (int w = 0; w < kSmallWaves; ++w) place[w][tid] = before + c[w];
-    }
-    __syncthreads();
-    for (int i = from; i < to; i += 64) {
-      const bool there = i + lane < to;
-      const uint32_t x = there ? item[cur][i + lane] : 0;
-      const uint32_t at = place_step((x >> shift) & (bins - 1), digit_bits, there, place[wave]);
-      if (there) item[cur ^ 1][at] = x;
-    }
-    __syncthreads();
-  }
-  const uint32_t* sorted = item[cur];
-  int32_t* head = (int32_t*)item[cur ^ 1];  // the first place of each key that occurs
-  // the sum of x over the threads before this one and the earlier `total`, which grows by the sum over all threads
-  auto scan = [&](uint32_t x, uint32_t& total) {
-    uint32_t incl = x;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const uint32_t y = __shfl_up(incl, o);
-      if (lane >= o) incl += y;
-    }
-    __syncthreads();  // the last scan's sums are read
-    if (lane == 63) wave_total[wave] = incl;
-    __syncthreads();
-    uint32_t before = total + incl - x;
-#pragma unroll
-    for (int w = 0; w < kSmallWaves; ++w) {
-      const uint32_t y = wave_total[w];
-      before += w < wave ? y : 0;
-      total += y;
-    }
-    return before;
-  };
-  uint32_t heads = 0;
-  for (int base = 0; base < T; base += kSmallThreads) {
-    const int p = base + tid;
-    const uint32_t x = p < T ? sorted[p] : 0, key = x >> LOG_ROWS;
-    const bool is = p < T && (p == 0 || sorted[p - 1] >> LOG_ROWS != key);
-    if (p < T) order[p] = x & (kRows - 1);
-    if (is && seen && (int32_t)key < L.n) seen[key] = 1;
-    const uint32_t at = scan(is, heads);
-    if (is) head[at] = p;
-  }
-  if (tid == 0) head[heads] = T;
-  __syncthreads();
-  // the keys from `limit` on are the last ones: key n alone
-  if ((int32_t)(sorted[T - 1] >> LOG_ROWS) >= limit) --heads;
-  for (int l = 0; l < L.lists; ++l) {
-    const int log_C = L.log_C[l], C = 1 << log_C;
-    uint32_t total = 0;  // runs, and joins from bit 16 on
-    for (uint32_t base = 0; base < heads; base += kSmallThreads) {
-      const uint32_t h = base + tid;
-      int first = 0, end = 0, key = 0;
-      if (h < heads) {
-        first = head[h];
-        end = head[h + 1];
-        key = sorted[first] >> LOG_ROWS;
-      }
-      const int runs = (end - first + C - 1) >> log_C;
-      const uint32_t at = scan(runs + (runs > 1 ? 1 << 16 : 0), total);
-      auto put = [&](int q, int first, int end, int key, int runs, int at) {
-        const int f = first + q * C;
-        L.runs[l][at + q] = {f, end - f < C ? end - f : C, key, runs > 1 ? run_slot(f, log_C, q == runs - 1) : -1};
-      };
-      constexpr int kOwn = 4;  // runs that the key's thread lists; more are the whole wave's work
-      for (int q = 0; q < kOwn; ++q)
-        if (q < runs) put(q, first, end, key, runs, at & 0xffff);
-      if (runs > 1) L.joins[l][at >> 16] = {first, end, key, 0};
-      for (uint64_t more = __ballot(runs > kOwn); more != 0; more &= more - 1) {
-        const int src = __builtin_ctzll(more);
-        const int f = __shfl(first, src), e = __shfl(end, src), k = __shfl(key, src), n = __shfl(runs, src);
-        const int a = __shfl((int)(at & 0xffff), src);
-        for (int q = kOwn + lane; q < n; q += 64) put(q, f, e, k, n, a);
-      }
-    }
-    if (tid == 0) {
-      counters[2 * l] = total & 0xffff;
-      counters[2 * l + 1] = total >> 16;
-    }
-  }
+__global__ __launch_bounds__(kSmallThreads) void group_small(GroupArgs a) {
+  group_rows<LOG_ROWS>(a);
 }
 
 // ------------------------------------------------------------ many rows
@@ -401,41 +222,50 @@ __global__ __launch_bounds__(kListThreads) void list_runs(const uint32_t* keys, 
     if (e_ != hipSuccess) return e_;   \
   } while (0)
 
+GroupArgs group_args(const Grouping& g, const int32_t* keys, bool keep_rest, uint8_t* seen, void* ws) {
+  char* w = (char*)ws;
+  GroupArgs a = {};
+  a.keys = keys;
+  a.T = (int32_t)g.T;
+  a.passes = g.passes;
+  a.digit = g.digit;
+  a.limit = keep_rest ? g.n + 1 : g.n;
+  a.lists.n = g.n;
+  a.lists.lists = g.lists;
+  for (int l = 0; l < g.lists; ++l) {
+    a.lists.log_C[l] = g.log_C[l];
+    a.lists.runs[l] = (Run*)(w + g.runs[l]);
+    a.lists.joins[l] = (Join*)(w + g.joins[l]);
+  }
+  a.order = (int32_t*)(w + g.order);
+  a.seen = seen;
+  a.counters = (int32_t*)(w + g.counters);
+  return a;
+}
+
 hipError_t launch_grouping(const Grouping& g, const int32_t* keys, bool keep_rest, uint8_t* seen, void* ws,
                            hipStream_t s) {
-  char* w = (char*)ws;
-  int32_t* counters = (int32_t*)(w + g.counters);
-  int32_t* order = (int32_t*)(w + g.order);
-  Lists L = {};
-  L.n = g.n;
-  L.lists = g.lists;
-  for (int l = 0; l < g.lists; ++l) {
-    L.log_C[l] = g.log_C[l];
-    L.runs[l] = (Run*)(w + g.runs[l]);
-    L.joins[l] = (Join*)(w + g.joins[l]);
-  }
-  const int32_t limit = keep_rest ? g.n + 1 : g.n;
+  const GroupArgs a = group_args(g, keys, keep_rest, seen, ws);
   if (g.blocks == 1) {
     if (g.T <= 4096)
-      TIM_TRY((group_small<12><<<1, kSmallThreads, 0, s>>>(keys, (int32_t)g.T, g.passes, g.digit, limit, L, order, seen,
-                                                           counters)));
+      TIM_TRY((group_small<12><<<1, kSmallThreads, 0, s>>>(a)));
     else
-      TIM_TRY((group_small<14><<<1, kSmallThreads, 0, s>>>(keys, (int32_t)g.T, g.passes, g.digit, limit, L, order, seen,
-                                                           counters)));
+      TIM_TRY((group_small<14><<<1, kSmallThreads, 0, s>>>(a)));
     return hipSuccess;
   }
+  char* w = (char*)ws;
   uint32_t* sorted = (uint32_t*)(w + g.keys);
   uint2* pairs = (uint2*)(w + g.pairs);
   uint32_t* hist = (uint32_t*)(w + g.hist);
   for (int pass = 0; pass < g.passes; ++pass) {
     const bool last = pass + 1 == g.passes;
     const Source src = {keys, pass == 0 ? nullptr : pairs, g.T, g.n, g.per_block, pass * g.digit, g.digit};
-    TIM_TRY((sort_count<<<g.blocks, kSortThreads, 0, s>>>(src, hist, pass == 0 ? counters : nullptr,
-                                                      pass == 0 ? seen : nullptr)));
-    TIM_TRY((sort_place<<<g.blocks, kSortThreads, 0, s>>>(src, hist, last ? nullptr : pairs, order, sorted)));
+    TIM_TRY((sort_count<<<g.blocks, kSortThreads, 0, s>>>(src, hist, pass == 0 ? a.counters : nullptr,
+                                                          pass == 0 ? seen : nullptr)));
+    TIM_TRY((sort_place<<<g.blocks, kSortThreads, 0, s>>>(src, hist, last ? nullptr : pairs, a.order, sorted)));
   }
   TIM_TRY((list_runs<<<(unsigned)((g.T + kListThreads - 1) / kListThreads), kListThreads, 0, s>>>(
-      sorted, (int32_t)g.T, limit, L, seen, counters)));
+      sorted, (int32_t)g.T, a.limit, a.lists, seen, a.counters)));
   return hipSuccess;
 }
 

@@ -121,6 +121,7 @@ inline PassShape pass_shape(int64_t T, int64_t N, int rp, bool contract) {
 struct AdapterPlan {
   Grouping g;  // runs of kAdapterRun rows; the backward's for grad_a and for grad_b
   int rp, x_chunks, g_chunks;
+  bool rows_alone;  // u by rows, beside the grouping
   PassShape of_x, of_grad;
   size_t u_part, v_part, u, v, a_part, b_part, seen, bytes;
 };
@@ -133,6 +134,8 @@ inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int
   p.g_chunks = chunks_of(N, p.of_grad.tiles * kPassCols);
   const int log_C[3] = {kLogAdapterRun, p.of_x.log_rows, p.of_grad.log_rows};
   p.g = plan_grouping(T, n, backward ? 3 : 1, log_C);
+  // few rows, whose adapters' weights for each come to at most 32 MB from the caches
+  p.rows_alone = T <= 1024 && T * p.rp * d * 2 <= (int64_t)32 << 20;
   size_t at = p.g.bytes;
   const size_t rows = group_align((size_t)T * p.rp * 4);
   p.u_part = at, at += rows * p.x_chunks;
