@@ -870,10 +870,10 @@ def logits_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: to
 # (include/tim_vocab.h)
 
 
-def _scratch(name, workspace, size, device) -> torch.Tensor:
-    """The caller's workspace, or a new one of the size."""
+def _scratch(name, workspace, device, size, *args) -> torch.Tensor:
+    """The caller's workspace, or a new one of size(*args) bytes."""
     if workspace is None:
-        return torch.empty(size, dtype=torch.uint8, device=device)
+        return torch.empty(size(*args), dtype=torch.uint8, device=device)
     _require_gpu(workspace)
     _on_one_gpu(name, device, workspace)
     return workspace
@@ -944,42 +944,70 @@ def embedding_backward(grad: torch.Tensor, tokens: torch.Tensor, V: int, scale: 
     if grad_table.shape != (V, d):
         raise ValueError("tim.embedding_backward: grad_table must be [V, d]")
     table_ld = _dense_rows("embedding_backward", "grad_table", grad_table)
-    ws = _scratch("embedding_backward", workspace, int(lib.tim_embedding_backward_workspace_size(T, V, d)), dev)
+    ws = _scratch("embedding_backward", workspace, dev, lib.tim_embedding_backward_workspace_size, T, V, d)
     _on_one_gpu("embedding_backward", dev, grad, tokens, grad_table)
     _launch(dev, lib.tim_embedding_backward, _ptr(grad), _DTYPES[grad.dtype], T, d, ld, _ptr(tokens), V, float(scale),
             _ptr(grad_table), table_ld, 1 if accumulate else 0, _ptr(ws), ws.numel() * ws.element_size())
     return grad_table
 
 
-class Adapters(NamedTuple):
+@dataclasses.dataclass
+class Adapters:
     """Low-rank adapters of a projection from d to N elements: adapter k adds scales[k] (x a[k]^T) b[k]^T. a [n, r, d] and
-    b [n, N, r] of one type (bf16 or fp16), contiguous; scales fp32 [n], None for ones."""
+    b [n, N, r] of one type (bf16 or fp16), contiguous; scales fp32 [n], None for ones. What the tensors hold may change
+    between calls, as training changes it."""
     a: torch.Tensor
     b: torch.Tensor
     scales: torch.Tensor | None = None
 
+    def __setattr__(self, field, value):
+        object.__setattr__(self, field, value)
+        object.__setattr__(self, "_built", None)
 
-def _adapters(name, ad, x, rows) -> tuple[_Adapters, int, int]:
+    def __getstate__(self):
+        return {f.name: getattr(self, f.name) for f in dataclasses.fields(self)}
+
+    def __setstate__(self, state):
+        for field, value in state.items():
+            setattr(self, field, value)
+
+    def _struct(self, name) -> _Adapters:
+        """The C struct. It is checked and filled once and kept until a field is set or a tensor's storage, size, strides or
+        type are others."""
+        a, b, scales = self.a, self.b, self.scales
+        layout = (_matrix_layout(a), _matrix_layout(b), None if scales is None else _matrix_layout(scales))
+        if self._built is not None and self._built[1] == layout:
+            return self._built[0]
+        if a.dtype not in (torch.bfloat16, torch.float16) or b.dtype != a.dtype:
+            raise TypeError(f"tim.{name}: a, b and x must be bf16, or all fp16")
+        if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
+            raise ValueError(f"tim.{name}: a [n, r, d] and b [n, N, r]")
+        n, r, d = a.shape
+        _int32(name, n, r, d, b.shape[1])
+        if scales is not None:
+            if scales.dtype != torch.float32:
+                raise TypeError(f"tim.{name}: scales must be fp32")
+            if scales.shape != (n,):
+                raise ValueError(f"tim.{name}: scales must be [n]")
+        _require_gpu(a, b, scales)
+        _on_one_gpu(name, a.device, b, scales)
+        s = _Adapters(_ptr(a), _ptr(b), _ptr(scales), _DTYPES[a.dtype], n, r, d, b.shape[1])
+        object.__setattr__(self, "_built", (s, layout))
+        return s
+
+
+def _adapters(name, adapters, x, rows) -> tuple[_Adapters, int, int]:
     """(C struct, T, row stride of x) of the adapters and the rows they apply to."""
-    if ad.a.dtype not in (torch.bfloat16, torch.float16) or ad.b.dtype != ad.a.dtype or x.dtype != ad.a.dtype:
+    ad = adapters._struct(name)
+    if x.dtype != adapters.a.dtype:
         raise TypeError(f"tim.{name}: a, b and x must be bf16, or all fp16")
-    if ad.a.dim() != 3 or ad.b.dim() != 3 or ad.a.shape[0] != ad.b.shape[0] or ad.a.shape[1] != ad.b.shape[2]:
-        raise ValueError(f"tim.{name}: a [n, r, d] and b [n, N, r]")
     x_ld = _dense_rows(name, "x", x)
-    n, r, d = ad.a.shape
-    if x.shape[1] != d:
+    T, d = x.shape
+    if d != ad.d:
         raise ValueError(f"tim.{name}: x must be [T, d]")
-    _int32(name, n, r, d, ad.b.shape[1])
-    T = x.shape[0]
     _row_vector(name, "rows", rows, T, torch.int32)
-    if ad.scales is not None:
-        if ad.scales.dtype != torch.float32:
-            raise TypeError(f"tim.{name}: scales must be fp32")
-        if ad.scales.shape != (n,):
-            raise ValueError(f"tim.{name}: scales must be [n]")
-    _require_gpu(ad.a, ad.b, ad.scales)
-    _on_one_gpu(name, x.device, x, rows, ad.a, ad.b, ad.scales)
-    return _Adapters(_ptr(ad.a), _ptr(ad.b), _ptr(ad.scales), _DTYPES[x.dtype], n, r, d, ad.b.shape[1]), T, x_ld
+    _on_one_gpu(name, x.device, x, rows, adapters.a)
+    return ad, T, x_ld
 
 
 def adapters_add_workspace_size(T: int, d: int, N: int, n: int, r: int) -> int:
@@ -996,10 +1024,10 @@ def adapters_add(base: torch.Tensor | None, x: torch.Tensor, rows: torch.Tensor,
     allowed."""
     lib = load_library()
     ad, T, x_ld = _adapters("adapters_add", adapters, x, rows)
-    dev = x.device
-    base_ld = ad.N
+    dev, N = x.device, ad.N
+    base_ld = N
     if base is not None:
-        if base.shape != (T, ad.N):
+        if base.shape != (T, N):
             raise ValueError("tim.adapters_add: base must be [T, N]")
         base_ld = _dense_rows("adapters_add", "base", base)
         _on_one_gpu("adapters_add", dev, base)
@@ -1007,14 +1035,18 @@ def adapters_add(base: torch.Tensor | None, x: torch.Tensor, rows: torch.Tensor,
             raise ValueError("tim.adapters_add: the output has base's type")
         dtype = base.dtype
     if out is None:
-        out = torch.empty((T, ad.N), dtype=x.dtype if dtype is None else dtype, device=dev)
-    elif out.shape != (T, ad.N) or (dtype is not None and out.dtype != dtype):
-        raise ValueError("tim.adapters_add: out must be [T, N] of the output's type")
+        out = x.new_empty(T, N) if base is None else base.new_empty(T, N)
+        out_ld = max(N, 1)
+        if base is None and dtype is not None and dtype != x.dtype:
+            out = torch.empty((T, N), dtype=dtype, device=dev)
+    else:
+        if out.shape != (T, N) or (dtype is not None and out.dtype != dtype):
+            raise ValueError("tim.adapters_add: out must be [T, N] of the output's type")
+        out_ld = _dense_rows("adapters_add", "out", out)
+        _on_one_gpu("adapters_add", dev, out)
     if out.dtype not in _DTYPES:
         raise TypeError("tim.adapters_add: the output is fp32, bf16 or fp16")
-    out_ld = _dense_rows("adapters_add", "out", out)
-    _on_one_gpu("adapters_add", dev, out)
-    ws = _scratch("adapters_add", workspace, int(lib.tim_adapters_add_workspace_size(T, ad.d, ad.N, ad.n, ad.r)), dev)
+    ws = _scratch("adapters_add", workspace, dev, lib.tim_adapters_add_workspace_size, T, ad.d, ad.N, ad.n, ad.r)
     _launch(dev, lib.tim_adapters_add, ctypes.byref(ad), _ptr(x), x_ld, _ptr(rows), T, _ptr(base), base_ld, _ptr(out),
             _DTYPES[out.dtype], out_ld, _ptr(ws), ws.numel() * ws.element_size())
     return out
@@ -1073,7 +1105,7 @@ def adapters_backward(grad: torch.Tensor, x: torch.Tensor, rows: torch.Tensor, a
             _require_gpu(t)
             _on_one_gpu(name, dev, t)
         weights.append(t if want else None)
-    ws = _scratch(name, workspace, int(lib.tim_adapters_backward_workspace_size(T, ad.d, ad.N, ad.n, ad.r)), dev)
+    ws = _scratch(name, workspace, dev, lib.tim_adapters_backward_workspace_size, T, ad.d, ad.N, ad.n, ad.r)
     grad_x = grad_x if want_x else None
     _launch(dev, lib.tim_adapters_backward, ctypes.byref(ad), _ptr(x), x_ld, _ptr(rows), T, _ptr(grad),
             _DTYPES[grad.dtype], grad_ld, _ptr(grad_x), gx_type, gx_ld, 1 if accumulate_x else 0, _ptr(weights[0]),

@@ -81,8 +81,18 @@ __device__ __forceinline__ V load_n(const T* p, int n) {
 }
 template <class T>
 using x4 = T __attribute__((ext_vector_type(4)));
+// x as the sum of three bf16 numbers, exactly where none overflows or is subnormal
+// (24 bits are three times 8); an infinity or NaN alone in the first.
+__device__ __forceinline__ void split3(float x, __bf16 (&t)[3]) {
+  t[0] = (__bf16)x;
+  const float r = __builtin_isfinite((float)t[0]) ? x - (float)t[0] : 0.f;
+  t[1] = (__bf16)r;
+  t[2] = (__bf16)(r - (float)t[1]);
+}
+
 struct ExpandArgs {
-  const float* u;  // [chunks, T, rp], summed and scaled here
+  const float* u;     // [chunks, T, rp], summed and scaled here
+  const void* terms;  // or null: u as bf16 [T, 3, rp], whose sums of three it is
   int64_t T;
   int32_t chunks, n, r, rp, N;
   const float* scales;

@@ -121,9 +121,11 @@ __global__ __launch_bounds__(kSmallThreads) void group_and_shrink(GroupArgs ga, 
 
 // out[row][j] = scale of the row's adapter * the sum of its chunks: in order over
 // `inner` chunks (1 or 2), then a sixteenth of these sums a group of 16 lanes, each
-// in order, then the groups in order. 64 consecutive elements a workgroup.
-__global__ __launch_bounds__(kThreads) void sum_chunks(const float* part, const int32_t* rows, int64_t T, int rp,
-                                                       int chunks, int inner, int n, const float* scales, float* out) {
+// in order, then the groups in order. 64 consecutive elements a workgroup. terms
+// (may be null): the same as three bf16 numbers each, [row][3][j].
+__global__ __launch_bounds__(kThreads) void sum_chunks(const float* part, const int32_t* rows, int64_t T, int r, int rp,
+                                                       int chunks, int inner, int n, const float* scales, float* out,
+                                                       __bf16* terms) {
   __shared__ f32x4 lds[16][16];
   const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 64, i = at + threadIdx.x % 16 * 4;
   if (at >= T * rp) return;
@@ -153,7 +155,24 @@ __global__ __launch_bounds__(kThreads) void sum_chunks(const float* part, const 
   if (group > 0 || !there) return;
 #pragma unroll
   for (int k = 1; k < 16; ++k) s += lds[k][threadIdx.x];
-  *(f32x4*)(out + i) = s * (scales ? scales[key] : 1.f);
+  s *= scales ? scales[key] : 1.f;
+  const int j = (int)(i % rp);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (j + e >= r) s[e] = 0.f;  // whatever the rows hold
+  *(f32x4*)(out + i) = s;
+  if (terms) {
+    x4<__bf16> q[3];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      __bf16 t[3];
+      split3(s[e], t);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) q[k][e] = t[k];
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *(x4<__bf16>*)(terms + (i / rp * 3 + k) * rp + j) = q[k];
+  }
 }
 
 // What follows the passes: of adapters with several runs of rows the runs' sums
@@ -242,11 +261,11 @@ hipError_t group_and_shrink_rows(const tim_adapters& ad, const void* x, int64_t 
   return ad.dtype == TIM_BF16 ? run_shrink<__bf16>(a, l, p.x_chunks, s) : run_shrink<_Float16>(a, l, p.x_chunks, s);
 }
 
-hipError_t launch_sum_chunks(const float* part, const int32_t* rows, int64_t T, int rp, int chunks, int inner, int n,
-                             const float* scales, float* out, hipStream_t s) {
+hipError_t launch_sum_chunks(const float* part, const int32_t* rows, int64_t T, int r, int rp, int chunks, int inner, int n,
+                             const float* scales, float* out, void* terms, hipStream_t s) {
   const int64_t blocks = (T * rp + 63) / 64, across = blocks < 1 << 20 ? blocks : 1 << 20;
   TIM_LAUNCH((sum_chunks<<<dim3((unsigned)across, (unsigned)((blocks + across - 1) / across)), kThreads, 0, s>>>(
-      part, rows, T, rp, chunks, inner, n, scales, out)));
+      part, rows, T, r, rp, chunks, inner, n, scales, out, (__bf16*)terms)));
   return hipSuccess;
 }
 
@@ -258,7 +277,7 @@ hipError_t launch_adapters_add(const tim_adapters& ad, const void* x, int64_t x_
   const AdapterPlan p = plan_adapters(T, ad.d, ad.N, ad.n, ad.r, false);
   const hipError_t e = group_and_shrink_rows(ad, x, x_ld, rows, T, true, nullptr, p, ws, s);
   if (e != hipSuccess) return e;
-  const ExpandArgs ea = {(const float*)((char*)ws + p.u_part), T, p.x_chunks, ad.n, ad.r, p.rp, ad.N, ad.scales, ad.b,
+  const ExpandArgs ea = {(const float*)((char*)ws + p.u_part), nullptr, T, p.x_chunks, ad.n, ad.r, p.rp, ad.N, ad.scales, ad.b,
                          base, base_ld, out, out_ld};
   return launch_expand(ea, ad.dtype, out_dtype, false, run_list(p.g, ws, 0), s);
 }
@@ -274,19 +293,21 @@ hipError_t launch_adapters_backward(const tim_adapters& ad, const AdapterGradArg
   float *u = nullptr, *v = (float*)(ws + p.v), *a_part = (float*)(ws + p.a_part), *b_part = (float*)(ws + p.b_part);
   if (a.grad_b) {
     u = (float*)(ws + p.u);
-    e = launch_sum_chunks((const float*)(ws + p.u_part), a.rows, a.T, p.rp, p.x_chunks, 1, ad.n, ad.scales, u, s);
+    e = launch_sum_chunks((const float*)(ws + p.u_part), a.rows, a.T, ad.r, p.rp, p.x_chunks, 1, ad.n, ad.scales, u, nullptr, s);
     if (e != hipSuccess) return e;
   }
   const PassArgs pb = {a.grad, a.grad_ld, a.T,      u,        ad.b,   (float*)(ws + p.v_part), ad.n, ad.r, p.rp,
                        ad.N,   a.grad_b,  b_part, a.accumulate_ab};
   e = launch_pass(pb, grad_dtype, ad.dtype, true, p.of_grad.tiles, lb, s);
   if (e != hipSuccess) return e;
+  // for the bf16 instructions of grad_x's product
+  void* terms = a.grad_x && ad.dtype == TIM_BF16 && p.rp <= 64 ? ws + p.v_terms : nullptr;
   if (a.grad_x || a.grad_a) {
-    e = launch_sum_chunks(pb.part, a.rows, a.T, p.rp, p.g_chunks, kChunkPair / p.of_grad.tiles, ad.n, ad.scales, v, s);
+    e = launch_sum_chunks(pb.part, a.rows, a.T, ad.r, p.rp, p.g_chunks, kChunkPair / p.of_grad.tiles, ad.n, ad.scales, v, terms, s);
     if (e != hipSuccess) return e;
   }
   if (a.grad_x) {
-    const ExpandArgs ea = {v, a.T, 1, ad.n, ad.r, p.rp, ad.d, nullptr, ad.a, a.accumulate_x ? a.grad_x : nullptr,
+    const ExpandArgs ea = {v, terms, a.T, 1, ad.n, ad.r, p.rp, ad.d, nullptr, ad.a, a.accumulate_x ? a.grad_x : nullptr,
                            a.gx_ld, a.grad_x, a.gx_ld};
     e = launch_expand(ea, ad.dtype, gx_dtype, true, l, s);
     if (e != hipSuccess) return e;

@@ -8,21 +8,26 @@ namespace tim {
 namespace {
 
 // out[row][c] = base[row][c] + sum_j u[row][j] w[c][j] for the rows of a run and
-// nt tiles of 64 columns a wave. The waves work by themselves: u and the first
-// tile's weights and rows of base are requested together, later ones a step
-// (16 rows of a tile) ahead, before the step's stores. The matrix instructions'
-// results pass through LDS, so that rows are read and written 64 columns at a time.
-template <class T, class O, bool FLAT, int JB>
+// 64 columns a wave. The first tile's weights and rows of base are requested
+// beside u, later ones a step (16 rows of a tile) ahead, before the step's
+// stores. The matrix instructions' results pass through LDS, so that rows are
+// read and written 64 columns at a time.
+//
+// AHEAD: a wave takes nt tiles by itself, u in registers. Otherwise the four
+// waves share u in LDS: its partial sums are then added up once (200 rows of 8
+// adapters of rank 64, d = N = 4096: 25 us a call against 30).
+template <class T, class O, bool FLAT, int JB, bool AHEAD>
 __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int nt) {
   constexpr int kTile = 64 + 4;    // a row of the 16 x 64 results
-  constexpr bool kHold = JB <= 4;  // u and a tile's weights stay in registers for all rows
+  constexpr bool kHold = JB <= 4;  // a tile's weights stay in registers for all rows
+  constexpr int kU = JB * 16 + 4;  // a row of u, apart in the banks
   __shared__ float tile[kWaves][16 * kTile];
+  __shared__ float shared_u[AHEAD ? 1 : 64 * kU];
   const Place at = place_of();
   const Run run = run_of(l, at.item);
   if (run.count == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
   const int c_first = (at.tile * kWaves + wave) * nt * 64;
-  if (c_first >= a.N) return;
   const int my_row = l.order[run.first + (lane < run.count ? lane : run.count - 1)];  // of the run's row `lane`
   const O* base = (const O*)a.base;
   if (run.key >= a.n) {  // no adapter
@@ -33,6 +38,7 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
     }
     return;
   }
+  if (AHEAD && c_first >= a.N) return;
   const int blocks = (run.count + 15) / 16, tiles = (a.N - c_first + 63) / 64 < nt ? (a.N - c_first + 63) / 64 : nt;
   const T* w = (const T*)a.w + (int64_t)run.key * a.r * a.N;
   // raw[nb][s]: the weight of rank jb * 16 + 4 g + s in column c0 + 16 nb + m; FLAT: raw[s][nb] in column c0 + 4 m + nb.
@@ -62,11 +68,11 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
     }
   };
   const float scale = a.scales ? a.scales[run.key] : 1.f;
-  // row m of a block, ranks jb * 16 + 4 g on
-  auto load_u = [&](int rb, int jb) {
-    const float* p = a.u + (int64_t)__shfl(my_row, rb * 16 + m) * a.rp + jb * 16 + g * 4;
+  // four ranks from j on of the run's row t
+  auto load_u = [&](int t, int j) {
+    const float* p = a.u + (int64_t)__shfl(my_row, t) * a.rp + j;
     f32x4 s = *(const f32x4*)p;
-#pragma unroll 4
+#pragma unroll 8
     for (int c = 1; c < a.chunks; ++c) s += *(const f32x4*)(p + (int64_t)c * a.T * a.rp);
     return s * scale;
   };
@@ -87,15 +93,24 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
 #pragma unroll
     for (int jb = 0; jb < JB; ++jb) weights(c_first, jb, raw[jb]);
   if (base) load_base(c_first, 0);
-  f32x4 u[kHold ? 4 : 1][kHold ? JB : 1];
-  if constexpr (kHold)
+  // u: where a wave takes several tiles by itself, for all blocks, row m of each; otherwise by way of LDS
+  f32x4 u[AHEAD ? 4 : 1][AHEAD ? JB : 1];
+  if constexpr (AHEAD) {
 #pragma unroll
     for (int rb = 0; rb < 4; ++rb)
       if (rb < blocks)
 #pragma unroll
-        for (int jb = 0; jb < JB; ++jb) u[rb][jb] = jb * 16 < a.rp ? load_u(rb, jb) : f32x4{};
+        for (int jb = 0; jb < JB; ++jb) u[rb][jb] = jb * 16 < a.rp ? load_u(rb * 16 + m, jb * 16 + g * 4) : f32x4{};
+  } else {
+    const int across = a.rp / 4;
+    for (int i = threadIdx.x; i < blocks * 16 * across; i += kThreads)
+      *(f32x4*)(shared_u + i / across * kU + i % across * 4) = load_u(i / across, i % across * 4);
+    __syncthreads();
+    if (c_first >= a.N) return;
+  }
+  auto from_lds = [&](int rb, int jb) { return *(const f32x4*)(shared_u + (rb * 16 + m) * kU + jb * 16 + g * 4); };
   float* const my = tile[wave];
-  for (int ct = 0; ct < tiles; ++ct) {
+  for (int ct = 0; ct < (AHEAD ? tiles : 1); ++ct) {
     const int c0 = c_first + ct * 64;
     f32x4 wf[kHold ? JB : 1][4];
     auto widen = [&](int k) {
@@ -107,30 +122,31 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
     if constexpr (kHold) {
 #pragma unroll
       for (int jb = 0; jb < JB; ++jb) widen(jb);
-      if (ct + 1 < tiles)
+      if (AHEAD && ct + 1 < tiles)
 #pragma unroll
         for (int jb = 0; jb < JB; ++jb) weights(c0 + 64, jb, raw[jb]);
     }
-#pragma unroll
+#pragma unroll(AHEAD ? 4 : 1)
     for (int rb = 0; rb < 4; ++rb) {
       if (rb >= blocks) break;
       f32x4 acc[4] = {};
-#pragma unroll
-      for (int jb = 0; jb < JB; ++jb) {
-        if (jb * 16 >= a.rp) break;
-        if constexpr (!kHold) {
-          weights(c0, jb, raw[0]);
-          widen(0);
-          u[0][0] = load_u(rb, jb);
-        }
-        const f32x4 uf = u[kHold ? rb : 0][kHold ? jb : 0];
+      auto multiply = [&](const f32x4(&h)[4], f32x4 uf) {
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
-          for (int nb = 0; nb < 4; ++nb) {
-            const f32x4(&h)[4] = wf[kHold ? jb : 0];
-            acc[nb] = mfma(FLAT ? h[s][nb] : h[nb][s], uf[s], acc[nb]);
-          }
+          for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(FLAT ? h[s][nb] : h[nb][s], uf[s], acc[nb]);
+      };
+      if constexpr (kHold) {
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb)
+          if (jb * 16 < a.rp) multiply(wf[jb], AHEAD ? u[AHEAD ? rb : 0][AHEAD ? jb : 0] : from_lds(rb, jb));
+      } else {
+#pragma unroll 1
+        for (int jb = 0; jb * 16 < a.rp; ++jb) {
+          weights(c0, jb, raw[0]);
+          widen(0);
+          multiply(wf[0], from_lds(rb, jb));
+        }
       }
       // lane: row m of the block, columns of the instruction's rows 4 g + i
 #pragma unroll
@@ -151,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
       if (base) {
         if (rb + 1 < blocks)
           load_base(c0, rb + 1);
-        else if (ct + 1 < tiles)
+        else if (AHEAD && ct + 1 < tiles)
           load_base(c0 + 64, 0);
       }
 #pragma unroll
@@ -176,21 +192,133 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
   }
 }
 
-template <class T, class O, bool FLAT>
-hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
-  // a wave takes four tiles where that leaves 16 waves for each of 256 CUs (48 rows of 32 adapters at d = 5120 on a
-  // head of 152064: 80 us against 95), of a high rank always one (its weights and rows of u fill the registers)
-  const int nt = a.rp <= 32 && l.max_runs * chunks_of(a.N, 4 * 64) >= 4096 ? 4 : 1;
+// out[row][c] = base[row][c] + sum_j u[row][j] w[j][c] on the bf16 matrix
+// instructions, for u as three bf16 numbers each, which hold all of its 24 bits
+// (ExpandArgs::terms). The rows of grad_x: 64 columns a wave, for all rows of a run.
+//
+// A lane takes 8 ranks of 4 columns and turns them in registers. Its results are
+// 16 columns of a row, stored as they are. KS: steps of 32 ranks; 0 for up to 16,
+// where one step holds the first and the second number and one the third.
+template <class O, int KS>
+__global__ __launch_bounds__(kThreads) void expand_flat(ExpandArgs a, RunList l) {
+  constexpr int kSteps = KS == 0 ? 1 : KS, kTerms = KS == 0 ? 2 : 3;
+  const Place at = place_of();
+  const Run run = run_of(l, at.item);
+  if (run.count == 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
+  const int c0 = ((int)at.tile * kWaves + wave) * 64;
+  if (c0 >= a.N) return;
+  const int my_row = l.order[run.first + (lane < run.count ? lane : run.count - 1)];  // of the run's row `lane`
+  const int blocks = (run.count + 15) / 16;
+  const bool there = run.key < a.n;
+  bf16x8 wf[kSteps][4], u[kSteps][kTerms][4];
+  if (there) {
+    const __bf16* w = (const __bf16*)a.w + (int64_t)run.key * a.r * a.N + c0 + 4 * m;
+#pragma unroll
+    for (int ks = 0; ks < kSteps; ++ks) {
+      const int j0 = ks * 32 + (KS == 0 ? g % 2 : g) * 8;
+      x4<__bf16> x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const __bf16* p = w + (int64_t)(j0 + e < a.r ? j0 + e : a.r - 1) * a.N;
+        x[e] = c0 + 64 <= a.N ? load_n<true, x4<__bf16>, 4>(p, 4) : load_some<x4<__bf16>, 4>(p, a.N - c0 - 4 * m);
+        if (a.r != a.rp && j0 + e >= a.r) x[e] = x4<__bf16>{};
+      }
+#pragma unroll
+      for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) wf[ks][nb][e] = x[e][nb];
+      if (KS == 2 && ks * 32 + g * 8 >= a.rp)  // a rank of up to 48
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb) wf[ks][nb] = bf16x8{};
+    }
+#pragma unroll
+    for (int rb = 0; rb < 4; ++rb)
+      if (rb < blocks) {
+        const __bf16* p = (const __bf16*)a.terms + (int64_t)__shfl(my_row, rb * 16 + m) * 3 * a.rp;
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+          for (int q = 0; q < kTerms; ++q) {
+            const int term = KS == 0 ? 2 * q + g / 2 : q, j = KS == 0 ? g % 2 * 8 : ks * 32 + g * 8;
+            u[ks][q][rb] = term < 3 && j < a.rp ? *(const bf16x8*)(p + term * a.rp + j) : bf16x8{};
+          }
+      }
+  }
+#pragma unroll
+  for (int rb = 0; rb < 4; ++rb) {
+    if (rb >= blocks) break;
+    f32x4 acc[4] = {};
+    if (there) {
+#pragma unroll
+      for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+        for (int q = 0; q < kTerms; ++q)
+#pragma unroll
+          for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(wf[ks][nb], u[ks][q][rb], acc[nb]);
+    }
+    const int64_t row = __shfl(my_row, rb * 16 + m);
+    const int c = c0 + 16 * g, n = a.N - c;
+    if (rb * 16 + m >= run.count || n <= 0) continue;
+    O* dst = (O*)a.out + row * a.out_ld + c;
+    const O* base = a.base ? (const O*)a.base + row * a.base_ld + c : nullptr;
+    constexpr int E = 16 / (int)sizeof(O);  // columns a store
+    typedef O ov __attribute__((ext_vector_type(E)));
+    if (n >= 16) {
+#pragma unroll
+      for (int s = 0; s < 16 / E; ++s) {
+        ov z, old = {};
+        if (base) old = load_n<true, ov, E>(base + s * E, E);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int k = s * E + e;  // acc[k % 4][k / 4]
+          const float y = acc[k % 4][k / 4];
+          z[e] = base ? (there ? narrow<O>((float)old[e] + y) : old[e]) : narrow<O>(y);
+        }
+        __builtin_memcpy(dst + s * E, &z, sizeof(z));
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (k < n) {
+          const float y = acc[k % 4][k / 4];
+          dst[k] = base ? (there ? narrow<O>((float)base[k] + y) : base[k]) : narrow<O>(y);
+        }
+    }
+  }
+}
+
+template <class T, class O, bool FLAT, bool AHEAD>
+hipError_t run_expand(const ExpandArgs& a, int nt, const RunList& l, hipStream_t s) {
   const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, nt * kWaves * 64));
   if (a.rp <= 16)
-    TIM_LAUNCH((expand<T, O, FLAT, 1><<<grid, kThreads, 0, s>>>(a, l, nt)));
+    TIM_LAUNCH((expand<T, O, FLAT, 1, AHEAD><<<grid, kThreads, 0, s>>>(a, l, nt)));
   else if (a.rp <= 32)
-    TIM_LAUNCH((expand<T, O, FLAT, 2><<<grid, kThreads, 0, s>>>(a, l, nt)));
+    TIM_LAUNCH((expand<T, O, FLAT, 2, AHEAD><<<grid, kThreads, 0, s>>>(a, l, nt)));
   else if (a.rp <= 64)
-    TIM_LAUNCH((expand<T, O, FLAT, 4><<<grid, kThreads, 0, s>>>(a, l, nt)));
+    TIM_LAUNCH((expand<T, O, FLAT, 4, false><<<grid, kThreads, 0, s>>>(a, l, nt)));
   else
-    TIM_LAUNCH((expand<T, O, FLAT, 16><<<grid, kThreads, 0, s>>>(a, l, nt)));
+    TIM_LAUNCH((expand<T, O, FLAT, 16, false><<<grid, kThreads, 0, s>>>(a, l, nt)));
   return hipSuccess;
+}
+template <class T, class O, bool FLAT>
+hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
+  if constexpr (FLAT && std::is_same_v<T, __bf16>) {
+    if (a.terms) {
+      const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, kWaves * 64));
+      if (a.rp <= 16)
+        TIM_LAUNCH((expand_flat<O, 0><<<grid, kThreads, 0, s>>>(a, l)));
+      else if (a.rp <= 32)
+        TIM_LAUNCH((expand_flat<O, 1><<<grid, kThreads, 0, s>>>(a, l)));
+      else
+        TIM_LAUNCH((expand_flat<O, 2><<<grid, kThreads, 0, s>>>(a, l)));
+      return hipSuccess;
+    }
+  }
+  // a wave takes four tiles where that leaves 16 waves for each of 256 CUs (48 rows of 32 adapters at d = 5120 on a
+  // head of 152064: 80 us against 95), of a high rank always one (its weights and rows of u fill the registers)
+  if (!FLAT && a.rp <= 32 && l.max_runs * chunks_of(a.N, 4 * 64) >= 4096) return run_expand<T, O, FLAT, !FLAT>(a, 4, l, s);
+  return run_expand<T, O, FLAT, false>(a, 1, l, s);
 }
 template <class T, class O>
 hipError_t run_expand(const ExpandArgs& a, bool flat, const RunList& l, hipStream_t s) {

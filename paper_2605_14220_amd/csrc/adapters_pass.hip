@@ -119,13 +119,10 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
           const int to = (jb * 16 + wave * 4 + e) * P::kW + lane;
           const float x = held_w[jb][e];
           if constexpr (P::FAST) {
-            const __bf16 hi = (__bf16)x;
-            const bool finite = __builtin_isfinite((float)hi);
-            const float r1 = finite ? x - (float)hi : 0.f;
-            const __bf16 mid = (__bf16)r1;
-            wt[to] = hi;
-            wt[JB * 16 * P::kW + to] = mid;
-            wt[2 * JB * 16 * P::kW + to] = (__bf16)(r1 - (float)mid);
+            __bf16 t[3];
+            split3(x, t);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) wt[k * JB * 16 * P::kW + to] = t[k];
           } else {
             wt[to] = x;
           }

@@ -123,7 +123,7 @@ struct AdapterPlan {
   int rp, x_chunks, g_chunks;
   bool rows_alone;  // u by rows, beside the grouping
   PassShape of_x, of_grad;
-  size_t u_part, v_part, u, v, a_part, b_part, seen, bytes;
+  size_t u_part, v_part, u, v, v_terms, a_part, b_part, seen, bytes;
 };
 inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r, bool backward) {
   AdapterPlan p = {};
@@ -143,6 +143,7 @@ inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int
     p.v_part = at, at += rows * p.g_chunks;
     p.u = at, at += rows;
     p.v = at, at += rows;
+    p.v_terms = at, at += group_align((size_t)T * p.rp * 6);
     p.a_part = at, at += p.g.max_joins[1] > 0 ? group_align((size_t)run_slots(T, log_C[1]) * r * d * 4) : 0;
     p.b_part = at, at += p.g.max_joins[2] > 0 ? group_align((size_t)run_slots(T, log_C[2]) * r * N * 4) : 0;
     p.seen = at, at += group_align((size_t)n);
