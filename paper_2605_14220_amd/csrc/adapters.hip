@@ -274,7 +274,7 @@ hipError_t launch_sum_chunks(const float* part, const int32_t* rows, int64_t T, 
 hipError_t launch_adapters_add(const tim_adapters& ad, const void* x, int64_t x_ld, const int32_t* rows, int64_t T,
                                const void* base, int64_t base_ld, void* out, int out_dtype, int64_t out_ld, void* ws,
                                hipStream_t s) {
-  const AdapterPlan p = plan_adapters(T, ad.d, ad.N, ad.n, ad.r, false);
+  const AdapterPlan p = plan_adapters(T, ad.d, ad.N, ad.n, ad.r, 0);
   const hipError_t e = group_and_shrink_rows(ad, x, x_ld, rows, T, true, nullptr, p, ws, s);
   if (e != hipSuccess) return e;
   const ExpandArgs ea = {(const float*)((char*)ws + p.u_part), nullptr, T, p.x_chunks, ad.n, ad.r, p.rp, ad.N, ad.scales, ad.b,
@@ -284,7 +284,7 @@ hipError_t launch_adapters_add(const tim_adapters& ad, const void* x, int64_t x_
 
 hipError_t launch_adapters_backward(const tim_adapters& ad, const AdapterGradArgs& a, int grad_dtype, int gx_dtype,
                                     void* workspace, hipStream_t s) {
-  const AdapterPlan p = plan_adapters(a.T, ad.d, ad.N, ad.n, ad.r, true);
+  const AdapterPlan p = plan_adapters(a.T, ad.d, ad.N, ad.n, ad.r, pass_cols(grad_dtype, ad.dtype));
   char* ws = (char*)workspace;
   uint8_t* seen = (uint8_t*)(ws + p.seen);
   hipError_t e = group_and_shrink_rows(ad, a.x, a.x_ld, a.rows, a.T, a.grad_b != nullptr, seen, p, ws, s);
@@ -303,7 +303,7 @@ hipError_t launch_adapters_backward(const tim_adapters& ad, const AdapterGradArg
   // for the bf16 instructions of grad_x's product
   void* terms = a.grad_x && ad.dtype == TIM_BF16 && p.rp <= 64 ? ws + p.v_terms : nullptr;
   if (a.grad_x || a.grad_a) {
-    e = launch_sum_chunks(pb.part, a.rows, a.T, ad.r, p.rp, p.g_chunks, kChunkPair / p.of_grad.tiles, ad.n, ad.scales, v, terms, s);
+    e = launch_sum_chunks(pb.part, a.rows, a.T, ad.r, p.rp, p.g_chunks, kTilePair / p.of_grad.tiles, ad.n, ad.scales, v, terms, s);
     if (e != hipSuccess) return e;
   }
   if (a.grad_x) {

@@ -8,18 +8,19 @@ namespace tim {
 namespace {
 
 // out[row][c] = base[row][c] + sum_j u[row][j] w[c][j] for the rows of a run and
-// 64 columns a wave. The first tile's weights and rows of base are requested
-// beside u, later ones a step (16 rows of a tile) ahead, before the step's
-// stores. The matrix instructions' results pass through LDS, so that rows are
+// 64 columns a wave. Weights and the first rows of base are requested beside u,
+// later rows of base a step (16 rows of a tile) ahead, before the step's stores. The matrix instructions' results pass through LDS, so that rows are
 // read and written 64 columns at a time.
 //
-// AHEAD: a wave takes nt tiles by itself, u in registers. Otherwise the four
+// AHEAD: a wave takes 4 / JB tiles by itself, u in registers and all tiles'
+// weights requested first. Otherwise the four
 // waves share u in LDS: its partial sums are then added up once (200 rows of 8
 // adapters of rank 64, d = N = 4096: 25 us a call against 30).
 template <class T, class O, bool FLAT, int JB, bool AHEAD>
-__global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int nt) {
+__global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
   constexpr int kTile = 64 + 4;    // a row of the 16 x 64 results
   constexpr bool kHold = JB <= 4;  // a tile's weights stay in registers for all rows
+  constexpr int NT = AHEAD ? 4 / JB : 1;
   constexpr int kU = JB * 16 + 4;  // a row of u, apart in the banks
   __shared__ float tile[kWaves][16 * kTile];
   __shared__ float shared_u[AHEAD ? 1 : 64 * kU];
@@ -27,19 +28,19 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
   const Run run = run_of(l, at.item);
   if (run.count == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
-  const int c_first = (at.tile * kWaves + wave) * nt * 64;
+  const int c_first = (at.tile * kWaves + wave) * NT * 64;
   const int my_row = l.order[run.first + (lane < run.count ? lane : run.count - 1)];  // of the run's row `lane`
   const O* base = (const O*)a.base;
   if (run.key >= a.n) {  // no adapter
     for (int t = 0; t < run.count; ++t) {
       const int64_t row = __shfl(my_row, t);
-      for (int c = c_first + lane; c < a.N && c < c_first + nt * 64; c += 64)
+      for (int c = c_first + lane; c < a.N && c < c_first + NT * 64; c += 64)
         ((O*)a.out)[row * a.out_ld + c] = base ? base[row * a.base_ld + c] : (O)0.f;
     }
     return;
   }
   if (AHEAD && c_first >= a.N) return;
-  const int blocks = (run.count + 15) / 16, tiles = (a.N - c_first + 63) / 64 < nt ? (a.N - c_first + 63) / 64 : nt;
+  const int blocks = (run.count + 15) / 16, tiles = (a.N - c_first + 63) / 64 < NT ? (a.N - c_first + 63) / 64 : NT;
   const T* w = (const T*)a.w + (int64_t)run.key * a.r * a.N;
   // raw[nb][s]: the weight of rank jb * 16 + 4 g + s in column c0 + 16 nb + m; FLAT: raw[s][nb] in column c0 + 4 m + nb.
   // Without FLAT the four ranks may reach into the next columns' weights (up to 15 columns on): zeros take their place.
@@ -76,7 +77,7 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
     for (int c = 1; c < a.chunks; ++c) s += *(const f32x4*)(p + (int64_t)c * a.T * a.rp);
     return s * scale;
   };
-  x4<T> raw[kHold ? JB : 1][4];
+  x4<T> raw[NT][kHold ? JB : 1][4];
   x4<O> old[4];
   // what lane (m, g) reads and writes of a step: row 4 q + g, columns 4 m .. 4 m + 3
   auto load_base = [&](int c0, int rb) {
@@ -91,7 +92,10 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
   };
   if constexpr (kHold)
 #pragma unroll
-    for (int jb = 0; jb < JB; ++jb) weights(c_first, jb, raw[jb]);
+    for (int ct = 0; ct < NT; ++ct)
+      if (ct == 0 || ct < tiles)
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) weights(c_first + ct * 64, jb, raw[ct][jb]);
   if (base) load_base(c_first, 0);
   // u: where a wave takes several tiles by itself, for all blocks, row m of each; otherwise by way of LDS
   f32x4 u[AHEAD ? 4 : 1][AHEAD ? JB : 1];
@@ -110,21 +114,20 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
   }
   auto from_lds = [&](int rb, int jb) { return *(const f32x4*)(shared_u + (rb * 16 + m) * kU + jb * 16 + g * 4); };
   float* const my = tile[wave];
-  for (int ct = 0; ct < (AHEAD ? tiles : 1); ++ct) {
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    if (AHEAD && ct >= tiles) break;
     const int c0 = c_first + ct * 64;
     f32x4 wf[kHold ? JB : 1][4];
-    auto widen = [&](int k) {
+    auto widen = [&](int jb) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int s = 0; s < 4; ++s) wf[k][q][s] = (float)raw[k][q][s];
+        for (int s = 0; s < 4; ++s) wf[jb][q][s] = (float)raw[ct][jb][q][s];
     };
     if constexpr (kHold) {
 #pragma unroll
       for (int jb = 0; jb < JB; ++jb) widen(jb);
-      if (AHEAD && ct + 1 < tiles)
-#pragma unroll
-        for (int jb = 0; jb < JB; ++jb) weights(c0 + 64, jb, raw[jb]);
     }
 #pragma unroll(AHEAD ? 4 : 1)
     for (int rb = 0; rb < 4; ++rb) {
@@ -143,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l, int 
       } else {
 #pragma unroll 1
         for (int jb = 0; jb * 16 < a.rp; ++jb) {
-          weights(c0, jb, raw[0]);
+          weights(c0, jb, raw[0][0]);
           widen(0);
           multiply(wf[0], from_lds(rb, jb));
         }
@@ -289,16 +292,17 @@ __global__ __launch_bounds__(kThreads) void expand_flat(ExpandArgs a, RunList l)
 }
 
 template <class T, class O, bool FLAT, bool AHEAD>
-hipError_t run_expand(const ExpandArgs& a, int nt, const RunList& l, hipStream_t s) {
-  const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, nt * kWaves * 64));
+hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
+  const int tiles = !AHEAD ? 1 : a.rp <= 16 ? 4 : 2;
+  const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, tiles * kWaves * 64));
   if (a.rp <= 16)
-    TIM_LAUNCH((expand<T, O, FLAT, 1, AHEAD><<<grid, kThreads, 0, s>>>(a, l, nt)));
+    TIM_LAUNCH((expand<T, O, FLAT, 1, AHEAD><<<grid, kThreads, 0, s>>>(a, l)));
   else if (a.rp <= 32)
-    TIM_LAUNCH((expand<T, O, FLAT, 2, AHEAD><<<grid, kThreads, 0, s>>>(a, l, nt)));
+    TIM_LAUNCH((expand<T, O, FLAT, 2, AHEAD><<<grid, kThreads, 0, s>>>(a, l)));
   else if (a.rp <= 64)
-    TIM_LAUNCH((expand<T, O, FLAT, 4, false><<<grid, kThreads, 0, s>>>(a, l, nt)));
+    TIM_LAUNCH((expand<T, O, FLAT, 4, false><<<grid, kThreads, 0, s>>>(a, l)));
   else
-    TIM_LAUNCH((expand<T, O, FLAT, 16, false><<<grid, kThreads, 0, s>>>(a, l, nt)));
+    TIM_LAUNCH((expand<T, O, FLAT, 16, false><<<grid, kThreads, 0, s>>>(a, l)));
   return hipSuccess;
 }
 template <class T, class O, bool FLAT>
@@ -315,10 +319,10 @@ hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
       return hipSuccess;
     }
   }
-  // a wave takes four tiles where that leaves 16 waves for each of 256 CUs (48 rows of 32 adapters at d = 5120 on a
+  // a wave takes several tiles where that leaves 16 waves for each of 256 CUs (48 rows of 32 adapters at d = 5120 on a
   // head of 152064: 80 us against 95), of a high rank always one (its weights and rows of u fill the registers)
-  if (!FLAT && a.rp <= 32 && l.max_runs * chunks_of(a.N, 4 * 64) >= 4096) return run_expand<T, O, FLAT, !FLAT>(a, 4, l, s);
-  return run_expand<T, O, FLAT, false>(a, 1, l, s);
+  if (!FLAT && a.rp <= 32 && l.max_runs * chunks_of(a.N, 4 * 64) >= 4096) return run_expand<T, O, FLAT, !FLAT>(a, l, s);
+  return run_expand<T, O, FLAT, false>(a, l, s);
 }
 template <class T, class O>
 hipError_t run_expand(const ExpandArgs& a, bool flat, const RunList& l, hipStream_t s) {

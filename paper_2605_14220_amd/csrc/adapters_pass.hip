@@ -8,34 +8,41 @@ namespace tim {
 namespace {
 
 // One pass over the columns of src = grad: for a run of one adapter's rows and
-// CT * 256 columns
+// CT tiles of columns
 //   out[c][j]      sum over the rows of src[row][c] w[row][j]
 //   part[row][j] sum over the columns of src[row][c] b[c][j]    (CONTRACT)
 // and without the contraction the first alone, [j][c], of src = x.
 //
-// 64 rows of 256 columns at a time lie in LDS, read from memory once, and are
+// 64 rows of 256 (otherwise 128) columns at a time lie in LDS, read from memory once, and are
 // read from there along the rows for one product and along the columns for the
-// other. A wave takes 64 columns of the first and 16 rows of the second.
+// other. A wave takes a quarter of the columns of the first and 16 rows of the
+// second.
 //
 // FAST, where all is bf16: both on the bf16 matrix instructions, w as the sum of
-// three bf16 numbers, which holds all of its 24 bits. Otherwise on the fp32 ones.
+// three bf16 numbers, which holds all of its 24 bits. Otherwise on the fp32 ones,
+// whose tile of 128 columns has the same bytes: three workgroups fit a CU, of one
+// with 256 columns one (the gradients of 150 rows on a head of 50257, fp32: 25 us).
 constexpr int kPassRows = 64;
 template <class S, class W, bool CONTRACT, int JB, int CT>
 struct Pass {
   static constexpr bool FAST = std::is_same_v<S, __bf16> && std::is_same_v<W, __bf16>;
   typedef std::conditional_t<FAST, __bf16, float> E;  // of the tile and of w in LDS
+  static constexpr int kCols = FAST ? kPassCols : kPassColsF32;  // of a tile
+  static constexpr int NB = kCols / 64;  // blocks of 16 columns a wave
   static constexpr int kTerms = FAST ? 3 : 1;
   static constexpr int kPad = 16 / (int)sizeof(E);
-  static constexpr int kRow = kPassCols + kPad;  // elements from row to row of the tile
+  static constexpr int kRow = kCols + kPad;  // elements from row to row of the tile
   static constexpr int kW = kPassRows + kPad;    // of w, [term][j][row]
-  static constexpr int kB = CT * kPassCols + 8;  // of b, [j][c]
-  static constexpr int kLoads = kPassRows * kPassCols * (int)sizeof(S) / 16 / kThreads;  // 16 bytes a thread
+  static constexpr int kB = CT * kCols + 8;  // of b, [j][c]
+  static constexpr int kLoads = kPassRows * kCols * (int)sizeof(S) / 16 / kThreads;  // 16 bytes a thread
   static constexpr int kV = 16 / (int)sizeof(S);
 };
 template <class S, class W, bool CONTRACT, int JB, int CT>
 __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   typedef Pass<S, W, CONTRACT, JB, CT> P;
   typedef typename P::E E;
+  constexpr int kCols = P::kCols, NB = P::NB;
+  typedef E en __attribute__((ext_vector_type(NB)));
   typedef S sv __attribute__((ext_vector_type(P::kV)));
   typedef E ev __attribute__((ext_vector_type(P::kV)));
   __shared__ __attribute__((aligned(16))) E tile[kPassRows * P::kRow];
@@ -46,8 +53,8 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   const Run run = run_of(l, at.item);
   if (run.count == 0 || run.key >= a.n) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane % 16, g = lane / 16;
-  const int c_first = at.tile * CT * kPassCols, j0 = blockIdx.z * JB * 16;
-  const int tiles = (a.N - c_first + kPassCols - 1) / kPassCols < CT ? (a.N - c_first + kPassCols - 1) / kPassCols : CT;
+  const int c_first = at.tile * CT * kCols, j0 = blockIdx.z * JB * 16;
+  const int tiles = (a.N - c_first + kCols - 1) / kCols < CT ? (a.N - c_first + kCols - 1) / kCols : CT;
   const int32_t* order = l.order + run.first;
   const float* w = a.w + j0;
 
@@ -56,7 +63,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
     rows[t] = order[t < run.count ? t : run.count - 1];
   if constexpr (CONTRACT) {
     // a thread takes 8 ranks of a column; the loads first, then their way into LDS
-    constexpr int kEach = JB * 16 * CT * kPassCols / 8 / kThreads;
+    constexpr int kEach = JB * 16 * CT * kCols / 8 / kThreads;
     const W* b = (const W*)a.b + ((int64_t)run.key * a.N + c_first) * a.r + j0;
     x8<W> x[kEach];
 #pragma unroll
@@ -74,14 +81,14 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   __syncthreads();  // rows
 
   // the tile's loads: thread t takes column group t % kAcross of the rows t / kAcross + k * kDown
-  constexpr int kAcross = kPassCols / P::kV, kDown = kThreads / kAcross;
+  constexpr int kAcross = kCols / P::kV, kDown = kThreads / kAcross;
   sv held[P::kLoads];
   f32x4 held_w[JB];
   const int lc = tid % kAcross * P::kV, lr = tid / kAcross;
   auto load_tile = [&](int t0, int ct) {
-    const int c = c_first + ct * kPassCols + lc;
+    const int c = c_first + ct * kCols + lc;
     const S* src = (const S*)a.src + c;
-    if (c_first + (ct + 1) * kPassCols <= a.N) {
+    if (c_first + (ct + 1) * kCols <= a.N) {
 #pragma unroll
       for (int k = 0; k < P::kLoads; ++k) held[k] = load_n<true, sv, P::kV>(src + rows[t0 + lr + k * kDown] * a.ld, 0);
     } else {
@@ -130,7 +137,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
     }
   };
 
-  f32x4 acc[CT][JB][4] = {};  // out
+  f32x4 acc[CT][JB][NB] = {};  // out
   f32x4 total[JB];            // part, over the tiles so far
   auto add_up = [](f32x4(&total)[JB], const f32x4(&sum)[JB], int ct) {
 #pragma unroll
@@ -154,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
           x4<E> x[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            x[e] = *(const x4<E>*)(tile + (ks * 32 + g * 8 + e) * P::kRow + wave * 64 + 4 * m);
+            x[e] = *(const x4<E>*)(tile + (ks * 32 + g * 8 + e) * P::kRow + wave * (16 * NB) + 4 * m);
           bf16x8 f[4];
 #pragma unroll
           for (int nb = 0; nb < 4; ++nb)
@@ -173,34 +180,34 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
         if constexpr (CONTRACT) {
           f32x4 sum[JB] = {};
 #pragma unroll
-          for (int ks = 0; ks < kPassCols / 32; ++ks) {
+          for (int ks = 0; ks < kCols / 32; ++ks) {
             const bf16x8 x = *(const bf16x8*)(tile + (wave * 16 + m) * P::kRow + ks * 32 + g * 8);
 #pragma unroll
             for (int jb = 0; jb < JB; ++jb)
-              sum[jb] = mfma(*(const bf16x8*)(bt + (jb * 16 + m) * P::kB + ct * kPassCols + ks * 32 + g * 8), x, sum[jb]);
+              sum[jb] = mfma(*(const bf16x8*)(bt + (jb * 16 + m) * P::kB + ct * kCols + ks * 32 + g * 8), x, sum[jb]);
           }
           add_up(total, sum, ct);
         }
       } else {
 #pragma unroll 4
         for (int q = 0; q < kPassRows / 4; ++q) {
-          const f32x4 x = *(const f32x4*)(tile + (q * 4 + g) * P::kRow + wave * 64 + 4 * m);
+          const en x = *(const en*)(tile + (q * 4 + g) * P::kRow + wave * (16 * NB) + NB * m);
 #pragma unroll
           for (int jb = 0; jb < JB; ++jb) {
             const float wf = wt[(jb * 16 + m) * P::kW + q * 4 + g];
 #pragma unroll
-            for (int nb = 0; nb < 4; ++nb)
+            for (int nb = 0; nb < NB; ++nb)
               acc[ct][jb][nb] = CONTRACT ? mfma(wf, x[nb], acc[ct][jb][nb]) : mfma(x[nb], wf, acc[ct][jb][nb]);
           }
         }
         if constexpr (CONTRACT) {
           f32x4 sum[JB] = {};
 #pragma unroll 4
-          for (int ks = 0; ks < kPassCols / 16; ++ks) {
+          for (int ks = 0; ks < kCols / 16; ++ks) {
             const f32x4 x = *(const f32x4*)(tile + (wave * 16 + m) * P::kRow + ks * 16 + g * 4);
 #pragma unroll
             for (int jb = 0; jb < JB; ++jb) {
-              const x4<W> bf = *(const x4<W>*)(bt + (jb * 16 + m) * P::kB + ct * kPassCols + ks * 16 + g * 4);
+              const x4<W> bf = *(const x4<W>*)(bt + (jb * 16 + m) * P::kB + ct * kCols + ks * 16 + g * 4);
 #pragma unroll
               for (int e = 0; e < 4; ++e) sum[jb] = mfma((float)bf[e], x[e], sum[jb]);
             }
@@ -223,27 +230,29 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   if (!a.out) return;
   const bool only = run.slot < 0, add = only && a.accumulate;
   float* out = only ? a.out + (int64_t)run.key * a.r * a.N : a.out_part + (int64_t)run.slot * a.r * a.N;
+  // runs of E elements next to each other in memory: four of the rank, or NB of the columns
+  constexpr int E4 = CONTRACT ? 4 : NB;
+  typedef float fe __attribute__((ext_vector_type(E4)));
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
     for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        // four elements next to each other in memory: of the rank, or of the columns
-        const int c0 = c_first + ct * kPassCols + wave * 64;
-        const int j = j0 + jb * 16 + (CONTRACT ? 4 * g : m), c = c0 + (CONTRACT ? 4 * m + q : 16 * g + 4 * q);
+      for (int q = 0; q < (CONTRACT ? NB : 4); ++q) {
+        const int c0 = c_first + ct * kCols + wave * (16 * NB);
+        const int j = j0 + jb * 16 + (CONTRACT ? 4 * g : m), c = c0 + (CONTRACT ? NB * m + q : NB * (4 * g + q));
         if (j >= a.r || c >= a.N) continue;
-        const f32x4 y = CONTRACT ? acc[ct][jb][q]
-                                 : f32x4{acc[ct][jb][0][q], acc[ct][jb][1][q], acc[ct][jb][2][q], acc[ct][jb][3][q]};
+        fe y;
+#pragma unroll
+        for (int e = 0; e < E4; ++e) y[e] = CONTRACT ? acc[ct][jb][q][e] : acc[ct][jb][e][q];
         float* p = out + (CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c);
         const int left = CONTRACT ? a.r - j : a.N - c;
-        if (left >= 4) {
-          f32x4 z = y;
-          if (add) z = load_n<true, f32x4, 4>(p, 4) + y;
-          __builtin_memcpy(p, &z, sizeof(z));
+        if (left >= E4) {
+          if (add) y += load_n<true, fe, E4>(p, E4);
+          __builtin_memcpy(p, &y, sizeof(y));
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+          for (int e = 0; e < E4; ++e)
             if (e < left) p[e] = add ? p[e] + y[e] : y[e];
         }
       }
@@ -251,7 +260,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
 
 template <class S, class W, bool CONTRACT, int JB, int CT>
 hipError_t run_pass(const PassArgs& a, const RunList& l, hipStream_t s) {
-  const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, CT * kPassCols), (unsigned)((a.rp + 63) / 64));
+  const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, CT * Pass<S, W, CONTRACT, JB, CT>::kCols), (unsigned)((a.rp + 63) / 64));
   TIM_LAUNCH((pass<S, W, CONTRACT, JB, CT><<<grid, kThreads, 0, s>>>(a, l)));
   return hipSuccess;
 }

@@ -118,6 +118,14 @@ __device__ __forceinline__ Place place_of() {
   const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
   return {id / gridDim.y, id % gridDim.y};
 }
+// Keeps the compiler from moving LDS accesses of a wave across it; the hardware
+// takes a wave's LDS accesses in order.
+__device__ __forceinline__ void lanes_in_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // A run of the list (count 0: past its end), asked for beside the list's length rather than after it.
 __device__ __forceinline__ Run run_of(const RunList& l, uint32_t item) {
   Run r = l.runs[item];
@@ -132,14 +140,6 @@ inline RunList run_list(const Grouping& g, const void* ws, int l) {
   const int32_t* c = (const int32_t*)(w + g.counters);
   return {(const int32_t*)(w + g.order), (const Run*)(w + g.runs[l]), (const Join*)(w + g.joins[l]), c + 2 * l,
           c + 2 * l + 1, g.max_runs[l], g.max_joins[l]};
-}
-
-// Keeps the compiler from moving LDS accesses of a wave across it; the hardware
-// takes a wave's LDS accesses in order.
-__device__ __forceinline__ void lanes_in_order() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_wave_barrier();
-  asm volatile("" ::: "memory");
 }
 
 // seen (may be null): a byte per key in [0, n), set to 1 for the keys that

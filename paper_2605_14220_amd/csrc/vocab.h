@@ -95,24 +95,27 @@ constexpr int kShrinkChunk = 512;  // elements of d whose products one workgroup
 inline int rank_padded(int r) { return (r + 15) / 16 * 16; }
 inline int chunks_of(int64_t n, int chunk) { return (int)((n + chunk - 1) / chunk); }
 
-// The pass over grad sums grad b over chunks of 256 columns, and two chunks in
-// order, whatever a workgroup takes: `tiles` chunks (1 or 2) of up to
-// 2^log_rows rows of one adapter. More tiles leave fewer partial sums of grad b,
-// more rows fewer of the weights' gradients; both have to leave work for 256 CUs.
-constexpr int kPassCols = 256, kChunkPair = 2;
+// The pass over grad sums grad b over tiles of 256 columns (128 where it runs on
+// the fp32 instructions), and two tiles in order, whatever a workgroup takes: 1 or
+// 2 tiles of up to 2^log_rows rows of one adapter. More tiles leave fewer partial
+// sums of grad b, more rows fewer of the weights' gradients; both have to leave
+// work for 256 CUs. (2047 rows on a head of 151936, rank 16: 161 us with two
+// tiles, with one 159 and 13 more to add up the sums, with four 183.)
+constexpr int kPassCols = 256, kPassColsF32 = 128, kTilePair = 2;
 constexpr int kLogMaxPassRows = 9, kMaxPassRows = 1 << kLogMaxPassRows;
 struct PassShape {
   int tiles, log_rows;
 };
-inline PassShape pass_shape(int64_t T, int64_t N, int rp, bool contract) {
+inline PassShape pass_shape(int64_t T, int64_t N, int cols, int rp, bool contract) {
   PassShape s = {1, kLogMaxPassRows};
-  auto workgroups = [&](int tiles, int log_rows) {
-    return ((T >> log_rows) + 1) * chunks_of(N, tiles * kPassCols);
-  };
-  while (contract && s.tiles < (rp <= 32 ? 2 : 1) && workgroups(s.tiles * 2, s.log_rows) >= 512)
-    s.tiles *= 2;
+  auto workgroups = [&](int tiles, int log_rows) { return ((T >> log_rows) + 1) * chunks_of(N, tiles * cols); };
+  if (contract && rp <= 16 && workgroups(2, s.log_rows) >= 512) s.tiles = 2;
   while (s.log_rows > 7 && workgroups(s.tiles, s.log_rows) < 512) --s.log_rows;
   return s;
+}
+// The columns of its tiles: whether grad and the adapters are bf16.
+inline int pass_cols(int dtype, int adapter_dtype) {
+  return dtype == TIM_BF16 && adapter_dtype == TIM_BF16 ? kPassCols : kPassColsF32;
 }
 
 // Workspaces: the grouping, then fp32 [chunks, T, rank_padded] of partial sums
@@ -125,13 +128,18 @@ struct AdapterPlan {
   PassShape of_x, of_grad;
   size_t u_part, v_part, u, v, v_terms, a_part, b_part, seen, bytes;
 };
-inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r, bool backward) {
+// cols: of the pass over grad (pass_cols); 0 for the forward.
+inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r, int cols) {
+  const bool backward = cols != 0;
   AdapterPlan p = {};
   p.rp = rank_padded(r);
   p.x_chunks = chunks_of(d, kShrinkChunk);
-  p.of_x = pass_shape(T, d, p.rp, false);
-  p.of_grad = pass_shape(T, N, p.rp, true);
-  p.g_chunks = chunks_of(N, p.of_grad.tiles * kPassCols);
+  // the pass over x runs on the bf16 instructions or not as x is, whatever grad is; its runs may be the same
+  p.of_x = pass_shape(T, d, kPassCols, p.rp, false);
+  if (backward) {
+    p.of_grad = pass_shape(T, N, cols, p.rp, true);
+    p.g_chunks = chunks_of(N, p.of_grad.tiles * cols);
+  }
   const int log_C[3] = {kLogAdapterRun, p.of_x.log_rows, p.of_grad.log_rows};
   p.g = plan_grouping(T, n, backward ? 3 : 1, log_C);
   // few rows, whose adapters' weights for each come to at most 32 MB from the caches
@@ -150,6 +158,12 @@ inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int
   }
   p.bytes = at;
   return p;
+}
+
+// Bytes of the backward's workspace, for either kind of pass over grad.
+inline size_t adapters_backward_workspace(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r) {
+  const size_t a = plan_adapters(T, d, N, n, r, kPassCols).bytes, b = plan_adapters(T, d, N, n, r, kPassColsF32).bytes;
+  return a > b ? a : b;
 }
 
 inline bool valid_adapter_shape(int64_t T, int64_t d, int64_t N, int64_t n, int64_t r) {
@@ -181,7 +195,7 @@ inline tim_status validate_adapters_add(const tim_adapters* ad, const void* x, i
   if (!out) return TIM_ERR_NULL;
   if (base == out && base_ld != out_ld) return TIM_ERR_SHAPE;
   if (!aligned_to(base, dtype_bytes(out_dtype)) || !aligned_to(out, dtype_bytes(out_dtype))) return TIM_ERR_VALUE;
-  if (!ws || !aligned16(ws) || ws_bytes < plan_adapters(T, ad->d, ad->N, ad->n, ad->r, false).bytes)
+  if (!ws || !aligned16(ws) || ws_bytes < plan_adapters(T, ad->d, ad->N, ad->n, ad->r, 0).bytes)
     return TIM_ERR_WORKSPACE;
   return TIM_OK;
 }
@@ -200,7 +214,7 @@ inline tim_status validate_adapters_backward(const tim_adapters* ad, const void*
   if (T == 0) return TIM_OK;
   if (!grad) return TIM_ERR_NULL;
   if (!aligned_to(grad, dtype_bytes(grad_dtype))) return TIM_ERR_VALUE;
-  if (!ws || !aligned16(ws) || ws_bytes < plan_adapters(T, ad->d, ad->N, ad->n, ad->r, true).bytes)
+  if (!ws || !aligned16(ws) || ws_bytes < adapters_backward_workspace(T, ad->d, ad->N, ad->n, ad->r))
     return TIM_ERR_WORKSPACE;
   return TIM_OK;
 }

@@ -39,7 +39,7 @@ tim_status tim_embedding_backward(const void* grad_out, int32_t dtype, int64_t T
 
 size_t tim_adapters_add_workspace_size(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r) {
   if (T <= 0 || !tim::valid_adapter_shape(T, d, N, n, r)) return 0;
-  return tim::plan_adapters(T, d, N, n, r, false).bytes;
+  return tim::plan_adapters(T, d, N, n, r, 0).bytes;
 }
 
 tim_status tim_adapters_add(const tim_adapters* adapters, const void* x, int64_t x_ld, const int32_t* rows, int64_t T,
@@ -54,7 +54,7 @@ tim_status tim_adapters_add(const tim_adapters* adapters, const void* x, int64_t
 
 size_t tim_adapters_backward_workspace_size(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r) {
   if (T <= 0 || !tim::valid_adapter_shape(T, d, N, n, r)) return 0;
-  return tim::plan_adapters(T, d, N, n, r, true).bytes;
+  return tim::adapters_backward_workspace(T, d, N, n, r);
 }
 
 tim_status tim_adapters_backward(const tim_adapters* adapters, const void* x, int64_t x_ld, const int32_t* rows,
