@@ -49,6 +49,15 @@ __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 c) {
   return c;
 #endif
 }
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4 mfma(bf16x4 a, bf16x4 b, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef short s4 __attribute__((ext_vector_type(4)));
+  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s4, a), __builtin_bit_cast(s4, b), c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
 template <class T>
 using x8 = std::conditional_t<std::is_same_v<T, __bf16>, bf16x8, f16x8>;
 

@@ -12,18 +12,22 @@ namespace {
 // later rows of base a step (16 rows of a tile) ahead, before the step's stores. The matrix instructions' results pass through LDS, so that rows are
 // read and written 64 columns at a time.
 //
-// AHEAD: a wave takes 4 / JB tiles by itself, u in registers and all tiles'
-// weights requested first. Otherwise the four
-// waves share u in LDS: its partial sums are then added up once (200 rows of 8
-// adapters of rank 64, d = N = 4096: 25 us a call against 30).
+// The four waves share u in LDS, where its partial sums are added up once (200
+// rows of 8 adapters of rank 64, d = N = 4096: 25 us a call, 30 with each wave's
+// own). AHEAD: a wave takes 4 / JB tiles, all their weights requested first.
 template <class T, class O, bool FLAT, int JB, bool AHEAD>
 __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
   constexpr int kTile = 64 + 4;    // a row of the 16 x 64 results
   constexpr bool kHold = JB <= 4;  // a tile's weights stay in registers for all rows
   constexpr int NT = AHEAD ? 4 / JB : 1;
-  constexpr int kU = JB * 16 + 4;  // a row of u, apart in the banks
+  // Four ranks of a row of u: on the bf16 instructions three terms, which hold all 24 bits, a third of the time of the
+  // fp32 instructions (fp16's range does not hold such terms).
+  constexpr bool FAST = std::is_same_v<T, __bf16>;
+  typedef std::conditional_t<FAST, bf16x4, f32x4> U;
+  constexpr int kTerms = FAST ? 3 : 1;
+  constexpr int kU = JB * 4 * kTerms + 1;  // of them, a row in LDS, apart in the banks
   __shared__ float tile[kWaves][16 * kTile];
-  __shared__ float shared_u[AHEAD ? 1 : 64 * kU];
+  __shared__ U shared_u[64 * kU];
   const Place at = place_of();
   const Run run = run_of(l, at.item);
   if (run.count == 0) return;
@@ -39,7 +43,6 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
     }
     return;
   }
-  if (AHEAD && c_first >= a.N) return;
   const int blocks = (run.count + 15) / 16, tiles = (a.N - c_first + 63) / 64 < NT ? (a.N - c_first + 63) / 64 : NT;
   const T* w = (const T*)a.w + (int64_t)run.key * a.r * a.N;
   // raw[nb][s]: the weight of rank jb * 16 + 4 g + s in column c0 + 16 nb + m; FLAT: raw[s][nb] in column c0 + 4 m + nb.
@@ -97,57 +100,76 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
 #pragma unroll
         for (int jb = 0; jb < JB; ++jb) weights(c_first + ct * 64, jb, raw[ct][jb]);
   if (base) load_base(c_first, 0);
-  // u: where a wave takes several tiles by itself, for all blocks, row m of each; otherwise by way of LDS
-  f32x4 u[AHEAD ? 4 : 1][AHEAD ? JB : 1];
-  if constexpr (AHEAD) {
+  auto in_terms = [](f32x4 x, U(&t)[kTerms]) {
+    if constexpr (FAST) {
 #pragma unroll
-    for (int rb = 0; rb < 4; ++rb)
-      if (rb < blocks)
+      for (int e = 0; e < 4; ++e) {
+        __bf16 q[3];
+        split3(x[e], q);
 #pragma unroll
-        for (int jb = 0; jb < JB; ++jb) u[rb][jb] = jb * 16 < a.rp ? load_u(rb * 16 + m, jb * 16 + g * 4) : f32x4{};
-  } else {
-    const int across = a.rp / 4;
-    for (int i = threadIdx.x; i < blocks * 16 * across; i += kThreads)
-      *(f32x4*)(shared_u + i / across * kU + i % across * 4) = load_u(i / across, i % across * 4);
-    __syncthreads();
-    if (c_first >= a.N) return;
-  }
-  auto from_lds = [&](int rb, int jb) { return *(const f32x4*)(shared_u + (rb * 16 + m) * kU + jb * 16 + g * 4); };
+        for (int k = 0; k < 3; ++k) t[k][e] = q[k];
+      }
+    } else {
+      t[0] = x;
+    }
+  };
+  const int across = a.rp / 4;
+  for (int i = threadIdx.x; i < blocks * 16 * across; i += kThreads)
+    in_terms(load_u(i / across, i % across * 4), *(U(*)[kTerms])(shared_u + i / across * kU + i % across * kTerms));
+  __syncthreads();
+  if (c_first >= a.N) return;
+  auto from_lds = [&](int rb, int jb) -> const U(&)[kTerms] {
+    return *(const U(*)[kTerms])(shared_u + (rb * 16 + m) * kU + (jb * 4 + g) * kTerms);
+  };
   float* const my = tile[wave];
 #pragma unroll
   for (int ct = 0; ct < NT; ++ct) {
     if (AHEAD && ct >= tiles) break;
     const int c0 = c_first + ct * 64;
-    f32x4 wf[kHold ? JB : 1][4];
-    auto widen = [&](int jb) {
+    // operands: the weights as they are, or turned (FLAT), or in fp32
+    typedef std::conditional_t<FAST, bf16x4, f32x4> W;
+    W wf[kHold ? JB : 1][4];
+    auto operands = [&](int jb) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int s = 0; s < 4; ++s) wf[jb][q][s] = (float)raw[ct][jb][q][s];
+        for (int s = 0; s < 4; ++s) {
+          const T x = FLAT ? raw[ct][jb][s][q] : raw[ct][jb][q][s];
+          if constexpr (FAST)
+            wf[jb][q][s] = x;
+          else
+            wf[jb][q][s] = (float)x;
+        }
     };
     if constexpr (kHold) {
 #pragma unroll
-      for (int jb = 0; jb < JB; ++jb) widen(jb);
+      for (int jb = 0; jb < JB; ++jb) operands(jb);
     }
-#pragma unroll(AHEAD ? 4 : 1)
-    for (int rb = 0; rb < 4; ++rb) {
-      if (rb >= blocks) break;
+#pragma unroll 1
+    for (int rb = 0; rb < blocks; ++rb) {
       f32x4 acc[4] = {};
-      auto multiply = [&](const f32x4(&h)[4], f32x4 uf) {
+      auto multiply = [&](const W(&h)[4], const U(&x)[kTerms]) {
+        if constexpr (FAST) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+          for (int k = 0; k < kTerms; ++k)
 #pragma unroll
-          for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(FLAT ? h[s][nb] : h[nb][s], uf[s], acc[nb]);
+            for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(h[nb], x[k], acc[nb]);
+        } else {
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(h[nb][s], x[0][s], acc[nb]);
+        }
       };
       if constexpr (kHold) {
 #pragma unroll
         for (int jb = 0; jb < JB; ++jb)
-          if (jb * 16 < a.rp) multiply(wf[jb], AHEAD ? u[AHEAD ? rb : 0][AHEAD ? jb : 0] : from_lds(rb, jb));
+          if (jb * 16 < a.rp) multiply(wf[jb], from_lds(rb, jb));
       } else {
 #pragma unroll 1
         for (int jb = 0; jb * 16 < a.rp; ++jb) {
           weights(c0, jb, raw[0][0]);
-          widen(0);
+          operands(0);
           multiply(wf[0], from_lds(rb, jb));
         }
       }
