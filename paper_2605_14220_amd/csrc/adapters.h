@@ -88,6 +88,13 @@ __device__ __forceinline__ V load_n(const T* p, int n) {
     return load_some<V, N>(p, n);
   }
 }
+// Past the caches, for rows that are too many to be found there again.
+template <class V, int N, class T>
+__device__ __forceinline__ V load_past(const T* p) {
+  typedef V by_element __attribute__((aligned(sizeof(T))));
+  return __builtin_nontemporal_load((const by_element*)p);
+}
+constexpr int64_t kCaches = (int64_t)256 << 20;
 template <class T>
 using x4 = T __attribute__((ext_vector_type(4)));
 // x as the sum of three bf16 numbers, exactly where none overflows or is subnormal
@@ -110,6 +117,7 @@ struct ExpandArgs {
   int64_t base_ld;
   void* out;
   int64_t out_ld;
+  int32_t past;  // out is larger than the caches
 };
 
 struct PassArgs {
@@ -122,6 +130,7 @@ struct PassArgs {
   float* out;       // [n, N, r], or [n, r, N] without the contraction
   float* out_part;  // [slots] of the same
   int32_t accumulate;
+  int32_t past;  // src is larger than the caches
 };
 
 // The products over the runs of a list, see adapters_expand.hip and adapters_pass.hip.

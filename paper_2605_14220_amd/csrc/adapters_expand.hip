@@ -206,7 +206,14 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[e] = narrow<O>(y[q][e]);
         if (n >= 4) {
-          __builtin_memcpy(dst, &z, sizeof(z));
+          if (a.past) {
+            asm volatile("" ::: "memory");  // or the compiler makes one store of the two
+            typedef x4<O> by_element __attribute__((aligned(sizeof(O))));
+            __builtin_nontemporal_store(z, (by_element*)dst);
+            asm volatile("" ::: "memory");
+          } else {
+            __builtin_memcpy(dst, &z, sizeof(z));
+          }
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -361,7 +368,10 @@ hipError_t run_expand(const ExpandArgs& a, int out_dtype, bool flat, const RunLi
 
 }  // namespace
 
-hipError_t launch_expand(const ExpandArgs& a, int dtype, int out_dtype, bool flat, const RunList& l, hipStream_t s) {
+hipError_t launch_expand(const ExpandArgs& args, int dtype, int out_dtype, bool flat, const RunList& l, hipStream_t s) {
+  ExpandArgs a = args;
+  // 4096 rows of 151936 fp32 logits 983 us against 996; 48 rows 68 against 65
+  a.past = a.T * a.N * dtype_bytes(out_dtype) > kCaches;
   return dtype == TIM_BF16 ? run_expand<__bf16>(a, out_dtype, flat, l, s)
                            : run_expand<_Float16>(a, out_dtype, flat, l, s);
 }

@@ -29,6 +29,13 @@ template <class T, int N>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& r) {
   __builtin_memcpy(p, &r, sizeof(r));
 }
+// Past the caches: what the table's zeros leave there, nobody reads (two
+// micro-batches of 301 rows, V 50257, d 1536: 73 us against 80).
+__device__ __forceinline__ void store_zeros(float* p) {
+  typedef float f4 __attribute__((ext_vector_type(4)));
+  typedef f4 f4_by4 __attribute__((aligned(4)));
+  __builtin_nontemporal_store(f4{}, (f4_by4*)p);
+}
 
 // A row is taken by `lanes` threads (a power of two up to 256), N elements at a
 // time; blockIdx.y walks slices of lanes * N elements. A thread takes kEmbedRows
@@ -98,7 +105,7 @@ hipError_t embed_out(const EmbedArgs& a, int out_dtype, hipStream_t s) {
 // Zeros in a row, by kThreads threads.
 __device__ __forceinline__ void zero_row(float* q, int64_t d) {
   int64_t c = (int64_t)(threadIdx.x % kThreads) * 4;
-  for (; c + 4 <= d; c += kThreads * 4) store_pack(q + c, Pack<float, 4>{});
+  for (; c + 4 <= d; c += kThreads * 4) store_zeros(q + c);
   for (int e = 0; c + e < d && e < 4; ++e) q[c + e] = 0.f;
 }
 __global__ __launch_bounds__(kThreads) void zero_all(float* p, int64_t d, int64_t ld) {
@@ -234,8 +241,13 @@ hipError_t grad_typed(const EmbedGradArgs& a, const EmbedPlan& p, char* ws, hipS
 }  // namespace
 
 hipError_t launch_zero_rows(float* p, int64_t rows, int64_t d, int64_t ld, hipStream_t s) {
-  zero_all<<<(unsigned)rows, kThreads, 0, s>>>(p, d, ld);
-  return hipGetLastError();
+  constexpr int64_t kRows = (int64_t)1 << 23;  // fewer than 2^32 threads a launch
+  for (int64_t r = 0; r < rows; r += kRows) {
+    zero_all<<<(unsigned)(rows - r < kRows ? rows - r : kRows), kThreads, 0, s>>>(p + r * ld, d, ld);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_embedding(const EmbedArgs& a, int dtype, int out_dtype, hipStream_t s) {
