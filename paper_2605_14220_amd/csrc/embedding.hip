@@ -215,7 +215,7 @@ hipError_t grad_typed(const EmbedGradArgs& a, const EmbedPlan& p, char* ws, hipS
   hipError_t e;
   uint8_t* seen = nullptr;
   int64_t zero_blocks = 0;
-  if (!a.accumulate && p.g.blocks == 1 && a.T <= 4096) {
+  if (!a.accumulate && p.g.small && a.T <= 4096) {
     group_and_zero<<<1 + (unsigned)((a.V + kZeroRows - 1) / kZeroRows), kSmallThreads, 0, s>>>(
         group_args(p.g, a.tokens, false, nullptr, ws), a.grad_table, a.V, a.d, a.grad_ld);
     e = hipGetLastError();

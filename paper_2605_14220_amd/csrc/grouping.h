@@ -35,9 +35,9 @@ __host__ __device__ inline int32_t run_slot(int32_t first, int log_C, bool last)
 }
 inline int64_t run_slots(int64_t T, int log_C) { return ((T >> log_C) + 1) * 2; }
 
-// Rows that one workgroup sorts in LDS, by the sorting passes it takes: with one
-// pass (up to 255 keys) 8192 rows take 9 us against 24 in several launches, with
-// three 4096 rows 16 against 28 and twice as many the same.
+// Rows that one workgroup sorts in LDS, by the sorting passes it takes. With one
+// pass (up to 255 keys) 8192 rows take 18 us, in launches of their own 24; with
+// more, 32 bits hold a key and the row's index only up to 4096 rows.
 inline int64_t group_small_rows(int passes) { return passes == 1 ? 16384 : 4096; }
 constexpr int kMaxRunLists = 3;
 
@@ -49,6 +49,7 @@ struct Grouping {
   int32_t lists;                // lists of runs
   int32_t log_C[kMaxRunLists];  // logarithms of their lengths
   int64_t max_runs[kMaxRunLists], max_joins[kMaxRunLists];
+  bool small;                   // one workgroup's work
   int32_t bits, passes, digit;  // of a key, sorting passes, bits a pass
   int32_t blocks, per_block;    // of the sort of many rows
   // offsets into the workspace
@@ -68,7 +69,8 @@ inline Grouping plan_grouping(int64_t T, int32_t n, int lists, const int* log_C)
   g.order = at, at += group_align((size_t)T * 4);
   // digits of at most 8 bits: a bin for each of 256 threads to add up
   g.passes = (g.bits + 7) / 8;
-  if (T <= group_small_rows(g.passes)) {
+  g.small = T <= group_small_rows(g.passes);
+  if (g.small) {
     g.digit = (g.bits + g.passes - 1) / g.passes;
     g.blocks = 1;
     g.per_block = (int32_t)T;

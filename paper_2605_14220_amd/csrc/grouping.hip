@@ -246,7 +246,7 @@ GroupArgs group_args(const Grouping& g, const int32_t* keys, bool keep_rest, uin
 hipError_t launch_grouping(const Grouping& g, const int32_t* keys, bool keep_rest, uint8_t* seen, void* ws,
                            hipStream_t s) {
   const GroupArgs a = group_args(g, keys, keep_rest, seen, ws);
-  if (g.blocks == 1) {
+  if (g.small) {
     if (g.T <= 4096)
       TIM_TRY((group_small<12><<<1, kSmallThreads, 0, s>>>(a)));
     else

@@ -80,7 +80,7 @@ extern "C" int64_t plan(int64_t T, int32_t n, int log_C, int what) {
   const int l[1] = {log_C};
   const tim::Grouping g = tim::plan_grouping(T, n, 1, l);
   return what == 0 ? g.max_runs[0] : what == 1 ? g.max_joins[0] : what == 2 ? tim::run_slots(T, log_C)
-       : what == 3 ? (int64_t)1 << (g.passes * g.digit) : what == 4 ? (int64_t)g.blocks * g.per_block : g.blocks;
+       : what == 3 ? (int64_t)1 << (g.passes * g.digit) : what == 4 ? (int64_t)g.blocks * g.per_block : what == 5 ? g.blocks : what == 6 ? g.small : g.digit;
 }
 extern "C" int32_t slot(int32_t first, int log_C, int last) { return tim::run_slot(first, log_C, last); }
 """)
@@ -119,6 +119,10 @@ extern "C" int32_t slot(int32_t first, int log_C, int last) { return tim::run_sl
             assert shim.plan(T, n, 6, 3) > n                      # the digits hold every key, n included
             assert shim.plan(T, n, 6, 4) >= T                     # the blocks hold every row
             assert 1 <= shim.plan(T, n, 6, 5) <= 256
+            if shim.plan(T, n, 6, 6):  # one workgroup: its LDS holds 256 digits, and key and index fit 32 bits
+                assert shim.plan(T, n, 6, 7) <= 8 and T <= 16384 and n < 1 << (20 if T <= 4096 else 18)
+            else:
+                assert shim.plan(T, n, 6, 7) <= 10 and T > 4096
 
 
 def _embed(lib, table=FAKE, dtype=BF16, V=10, d=8, ld=8, tokens=FAKE, T=4, scale=1.0, out=FAKE, out_dtype=F32, out_ld=8):
