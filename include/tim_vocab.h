@@ -106,9 +106,11 @@ typedef struct {
  * out     out_dtype [T, N], row stride out_ld >= N; may be base itself with the
  *         same stride, otherwise no overlap with the inputs.
  * Arithmetic: x a^T is accumulated in fp32 in an order that depends on d alone
- * and kept in fp32, its product with b^T is accumulated in fp32 over ascending
- * groups of the rank; one rounding of the sum with base to out_dtype. NaN and
- * infinities in a row or its adapter reach that row only.
+ * and kept in fp32; its product with b^T is accumulated in fp32 over ascending
+ * groups of 16 ranks (bf16 adapters: with the fp32 number as the sum of three bf16
+ * ones, which hold its 24 bits; beyond bf16's largest number it becomes infinite).
+ * One rounding of the sum with base to out_dtype. NaN and infinities in a row or
+ * its adapter reach that row only.
  * workspace  tim_adapters_add_workspace_size(T, d, N, n, r) bytes, 16-byte
  *         aligned.
  * Errors: TIM_ERR_SHAPE (T, n, r, d, N, strides), TIM_ERR_VALUE (dtypes,
@@ -134,11 +136,12 @@ tim_status tim_adapters_add(const tim_adapters* adapters, const void* x, int64_t
  *          added to, else written, zeros for an adapter without rows.
  * workspace  tim_adapters_backward_workspace_size(T, d, N, n, r) bytes, 16-byte
  *          aligned.
- * Arithmetic: u and v are accumulated and kept in fp32; grad_a and grad_b are
- * fp32 chains over runs of an adapter's rows by ascending t, the runs' sums
- * joined by a chain; no atomics on them. A row's grad_x is bitwise independent
- * of the other rows and of T, an adapter's grad_a and grad_b of other adapters'
- * rows. Errors as tim_adapters_add; TIM_ERR_VALUE also for accumulate_x or
+ * Arithmetic: u and v are accumulated and kept in fp32 (in products with bf16 as
+ * in tim_adapters_add); grad_a and grad_b are fp32 chains over runs of an adapter's
+ * rows by ascending t, of 128, 256 or 512 rows as T, the width, r and the types
+ * say, the runs' sums joined by a chain; no atomics on them. A row's grad_x is
+ * bitwise independent of the other rows and of T; for given T an adapter's grad_a
+ * and grad_b are bitwise independent of the other adapters' rows. Errors as tim_adapters_add; TIM_ERR_VALUE also for accumulate_x or
  * accumulate_ab not 0 or 1. T == 0 writes zeros to grad_a and grad_b unless
  * accumulating. */
 size_t tim_adapters_backward_workspace_size(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r);
