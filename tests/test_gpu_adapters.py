@@ -62,7 +62,8 @@ SIZES = [(1, 1, 1, 1, 1, "one", 0), (1, 2048, 1000, 4, 16, "one", 0), (2, 33, 7,
          (70, 40, 90, 2, 256, "mixed", 0), (333, 500, 130, 3, 8, "runs", 0), (700, 64, 70, 2, 5, "mixed", 0),
          (1500, 40, 66, 1, 12, "one", 0), (5000, 24, 33, 7, 3, "mixed", 0), (100, 48, 40, 3, 4, "none", 0),
          (4097, 20, 16, 1000, 2, "mixed", 0), (40, 3001, 20, 2, 1, "mixed", 0),
-         (70, 24, 33001, 2, 16, "mixed", 1), (150, 24, 32768, 2, 20, "runs", 0)]
+         (70, 24, 33001, 2, 16, "mixed", 1), (150, 24, 32768, 2, 20, "runs", 0),
+         (17000, 12, 20, 3, 2, "mixed", 0), (1025, 520, 600, 3, 48, "runs", 1)]
 
 
 def _whole(T, d, N, n, r, kind, dtype, seed):
@@ -82,7 +83,7 @@ def _whole(T, d, N, n, r, kind, dtype, seed):
 
 
 @pytest.mark.parametrize("case", range(len(SIZES)))
-@pytest.mark.parametrize("dtype,out", [(BF16, F32), (F16, F16), (BF16, BF16), (F16, F32)])
+@pytest.mark.parametrize("dtype,out", [(BF16, F32), (F16, F16), (BF16, BF16), (F16, F32), (BF16, F16), (F16, BF16)])
 def test_whole_numbers(case, dtype, out):
     T, d, N, n, r, kind, pad = SIZES[case]
     x, a, b, grad, scales, rows = _whole(T, d, N, n, r, kind, dtype, 7 * case)
@@ -155,6 +156,34 @@ def test_numbers(case, dtype, out):
     check("grad_x", got[0], want[0], size[0], N + r + 3, eps)
     check("grad_a", got[1], want[1], size[1], N + T + 3, 2.0 ** -24)
     check("grad_b", got[2], want[2], size[2], d + T + 3, 2.0 ** -24)
+
+
+def test_more_elements_than_31_bits():
+    """Outputs and gradients of 2.25e9 elements, past the caches and in whole numbers: every row against its own few
+    values, the weights' gradients against exact sums."""
+    T, N, d, r = 15000, 150001, 8, 1
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.randint(-2, 3, (T, d), generator=g, device="cuda").to(BF16)
+    a = torch.randint(-1, 2, (1, r, d), generator=g, device="cuda").to(BF16)
+    b = torch.randint(-2, 3, (1, N, r), generator=g, device="cuda").to(BF16)
+    rows = torch.zeros(T, dtype=torch.int32, device="cuda")
+    rows[::7] = -1
+    u = (x.double() @ a[0].double().T)[:, 0] * (rows == 0)
+    y = tim.adapters_add(None, x, rows, tim.Adapters(a, b))  # at most 16 * 2 in magnitude: exact in bf16
+    for t in range(0, T, 1000):
+        want = u[t:t + 1000, None] * b[0, :, 0].double()
+        assert torch.equal(y[t:t + 1000].double(), want)
+    base = tim.adapters_add(y, x, rows, tim.Adapters(a, b), out=y)
+    assert torch.equal(base[T - 1].double(), 2 * u[T - 1] * b[0, :, 0].double())
+    # gradients: y itself, as whole numbers
+    gx, ga, gb = tim.adapters_backward(y, x, rows, tim.Adapters(a, b), dtype=F32)
+    bb = (b.double() ** 2).sum()
+    v = 2 * u * bb  # exact in fp64; in fp32 below 2^24 times a power of two only if bb is small, so bounds instead
+    assert ((gx.double() - v[:, None] * a[0, 0].double()).abs() <= 2.0 ** -23 * N * (v[:, None] * a[0, 0].double()).abs()).all()
+    assert torch.equal(gb[0, :, 0].double(), 2 * (u * u).sum() * b[0, :, 0].double())
+    want = v @ x.double()
+    size = (v.abs()[:, None] * x.double().abs()).sum(0)
+    assert ((ga[0, 0].double() - want).abs() <= (N + T + 3) * 2.0 ** -23 * size * (1 + 2.0 ** -5)).all()
 
 
 def test_gradients_are_the_derivative():
