@@ -82,14 +82,19 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
   };
   x4<T> raw[NT][kHold ? JB : 1][4];
   x4<O> old[4];
-  // what lane (m, g) reads and writes of a step: row 4 q + g, columns 4 m .. 4 m + 3
+  // what lane (m, g) reads and writes of a step: row 4 q + g, columns 4 m .. 4 m + 3; with one block the same rows in every
+  // tile
+  int32_t only[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) only[q] = __shfl(my_row, 4 * q + g);
+  auto row_of = [&](int rb, int q) { return blocks == 1 ? only[q] : __shfl(my_row, rb * 16 + q * 4 + g); };
   auto load_base = [&](int c0, int rb) {
     const int c = c0 + 4 * m;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int t = rb * 16 + q * 4;
       if (t >= run.count) break;
-      const O* p = base + __shfl(my_row, t + g) * a.base_ld + c;
+      const O* p = base + row_of(rb, q) * a.base_ld + c;
       old[q] = c0 + 64 <= a.N ? load_n<true, x4<O>, 4>(p, 4) : load_some<x4<O>, 4>(p, a.N - c);
     }
   };
@@ -199,7 +204,7 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
       for (int q = 0; q < 4; ++q) {
         if (rb * 16 + q * 4 >= run.count) break;
         const int t = rb * 16 + q * 4 + g, c = c0 + 4 * m, n = a.N - c;
-        const int64_t row = __shfl(my_row, t);
+        const int64_t row = row_of(rb, q);
         if (t >= run.count || n <= 0) continue;
         O* dst = (O*)a.out + row * a.out_ld + c;
         x4<O> z;

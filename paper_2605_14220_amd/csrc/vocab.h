@@ -106,10 +106,11 @@ constexpr int kLogMaxPassRows = 9, kMaxPassRows = 1 << kLogMaxPassRows;
 struct PassShape {
   int tiles, log_rows;
 };
-inline PassShape pass_shape(int64_t T, int64_t N, int cols, int rp, bool contract) {
+inline PassShape pass_shape(int64_t T, int64_t N, int n, int cols, int rp, bool contract) {
   PassShape s = {1, kLogMaxPassRows};
   auto workgroups = [&](int tiles, int log_rows) { return ((T >> log_rows) + 1) * chunks_of(N, tiles * cols); };
-  if (contract && rp <= 16 && workgroups(2, s.log_rows) >= 512) s.tiles = 2;
+  const int64_t adapters = n < T ? n : T;
+  if (contract && rp <= 16 && ((T >> s.log_rows) + adapters) * chunks_of(N, 2 * cols) >= 384) s.tiles = 2;
   while (s.log_rows > 7 && workgroups(s.tiles, s.log_rows) < 512) --s.log_rows;
   return s;
 }
@@ -135,9 +136,9 @@ inline AdapterPlan plan_adapters(int64_t T, int32_t d, int32_t N, int32_t n, int
   p.rp = rank_padded(r);
   p.x_chunks = chunks_of(d, kShrinkChunk);
   // the pass over x runs on the bf16 instructions or not as x is, whatever grad is; its runs may be the same
-  p.of_x = pass_shape(T, d, kPassCols, p.rp, false);
+  p.of_x = pass_shape(T, d, n, kPassCols, p.rp, false);
   if (backward) {
-    p.of_grad = pass_shape(T, N, cols, p.rp, true);
+    p.of_grad = pass_shape(T, N, n, cols, p.rp, true);
     p.g_chunks = chunks_of(N, p.of_grad.tiles * cols);
   }
   const int log_C[3] = {kLogAdapterRun, p.of_x.log_rows, p.of_grad.log_rows};
