@@ -15,8 +15,10 @@ namespace {
 // The four waves share u in LDS, where its partial sums are added up once (200
 // rows of 8 adapters of rank 64, d = N = 4096: 25 us a call, 30 with each wave's
 // own). AHEAD: a wave takes 4 / JB tiles, all their weights requested first.
+// Registers for four workgroups a CU where nothing spills (333 rows, d 1536, N
+// 50257, rank 9, fp16: 29 us against 31; with AHEAD 4096 rows 1003 against 982).
 template <class T, class O, bool FLAT, int JB, bool AHEAD>
-__global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
+__global__ __launch_bounds__(kThreads, !AHEAD && JB <= 2 ? 4 : 1) void expand(ExpandArgs a, RunList l) {
   constexpr int kTile = 64 + 4;    // a row of the 16 x 64 results
   constexpr bool kHold = JB <= 4;  // a tile's weights stay in registers for all rows
   constexpr int NT = AHEAD ? 4 / JB : 1;
@@ -236,39 +238,41 @@ __global__ __launch_bounds__(kThreads) void expand(ExpandArgs a, RunList l) {
 // A lane takes 8 ranks of 4 columns and turns them in registers. Its results are
 // 16 columns of a row, stored as they are. KS: steps of 32 ranks; 0 for up to 16,
 // where one step holds the first and the second number and one the third.
-template <class O, int KS>
-__global__ __launch_bounds__(kThreads) void expand_flat(ExpandArgs a, RunList l) {
+template <class O, int KS, int NT>
+__global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandArgs a, RunList l) {
   constexpr int kSteps = KS == 0 ? 1 : KS, kTerms = KS == 0 ? 2 : 3;
   const Place at = place_of();
   const Run run = run_of(l, at.item);
   if (run.count == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % 16, g = lane / 16;
-  const int c0 = ((int)at.tile * kWaves + wave) * 64;
-  if (c0 >= a.N) return;
+  const int c_first = ((int)at.tile * kWaves + wave) * NT * 64;
+  if (c_first >= a.N) return;
   const int my_row = l.order[run.first + (lane < run.count ? lane : run.count - 1)];  // of the run's row `lane`
   const int blocks = (run.count + 15) / 16;
   const bool there = run.key < a.n;
-  bf16x8 wf[kSteps][4], u[kSteps][kTerms][4];
+  bf16x8 wf[NT][kSteps][4], u[kSteps][kTerms][4];
   if (there) {
-    const __bf16* w = (const __bf16*)a.w + (int64_t)run.key * a.r * a.N + c0 + 4 * m;
 #pragma unroll
-    for (int ks = 0; ks < kSteps; ++ks) {
-      const int j0 = ks * 32 + (KS == 0 ? g % 2 : g) * 8;
-      x4<__bf16> x[8];
+    for (int ct = 0; ct < NT; ++ct)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const __bf16* p = w + (int64_t)(j0 + e < a.r ? j0 + e : a.r - 1) * a.N;
-        x[e] = c0 + 64 <= a.N ? load_n<true, x4<__bf16>, 4>(p, 4) : load_some<x4<__bf16>, 4>(p, a.N - c0 - 4 * m);
-        if (a.r != a.rp && j0 + e >= a.r) x[e] = x4<__bf16>{};
+      for (int ks = 0; ks < kSteps; ++ks) {
+        const int c0 = c_first + ct * 64, j0 = ks * 32 + (KS == 0 ? g % 2 : g) * 8;
+        const __bf16* w = (const __bf16*)a.w + (int64_t)run.key * a.r * a.N + c0 + 4 * m;
+        x4<__bf16> x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const __bf16* p = w + (int64_t)(j0 + e < a.r ? j0 + e : a.r - 1) * a.N;
+          x[e] = c0 + 64 <= a.N ? load_n<true, x4<__bf16>, 4>(p, 4) : load_some<x4<__bf16>, 4>(p, a.N - c0 - 4 * m);
+          if (a.r != a.rp && j0 + e >= a.r) x[e] = x4<__bf16>{};
+        }
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) wf[ct][ks][nb][e] = x[e][nb];
+        if (KS == 2 && j0 >= a.rp)  // a rank of up to 48
+#pragma unroll
+          for (int nb = 0; nb < 4; ++nb) wf[ct][ks][nb] = bf16x8{};
       }
-#pragma unroll
-      for (int nb = 0; nb < 4; ++nb)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) wf[ks][nb][e] = x[e][nb];
-      if (KS == 2 && ks * 32 + g * 8 >= a.rp)  // a rank of up to 48
-#pragma unroll
-        for (int nb = 0; nb < 4; ++nb) wf[ks][nb] = bf16x8{};
-    }
 #pragma unroll
     for (int rb = 0; rb < 4; ++rb)
       if (rb < blocks) {
@@ -285,42 +289,45 @@ __global__ __launch_bounds__(kThreads) void expand_flat(ExpandArgs a, RunList l)
 #pragma unroll
   for (int rb = 0; rb < 4; ++rb) {
     if (rb >= blocks) break;
-    f32x4 acc[4] = {};
-    if (there) {
-#pragma unroll
-      for (int ks = 0; ks < kSteps; ++ks)
-#pragma unroll
-        for (int q = 0; q < kTerms; ++q)
-#pragma unroll
-          for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(wf[ks][nb], u[ks][q][rb], acc[nb]);
-    }
     const int64_t row = __shfl(my_row, rb * 16 + m);
-    const int c = c0 + 16 * g, n = a.N - c;
-    if (rb * 16 + m >= run.count || n <= 0) continue;
-    O* dst = (O*)a.out + row * a.out_ld + c;
-    const O* base = a.base ? (const O*)a.base + row * a.base_ld + c : nullptr;
-    constexpr int E = 16 / (int)sizeof(O);  // columns a store
-    typedef O ov __attribute__((ext_vector_type(E)));
-    if (n >= 16) {
 #pragma unroll
-      for (int s = 0; s < 16 / E; ++s) {
-        ov z, old = {};
-        if (base) old = load_n<true, ov, E>(base + s * E, E);
+    for (int ct = 0; ct < NT; ++ct) {
+      f32x4 acc[4] = {};
+      if (there) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int k = s * E + e;  // acc[k % 4][k / 4]
-          const float y = acc[k % 4][k / 4];
-          z[e] = base ? (there ? narrow<O>((float)old[e] + y) : old[e]) : narrow<O>(y);
-        }
-        __builtin_memcpy(dst + s * E, &z, sizeof(z));
+        for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+          for (int q = 0; q < kTerms; ++q)
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(wf[ct][ks][nb], u[ks][q][rb], acc[nb]);
       }
-    } else {
+      const int c = c_first + ct * 64 + 16 * g, n = a.N - c;
+      if (rb * 16 + m >= run.count || n <= 0) continue;
+      O* dst = (O*)a.out + row * a.out_ld + c;
+      const O* base = a.base ? (const O*)a.base + row * a.base_ld + c : nullptr;
+      constexpr int E = 16 / (int)sizeof(O);  // columns a store
+      typedef O ov __attribute__((ext_vector_type(E)));
+      if (n >= 16) {
 #pragma unroll
-      for (int k = 0; k < 16; ++k)
-        if (k < n) {
-          const float y = acc[k % 4][k / 4];
-          dst[k] = base ? (there ? narrow<O>((float)base[k] + y) : base[k]) : narrow<O>(y);
+        for (int s = 0; s < 16 / E; ++s) {
+          ov z, old = {};
+          if (base) old = load_n<true, ov, E>(base + s * E, E);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const int k = s * E + e;  // acc[k % 4][k / 4]
+            const float y = acc[k % 4][k / 4];
+            z[e] = base ? (there ? narrow<O>((float)old[e] + y) : old[e]) : narrow<O>(y);
+          }
+          __builtin_memcpy(dst + s * E, &z, sizeof(z));
         }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          if (k < n) {
+            const float y = acc[k % 4][k / 4];
+            dst[k] = base ? (there ? narrow<O>((float)base[k] + y) : base[k]) : narrow<O>(y);
+          }
+      }
     }
   }
 }
@@ -343,13 +350,20 @@ template <class T, class O, bool FLAT>
 hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
   if constexpr (FLAT && std::is_same_v<T, __bf16>) {
     if (a.terms) {
-      const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, kWaves * 64));
-      if (a.rp <= 16)
-        TIM_LAUNCH((expand_flat<O, 0><<<grid, kThreads, 0, s>>>(a, l)));
+      // a wave takes two tiles where that leaves a workgroup of four waves four times for each of 256 CUs (8192
+      // rows of rank 32, d = 4096: 138 us a call against 142; 146 with registers for three workgroups a CU)
+      const int tiles = a.rp <= 32 && l.max_runs * chunks_of(a.N, 2 * kWaves * 64) >= 1024 ? 2 : 1;
+      const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, tiles * kWaves * 64));
+      if (a.rp <= 16 && tiles == 2)
+        TIM_LAUNCH((expand_flat<O, 0, 2><<<grid, kThreads, 0, s>>>(a, l)));
+      else if (a.rp <= 16)
+        TIM_LAUNCH((expand_flat<O, 0, 1><<<grid, kThreads, 0, s>>>(a, l)));
+      else if (a.rp <= 32 && tiles == 2)
+        TIM_LAUNCH((expand_flat<O, 1, 2><<<grid, kThreads, 0, s>>>(a, l)));
       else if (a.rp <= 32)
-        TIM_LAUNCH((expand_flat<O, 1><<<grid, kThreads, 0, s>>>(a, l)));
+        TIM_LAUNCH((expand_flat<O, 1, 1><<<grid, kThreads, 0, s>>>(a, l)));
       else
-        TIM_LAUNCH((expand_flat<O, 2><<<grid, kThreads, 0, s>>>(a, l)));
+        TIM_LAUNCH((expand_flat<O, 2, 1><<<grid, kThreads, 0, s>>>(a, l)));
       return hipSuccess;
     }
   }
