@@ -16,7 +16,7 @@ namespace {
 // rows of 8 adapters of rank 64, d = N = 4096: 25 us a call, 30 with each wave's
 // own). AHEAD: a wave takes 4 / JB tiles, all their weights requested first.
 // Registers for four workgroups a CU where nothing spills (333 rows, d 1536, N
-// 50257, rank 9, fp16: 29 us against 31; with AHEAD 4096 rows 1003 against 982).
+// 50257, rank 9, fp16: 29 us against 31).
 template <class T, class O, bool FLAT, int JB, bool AHEAD>
 __global__ __launch_bounds__(kThreads, !AHEAD && JB <= 2 ? 4 : 1) void expand(ExpandArgs a, RunList l) {
   constexpr int kTile = 64 + 4;    // a row of the 16 x 64 results
@@ -367,9 +367,12 @@ hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
       return hipSuccess;
     }
   }
-  // a wave takes several tiles where that leaves 16 waves for each of 256 CUs (48 rows of 32 adapters at d = 5120 on a
-  // head of 152064: 80 us against 95), of a high rank always one (its weights and rows of u fill the registers)
-  if (!FLAT && a.rp <= 32 && l.max_runs * chunks_of(a.N, 4 * 64) >= 4096) return run_expand<T, O, FLAT, !FLAT>(a, l, s);
+  // A wave takes several tiles where that leaves 16 waves for each of 256 CUs and the runs hold less than a block of 16
+  // rows: what it waits for are then the weights, otherwise the rows. (48 rows of 32 adapters at d = 5120 on a head of
+  // 152064 63 us against 74, 4096 rows of 4 adapters at d = 4096 on one of 151936 984 against 900; of a high rank the
+  // weights of several tiles do not fit the registers.)
+  if (!FLAT && a.rp <= 32 && l.max_runs * chunks_of(a.N, 4 * 64) >= 4096 && a.T < 16 * l.max_runs)
+    return run_expand<T, O, FLAT, !FLAT>(a, l, s);
   return run_expand<T, O, FLAT, false>(a, l, s);
 }
 template <class T, class O>
@@ -389,7 +392,7 @@ hipError_t run_expand(const ExpandArgs& a, int out_dtype, bool flat, const RunLi
 
 hipError_t launch_expand(const ExpandArgs& args, int dtype, int out_dtype, bool flat, const RunList& l, hipStream_t s) {
   ExpandArgs a = args;
-  // 4096 rows of 151936 fp32 logits 983 us against 996; 48 rows 68 against 65
+  // 4096 rows of 151936 fp32 logits, with several tiles a wave, 983 us against 996; 48 rows 68 against 65
   a.past = a.T * a.N * dtype_bytes(out_dtype) > kCaches;
   return dtype == TIM_BF16 ? run_expand<__bf16>(a, out_dtype, flat, l, s)
                            : run_expand<_Float16>(a, out_dtype, flat, l, s);

@@ -99,8 +99,10 @@ inline int chunks_of(int64_t n, int chunk) { return (int)((n + chunk - 1) / chun
 // the fp32 instructions), and two tiles in order, whatever a workgroup takes: 1 or
 // 2 tiles of up to 2^log_rows rows of one adapter. More tiles leave fewer partial
 // sums of grad b, more rows fewer of the weights' gradients; both have to leave
-// work for 256 CUs. (2047 rows on a head of 151936, rank 16: 161 us with two
-// tiles, with one 159 and 13 more to add up the sums, with four 183.)
+// work for 256 CUs. (2047 rows on a head of 151936, rank 16, with loads through the
+// caches: 161 us with two tiles, with one 159 and 13 more to add up the sums, with
+// four 183. 150 rows of 2 adapters on one of 50257, fp32: 21 us with two tiles, 24
+// with one, whose 786 workgroups are a second round of 18.)
 constexpr int kPassCols = 256, kPassColsF32 = 128, kTilePair = 2;
 constexpr int kLogMaxPassRows = 9, kMaxPassRows = 1 << kLogMaxPassRows;
 struct PassShape {

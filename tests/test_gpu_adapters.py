@@ -63,7 +63,8 @@ SIZES = [(1, 1, 1, 1, 1, "one", 0), (1, 2048, 1000, 4, 16, "one", 0), (2, 33, 7,
          (1500, 40, 66, 1, 12, "one", 0), (5000, 24, 33, 7, 3, "mixed", 0), (100, 48, 40, 3, 4, "none", 0),
          (4097, 20, 16, 1000, 2, "mixed", 0), (40, 3001, 20, 2, 1, "mixed", 0),
          (70, 24, 33001, 2, 16, "mixed", 1), (150, 24, 32768, 2, 20, "runs", 0),
-         (17000, 12, 20, 3, 2, "mixed", 0), (1025, 520, 600, 3, 48, "runs", 1)]
+         (17000, 12, 20, 3, 2, "mixed", 0), (1025, 520, 600, 3, 48, "runs", 1),
+         (40, 24, 33001, 31, 16, "mixed", 1), (45, 24, 33001, 31, 27, "mixed", 0)]
 
 
 def _whole(T, d, N, n, r, kind, dtype, seed):
@@ -156,6 +157,33 @@ def test_numbers(case, dtype, out):
     check("grad_x", got[0], want[0], size[0], N + r + 3, eps)
     check("grad_a", got[1], want[1], size[1], N + T + 3, 2.0 ** -24)
     check("grad_b", got[2], want[2], size[2], d + T + 3, 2.0 ** -24)
+
+
+@pytest.mark.parametrize("r", [16, 24, 40])
+def test_many_rows_of_a_projection(r):
+    """Runs and columns enough for every kernel's widest shape, in whole numbers against float64 products on the GPU."""
+    T, d, N, n = 8200, 4100, 2052, 2
+    g = torch.Generator(device="cuda").manual_seed(r)
+    ints = lambda *s: torch.randint(-1, 2, s, generator=g, device="cuda").to(BF16)
+    x, a, b, grad = ints(T, d), ints(n, r, d), ints(n, N, r), ints(T, N)
+    x *= torch.rand(T, d, generator=g, device="cuda") < 0.01
+    grad *= torch.rand(T, N, generator=g, device="cuda") < 0.02
+    rows = torch.randint(-1, n, (T,), generator=g, device="cuda", dtype=torch.int32)
+    ad = tim.Adapters(a, b)
+    y = tim.adapters_add(None, x, rows, ad, dtype=F32)
+    gx, ga, gb = tim.adapters_backward(grad, x, rows, ad, dtype=F32)
+    wy, wx = torch.zeros(T, N, dtype=torch.float64, device="cuda"), torch.zeros(T, d, dtype=torch.float64, device="cuda")
+    X, G = x.double(), grad.double()
+    for k in range(n):
+        m = (rows == k).double()[:, None]
+        A, B = a[k].double(), b[k].double()
+        u, v = m * (X @ A.T), m * (G @ B)
+        wy += u @ B.T
+        wx += v @ A
+        assert torch.equal(ga[k].double(), v.T.contiguous() @ X)
+        assert torch.equal(gb[k].double(), G.T.contiguous() @ u)
+    assert torch.equal(y.double(), wy) and torch.equal(gx.double(), wx)
+    assert torch.equal(tim.adapters_backward(grad, x, rows, ad, want_a=False, want_b=False)[0], wx.to(BF16))
 
 
 def test_more_elements_than_31_bits():
