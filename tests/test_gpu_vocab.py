@@ -244,3 +244,26 @@ def test_embedding_many_distinct_and_sorted_inputs():
             tok = tok.to(torch.int32).cuda()
             got = tim.embedding_backward(grad, tok, V)
             assert torch.equal(got[tok.long()], grad)
+
+
+@pytest.mark.parametrize("T", [5, 90, 2000, 17000])
+def test_whatever_the_workspace_holds(T):
+    """A workspace of NaN bits and one of zeros give the same bits: everything read from it was written by the call."""
+    m = _model(T=T, V=520, n=3, r=20)
+    d, V, n, r = 256, 520, 3, 20
+    x = tim.embedding(m["W"], m["inp"], 16.0)
+    dy = torch.randn(T, V, device="cuda")
+    sizes = (tim.adapters_add_workspace_size(T, d, V, n, r), tim.adapters_backward_workspace_size(T, d, V, n, r),
+             tim.embedding_backward_workspace_size(T, V, d))
+    results = []
+    for byte in (0, 255):
+        ws = [torch.full((s,), byte, dtype=torch.uint8, device="cuda") for s in sizes]
+        out = [tim.adapters_add(dy, x, m["rows"], m["ad"], workspace=ws[0])]
+        for g in (dy, dy.to(BF16)):
+            out += tim.adapters_backward(g, x, m["rows"], m["ad"], dtype=F32, workspace=ws[1].fill_(byte))
+        out += [tim.embedding_backward(out[1], m["inp"], V, workspace=ws[2]),
+                tim.embedding_backward(out[1], m["inp"], V, grad_table=torch.ones(V, d, device="cuda"), accumulate=True,
+                                       workspace=ws[2].fill_(byte))]
+        results.append(out)
+    for a, b in zip(*results):
+        assert bits_equal(a, b)
