@@ -109,8 +109,8 @@ typedef struct {
  * and kept in fp32; its product with b^T is accumulated in fp32 over ascending
  * groups of 16 ranks (bf16 adapters: with the fp32 number as the sum of three bf16
  * ones, which hold its 24 bits; beyond bf16's largest number it becomes infinite).
- * One rounding of the sum with base to out_dtype. NaN and infinities in a row or
- * its adapter reach that row only.
+ * One rounding of the sum with base to out_dtype. Infinities and NaN give what the
+ * formula gives; those in a row or its adapter reach that row only.
  * workspace  tim_adapters_add_workspace_size(T, d, N, n, r) bytes, 16-byte
  *         aligned.
  * Errors: TIM_ERR_SHAPE (T, n, r, d, N, strides), TIM_ERR_VALUE (dtypes,

@@ -98,12 +98,37 @@ constexpr int64_t kCaches = (int64_t)256 << 20;
 template <class T>
 using x4 = T __attribute__((ext_vector_type(4)));
 // x as the sum of three bf16 numbers, exactly where none overflows or is subnormal
-// (24 bits are three times 8); an infinity or NaN alone in the first.
+// (24 bits are three times 8); an infinity or NaN alone in the first. In a product
+// with an infinity terms of 0 or of the other sign give NaN: elements that come out
+// as NaN are summed again from x itself (again_if_nan), the same way for an element
+// whatever else the tile holds.
 __device__ __forceinline__ void split3(float x, __bf16 (&t)[3]) {
   t[0] = (__bf16)x;
   const float r = __builtin_isfinite((float)t[0]) ? x - (float)t[0] : 0.f;
   t[1] = (__bf16)r;
   t[2] = (__bf16)(r - (float)t[1]);
+}
+
+__device__ __forceinline__ float join3(const __bf16* t, int64_t step) {
+  return ((float)t[0] + (float)t[step]) + (float)t[2 * step];
+}
+// The elements k of y (16, y[k / 4][k % 4], or turned y[k % 4][k / 4]) that are NaN,
+// as a bit each; they are 0 afterwards.
+template <bool TURNED>
+__device__ __forceinline__ uint32_t take_nan(f32x4 (&y)[4]) {
+  bool any = false;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    any |= __builtin_isunordered(y[q][0], y[q][1]) || __builtin_isunordered(y[q][2], y[q][3]);
+  uint32_t bad = 0;
+  if (any) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int i = TURNED ? k % 4 : k / 4, e = TURNED ? k / 4 : k % 4;
+      if (y[i][e] != y[i][e]) bad |= 1u << k, y[i][e] = 0.f;
+    }
+  }
+  return bad;
 }
 
 struct ExpandArgs {

@@ -193,8 +193,21 @@ __global__ __launch_bounds__(kThreads, !AHEAD && JB <= 2 ? 4 : 1) void expand(Ex
       lanes_in_order();
       f32x4 y[4];
 #pragma unroll
+      for (int q = 0; q < 4; ++q) y[q] = *(const f32x4*)(my + (q * 4 + g) * kTile + 4 * m);
+      if constexpr (FAST) {
+        for (uint32_t bad = take_nan<false>(y); bad; bad &= bad - 1) {
+          const int k = __builtin_ctz(bad), t = rb * 16 + k / 4 * 4 + g, c = c0 + 4 * m + k % 4;
+          float s = 0.f;
+          for (int j = 0; j < a.r && c < a.N && t < run.count; ++j)
+            s = fmaf(join3((const __bf16*)(shared_u + t * kU + j / 4 * kTerms) + j % 4, 4),
+                     (float)(FLAT ? w[(int64_t)j * a.N + c] : w[(int64_t)c * a.r + j]), s);
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (i == k) y[i / 4][i % 4] = s;
+        }
+      }
+#pragma unroll
       for (int q = 0; q < 4; ++q) {
-        y[q] = *(const f32x4*)(my + (q * 4 + g) * kTile + 4 * m);
         if (base) y[q] += f32x4{(float)old[q][0], (float)old[q][1], (float)old[q][2], (float)old[q][3]};
       }
       lanes_in_order();
@@ -252,6 +265,7 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
   const int my_row = l.order[run.first + (lane < run.count ? lane : run.count - 1)];  // of the run's row `lane`
   const int blocks = (run.count + 15) / 16;
   const bool there = run.key < a.n;
+  uint64_t again[NT] = {};  // elements that came out as NaN and count as 0 at first (split3)
   bf16x8 wf[NT][kSteps][4], u[kSteps][kTerms][4];
   if (there) {
 #pragma unroll
@@ -305,6 +319,7 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
       }
       const int c = c_first + ct * 64 + 16 * g, n = a.N - c;
       if (rb * 16 + m >= run.count || n <= 0) continue;
+      if (there) again[ct] |= (uint64_t)take_nan<true>(acc) << (rb * 16);
       O* dst = (O*)a.out + row * a.out_ld + c;
       const O* base = a.base ? (const O*)a.base + row * a.base_ld + c : nullptr;
       constexpr int E = 16 / (int)sizeof(O);  // columns a store
@@ -332,6 +347,18 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
       }
     }
   }
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct)
+    for (; again[ct]; again[ct] &= again[ct] - 1) {
+      const int at = __builtin_ctzll(again[ct]), c = c_first + ct * 64 + 16 * g + at % 16;
+      if (c >= a.N) continue;
+      const int64_t row = l.order[run.first + at / 16 * 16 + m];
+      const __bf16 *u = (const __bf16*)a.terms + row * 3 * a.rp, *w = (const __bf16*)a.w + (int64_t)run.key * a.r * a.N + c;
+      float s = 0.f;
+      for (int j = 0; j < a.r; ++j) s = fmaf(join3(u + j, a.rp), (float)w[(int64_t)j * a.N], s);
+      O* dst = (O*)a.out + row * a.out_ld + c;
+      *dst = narrow<O>(a.base ? (float)*dst + s : s);
+    }
 }
 
 template <class T, class O, bool FLAT, bool AHEAD>

@@ -241,20 +241,31 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   // runs of E elements next to each other in memory: four of the rank, or NB of the columns
   constexpr int E4 = CONTRACT ? 4 : NB;
   typedef float fe __attribute__((ext_vector_type(E4)));
+  constexpr int kQ = CONTRACT ? NB : 4;
+  auto column = [&](int ct, int q) {
+    return c_first + ct * kCols + wave * (16 * NB) + (CONTRACT ? NB * m + q : NB * (4 * g + q));
+  };
+  auto rank = [&](int jb) { return j0 + jb * 16 + (CONTRACT ? 4 * g : m); };
+  uint64_t again = 0;  // a bit an element that came out as NaN and counts as 0 here (split3)
+  static_assert(!P::FAST || CT * JB * kQ * E4 <= 64, "a bit an element");
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
     for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
-      for (int q = 0; q < (CONTRACT ? NB : 4); ++q) {
-        const int c0 = c_first + ct * kCols + wave * (16 * NB);
-        const int j = j0 + jb * 16 + (CONTRACT ? 4 * g : m), c = c0 + (CONTRACT ? NB * m + q : NB * (4 * g + q));
+      for (int q = 0; q < kQ; ++q) {
+        const int j = rank(jb), c = column(ct, q);
         if (j >= a.r || c >= a.N) continue;
         fe y;
 #pragma unroll
         for (int e = 0; e < E4; ++e) y[e] = CONTRACT ? acc[ct][jb][q][e] : acc[ct][jb][e][q];
         float* p = out + (CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c);
         const int left = CONTRACT ? a.r - j : a.N - c;
+        if constexpr (P::FAST) {
+#pragma unroll
+          for (int e = 0; e < E4; ++e)
+            if (e < left && y[e] != y[e]) again |= 1ull << (((ct * JB + jb) * kQ + q) * E4 + e), y[e] = 0.f;
+        }
         if (left >= E4) {
           if (add) y += load_n<true, fe, E4>(p, E4);
           __builtin_memcpy(p, &y, sizeof(y));
@@ -264,6 +275,15 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
             if (e < left) p[e] = add ? p[e] + y[e] : y[e];
         }
       }
+#pragma unroll 1
+  for (; again; again &= again - 1) {
+    const int at = __builtin_ctzll(again), e = at % E4, q = at / E4 % kQ, jb = at / (E4 * kQ) % JB, ct = at / (E4 * kQ * JB);
+    const int j = rank(jb) + (CONTRACT ? e : 0), c = column(ct, q) + (CONTRACT ? 0 : e);
+    float s = 0.f;
+    for (int t = 0; t < run.count; ++t)
+      s = fmaf((float)((const S*)a.src)[rows[t] * a.ld + c], a.w[(int64_t)rows[t] * a.rp + j], s);
+    out[CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c] += s;
+  }
 }
 
 template <class S, class W, bool CONTRACT, int JB, int CT>

@@ -316,3 +316,51 @@ def test_no_rows():
     assert gx.shape == (0, 4) and (ga == 0).all() and (gb == 0).all()
     tim.adapters_backward(torch.empty(0, 5, device="cuda"), x, none, ad, grad_a=old.fill_(1), grad_b=gb, accumulate=True)
     assert (old == 1).all()
+
+
+def _formula(base, x, rows, a, b, scales, grad):
+    """(out, grad_x, grad_a, grad_b) in float64, every product taken: 0 times an infinity is NaN in it."""
+    T, (n, r, d), N = x.shape[0], a.shape, b.shape[1]
+    x, a, b, grad, s = x.double(), a.double(), b.double(), grad.double(), scales.double()
+    out, gx = base.double().clone(), torch.zeros(T, d, dtype=torch.float64)
+    ga, gb = torch.zeros(n, r, d, dtype=torch.float64), torch.zeros(n, N, r, dtype=torch.float64)
+    for t in range(T):
+        k = int(rows[t])
+        if 0 <= k < n:
+            u, v = s[k] * (a[k] * x[t]).sum(1), s[k] * (b[k] * grad[t][:, None]).sum(0)
+            out[t] += (b[k] * u).sum(1)
+            gx[t] = (a[k] * v[:, None]).sum(0)
+            ga[k] += v[:, None] * x[t]
+            gb[k] += grad[t][:, None] * u
+    return out, gx, ga, gb
+
+
+# every kernel of the products: ranks of 1, 2, 4 and more blocks of 16, several tiles a wave, several blocks of rows
+INFINITE = [(40, 70, 90, 3, 5, "mixed"), (70, 40, 300, 1, 16, "one"), (33, 130, 600, 2, 25, "mixed"),
+            (90, 64, 80, 2, 44, "runs"), (20, 50, 70, 2, 64, "mixed"), (18, 40, 66, 2, 100, "mixed"),
+            (40, 24, 33001, 31, 16, "mixed"), (45, 24, 33001, 31, 27, "mixed")]
+
+
+@pytest.mark.parametrize("case", range(len(INFINITE)))
+@pytest.mark.parametrize("dtype,out", [(BF16, F32), (BF16, BF16), (F16, F32)])
+@pytest.mark.parametrize("where", ["a", "b", "x", "grad"])
+def test_infinities_give_what_the_formula_gives(case, dtype, out, where):
+    """An infinity times a number is an infinity, times 0 NaN, and nothing else changes: in whole numbers, which are exact."""
+    T, d, N, n, r, kind = INFINITE[case]
+    x, a, b, grad, scales, rows = _whole(T, d, N, n, r, kind, dtype, 31 * case)
+    g = torch.Generator().manual_seed(case)
+    base = torch.randint(-100, 101, (T, N), generator=g).to(out)
+    t = {"a": a, "b": b, "x": x, "grad": grad}[where].view(-1)
+    for value in (float("inf"), float("-inf")):
+        t[torch.randint(0, t.numel(), (6,), generator=g)] = value
+    print(INFINITE[case], dtype, out, where, flush=True)
+    want = _formula(base, x, rows, a, b, scales, grad)
+    ad = tim.Adapters(a.cuda(), b.cuda(), scales.cuda())
+    xd, rd, gd = x.cuda(), rows.cuda(), grad.to(out).cuda()
+    got = (tim.adapters_add(base.cuda(), xd, rd, ad), *tim.adapters_backward(gd, xd, rd, ad, dtype=out))
+    one = torch.ones(n, N, r, device="cuda")
+    added = tim.adapters_backward(gd, xd, rd, ad, want_x=False, want_a=False, grad_b=one, accumulate=True)[2]
+    for name, y, w in zip(("out", "grad_x", "grad_a", "grad_b", "grad_b added"), (*got, added), (*want, want[3] + 1)):
+        y, w = y.cpu(), w.to(y.dtype)
+        wrong = ~((y == w) | (torch.isnan(y) & torch.isnan(w)))
+        assert not wrong.any(), (name, int(wrong.sum()), y[wrong][:4], w[wrong][:4])
