@@ -112,23 +112,8 @@ __device__ __forceinline__ void split3(float x, __bf16 (&t)[3]) {
 __device__ __forceinline__ float join3(const __bf16* t, int64_t step) {
   return ((float)t[0] + (float)t[step]) + (float)t[2 * step];
 }
-// The elements k of y (16, y[k / 4][k % 4], or turned y[k % 4][k / 4]) that are NaN,
-// as a bit each; they are 0 afterwards.
-template <bool TURNED>
-__device__ __forceinline__ uint32_t take_nan(f32x4 (&y)[4]) {
-  bool any = false;
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-    any |= __builtin_isunordered(y[q][0], y[q][1]) || __builtin_isunordered(y[q][2], y[q][3]);
-  uint32_t bad = 0;
-  if (any) {
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      const int i = TURNED ? k % 4 : k / 4, e = TURNED ? k / 4 : k % 4;
-      if (y[i][e] != y[i][e]) bad |= 1u << k, y[i][e] = 0.f;
-    }
-  }
-  return bad;
+__device__ __forceinline__ bool has_nan(f32x4 y) {
+  return __builtin_isunordered(y[0], y[1]) || __builtin_isunordered(y[2], y[3]);
 }
 
 struct ExpandArgs {

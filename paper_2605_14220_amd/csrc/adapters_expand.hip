@@ -193,21 +193,8 @@ __global__ __launch_bounds__(kThreads, !AHEAD && JB <= 2 ? 4 : 1) void expand(Ex
       lanes_in_order();
       f32x4 y[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) y[q] = *(const f32x4*)(my + (q * 4 + g) * kTile + 4 * m);
-      if constexpr (FAST) {
-        for (uint32_t bad = take_nan<false>(y); bad; bad &= bad - 1) {
-          const int k = __builtin_ctz(bad), t = rb * 16 + k / 4 * 4 + g, c = c0 + 4 * m + k % 4;
-          float s = 0.f;
-          for (int j = 0; j < a.r && c < a.N && t < run.count; ++j)
-            s = fmaf(join3((const __bf16*)(shared_u + t * kU + j / 4 * kTerms) + j % 4, 4),
-                     (float)(FLAT ? w[(int64_t)j * a.N + c] : w[(int64_t)c * a.r + j]), s);
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (i == k) y[i / 4][i % 4] = s;
-        }
-      }
-#pragma unroll
       for (int q = 0; q < 4; ++q) {
+        y[q] = *(const f32x4*)(my + (q * 4 + g) * kTile + 4 * m);
         if (base) y[q] += f32x4{(float)old[q][0], (float)old[q][1], (float)old[q][2], (float)old[q][3]};
       }
       lanes_in_order();
@@ -224,6 +211,22 @@ __global__ __launch_bounds__(kThreads, !AHEAD && JB <= 2 ? 4 : 1) void expand(Ex
         const int64_t row = row_of(rb, q);
         if (t >= run.count || n <= 0) continue;
         O* dst = (O*)a.out + row * a.out_ld + c;
+        if constexpr (FAST) {
+          if (__builtin_expect(has_nan(y[q]), 0)) {  // see split3
+#pragma unroll 1
+            for (int e = 0; e < 4 && e < n; ++e) {
+              float s = 0.f;
+#pragma unroll 1
+              for (int j = 0; j < a.r; ++j)
+                s = fmaf(join3((const __bf16*)(shared_u + t * kU + j / 4 * kTerms) + j % 4, 4),
+                         (float)(FLAT ? w[(int64_t)j * a.N + c + e] : w[(int64_t)(c + e) * a.r + j]), s);
+              if (base) s += (float)base[row * a.base_ld + c + e];
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (i == e && y[q][i] != y[q][i]) y[q][i] = s;
+            }
+          }
+        }
         x4<O> z;
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[e] = narrow<O>(y[q][e]);
@@ -319,7 +322,11 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
       }
       const int c = c_first + ct * 64 + 16 * g, n = a.N - c;
       if (rb * 16 + m >= run.count || n <= 0) continue;
-      if (there) again[ct] |= (uint64_t)take_nan<true>(acc) << (rb * 16);
+      if (__builtin_expect(has_nan(acc[0]) || has_nan(acc[1]) || has_nan(acc[2]) || has_nan(acc[3]), 0)) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          if (acc[k % 4][k / 4] != acc[k % 4][k / 4]) again[ct] |= 1ull << (rb * 16 + k), acc[k % 4][k / 4] = 0.f;
+      }
       O* dst = (O*)a.out + row * a.out_ld + c;
       const O* base = a.base ? (const O*)a.base + row * a.base_ld + c : nullptr;
       constexpr int E = 16 / (int)sizeof(O);  // columns a store
@@ -349,12 +356,13 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
   }
 #pragma unroll
   for (int ct = 0; ct < NT; ++ct)
-    for (; again[ct]; again[ct] &= again[ct] - 1) {
+    for (; __builtin_expect(again[ct] != 0, 0); again[ct] &= again[ct] - 1) {
       const int at = __builtin_ctzll(again[ct]), c = c_first + ct * 64 + 16 * g + at % 16;
       if (c >= a.N) continue;
       const int64_t row = l.order[run.first + at / 16 * 16 + m];
       const __bf16 *u = (const __bf16*)a.terms + row * 3 * a.rp, *w = (const __bf16*)a.w + (int64_t)run.key * a.r * a.N + c;
       float s = 0.f;
+#pragma unroll 1
       for (int j = 0; j < a.r; ++j) s = fmaf(join3(u + j, a.rp), (float)w[(int64_t)j * a.N], s);
       O* dst = (O*)a.out + row * a.out_ld + c;
       *dst = narrow<O>(a.base ? (float)*dst + s : s);

@@ -246,8 +246,23 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
     return c_first + ct * kCols + wave * (16 * NB) + (CONTRACT ? NB * m + q : NB * (4 * g + q));
   };
   auto rank = [&](int jb) { return j0 + jb * 16 + (CONTRACT ? 4 * g : m); };
-  uint64_t again = 0;  // a bit an element that came out as NaN and counts as 0 here (split3)
-  static_assert(!P::FAST || CT * JB * kQ * E4 <= 64, "a bit an element");
+  uint64_t again = 0;  // a bit an element that came out as NaN and counts as 0 at first (split3)
+  if constexpr (P::FAST) {
+    static_assert(NB == 4 && kQ == 4 && E4 == 4 && CT * JB <= 4, "a bit an element");
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < CT * JB * 4; ++i) any |= has_nan(acc[i / 4 / JB][i / 4 % JB][i % 4]);
+    if (__builtin_expect(any, 0)) {
+#pragma unroll
+      for (int i = 0; i < CT * JB * 16; ++i) {
+        const int ct = i / 16 / JB, jb = i / 16 % JB, q = i / 4 % 4, e = i % 4;
+        f32x4& y = acc[ct][jb][CONTRACT ? q : e];
+        const int k = CONTRACT ? e : q;
+        if (rank(jb) + (CONTRACT ? e : 0) < a.r && column(ct, q) + (CONTRACT ? 0 : e) < a.N && y[k] != y[k])
+          again |= 1ull << i, y[k] = 0.f;
+      }
+    }
+  }
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -261,11 +276,6 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
         for (int e = 0; e < E4; ++e) y[e] = CONTRACT ? acc[ct][jb][q][e] : acc[ct][jb][e][q];
         float* p = out + (CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c);
         const int left = CONTRACT ? a.r - j : a.N - c;
-        if constexpr (P::FAST) {
-#pragma unroll
-          for (int e = 0; e < E4; ++e)
-            if (e < left && y[e] != y[e]) again |= 1ull << (((ct * JB + jb) * kQ + q) * E4 + e), y[e] = 0.f;
-        }
         if (left >= E4) {
           if (add) y += load_n<true, fe, E4>(p, E4);
           __builtin_memcpy(p, &y, sizeof(y));
@@ -275,11 +285,11 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
             if (e < left) p[e] = add ? p[e] + y[e] : y[e];
         }
       }
-#pragma unroll 1
-  for (; again; again &= again - 1) {
-    const int at = __builtin_ctzll(again), e = at % E4, q = at / E4 % kQ, jb = at / (E4 * kQ) % JB, ct = at / (E4 * kQ * JB);
+  for (; __builtin_expect(again != 0, 0); again &= again - 1) {
+    const int at = __builtin_ctzll(again), e = at % 4, q = at / 4 % 4, jb = at / 16 % JB, ct = at / 16 / JB;
     const int j = rank(jb) + (CONTRACT ? e : 0), c = column(ct, q) + (CONTRACT ? 0 : e);
     float s = 0.f;
+#pragma unroll 1
     for (int t = 0; t < run.count; ++t)
       s = fmaf((float)((const S*)a.src)[rows[t] * a.ld + c], a.w[(int64_t)rows[t] * a.rp + j], s);
     out[CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c] += s;
