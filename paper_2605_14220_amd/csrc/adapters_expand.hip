@@ -268,7 +268,7 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
   const int my_row = l.order[run.first + (lane < run.count ? lane : run.count - 1)];  // of the run's row `lane`
   const int blocks = (run.count + 15) / 16;
   const bool there = run.key < a.n;
-  uint64_t again[NT] = {};  // elements that came out as NaN and count as 0 at first (split3)
+  uint64_t again[NT] = {};  // elements that came out as NaN (split3); added to base, they count as 0 at first
   bf16x8 wf[NT][kSteps][4], u[kSteps][kTerms][4];
   if (there) {
 #pragma unroll
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
       if (__builtin_expect(has_nan(acc[0]) || has_nan(acc[1]) || has_nan(acc[2]) || has_nan(acc[3]), 0)) {
 #pragma unroll
         for (int k = 0; k < 16; ++k)
-          if (acc[k % 4][k / 4] != acc[k % 4][k / 4]) again[ct] |= 1ull << (rb * 16 + k), acc[k % 4][k / 4] = 0.f;
+          if (acc[k % 4][k / 4] != acc[k % 4][k / 4]) again[ct] |= 1ull << (rb * 16 + k);
       }
       O* dst = (O*)a.out + row * a.out_ld + c;
       const O* base = a.base ? (const O*)a.base + row * a.base_ld + c : nullptr;
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
           for (int e = 0; e < E; ++e) {
             const int k = s * E + e;  // acc[k % 4][k / 4]
             const float y = acc[k % 4][k / 4];
-            z[e] = base ? (there ? narrow<O>((float)old[e] + y) : old[e]) : narrow<O>(y);
+            z[e] = base ? (there && y == y ? narrow<O>((float)old[e] + y) : old[e]) : narrow<O>(y);
           }
           __builtin_memcpy(dst + s * E, &z, sizeof(z));
         }
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
         for (int k = 0; k < 16; ++k)
           if (k < n) {
             const float y = acc[k % 4][k / 4];
-            dst[k] = base ? (there ? narrow<O>((float)base[k] + y) : base[k]) : narrow<O>(y);
+            dst[k] = base ? (there && y == y ? narrow<O>((float)base[k] + y) : base[k]) : narrow<O>(y);
           }
       }
     }

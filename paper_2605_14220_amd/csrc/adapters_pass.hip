@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
     return c_first + ct * kCols + wave * (16 * NB) + (CONTRACT ? NB * m + q : NB * (4 * g + q));
   };
   auto rank = [&](int jb) { return j0 + jb * 16 + (CONTRACT ? 4 * g : m); };
-  uint64_t again = 0;  // a bit an element that came out as NaN and counts as 0 at first (split3)
+  uint64_t again = 0;  // a bit an element that came out as NaN (split3); added, it counts as 0 at first
   if constexpr (P::FAST) {
     static_assert(NB == 4 && kQ == 4 && E4 == 4 && CT * JB <= 4, "a bit an element");
     bool any = false;
@@ -256,10 +256,8 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
 #pragma unroll
       for (int i = 0; i < CT * JB * 16; ++i) {
         const int ct = i / 16 / JB, jb = i / 16 % JB, q = i / 4 % 4, e = i % 4;
-        f32x4& y = acc[ct][jb][CONTRACT ? q : e];
-        const int k = CONTRACT ? e : q;
-        if (rank(jb) + (CONTRACT ? e : 0) < a.r && column(ct, q) + (CONTRACT ? 0 : e) < a.N && y[k] != y[k])
-          again |= 1ull << i, y[k] = 0.f;
+        const float y = CONTRACT ? acc[ct][jb][q][e] : acc[ct][jb][e][q];
+        if (rank(jb) + (CONTRACT ? e : 0) < a.r && column(ct, q) + (CONTRACT ? 0 : e) < a.N && y != y) again |= 1ull << i;
       }
     }
   }
@@ -276,6 +274,10 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
         for (int e = 0; e < E4; ++e) y[e] = CONTRACT ? acc[ct][jb][q][e] : acc[ct][jb][e][q];
         float* p = out + (CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c);
         const int left = CONTRACT ? a.r - j : a.N - c;
+        if (P::FAST && add) {
+#pragma unroll
+          for (int e = 0; e < E4; ++e) y[e] = y[e] == y[e] ? y[e] : 0.f;
+        }
         if (left >= E4) {
           if (add) y += load_n<true, fe, E4>(p, E4);
           __builtin_memcpy(p, &y, sizeof(y));
@@ -292,7 +294,8 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
 #pragma unroll 1
     for (int t = 0; t < run.count; ++t)
       s = fmaf((float)((const S*)a.src)[rows[t] * a.ld + c], a.w[(int64_t)rows[t] * a.rp + j], s);
-    out[CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c] += s;
+    float* p = out + (CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c);
+    *p = add ? *p + s : s;
   }
 }
 

@@ -358,9 +358,10 @@ def test_infinities_give_what_the_formula_gives(case, dtype, out, where):
     ad = tim.Adapters(a.cuda(), b.cuda(), scales.cuda())
     xd, rd, gd = x.cuda(), rows.cuda(), grad.to(out).cuda()
     got = (tim.adapters_add(base.cuda(), xd, rd, ad), *tim.adapters_backward(gd, xd, rd, ad, dtype=out))
-    one = torch.ones(n, N, r, device="cuda")
-    added = tim.adapters_backward(gd, xd, rd, ad, want_x=False, want_a=False, grad_b=one, accumulate=True)[2]
-    for name, y, w in zip(("out", "grad_x", "grad_a", "grad_b", "grad_b added"), (*got, added), (*want, want[3] + 1)):
+    ones = [torch.ones_like(t) for t in got[1:]]
+    tim.adapters_backward(gd, xd, rd, ad, grad_x=ones[0], accumulate_x=True, grad_a=ones[1], grad_b=ones[2], accumulate=True)
+    names = ("out", "grad_x", "grad_a", "grad_b", "grad_x added", "grad_a added", "grad_b added")
+    for name, y, w in zip(names, (*got, *ones), (*want, *(t + 1 for t in want[1:]))):
         y, w = y.cpu(), w.to(y.dtype)
         wrong = ~((y == w) | (torch.isnan(y) & torch.isnan(w)))
         assert not wrong.any(), (name, int(wrong.sum()), y[wrong][:4], w[wrong][:4])
