@@ -257,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
       for (int i = 0; i < CT * JB * 16; ++i) {
         const int ct = i / 16 / JB, jb = i / 16 % JB, q = i / 4 % 4, e = i % 4;
         const float y = CONTRACT ? acc[ct][jb][q][e] : acc[ct][jb][e][q];
-        if (rank(jb) + (CONTRACT ? e : 0) < a.r && column(ct, q) + (CONTRACT ? 0 : e) < a.N && y != y) again |= 1ull << i;
+        if (y != y) again |= 1ull << i;
       }
     }
   }
@@ -290,6 +290,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   for (; __builtin_expect(again != 0, 0); again &= again - 1) {
     const int at = __builtin_ctzll(again), e = at % 4, q = at / 4 % 4, jb = at / 16 % JB, ct = at / 16 / JB;
     const int j = rank(jb) + (CONTRACT ? e : 0), c = column(ct, q) + (CONTRACT ? 0 : e);
+    if (j >= a.r || c >= a.N) continue;
     float s = 0.f;
 #pragma unroll 1
     for (int t = 0; t < run.count; ++t)
