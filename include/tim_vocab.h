@@ -48,7 +48,7 @@ extern "C" {
  *         the inputs.
  * scale   any finite fp32 value.
  * Errors: TIM_ERR_SHAPE (T < 0, V, d, strides), TIM_ERR_VALUE (dtypes, scale,
- * alignment to the element), TIM_ERR_NULL. */
+ * alignment to the element, overlap), TIM_ERR_NULL. */
 tim_status tim_embedding(const void* table, int32_t dtype, int32_t V, int32_t d, int64_t ld, const int32_t* tokens,
                          int64_t T, float scale, void* out, int32_t out_dtype, int64_t out_ld, hipStream_t stream);
 
@@ -64,6 +64,7 @@ tim_status tim_embedding(const void* table, int32_t dtype, int32_t V, int32_t d,
  *             1 the sums are added to the rows of the tokens that occur and no
  *             other row is touched; with 0 every row is written, zeros where a
  *             token does not occur (elements d .. grad_ld - 1 stay untouched).
+ *             No overlap with the inputs.
  * workspace   tim_embedding_backward_workspace_size(T, V, d) bytes, 16-byte
  *             aligned; 0 for invalid arguments or T == 0.
  * Errors as tim_embedding; TIM_ERR_VALUE also for accumulate not 0 or 1;
@@ -114,7 +115,7 @@ typedef struct {
  * workspace  tim_adapters_add_workspace_size(T, d, N, n, r) bytes, 16-byte
  *         aligned.
  * Errors: TIM_ERR_SHAPE (T, n, r, d, N, strides), TIM_ERR_VALUE (dtypes,
- * alignment to the element), TIM_ERR_NULL, TIM_ERR_WORKSPACE. */
+ * alignment to the element, overlap), TIM_ERR_NULL, TIM_ERR_WORKSPACE. */
 size_t tim_adapters_add_workspace_size(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r);
 tim_status tim_adapters_add(const tim_adapters* adapters, const void* x, int64_t x_ld, const int32_t* rows, int64_t T,
                             const void* base, int64_t base_ld, void* out, int32_t out_dtype, int64_t out_ld,
@@ -134,6 +135,8 @@ tim_status tim_adapters_add(const tim_adapters* adapters, const void* x, int64_t
  *          written, zeros for a row without an adapter.
  * grad_a, grad_b  contiguous; either may be NULL. With accumulate_ab = 1 both are
  *          added to, else written, zeros for an adapter without rows.
+ * The gradients written overlap neither each other nor an input (grad_x may lie in
+ * the same buffer's columns beside x or grad).
  * workspace  tim_adapters_backward_workspace_size(T, d, N, n, r) bytes, 16-byte
  *          aligned.
  * Arithmetic: u and v are accumulated and kept in fp32 (in products with bf16 as

@@ -889,7 +889,7 @@ def embedding(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, dty
               out: torch.Tensor | None = None) -> torch.Tensor:
     """scale * table[tokens]: rows [T, d] of table [V, d] (fp32, bf16 or fp16, dense rows) for tokens int32 [T], each
     element formed in fp32 and rounded once to dtype (the table's by default); zeros for a token outside [0, V)
-    (padding). out, if given, may have padded rows."""
+    (padding). out, if given, may have padded rows, and shares no memory with the inputs."""
     lib = load_library()
     if table.dtype not in _DTYPES:
         raise TypeError("tim.embedding: the table must be fp32, bf16 or fp16")
@@ -925,7 +925,8 @@ def embedding_backward(grad: torch.Tensor, tokens: torch.Tensor, V: int, scale: 
                        workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient fp32 [V, d] of the embedding's table from that of its rows, grad [T, d] (fp32, bf16 or fp16, dense
     rows). With accumulate the sums are added to grad_table (the grad_w of logprobs_backward for a tied head) in the rows
-    of the tokens that occur; otherwise every row is written. Deterministic."""
+    of the tokens that occur; otherwise every row is written. grad_table shares no memory with the inputs.
+    Deterministic."""
     lib = load_library()
     if grad.dtype not in _DTYPES:
         raise TypeError("tim.embedding_backward: grad must be fp32, bf16 or fp16")
@@ -1065,7 +1066,8 @@ def adapters_backward(grad: torch.Tensor, x: torch.Tensor, rows: torch.Tensor, a
     """(grad_x [T, d] or None, grad_a fp32 [n, r, d] or None, grad_b fp32 [n, N, r] or None) through adapters_add, from
     the gradient [T, N] of its output (fp32, bf16 or fp16, dense rows). grad_x is of dtype (x's by default); with
     accumulate_x it is added to the grad_x given, with accumulate grad_a and grad_b to theirs. Rows without an adapter and
-    adapters without rows get zeros, or nothing added."""
+    adapters without rows get zeros, or nothing added. The gradients share no memory with each other or with the inputs:
+    grad_x cannot take x's place."""
     lib = load_library()
     name = "adapters_backward"
     ad, T, x_ld = _adapters(name, adapters, x, rows)

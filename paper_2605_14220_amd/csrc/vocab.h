@@ -9,6 +9,7 @@
 #include <cstdint>
 
 #include "grouping.h"
+#include "overlap.h"
 #include "policy.h"
 #include "tim_vocab.h"
 
@@ -27,6 +28,9 @@ inline tim_status validate_embedding(const void* table, int32_t dtype, int32_t V
   if (T == 0) return TIM_OK;
   if (!table || !tokens || !out) return TIM_ERR_NULL;
   if (!aligned_to(table, dtype_bytes(dtype)) || !aligned_to(tokens, 4) || !aligned_to(out, dtype_bytes(out_dtype)))
+    return TIM_ERR_VALUE;
+  const Rows o = rows_of(out, T, d, out_ld, dtype_bytes(out_dtype));
+  if (share_bytes(o, rows_of(table, V, d, ld, dtype_bytes(dtype))) || share_bytes(o, flat(tokens, T, 4)))
     return TIM_ERR_VALUE;
   return TIM_OK;
 }
@@ -60,6 +64,9 @@ inline tim_status validate_embedding_backward(const void* grad_out, int32_t dtyp
   if (!grad_out || !tokens) return TIM_ERR_NULL;
   if (!aligned_to(grad_out, dtype_bytes(dtype)) || !aligned_to(tokens, 4)) return TIM_ERR_VALUE;
   if (!ws || !aligned16(ws) || ws_bytes < plan_embedding_backward(T, V, d).bytes) return TIM_ERR_WORKSPACE;
+  const Rows o = rows_of(grad_table, V, d, grad_ld, 4);
+  if (share_bytes(o, rows_of(grad_out, T, d, ld, dtype_bytes(dtype))) || share_bytes(o, flat(tokens, T, 4)))
+    return TIM_ERR_VALUE;
   return TIM_OK;
 }
 
@@ -187,6 +194,14 @@ inline tim_status validate_adapters(const tim_adapters* ad, const void* x, int64
   return TIM_OK;
 }
 
+// Whether `out` has a byte in common with the adapters, the rows or x.
+inline bool shares_adapters(const Rows& out, const tim_adapters& ad, const void* x, int64_t x_ld, const int32_t* rows,
+                            int64_t T) {
+  return share_bytes(out, rows_of(x, T, ad.d, x_ld, 2)) || share_bytes(out, flat(rows, T, 4)) ||
+         share_bytes(out, flat(ad.a, ad.n, (int64_t)ad.r * ad.d * 2)) ||
+         share_bytes(out, flat(ad.b, ad.n, (int64_t)ad.r * ad.N * 2)) || share_bytes(out, flat(ad.scales, ad.n, 4));
+}
+
 inline tim_status validate_adapters_add(const tim_adapters* ad, const void* x, int64_t x_ld, const int32_t* rows,
                                         int64_t T, const void* base, int64_t base_ld, const void* out,
                                         int32_t out_dtype, int64_t out_ld, const void* ws, size_t ws_bytes) {
@@ -200,6 +215,10 @@ inline tim_status validate_adapters_add(const tim_adapters* ad, const void* x, i
   if (!aligned_to(base, dtype_bytes(out_dtype)) || !aligned_to(out, dtype_bytes(out_dtype))) return TIM_ERR_VALUE;
   if (!ws || !aligned16(ws) || ws_bytes < plan_adapters(T, ad->d, ad->N, ad->n, ad->r, 0).bytes)
     return TIM_ERR_WORKSPACE;
+  const int bytes = dtype_bytes(out_dtype);
+  const Rows o = rows_of(out, T, ad->N, out_ld, bytes);
+  if (shares_adapters(o, *ad, x, x_ld, rows, T) || (base != out && share_bytes(o, rows_of(base, T, ad->N, base_ld, bytes))))
+    return TIM_ERR_VALUE;
   return TIM_OK;
 }
 
@@ -219,6 +238,13 @@ inline tim_status validate_adapters_backward(const tim_adapters* ad, const void*
   if (!aligned_to(grad, dtype_bytes(grad_dtype))) return TIM_ERR_VALUE;
   if (!ws || !aligned16(ws) || ws_bytes < adapters_backward_workspace(T, ad->d, ad->N, ad->n, ad->r))
     return TIM_ERR_WORKSPACE;
+  const Rows outs[3] = {rows_of(grad_x, T, ad->d, gx_ld, grad_x ? dtype_bytes(gx_dtype) : 0),
+                        flat(grad_a, ad->n, (int64_t)ad->r * ad->d * 4), flat(grad_b, ad->n, (int64_t)ad->r * ad->N * 4)};
+  for (int i = 0; i < 3; ++i)
+    if (shares_adapters(outs[i], *ad, x, x_ld, rows, T) ||
+        share_bytes(outs[i], rows_of(grad, T, ad->N, grad_ld, dtype_bytes(grad_dtype))) ||
+        share_bytes(outs[i], outs[(i + 1) % 3]))
+      return TIM_ERR_VALUE;
   return TIM_OK;
 }
 

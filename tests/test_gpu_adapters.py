@@ -365,3 +365,26 @@ def test_infinities_give_what_the_formula_gives(case, dtype, out, where):
         y, w = y.cpu(), w.to(y.dtype)
         wrong = ~((y == w) | (torch.isnan(y) & torch.isnan(w)))
         assert not wrong.any(), (name, int(wrong.sum()), y[wrong][:4], w[wrong][:4])
+
+
+def test_outputs_beside_and_over_inputs():
+    """grad_x in the columns beside x and out beside base, in one buffer each: as apart. Over an input: refused, with nothing
+    written."""
+    T, d, N = 70, 24, 40
+    x, a, b, grad, scales, rows = [t.cuda() for t in _whole(T, d, N, 3, 5, "mixed", BF16, 9)]
+    ad = tim.Adapters(a, b, scales)
+    base = torch.randn(T, N, device="cuda").to(BF16)
+    want = tim.adapters_backward(grad, x, rows, ad)
+    out = tim.adapters_add(base, x, rows, ad)
+    both, two = torch.zeros(T, 2 * d, dtype=BF16, device="cuda"), torch.zeros(T, 2 * N, dtype=BF16, device="cuda")
+    both[:, :d], two[:, N:] = x, base
+    got = tim.adapters_backward(grad, both[:, :d], rows, ad, grad_x=both[:, d:])
+    assert all(torch.equal(p, q) for p, q in zip(got, want)) and torch.equal(both[:, :d], x)
+    assert torch.equal(tim.adapters_add(two[:, N:], x, rows, ad, out=two[:, :N]), out) and torch.equal(two[:, N:], base)
+    kept = x.clone(), grad.clone(), base.clone()
+    for gx in (x, grad[:, :d], grad[:, N - d:]):
+        with pytest.raises(RuntimeError):
+            tim.adapters_backward(grad, x, rows, ad, grad_x=gx)
+    with pytest.raises(RuntimeError):
+        tim.adapters_add(base[1:], x[1:], rows[1:], ad, out=base[:-1])
+    assert torch.equal(x, kept[0]) and torch.equal(grad, kept[1]) and torch.equal(base, kept[2])

@@ -243,3 +243,68 @@ def test_adapters_can_be_copied_and_pickled():
     for c in (copy.deepcopy(ad), copy.copy(ad), pickle.loads(pickle.dumps(ad))):
         assert torch.equal(c.a, ad.a) and torch.equal(c.b, ad.b) and torch.equal(c.scales, ad.scales)
         assert c._built is None
+
+
+# ------------------------------------------------------------------ outputs over inputs
+
+
+def test_rows_that_share_bytes(tmp_path):
+    """Against the bytes themselves, written out."""
+    src = tmp_path / "shim.cpp"
+    src.write_text("""
+#include "overlap.h"
+extern "C" int share(int64_t a, int64_t rows_a, int64_t width_a, int64_t ld_a, int64_t b, int64_t rows_b, int64_t width_b,
+                     int64_t ld_b) {
+  return tim::share_bytes({(const void*)a, rows_a, width_a, ld_a}, {(const void*)b, rows_b, width_b, ld_b});
+}
+""")
+    so = str(tmp_path / "shim.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC, "-o", so, str(src)], check=True)
+    share = ctypes.CDLL(so).share
+    share.argtypes = [ctypes.c_int64] * 8
+    import random
+    rng = random.Random(1)
+    seen = [0, 0]
+    for _ in range(20000):
+        def rows():
+            width = rng.randint(1, 9)
+            return rng.randint(100, 160), rng.randint(1, 6), width, width + rng.choice([0, 1, 2, 7, 13])
+        a, b = rows(), rows()
+        if rng.random() < 0.4:
+            b = (*b[:3], max(a[3], b[2]))
+        of = lambda p, n, width, ld: {p + i * ld + k for i in range(n) for k in range(width)}
+        want = bool(of(*a) & of(*b))
+        seen[want] += 1
+        assert share(*a, *b) == share(*b, *a) == want, (a, b)
+    assert min(seen) > 2000
+    assert not share(0, 5, 4, 4, 100, 5, 4, 4) and not share(100, 0, 4, 4, 100, 5, 4, 4)  # nothing there
+    far = 1 << 46
+    assert not share(far, 1 << 23, 1 << 20, 1 << 40, 1 << 45, 1, 8, 8) and share(far, 1 << 23, 8, 1 << 40, far + (5 << 40) + 7, 1, 1, 1)
+
+
+AT = {k: (i + 1) << 24 for i, k in enumerate(("x", "rows", "grad", "base", "out", "gx", "ga", "gb", "ws"))}  # 16 MiB apart
+AT_AD = dict(a=20 << 24, b=21 << 24, scales=22 << 24)
+
+
+@pytest.mark.parametrize("over", ["x", "rows", "a", "b", "scales"])
+def test_outputs_over_inputs_are_refused(lib, over):
+    there = {**AT, **AT_AD}[over]
+    add = {k: AT[k] for k in ("x", "rows", "base", "out", "ws")}
+    assert _add(lib, ad=AT_AD, **{**add, "out": there}) == VALUE
+    back = {k: AT[k] for k in ("x", "rows", "grad", "gx", "ga", "gb", "ws")}
+    for k in ("gx", "ga", "gb"):
+        assert _back(lib, ad=AT_AD, **{**back, k: there}) == VALUE
+        assert _back(lib, ad=AT_AD, **{**back, k: AT["grad"] + 4}) == VALUE
+        for m in ("gx", "ga", "gb"):
+            if k != m:
+                assert _back(lib, ad=AT_AD, **{**back, k: AT[m]}) == VALUE
+
+
+def test_shifted_outputs_are_refused(lib):
+    add = {k: AT[k] for k in ("x", "rows", "base", "out", "ws")}
+    for shift in (4, 64, -64, 4 * 5 * 16 - 4):  # base's rows one on, and its last element
+        assert _add(lib, ad=AT_AD, **{**add, "out": AT["base"] + shift}) == VALUE
+    assert _embed(lib, table=AT["x"], tokens=AT["rows"], out=AT["x"] + 10 * 8 * 2 - 4) == VALUE
+    assert _embed(lib, table=AT["x"], tokens=AT["rows"], out=AT["rows"] + 12) == VALUE
+    assert _embed_back(lib, grad=AT["x"], tokens=AT["rows"], table=AT["x"], ws=AT["ws"]) == VALUE
+    assert _embed_back(lib, grad=AT["x"], tokens=AT["rows"], table=AT["rows"] - 4, ws=AT["ws"]) == VALUE
