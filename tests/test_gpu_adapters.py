@@ -388,3 +388,107 @@ def test_outputs_beside_and_over_inputs():
     with pytest.raises(RuntimeError):
         tim.adapters_add(base[1:], x[1:], rows[1:], ad, out=base[:-1])
     assert torch.equal(x, kept[0]) and torch.equal(grad, kept[1]) and torch.equal(base, kept[2])
+
+
+def _few(rows, cols, top, keep, dtype, g):
+    """Whole numbers up to top in magnitude, a share `keep` of them not 0, made on the GPU."""
+    z = torch.randint(-top, top + 1, (rows, cols), generator=g, device="cuda", dtype=torch.int8)
+    return z.to(dtype).mul_(torch.rand(rows, cols, generator=g, device="cuda") < keep)
+
+
+def _check_exact(grad, x, rows, a, b, got, step):
+    """Gradients of whole numbers against float64 products, `step` rows of grad at a time."""
+    for k in range(a.shape[0]):
+        mine = (rows == k).nonzero()[:, 0]
+        A, B = a[k].double(), b[k].double()
+        ga, gb = torch.zeros_like(A), torch.zeros_like(B)
+        for t in range(0, len(mine), step):
+            i = mine[t:t + step]
+            X, G = x[i].double(), grad[i].double()
+            u, v = X @ A.T.contiguous(), G @ B
+            assert torch.equal(got[0][i].double(), v @ A)
+            ga += v.T.contiguous() @ X
+            gb += G.T.contiguous() @ u
+        assert ga.abs().max() < 2 ** 24 and gb.abs().max() < 2 ** 24
+        assert torch.equal(got[1][k].double(), ga) and torch.equal(got[2][k].double(), gb)
+
+
+@pytest.mark.parametrize("T", [700, 1500])
+@pytest.mark.parametrize("r", [9, 16])
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (BF16, F32), (BF16, F16), (F16, F16), (F16, F32)])
+def test_long_runs_on_a_wide_head(T, r, dtype, out):
+    """Two tiles of columns a workgroup beside runs of several blocks of 64 rows (256 or 512 rows, as T is), with gradients
+    that the caches hold and larger ones; to the last bit, for sums of few small whole numbers are exact in any order."""
+    d, N, n = 72, 100003, 2
+    g = torch.Generator(device="cuda").manual_seed(r)
+    x, a = _few(T, d, 2, 0.3, dtype, g), _few(n * r, d, 2, 1.0, dtype, g).view(n, r, d)
+    b, grad = _few(n * N, r, 2, 0.5, dtype, g).view(n, N, r), _few(T, N, 2, 40 / N, out, g)
+    rows = torch.randint(-1, n, (T,), generator=g, device="cuda", dtype=torch.int32)
+    grad[:, N - 1] = 1  # the last tile's end
+    grad[rows < 0] = float("nan")
+    print(T, r, dtype, out, flush=True)
+    got = tim.adapters_backward(grad, x, rows, tim.Adapters(a, b), dtype=F32)
+    assert (got[0][rows < 0] == 0).all()
+    _check_exact(grad, x, rows, a, b, got, 400)
+
+
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_gradients_of_more_than_31_bits_of_elements(out):
+    T, d, N, n, r = 15000, 40, 150001, 2, 16
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, a = _few(T, d, 1, 0.2, BF16, g), _few(n * r, d, 1, 1.0, BF16, g).view(n, r, d)
+    b = _few(n * N, r, 1, 0.02, BF16, g).view(n, N, r)
+    grad = torch.empty(T, N, dtype=out, device="cuda")
+    for t in range(0, T, 1000):
+        grad[t:t + 1000] = _few(1000, N, 1, 0.01, out, g)
+    rows = torch.randint(-1, n, (T,), generator=g, device="cuda", dtype=torch.int32)
+    got = tim.adapters_backward(grad, x, rows, tim.Adapters(a, b), dtype=F32)
+    _check_exact(grad, x, rows, a, b, got, 1000)
+
+
+@pytest.mark.parametrize("r", [16, 27])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_a_row_depends_on_itself_only_whatever_kernels_are_chosen(r, out):
+    """out and grad_x bit for bit for row counts on both sides of every choice: tiles of columns a workgroup (two from few
+    rows of many adapters on), tiles a wave in the forward (several for runs of few rows) and in grad_x's product (two for
+    many runs)."""
+    d, N, n = 4100, 50257, 40
+    g = torch.Generator(device="cuda").manual_seed(r)
+    normal = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    ad = tim.Adapters((normal(n, r, d) / d ** 0.5).to(BF16), (0.1 * normal(n, N, r)).to(BF16), torch.rand(n, generator=g, device="cuda"))
+    x, base, grad = normal(1, d).to(BF16), normal(1, N).to(out), normal(1, N).to(out)
+    one = torch.full((1,), 3, dtype=torch.int32, device="cuda")
+    y0 = tim.adapters_add(base, x, one, ad)
+    x0 = tim.adapters_backward(grad, x, one, ad, dtype=F32, want_a=False, want_b=False)[0]
+    for T in (2, 5, 65, 700, 8200):
+        at = T * 2 // 3
+        X, Y, G = normal(T, d).to(BF16), normal(T, N).to(out), normal(T, N).to(out)
+        X[at], Y[at], G[at] = x[0], base[0], grad[0]
+        rows = torch.randint(-1, n, (T,), generator=g, device="cuda", dtype=torch.int32)
+        rows[at] = 3
+        print(T, r, out, flush=True)
+        assert torch.equal(tim.adapters_add(Y, X, rows, ad)[at], y0[0])
+        for want in (False, True):
+            got = tim.adapters_backward(G, X, rows, ad, dtype=F32, want_a=want, want_b=want)
+            assert torch.equal(got[0][at], x0[0])
+
+
+@pytest.mark.parametrize("r,N,dtype,out", [(16, 3000, BF16, BF16), (16, 33001, BF16, F32), (40, 3000, BF16, BF16),
+                                           (9, 700, F16, F16)])
+def test_an_adapters_gradients_depend_on_its_rows_only(r, N, dtype, out):
+    """grad_a and grad_b bit for bit when the other adapters' rows hold other values, NaN, or change their adapter."""
+    T, d, n = 1500, 600, 4
+    g = torch.Generator(device="cuda").manual_seed(r)
+    normal = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    ad = tim.Adapters((normal(n, r, d) / d ** 0.5).to(dtype), (0.1 * normal(n, N, r)).to(dtype), torch.rand(n, generator=g, device="cuda"))
+    x, grad = normal(T, d).to(dtype), normal(T, N).to(out)
+    rows = torch.randint(-1, n, (T,), generator=g, device="cuda", dtype=torch.int32)
+    rows[torch.rand(T, generator=g, device="cuda") < 0.5] = 2  # runs of more than a workgroup takes
+    first = tim.adapters_backward(grad, x, rows, ad, want_x=False)
+    mine = (rows == 2)[:, None]
+    others = torch.randint(-1, 2, (T,), generator=g, device="cuda", dtype=torch.int32)  # none is left with adapter 3
+    for fill in (normal(T, N), torch.full((T, N), float("nan"), device="cuda")):
+        got = tim.adapters_backward(torch.where(mine, grad, fill.to(out)), torch.where(mine, x, normal(T, d).to(dtype)),
+                                    torch.where(mine[:, 0], rows, others), ad, want_x=False)
+        assert torch.equal(got[1][2], first[1][2]) and torch.equal(got[2][2], first[2][2])
+        assert (got[1][3] == 0).all() and (got[2][3] == 0).all()
