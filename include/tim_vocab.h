@@ -141,10 +141,11 @@ tim_status tim_adapters_add(const tim_adapters* adapters, const void* x, int64_t
  *          aligned.
  * Arithmetic: u and v are accumulated and kept in fp32 (in products with bf16 as
  * in tim_adapters_add); grad_a and grad_b are fp32 chains over runs of an adapter's
- * rows by ascending t, of 128, 256 or 512 rows as T, the width, r and the types
+ * rows by ascending t, of 128, 256 or 512 rows as T, n, the width, r and the types
  * say, the runs' sums joined by a chain; no atomics on them. A row's grad_x is
- * bitwise independent of the other rows and of T; for given T an adapter's grad_a
- * and grad_b are bitwise independent of the other adapters' rows. Errors as tim_adapters_add; TIM_ERR_VALUE also for accumulate_x or
+ * bitwise independent of the other rows, of T and of n; for given T and n an
+ * adapter's grad_a and grad_b are bitwise independent of the other adapters and
+ * their rows. Errors as tim_adapters_add; TIM_ERR_VALUE also for accumulate_x or
  * accumulate_ab not 0 or 1. T == 0 writes zeros to grad_a and grad_b unless
  * accumulating. */
 size_t tim_adapters_backward_workspace_size(int64_t T, int32_t d, int32_t N, int32_t n, int32_t r);
