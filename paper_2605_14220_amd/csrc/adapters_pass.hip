@@ -38,7 +38,12 @@ struct Pass {
   static constexpr int kB = CT * kCols + 8;  // of b, [j][c]
   static constexpr int kLoads = kPassRows * kCols * (int)sizeof(S) / 16 / kThreads;  // 16 bytes a thread
   static constexpr int kV = 16 / (int)sizeof(S);
+  static constexpr int kLds = (kPassRows * kRow + kTerms * JB * 16 * kW) * (int)sizeof(E) +
+                              (CONTRACT ? JB * 16 * kB : 1) * (int)sizeof(W) + kMaxPassRows * 4;
 };
+static_assert(kPassesAtOnce == 256 * (160 * 1024 / Pass<__bf16, __bf16, true, 1, 1>::kLds) &&
+                  kPassesAtOnce == 256 * (160 * 1024 / Pass<float, __bf16, true, 1, 1>::kLds),
+              "workgroups of one tile that 256 CUs hold");
 template <class S, class W, bool CONTRACT, int JB, int CT>
 __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
   typedef Pass<S, W, CONTRACT, JB, CT> P;

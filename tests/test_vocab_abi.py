@@ -125,6 +125,54 @@ extern "C" int32_t slot(int32_t first, int log_C, int last) { return tim::run_sl
                 assert shim.plan(T, n, 6, 7) <= 10 and T > 4096
 
 
+def test_shapes_of_the_pass_over_grad(tmp_path):
+    """The workgroups' tiles and rows: of tiles and rows that the kernels have, two tiles only where one tile a workgroup
+    would be more than 768 workgroups and for ranks up to 16, rows that leave 512 workgroups where 128 would; partial sums
+    of grad b for every pair of tiles; a workspace that holds the plans of both kinds of instructions."""
+    src = tmp_path / "shim.cpp"
+    src.write_text("""
+#include "adapters_plan.h"
+extern "C" int shape(int64_t T, int64_t N, int n, int cols, int rp, int contract, int what) {
+  const tim::PassShape s = tim::pass_shape(T, N, n, cols, rp, contract);
+  return what ? s.log_rows : s.tiles;
+}
+extern "C" int64_t plan(int64_t T, int d, int N, int n, int r, int cols, int what) {
+  const tim::AdapterPlan p = tim::plan_adapters(T, d, N, n, r, cols);
+  return what == 0 ? (int64_t)p.bytes : what == 1 ? p.g_chunks : p.of_grad.tiles;
+}
+""")
+    so = str(tmp_path / "shim.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__=1", "-shared", "-fPIC", "-I", CSRC, "-I",
+                    os.path.join(ROOT, "include"), "-isystem", "/opt/rocm/include", "-o", so, str(src)], check=True)
+    shim = ctypes.CDLL(so)
+    i64, i32 = ctypes.c_int64, ctypes.c_int
+    shim.shape.argtypes, shim.plan.restype, shim.plan.argtypes = [i64, i64, i32, i32, i32, i32, i32], i64, [i64] + [i32] * 6
+    import random
+    rng = random.Random(2)
+    two = 0
+    for _ in range(4000):
+        T, N = int(2 ** rng.uniform(0, 23)), int(2 ** rng.uniform(0, 20))
+        n, r, cols = int(2 ** rng.uniform(0, 12)), rng.randint(1, 256), rng.choice([128, 256])
+        rp = (r + 15) // 16 * 16
+        tiles, log_rows = (shim.shape(T, N, n, cols, rp, 1, w) for w in (0, 1))
+        one_each = ((T >> 9) + min(n, T)) * -(-N // cols)
+        assert tiles == (2 if rp == 16 and one_each > 768 else 1) and 7 <= log_rows <= 9
+        count = lambda log: ((T >> log) + 1) * -(-N // (tiles * cols))
+        assert log_rows == 7 or count(log_rows) >= 512
+        assert log_rows == 9 or count(log_rows + 1) < 512
+        assert shim.shape(T, N, n, cols, rp, 0, 0) == 1
+        two += tiles == 2
+        d = int(2 ** rng.uniform(0, 14))
+        assert shim.plan(T, d, N, n, r, cols, 2) == tiles and shim.plan(T, d, N, n, r, cols, 1) == -(-N // (tiles * cols))
+        assert tim.adapters_backward_workspace_size(T, d, N, n, r) == max(shim.plan(T, d, N, n, r, c, 0) for c in (128, 256))
+        assert tim.adapters_add_workspace_size(T, d, N, n, r) == shim.plan(T, d, N, n, r, 0, 0)
+    assert two > 50
+    # both sides of the limit, each with an adapter more in the set
+    for cols in (128, 256):
+        assert [shim.shape(150, 384 * cols + k, 2, cols, 16, 1, 0) for k in (0, 1)] == [1, 2]
+        assert [shim.shape(150, 256 * cols, n, cols, 16, 1, 0) for n in (3, 4)] == [1, 2]
+
+
 def _embed(lib, table=FAKE, dtype=BF16, V=10, d=8, ld=8, tokens=FAKE, T=4, scale=1.0, out=FAKE, out_dtype=F32, out_ld=8):
     return lib.tim_embedding(table, dtype, V, d, ld, tokens, T, scale, out, out_dtype, out_ld, None)
 
