@@ -373,14 +373,21 @@ template <class T, class O, bool FLAT, bool AHEAD>
 hipError_t run_expand(const ExpandArgs& a, const RunList& l, hipStream_t s) {
   const int tiles = !AHEAD ? 1 : a.rp <= 16 ? 4 : 2;
   const dim3 grid((unsigned)l.max_runs, (unsigned)chunks_of(a.N, tiles * kWaves * 64));
-  if (a.rp <= 16)
-    TIM_LAUNCH((expand<T, O, FLAT, 1, AHEAD><<<grid, kThreads, 0, s>>>(a, l)));
-  else if (a.rp <= 32)
-    TIM_LAUNCH((expand<T, O, FLAT, 2, AHEAD><<<grid, kThreads, 0, s>>>(a, l)));
-  else if (a.rp <= 64)
-    TIM_LAUNCH((expand<T, O, FLAT, 4, false><<<grid, kThreads, 0, s>>>(a, l)));
-  else
-    TIM_LAUNCH((expand<T, O, FLAT, 16, false><<<grid, kThreads, 0, s>>>(a, l)));
+  if constexpr (!FLAT || !std::is_same_v<T, __bf16>) {  // those have terms up to rank 64
+    if (a.rp <= 16) {
+      TIM_LAUNCH((expand<T, O, FLAT, 1, AHEAD><<<grid, kThreads, 0, s>>>(a, l)));
+      return hipSuccess;
+    }
+    if (a.rp <= 32) {
+      TIM_LAUNCH((expand<T, O, FLAT, 2, AHEAD><<<grid, kThreads, 0, s>>>(a, l)));
+      return hipSuccess;
+    }
+    if (a.rp <= 64) {
+      TIM_LAUNCH((expand<T, O, FLAT, 4, false><<<grid, kThreads, 0, s>>>(a, l)));
+      return hipSuccess;
+    }
+  }
+  TIM_LAUNCH((expand<T, O, FLAT, 16, false><<<grid, kThreads, 0, s>>>(a, l)));
   return hipSuccess;
 }
 template <class T, class O, bool FLAT>
