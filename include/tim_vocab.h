@@ -105,7 +105,7 @@ typedef struct {
  *         projection's output (logits of tim_logits with their temperature of
  *         1, say). NULL: zeros.
  * out     out_dtype [T, N], row stride out_ld >= N; may be base itself with the
- *         same stride, otherwise no overlap with the inputs.
+ *         same stride, and x may lie there, otherwise no overlap with the inputs.
  * Arithmetic: x a^T is accumulated in fp32 in an order that depends on d alone
  * and kept in fp32; its product with b^T is accumulated in fp32 over ascending
  * groups of 16 ranks (bf16 adapters: with the fp32 number as the sum of three bf16
@@ -135,8 +135,8 @@ tim_status tim_adapters_add(const tim_adapters* adapters, const void* x, int64_t
  *          written, zeros for a row without an adapter.
  * grad_a, grad_b  contiguous; either may be NULL. With accumulate_ab = 1 both are
  *          added to, else written, zeros for an adapter without rows.
- * The gradients written overlap neither each other nor an input (grad_x may lie in
- * the same buffer's columns beside x or grad).
+ * The gradients written overlap neither each other nor an input, but grad_x may lie
+ * over grad (over x it may not: in the same buffer's columns beside it).
  * workspace  tim_adapters_backward_workspace_size(T, d, N, n, r) bytes, 16-byte
  *          aligned.
  * Arithmetic: u and v are accumulated and kept in fp32 (in products with bf16 as

@@ -1021,8 +1021,8 @@ def adapters_add(base: torch.Tensor | None, x: torch.Tensor, rows: torch.Tensor,
                  workspace: torch.Tensor | None = None) -> torch.Tensor:
     """base [T, N] (a shared projection's output, the head's logits among them; None: zeros) plus the adapter of each row
     of x [T, d]: row t's is adapters rows[t] (int32 [T]), none where that is outside [0, n). fp32 sums, rounded once to
-    base's type (to dtype without a base, x's by default). out may be base itself (in place), but no other overlap is
-    allowed."""
+    base's type (to dtype without a base, x's by default). out may be base itself (in place), and x may be too, but no other
+    overlap is allowed."""
     lib = load_library()
     ad, T, x_ld = _adapters("adapters_add", adapters, x, rows)
     dev, N = x.device, ad.N
@@ -1066,8 +1066,8 @@ def adapters_backward(grad: torch.Tensor, x: torch.Tensor, rows: torch.Tensor, a
     """(grad_x [T, d] or None, grad_a fp32 [n, r, d] or None, grad_b fp32 [n, N, r] or None) through adapters_add, from
     the gradient [T, N] of its output (fp32, bf16 or fp16, dense rows). grad_x is of dtype (x's by default); with
     accumulate_x it is added to the grad_x given, with accumulate grad_a and grad_b to theirs. Rows without an adapter and
-    adapters without rows get zeros, or nothing added. The gradients share no memory with each other or with the inputs:
-    grad_x cannot take x's place."""
+    adapters without rows get zeros, or nothing added. The gradients share no memory with each other or with the inputs,
+    but grad_x may take grad's place (not x's)."""
     lib = load_library()
     name = "adapters_backward"
     ad, T, x_ld = _adapters(name, adapters, x, rows)

@@ -115,11 +115,9 @@ inline tim_status validate_adapters(const tim_adapters* ad, const void* x, int64
   return TIM_OK;
 }
 
-// Whether `out` has a byte in common with the adapters, the rows or x.
-inline bool shares_adapters(const Rows& out, const tim_adapters& ad, const void* x, int64_t x_ld, const int32_t* rows,
-                            int64_t T) {
-  return share_bytes(out, rows_of(x, T, ad.d, x_ld, 2)) || share_bytes(out, flat(rows, T, 4)) ||
-         share_bytes(out, flat(ad.a, ad.n, (int64_t)ad.r * ad.d * 2)) ||
+// Whether `out` has a byte in common with the adapters or the rows' indices.
+inline bool shares_adapters(const Rows& out, const tim_adapters& ad, const int32_t* rows, int64_t T) {
+  return share_bytes(out, flat(rows, T, 4)) || share_bytes(out, flat(ad.a, ad.n, (int64_t)ad.r * ad.d * 2)) ||
          share_bytes(out, flat(ad.b, ad.n, (int64_t)ad.r * ad.N * 2)) || share_bytes(out, flat(ad.scales, ad.n, 4));
 }
 
@@ -136,9 +134,10 @@ inline tim_status validate_adapters_add(const tim_adapters* ad, const void* x, i
   if (!aligned_to(base, dtype_bytes(out_dtype)) || !aligned_to(out, dtype_bytes(out_dtype))) return TIM_ERR_VALUE;
   if (!ws || !aligned16(ws) || ws_bytes < plan_adapters(T, ad->d, ad->N, ad->n, ad->r, 0).bytes)
     return TIM_ERR_WORKSPACE;
+  // x may lie under out: launch_adapters_add reads all of it first
   const int bytes = dtype_bytes(out_dtype);
   const Rows o = rows_of(out, T, ad->N, out_ld, bytes);
-  if (shares_adapters(o, *ad, x, x_ld, rows, T) || (base != out && share_bytes(o, rows_of(base, T, ad->N, base_ld, bytes))))
+  if (shares_adapters(o, *ad, rows, T) || (base != out && share_bytes(o, rows_of(base, T, ad->N, base_ld, bytes))))
     return TIM_ERR_VALUE;
   return TIM_OK;
 }
@@ -161,9 +160,10 @@ inline tim_status validate_adapters_backward(const tim_adapters* ad, const void*
     return TIM_ERR_WORKSPACE;
   const Rows outs[3] = {rows_of(grad_x, T, ad->d, gx_ld, grad_x ? dtype_bytes(gx_dtype) : 0),
                         flat(grad_a, ad->n, (int64_t)ad->r * ad->d * 4), flat(grad_b, ad->n, (int64_t)ad->r * ad->N * 4)};
+  // grad may lie under grad_x: launch_adapters_backward reads all of it before it writes there, but x after
+  const Rows of_x = rows_of(x, T, ad->d, x_ld, 2), of_grad = rows_of(grad, T, ad->N, grad_ld, dtype_bytes(grad_dtype));
   for (int i = 0; i < 3; ++i)
-    if (shares_adapters(outs[i], *ad, x, x_ld, rows, T) ||
-        share_bytes(outs[i], rows_of(grad, T, ad->N, grad_ld, dtype_bytes(grad_dtype))) ||
+    if (shares_adapters(outs[i], *ad, rows, T) || share_bytes(outs[i], of_x) || (i > 0 && share_bytes(outs[i], of_grad)) ||
         share_bytes(outs[i], outs[(i + 1) % 3]))
       return TIM_ERR_VALUE;
   return TIM_OK;

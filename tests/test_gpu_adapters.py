@@ -382,12 +382,33 @@ def test_outputs_beside_and_over_inputs():
     assert all(torch.equal(p, q) for p, q in zip(got, want)) and torch.equal(both[:, :d], x)
     assert torch.equal(tim.adapters_add(two[:, N:], x, rows, ad, out=two[:, :N]), out) and torch.equal(two[:, N:], base)
     kept = x.clone(), grad.clone(), base.clone()
-    for gx in (x, grad[:, :d], grad[:, N - d:]):
-        with pytest.raises(RuntimeError):
-            tim.adapters_backward(grad, x, rows, ad, grad_x=gx)
+    with pytest.raises(RuntimeError):
+        tim.adapters_backward(grad, x, rows, ad, grad_x=x)
     with pytest.raises(RuntimeError):
         tim.adapters_add(base[1:], x[1:], rows[1:], ad, out=base[:-1])
     assert torch.equal(x, kept[0]) and torch.equal(grad, kept[1]) and torch.equal(base, kept[2])
+
+
+@pytest.mark.parametrize("T,d,r", [(70, 48, 5), (1500, 600, 24), (300, 260, 80)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_a_residual_in_place(T, d, r, dtype):
+    """x + its adapter over x, and its gradient over grad: as out of place."""
+    x, a, b, grad, scales, rows = [t.cuda() for t in _whole(T, d, d, 3, r, "mixed", dtype, T)]
+    ad = tim.Adapters(a, b, scales)
+    out = tim.adapters_add(x, x, rows, ad)
+    gx = tim.adapters_backward(grad, x, rows, ad, grad_x=grad.clone(), accumulate_x=True)
+    plain = tim.adapters_backward(grad, x, rows, ad)
+    assert torch.equal(gx[0], (grad.float() + tim.adapters_backward(grad, x, rows, ad, dtype=F32)[0]).to(dtype))
+    ga, gb = torch.empty_like(gx[1]), torch.empty_like(gx[2])
+    place = grad.clone()
+    tim.adapters_backward(place, x, rows, ad, grad_x=place, accumulate_x=True, grad_a=ga, grad_b=gb)
+    assert torch.equal(place, gx[0]) and torch.equal(ga, gx[1]) and torch.equal(gb, gx[2])
+    place = grad.clone()
+    tim.adapters_backward(place, x, rows, ad, grad_x=place)
+    assert torch.equal(place, plain[0])
+    y = x.clone()
+    tim.adapters_add(y, y, rows, ad, out=y)
+    assert torch.equal(y, out)
 
 
 def _few(rows, cols, top, keep, dtype, g):
