@@ -1,15 +1,21 @@
 // Low-rank adapters of many requests beside a shared projection, and their
 // gradients, on gfx950. Rows are grouped by adapter (grouping.h); a workgroup
-// takes a run of up to 64 rows of one adapter:
+// takes a run of rows of one adapter:
 //
-//   shrink   u = x a^T          contraction over d, 1024 elements a workgroup
-//   expand   out = base + u b^T 256 columns a workgroup (backward: v a)
-//   contract v = grad b         contraction over N, 1024 elements a workgroup
-//   outer    sum_t src[t] w[t]  up to 512 rows of one adapter, 256 columns a workgroup
+//   shrink  u = x a^T            up to 64 rows, 512 elements of d
+//   expand  out = base + u b^T   up to 64 rows, 256 columns (512 or 1024 where runs are short);
+//           grad_x (+)= v a      for bf16 up to rank 64 by expand_flat, 256 or 512 columns
+//   pass    v = grad b           up to 512 rows of one or two tiles of 256 columns (of 128 on the fp32
+//           grad_b = grad^T u    instructions): grad is read once for both
+//           grad_a = v^T x       the same pass over x, without the first product
 //
 // x, a and b are 16 bits wide; their products with each other run on the 16-bit
-// matrix instructions. u and v stay in fp32, and so do the products that they
-// enter (16x16x4 fp32 MFMA): what a call moves, not what it computes, bounds it.
+// matrix instructions, and so does bf16 grad times bf16 b. u and v stay in fp32.
+// Where all else is bf16 the products that they enter run on the bf16 instructions,
+// each as the sum of three bf16 numbers (split3); with fp16, and with grad of
+// another type than the adapters', on the fp32 ones (16x16x4), for fp16's exponents
+// do not hold such terms as they are. What a call moves, not what it computes,
+// bounds it.
 
 #pragma once
 

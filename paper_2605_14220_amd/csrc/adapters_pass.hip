@@ -22,8 +22,8 @@ namespace {
 // three bf16 numbers, which holds all of its 24 bits. Otherwise on the fp32 ones,
 // whose tile of 128 columns has the same bytes: three workgroups fit a CU, with 256
 // columns one. 2047 rows on a head of 151936 (rank 16, bf16) take 150 us, 4.2 TB/s;
-// 150 rows on one of 50257 (rank 9, fp32) 21 us, the latency of one workgroup's
-// eight tiles.
+// 150 rows on one of 50257 (rank 9, fp32) 20 us, the latency of one workgroup's
+// four tiles: two blocks of rows, two tiles of columns.
 constexpr int kPassRows = 64;
 template <class S, class W, bool CONTRACT, int JB, int CT>
 struct Pass {
