@@ -28,6 +28,7 @@
 namespace tim {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -105,9 +106,7 @@ template <class T>
 using x4 = T __attribute__((ext_vector_type(4)));
 // x as the sum of three bf16 numbers, exactly where none overflows or is subnormal
 // (24 bits are three times 8); an infinity or NaN alone in the first. In a product
-// with an infinity terms of 0 or of the other sign give NaN: elements that come out
-// as NaN are summed again from x itself (again_if_nan), the same way for an element
-// whatever else the tile holds.
+// with an infinity terms of 0 or of the other sign give NaN, see sign_of.
 __device__ __forceinline__ void split3(float x, __bf16 (&t)[3]) {
   t[0] = (__bf16)x;
   const float r = __builtin_isfinite((float)t[0]) ? x - (float)t[0] : 0.f;
@@ -115,8 +114,21 @@ __device__ __forceinline__ void split3(float x, __bf16 (&t)[3]) {
   t[2] = (__bf16)(r - (float)t[1]);
 }
 
-__device__ __forceinline__ float join3(const __bf16* t, int64_t step) {
-  return ((float)t[0] + (float)t[step]) + (float)t[2 * step];
+// A sum of products with such terms is NaN only where an operand is not finite. Then
+// the sum with sign_of(x) in place of x, which no finite numbers make overflow, tells
+// what it is: an infinity of that sign, or NaN (pass, whose rows are many, takes x
+// itself). It is taken where a tile's sums hold NaN, for those elements alone: the
+// others keep their bits. The look for NaN costs 0 to 1.7% of a call (48 rows on a
+// head of 152064 60.5 us with it and without, 8192 rows' gradients 140.1 and 137.8);
+// a NaN for each of 2047 rows takes their gradients from 212 to 900 us.
+__device__ __forceinline__ __bf16 sign_of(float x) {
+  return (__bf16)(x == 0.f || !__builtin_isfinite(x) ? x : __builtin_copysignf(0x1p-20f, x));
+}
+template <class V, int N>
+__device__ __forceinline__ V signs_of(V x) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) x[e] = sign_of((float)x[e]);
+  return x;
 }
 __device__ __forceinline__ bool has_nan(f32x4 y) {
   return __builtin_isunordered(y[0], y[1]) || __builtin_isunordered(y[2], y[3]);

@@ -183,14 +183,17 @@ __global__ __launch_bounds__(kThreads, !AHEAD && JB <= 2 ? 4 : 1) void expand(Ex
         }
       }
       // lane: row m of the block, columns of the instruction's rows 4 g + i
+      auto turn = [&]() {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if constexpr (FLAT)
-          *(f32x4*)(my + m * kTile + 16 * g + 4 * q) = f32x4{acc[0][q], acc[1][q], acc[2][q], acc[3][q]};
-        else
-          *(f32x4*)(my + m * kTile + 16 * q + 4 * g) = acc[q];
-      }
-      lanes_in_order();
+        for (int q = 0; q < 4; ++q) {
+          if constexpr (FLAT)
+            *(f32x4*)(my + m * kTile + 16 * g + 4 * q) = f32x4{acc[0][q], acc[1][q], acc[2][q], acc[3][q]};
+          else
+            *(f32x4*)(my + m * kTile + 16 * q + 4 * g) = acc[q];
+        }
+        lanes_in_order();
+      };
+      turn();
       f32x4 y[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -209,24 +212,38 @@ __global__ __launch_bounds__(kThreads, !AHEAD && JB <= 2 ? 4 : 1) void expand(Ex
         if (rb * 16 + q * 4 >= run.count) break;
         const int t = rb * 16 + q * 4 + g, c = c0 + 4 * m, n = a.N - c;
         const int64_t row = row_of(rb, q);
-        if (t >= run.count || n <= 0) continue;
-        O* dst = (O*)a.out + row * a.out_ld + c;
         if constexpr (FAST) {
-          if (__builtin_expect(has_nan(y[q]), 0)) {  // see split3
-#pragma unroll 1
-            for (int e = 0; e < 4 && e < n; ++e) {
-              float s = 0.f;
-#pragma unroll 1
-              for (int j = 0; j < a.r; ++j)
-                s = fmaf(join3((const __bf16*)(shared_u + t * kU + j / 4 * kTerms) + j % 4, 4),
-                         (float)(FLAT ? w[(int64_t)j * a.N + c + e] : w[(int64_t)(c + e) * a.r + j]), s);
-              if (base) s += (float)base[row * a.base_ld + c + e];
+          if (__builtin_expect(__ballot(has_nan(y[q])) != 0, 0)) {  // see sign_of
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (i == e && y[q][i] != y[q][i]) y[q][i] = s;
+            for (int nb = 0; nb < 4; ++nb) acc[nb] = f32x4{};
+            auto signs = [&](const W(&h)[4], const U(&x)[kTerms]) {
+              const U u = signs_of<U, 4>(x[0]);
+#pragma unroll
+              for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(h[nb], u, acc[nb]);
+            };
+            if constexpr (kHold) {
+#pragma unroll
+              for (int jb = 0; jb < JB; ++jb)
+                if (jb * 16 < a.rp) signs(wf[jb], from_lds(rb, jb));
+            } else {
+#pragma unroll 1
+              for (int jb = 0; jb * 16 < a.rp; ++jb) {
+                weights(c0, jb, raw[0][0]);
+                operands(0);
+                signs(wf[0], from_lds(rb, jb));
+              }
             }
+            turn();
+            const f32x4 s = *(const f32x4*)(my + (q * 4 + g) * kTile + 4 * m);
+            lanes_in_order();
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (y[q][e] != y[q][e] && __builtin_isinf(s[e]) && t < run.count && e < n)
+                y[q][e] = s[e] + (base ? (float)base[row * a.base_ld + c + e] : 0.f);
           }
         }
+        if (t >= run.count || n <= 0) continue;
+        O* dst = (O*)a.out + row * a.out_ld + c;
         x4<O> z;
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[e] = narrow<O>(y[q][e]);
@@ -268,43 +285,54 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
   const int my_row = l.order[run.first + (lane < run.count ? lane : run.count - 1)];  // of the run's row `lane`
   const int blocks = (run.count + 15) / 16;
   const bool there = run.key < a.n;
-  uint64_t again[NT] = {};  // elements that came out as NaN (split3); added to base, they count as 0 at first
-  bf16x8 wf[NT][kSteps][4], u[kSteps][kTerms][4];
+  auto load_weights = [&](int ct, bf16x8(&wf)[kSteps][4]) {
+#pragma unroll
+    for (int ks = 0; ks < kSteps; ++ks) {
+      const int c0 = c_first + ct * 64, j0 = ks * 32 + (KS == 0 ? g % 2 : g) * 8;
+      const __bf16* w = (const __bf16*)a.w + (int64_t)run.key * a.r * a.N + c0 + 4 * m;
+      x4<__bf16> x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const __bf16* p = w + (int64_t)(j0 + e < a.r ? j0 + e : a.r - 1) * a.N;
+        x[e] = c0 + 64 <= a.N ? load_n<true, x4<__bf16>, 4>(p, 4) : load_some<x4<__bf16>, 4>(p, a.N - c0 - 4 * m);
+        if (a.r != a.rp && j0 + e >= a.r) x[e] = x4<__bf16>{};
+      }
+#pragma unroll
+      for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) wf[ks][nb][e] = x[e][nb];
+      if (KS == 2 && j0 >= a.rp)  // a rank of up to 48
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb) wf[ks][nb] = bf16x8{};
+    }
+  };
+  auto load_u = [&](int rb, bf16x8(&u)[kSteps][kTerms]) {
+    const __bf16* p = (const __bf16*)a.terms + (int64_t)__shfl(my_row, rb * 16 + m) * 3 * a.rp;
+#pragma unroll
+    for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+      for (int q = 0; q < kTerms; ++q) {
+        const int term = KS == 0 ? 2 * q + g / 2 : q, j = KS == 0 ? g % 2 * 8 : ks * 32 + g * 8;
+        u[ks][q] = term < 3 && j < a.rp ? *(const bf16x8*)(p + term * a.rp + j) : bf16x8{};
+      }
+  };
+  auto multiply = [&](const bf16x8(&wf)[kSteps][4], const bf16x8(&u)[kSteps][kTerms], f32x4(&acc)[4]) {
+#pragma unroll
+    for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+      for (int q = 0; q < kTerms; ++q)
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(wf[ks][nb], u[ks][q], acc[nb]);
+  };
+  bf16x8 wf[NT][kSteps][4], u[4][kSteps][kTerms];
   if (there) {
 #pragma unroll
-    for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-      for (int ks = 0; ks < kSteps; ++ks) {
-        const int c0 = c_first + ct * 64, j0 = ks * 32 + (KS == 0 ? g % 2 : g) * 8;
-        const __bf16* w = (const __bf16*)a.w + (int64_t)run.key * a.r * a.N + c0 + 4 * m;
-        x4<__bf16> x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const __bf16* p = w + (int64_t)(j0 + e < a.r ? j0 + e : a.r - 1) * a.N;
-          x[e] = c0 + 64 <= a.N ? load_n<true, x4<__bf16>, 4>(p, 4) : load_some<x4<__bf16>, 4>(p, a.N - c0 - 4 * m);
-          if (a.r != a.rp && j0 + e >= a.r) x[e] = x4<__bf16>{};
-        }
-#pragma unroll
-        for (int nb = 0; nb < 4; ++nb)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) wf[ct][ks][nb][e] = x[e][nb];
-        if (KS == 2 && j0 >= a.rp)  // a rank of up to 48
-#pragma unroll
-          for (int nb = 0; nb < 4; ++nb) wf[ct][ks][nb] = bf16x8{};
-      }
+    for (int ct = 0; ct < NT; ++ct) load_weights(ct, wf[ct]);
 #pragma unroll
     for (int rb = 0; rb < 4; ++rb)
-      if (rb < blocks) {
-        const __bf16* p = (const __bf16*)a.terms + (int64_t)__shfl(my_row, rb * 16 + m) * 3 * a.rp;
-#pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks)
-#pragma unroll
-          for (int q = 0; q < kTerms; ++q) {
-            const int term = KS == 0 ? 2 * q + g / 2 : q, j = KS == 0 ? g % 2 * 8 : ks * 32 + g * 8;
-            u[ks][q][rb] = term < 3 && j < a.rp ? *(const bf16x8*)(p + term * a.rp + j) : bf16x8{};
-          }
-      }
+      if (rb < blocks) load_u(rb, u[rb]);
   }
+  uint64_t nan = 0;  // sums that are NaN: added to base they count as 0 at first
 #pragma unroll
   for (int rb = 0; rb < 4; ++rb) {
     if (rb >= blocks) break;
@@ -313,20 +341,11 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
     for (int ct = 0; ct < NT; ++ct) {
       f32x4 acc[4] = {};
       if (there) {
-#pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks)
-#pragma unroll
-          for (int q = 0; q < kTerms; ++q)
-#pragma unroll
-            for (int nb = 0; nb < 4; ++nb) acc[nb] = mfma(wf[ct][ks][nb], u[ks][q][rb], acc[nb]);
+        multiply(wf[ct], u[rb], acc);
+        nan |= __ballot(has_nan(acc[0]) || has_nan(acc[1]) || has_nan(acc[2]) || has_nan(acc[3]));
       }
       const int c = c_first + ct * 64 + 16 * g, n = a.N - c;
       if (rb * 16 + m >= run.count || n <= 0) continue;
-      if (__builtin_expect(has_nan(acc[0]) || has_nan(acc[1]) || has_nan(acc[2]) || has_nan(acc[3]), 0)) {
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-          if (acc[k % 4][k / 4] != acc[k % 4][k / 4]) again[ct] |= 1ull << (rb * 16 + k);
-      }
       O* dst = (O*)a.out + row * a.out_ld + c;
       const O* base = a.base ? (const O*)a.base + row * a.base_ld + c : nullptr;
       constexpr int E = 16 / (int)sizeof(O);  // columns a store
@@ -354,19 +373,36 @@ __global__ __launch_bounds__(kThreads, KS < 2 ? 4 : 1) void expand_flat(ExpandAr
       }
     }
   }
-#pragma unroll
-  for (int ct = 0; ct < NT; ++ct)
-    for (; __builtin_expect(again[ct] != 0, 0); again[ct] &= again[ct] - 1) {
-      const int at = __builtin_ctzll(again[ct]), c = c_first + ct * 64 + 16 * g + at % 16;
-      if (c >= a.N) continue;
-      const int64_t row = l.order[run.first + at / 16 * 16 + m];
-      const __bf16 *u = (const __bf16*)a.terms + row * 3 * a.rp, *w = (const __bf16*)a.w + (int64_t)run.key * a.r * a.N + c;
-      float s = 0.f;
+  if (__builtin_expect(nan == 0, 1)) return;
+  // the same sums once more, and what those that are NaN are (sign_of)
 #pragma unroll 1
-      for (int j = 0; j < a.r; ++j) s = fmaf(join3(u + j, a.rp), (float)w[(int64_t)j * a.N], s);
+  for (int ct = 0; ct < NT; ++ct) {
+    load_weights(ct, wf[0]);
+#pragma unroll 1
+    for (int rb = 0; rb < blocks; ++rb) {
+      load_u(rb, u[0]);
+      f32x4 acc[4] = {}, signs[4] = {};
+      multiply(wf[0], u[0], acc);
+#pragma unroll
+      for (int ks = 0; ks < kSteps; ++ks) {
+        i32x4 first = __builtin_bit_cast(i32x4, signs_of<bf16x8, 8>(u[0][ks][0]));
+        if (KS == 0)  // the lanes of the second terms take the first ones too
+#pragma unroll
+          for (int e = 0; e < 4; ++e) first[e] = __shfl(first[e], lane % 32);
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb) signs[nb] = mfma(wf[0][ks][nb], __builtin_bit_cast(bf16x8, first), signs[nb]);
+      }
+      const int64_t row = __shfl(my_row, rb * 16 + m);
+      const int c = c_first + ct * 64 + 16 * g;
       O* dst = (O*)a.out + row * a.out_ld + c;
-      *dst = narrow<O>(a.base ? (float)*dst + s : s);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const float y = acc[k % 4][k / 4], s = signs[k % 4][k / 4];
+        if (y == y || rb * 16 + m >= run.count || c + k >= a.N) continue;
+        dst[k] = narrow<O>((a.base ? (float)dst[k] : 0.f) + (__builtin_isinf(s) ? s : y));
+      }
     }
+  }
 }
 
 template <class T, class O, bool FLAT, bool AHEAD>

@@ -251,7 +251,7 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
     return c_first + ct * kCols + wave * (16 * NB) + (CONTRACT ? NB * m + q : NB * (4 * g + q));
   };
   auto rank = [&](int jb) { return j0 + jb * 16 + (CONTRACT ? 4 * g : m); };
-  uint64_t again = 0;  // a bit an element that came out as NaN (split3); added, it counts as 0 at first
+  uint64_t again = 0;  // a bit an element that came out as NaN (sign_of); added, it counts as 0 at first
   if constexpr (P::FAST) {
     static_assert(NB == 4 && kQ == 4 && E4 == 4 && CT * JB <= 4, "a bit an element");
     bool any = false;
@@ -292,16 +292,38 @@ __global__ __launch_bounds__(kThreads) void pass(PassArgs a, RunList l) {
             if (e < left) p[e] = add ? p[e] + y[e] : y[e];
         }
       }
-  for (; __builtin_expect(again != 0, 0); again &= again - 1) {
-    const int at = __builtin_ctzll(again), e = at % 4, q = at / 4 % 4, jb = at / 16 % JB, ct = at / 16 / JB;
-    const int j = rank(jb) + (CONTRACT ? e : 0), c = column(ct, q) + (CONTRACT ? 0 : e);
-    if (j >= a.r || c >= a.N) continue;
-    float s = 0.f;
+  if (__builtin_expect(again == 0, 1)) return;
+  // the blocks of 16 elements that hold NaN once more, from w itself
 #pragma unroll 1
-    for (int t = 0; t < run.count; ++t)
-      s = fmaf((float)((const S*)a.src)[rows[t] * a.ld + c], a.w[(int64_t)rows[t] * a.rp + j], s);
-    float* p = out + (CONTRACT ? (int64_t)c * a.r + j : (int64_t)j * a.N + c);
-    *p = add ? *p + s : s;
+  for (int i = 0; i < CT * JB; ++i, again >>= 16) {
+    const int j = rank(i % JB), c = column(i / JB, 0);
+    if (!(again & 0xffff) || j >= a.r || c >= a.N) continue;
+    float sum[16] = {};
+#pragma unroll 4
+    for (int t = 0; t < run.count; ++t) {
+      const S* src = (const S*)a.src + rows[t] * a.ld + c;
+      const float* wr = a.w + (int64_t)rows[t] * a.rp + j;
+      if constexpr (CONTRACT) {
+        const x4<S> x = load_some<x4<S>, 4>(src, a.N - c);
+        const f32x4 y = *(const f32x4*)wr;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) sum[k] = fmaf((float)x[k / 4], y[k % 4], sum[k]);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const x4<S> x = load_some<x4<S>, 4>(src + 4 * q, a.N - c - 4 * q);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[q * 4 + e] = fmaf((float)x[e], *wr, sum[q * 4 + e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int jk = j + (CONTRACT ? k % 4 : 0), ck = c + (CONTRACT ? k / 4 : k);
+      if (!(again >> k & 1) || jk >= a.r || ck >= a.N) continue;
+      float* p = out + (CONTRACT ? (int64_t)ck * a.r + jk : (int64_t)jk * a.N + ck);
+      *p = add ? *p + sum[k] : sum[k];
+    }
   }
 }
 

@@ -351,17 +351,26 @@ def test_infinities_give_what_the_formula_gives(case, dtype, out, where):
     g = torch.Generator().manual_seed(case)
     base = torch.randint(-100, 101, (T, N), generator=g).to(out)
     t = {"a": a, "b": b, "x": x, "grad": grad}[where].view(-1)
+    some = lambda t, n: torch.randint(0, t.numel(), (n,), generator=g)
     for value in (float("inf"), float("-inf")):
-        t[torch.randint(0, t.numel(), (6,), generator=g)] = value
+        t[some(t, 6)] = value
+        base.view(-1)[some(base, 6)] = value
+    base.view(-1)[some(base, 6)] = float("nan")
     print(INFINITE[case], dtype, out, where, flush=True)
     want = _formula(base, x, rows, a, b, scales, grad)
     ad = tim.Adapters(a.cuda(), b.cuda(), scales.cuda())
     xd, rd, gd = x.cuda(), rows.cuda(), grad.to(out).cuda()
     got = (tim.adapters_add(base.cuda(), xd, rd, ad), *tim.adapters_backward(gd, xd, rd, ad, dtype=out))
-    ones = [torch.ones_like(t) for t in got[1:]]
-    tim.adapters_backward(gd, xd, rd, ad, grad_x=ones[0], accumulate_x=True, grad_a=ones[1], grad_b=ones[2], accumulate=True)
-    names = ("out", "grad_x", "grad_a", "grad_b", "grad_x added", "grad_a added", "grad_b added")
-    for name, y, w in zip(names, (*got, *ones), (*want, *(t + 1 for t in want[1:]))):
+    place = base.cuda()
+    tim.adapters_add(place, xd, rd, ad, out=place)
+    old = [torch.ones_like(t) for t in got[1:]]
+    for o in old:
+        o.view(-1)[some(o, 4)] = float("inf")
+        o.view(-1)[some(o, 4)] = float("nan")
+    sums = [o.cpu().double() + w for o, w in zip(old, want[1:])]
+    tim.adapters_backward(gd, xd, rd, ad, grad_x=old[0], accumulate_x=True, grad_a=old[1], grad_b=old[2], accumulate=True)
+    names = ("out", "grad_x", "grad_a", "grad_b", "out in place", "grad_x added", "grad_a added", "grad_b added")
+    for name, y, w in zip(names, (*got, place, *old), (*want, want[0], *sums)):
         y, w = y.cpu(), w.to(y.dtype)
         wrong = ~((y == w) | (torch.isnan(y) & torch.isnan(w)))
         assert not wrong.any(), (name, int(wrong.sum()), y[wrong][:4], w[wrong][:4])
