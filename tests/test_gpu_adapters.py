@@ -522,3 +522,20 @@ def test_an_adapters_gradients_depend_on_its_rows_only(r, N, dtype, out):
                                     torch.where(mine[:, 0], rows, others), ad, want_x=False)
         assert torch.equal(got[1][2], first[1][2]) and torch.equal(got[2][2], first[2][2])
         assert (got[1][3] == 0).all() and (got[2][3] == 0).all()
+
+
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_adapters_without_rows_change_no_row(out):
+    """out and grad_x bit for bit with a set of 2 adapters and the same two among 60, where the set's size chooses other
+    kernels; the gradients of those without rows are zeros."""
+    T, d, N, r = 150, 700, 33000, 16
+    g = torch.Generator(device="cuda").manual_seed(5)
+    normal = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    a, b = (normal(60, r, d) / d ** 0.5).to(BF16), (0.1 * normal(60, N, r)).to(BF16)
+    x, base, grad = normal(T, d).to(BF16), normal(T, N).to(out), normal(T, N).to(out)
+    rows = torch.randint(-1, 2, (T,), generator=g, device="cuda", dtype=torch.int32)
+    few, many = tim.Adapters(a[:2].contiguous(), b[:2].contiguous()), tim.Adapters(a, b)
+    assert torch.equal(tim.adapters_add(base, x, rows, few), tim.adapters_add(base, x, rows, many))
+    one, all_ = (tim.adapters_backward(grad, x, rows, ad, dtype=F32) for ad in (few, many))
+    assert torch.equal(one[0], all_[0])
+    assert (all_[1][2:] == 0).all() and (all_[2][2:] == 0).all()
